@@ -349,6 +349,114 @@ ckm_status ckm_round_eval_noalloc(const ckm_graph* g, const double* d_s_frac, in
                                   int64_t* d_cost, uint8_t* d_feasible, int32_t* d_best_k,
                                   uint64_t* d_best_S, uint64_t* d_best_R, int32_t* d_status, void* stream);
 
+/* ---- training-node operators -------------------------------------------
+ * The nodes of a transformer training graph that a schedule computes again
+ * first, because they move bytes and multiply no matrices: dropout (with the
+ * residual sum), layer norm, and the scale, masks, softmax and dropout of
+ * attention scores, each with its gradient. A node computed again in another
+ * stage has the bits it had before: dropout draws are a function of (seed,
+ * site, row, column), no mask is stored, and no sum depends on scheduling.
+ *
+ * All pointers are device memory of the current HIP device except the structs
+ * and stride arrays, which are read before the call returns. Calls enqueue
+ * kernel launches on `stream` (NULL: the null stream) and nothing else, so they can be captured
+ * into a HIP graph. Rows start anywhere (pointers need only their element's
+ * alignment, rows any stride of at least 0); an output's rows must not overlap
+ * each other. An output may be an input itself (the same pointer and strides)
+ * but must not overlap one otherwise. */
+
+typedef enum { CKM_F32 = 0, CKM_F16 = 1, CKM_BF16 = 2 } ckm_dtype;
+
+#define CKM_MAX_ROWS 0x7fffffff     /* rows of an operand */
+#define CKM_MAX_COLS (1 << 30)      /* columns of a dropout, keys of a softmax */
+#define CKM_MAX_NORM_COLS 32768     /* columns of a layer norm */
+
+/* A dropout D. Element (row, col) takes 16-bit draw col % 8 of Philox4x32-10
+ * with key = seed and counter = (col / 8, row, site low, site high) (the
+ * generator and draw order of the rounding). It is kept iff the draw is below
+ * keep, and is then multiplied by 65536 / keep; dropped elements are 0, whatever
+ * they held. keep = floor((1 - p) 65536) for a drop probability p: 65536 keeps
+ * all, 0 none. site names the place and step (layers, training steps): equal
+ * (seed, site) mean equal masks, in a gradient or a second computation.
+ * d_site: NULL, or a device uint64 that is added to site when the kernel runs
+ * (the step counter of a captured graph). */
+typedef struct ckm_drop {
+  uint64_t seed;
+  uint64_t site;
+  const uint64_t* d_site;
+  uint32_t keep;
+} ckm_drop;
+
+/* y = residual + D(x) on rows x cols elements with row strides ld_*; residual
+ * may be NULL. The gradient is the same call on dy without a residual (the
+ * residual's own gradient is dy). Binary32 arithmetic, one rounding. */
+ckm_status ckm_dropout_async(ckm_dtype type, int64_t rows, int64_t cols, const void* d_x, int64_t ld_x,
+                             const void* d_residual, int64_t ld_residual, const ckm_drop* drop, void* d_y,
+                             int64_t ld_y, void* stream);
+
+/* Layer norm of each row of h: y = (h - mean) rstd weight + bias, rstd = 1 /
+ * sqrt(var + eps), var the mean of (h - mean)^2. h = x; with a residual or a
+ * dropout (either may be NULL) h = residual + D(x) rounded to the tensors' type,
+ * as ckm_dropout_async gives it, and is written to d_h unless that is NULL.
+ * weight, bias: cols elements of wtype, which is type or CKM_F32; NULL: 1 and 0.
+ * stats (may be NULL): float [rows][2], mean and rstd. */
+ckm_status ckm_layer_norm_async(ckm_dtype type, ckm_dtype wtype, int64_t rows, int64_t cols, const void* d_x,
+                                int64_t ld_x, const void* d_residual, int64_t ld_residual, const ckm_drop* drop,
+                                const void* d_weight, const void* d_bias, float eps, void* d_h, int64_t ld_h,
+                                void* d_y, int64_t ld_y, float* d_stats, void* stream);
+
+/* Its gradient. dy: of y. dres: NULL, or a gradient that reaches h past the norm
+ * (the residual path's), added to dh. dh: of h, which is also the residual's.
+ * dx: of x through the dropout, D(dh); only with a dropout (without one dx is
+ * dh). dweight = sum over rows of dy (h - mean) rstd and dbias = sum over rows of
+ * dy, of wtype, summed in binary32 in an order that rows and cols fix. Any of
+ * the four outputs may be NULL. work: ckm_layer_norm_workspace_size bytes,
+ * aligned to 16. rows = 0 gives zero weight gradients. */
+ckm_status ckm_layer_norm_workspace_size(int64_t rows, int64_t cols, size_t* bytes);
+ckm_status ckm_layer_norm_backward_async(ckm_dtype type, ckm_dtype wtype, int64_t rows, int64_t cols,
+                                         const void* d_dy, int64_t ld_dy, const void* d_h, int64_t ld_h,
+                                         const float* d_stats, const void* d_weight, const void* d_dres,
+                                         int64_t ld_dres, const ckm_drop* drop, void* d_dh, int64_t ld_dh,
+                                         void* d_dx, int64_t ld_dx, void* d_dweight, void* d_dbias, void* d_work,
+                                         size_t work_bytes, void* stream);
+
+/* Attention scores [batch][heads][queries][keys]. Query i of sequence b sees key
+ * j iff j < d_lengths[b] (NULL: keys; values are clamped to [0, keys]), and with
+ * CKM_SCORES_CAUSAL j <= i + keys - queries (the last query sees every key), and
+ * the mask lets it: CKM_MASK_BOOL: uint8, 0 hides; CKM_MASK_ADD: values of the
+ * scores' type added after the scale, -inf hides. mask_stride: elements between
+ * batches, heads and queries, 0 to share one; keys are contiguous. Scores and
+ * gradients where a key is not seen are never used. */
+enum { CKM_SCORES_CAUSAL = 1u };
+enum { CKM_MASK_NONE = 0, CKM_MASK_BOOL = 1, CKM_MASK_ADD = 2 };
+typedef struct ckm_scores {
+  int64_t batch, heads, queries, keys;
+  float scale;
+  uint32_t flags;
+  const int32_t* d_lengths;
+  const void* d_mask;
+  int32_t mask_kind;
+  int64_t mask_stride[3];
+} ckm_scores;
+
+/* y = D(softmax(scale x + mask)) over the seen keys, 0 at the others; a row that
+ * sees nothing (or only scores of -inf) is all 0. The dropout's row is (b heads + h) queries + i. x_stride,
+ * y_stride: elements between batches, heads and queries. stats (may be NULL):
+ * float [batch][heads][queries][2], the largest logit and 1 / the sum of
+ * exponentials; 0 and 0 for a row that sees nothing. work:
+ * ckm_softmax_workspace_size bytes (0 unless rows are long), aligned to 8. */
+ckm_status ckm_softmax_workspace_size(const ckm_scores* scores, size_t* bytes);
+ckm_status ckm_softmax_async(ckm_dtype type, const ckm_scores* scores, const void* d_x, const int64_t* x_stride,
+                             const ckm_drop* drop, void* d_y, const int64_t* y_stride, float* d_stats,
+                             void* d_work, size_t work_bytes, void* stream);
+
+/* The scores' gradient dx from dy, the scores x and the forward call's stats, with
+ * the same struct and dropout; 0 where a key is not seen. */
+ckm_status ckm_softmax_backward_async(ckm_dtype type, const ckm_scores* scores, const void* d_dy,
+                                      const int64_t* dy_stride, const void* d_x, const int64_t* x_stride,
+                                      const float* d_stats, const ckm_drop* drop, void* d_dx,
+                                      const int64_t* dx_stride, void* d_work, size_t work_bytes, void* stream);
+
 /* Thread-local text describing the calling thread's last non-OK status. */
 const char* ckm_last_error(void);
 

@@ -29,6 +29,9 @@ EXPORTS = (
     "ckm_evaluate_async", "ckm_select_async", "ckm_round_eval_async", "ckm_eval_schedules", "ckm_eval_schedules_async", "ckm_threshold_eval",
     "ckm_threshold_eval_async", "ckm_plan", "ckm_plan_async", "ckm_max_batch",
     "ckm_max_batch_async", "ckm_round_eval_noalloc", "ckm_last_error",
+    "ckm_dropout_async", "ckm_layer_norm_async", "ckm_layer_norm_workspace_size",
+    "ckm_layer_norm_backward_async", "ckm_softmax_workspace_size", "ckm_softmax_async",
+    "ckm_softmax_backward_async",   # bound by ops.py
 )
 NOALLOC_SCRATCH_BYTES = 256 << 20
 PLAN_EARLY_FREE = 1
@@ -97,6 +100,22 @@ def lib():
         L.ckm_max_batch.restype = C.c_int
         L.ckm_max_batch_async.argtypes = [p, i32, i64, i64, p, p, p, p, p, sz, p]
         L.ckm_max_batch_async.restype = C.c_int
+        f32, t = C.c_float, C.c_int
+        L.ckm_dropout_async.argtypes = [t, i64, i64, p, i64, p, i64, p, p, i64, p]
+        L.ckm_dropout_async.restype = C.c_int
+        L.ckm_layer_norm_async.argtypes = [t, t, i64, i64, p, i64, p, i64, p, p, p, f32, p, i64, p, i64, p, p]
+        L.ckm_layer_norm_async.restype = C.c_int
+        L.ckm_layer_norm_workspace_size.argtypes = [i64, i64, p]
+        L.ckm_layer_norm_workspace_size.restype = C.c_int
+        L.ckm_layer_norm_backward_async.argtypes = [t, t, i64, i64, p, i64, p, i64, p, p, p, i64, p, p, i64, p, i64, p,
+                                                    p, p, sz, p]
+        L.ckm_layer_norm_backward_async.restype = C.c_int
+        L.ckm_softmax_workspace_size.argtypes = [p, p]
+        L.ckm_softmax_workspace_size.restype = C.c_int
+        L.ckm_softmax_async.argtypes = [t, p, p, p, p, p, p, p, p, sz, p]
+        L.ckm_softmax_async.restype = C.c_int
+        L.ckm_softmax_backward_async.argtypes = [t, p, p, p, p, p, p, p, p, p, p, sz, p]
+        L.ckm_softmax_backward_async.restype = C.c_int
         L.ckm_last_error.argtypes = []
         L.ckm_last_error.restype = C.c_char_p
         _lib = L

@@ -1,0 +1,220 @@
+// Device helpers and launch declarations shared by the training-node
+// operators: dropout (ckm_dropout.hip), layer norm (ckm_layer_norm.hip) and
+// the attention softmax (ckm_softmax.hip).
+//
+// All three work on rows. A thread holds groups of eight consecutive columns:
+// 16 bytes of a 16-bit type, and exactly the eight draws of one Philox output.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "ckm.h"
+#include "ckm_internal.h"
+
+namespace ckm {
+
+constexpr int kVec = 8;   // columns of a group
+
+// A dropout as the kernels take it: on is false without one, and when every
+// element is kept (keep = 65536, factor 1).
+struct DropArgs {
+  uint32_t k0 = 0, k1 = 0;            // Philox key: the seed
+  uint64_t site = 0;                  // counter words 2 and 3, plus *d_site when given
+  const uint64_t* d_site = nullptr;
+  uint32_t keep = 0;                  // a draw below this keeps the element
+  float scale = 0.0f;                 // 65536 / keep
+  bool on = false;
+};
+
+// Checks a caller's ckm_drop (NULL: no dropout) and converts it.
+ckm_status drop_args(const ckm_drop* d, DropArgs* out);
+// Checks that a matrix of rows x cols elements of `elt` bytes behind `p` is
+// addressable: aligned to its type, row stride (elements) not negative, and at
+// least cols for an output of more than one row.
+ckm_status check_matrix(const void* p, const char* name, int64_t rows, int64_t cols, int64_t ld, size_t elt,
+                        bool output);
+inline size_t dtype_bytes(int t) { return t == CKM_F32 ? 4 : 2; }
+inline bool dtype_ok(int t) { return t == CKM_F32 || t == CKM_F16 || t == CKM_BF16; }
+// CKM_OK, or CKM_E_DEVICE with the launch's error.
+ckm_status launched(const char* what);
+
+// ---- device side ----------------------------------------------------------
+
+// Eight elements at p, which need only be aligned to their own size: rows of
+// odd length or stride start anywhere, and the hardware takes such addresses.
+template <typename T>
+struct Raw8 {
+  T e[kVec];
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T* p) {
+  Raw8<T> r;
+  __builtin_memcpy(&r, p, sizeof(r));
+  return r;
+}
+// The group's elements that lie in the row (left of them, 1 or more); zeros past it.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_group(const T* p, int left) {
+  if (left >= kVec) return load8(p);
+  Raw8<T> r;
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) r.e[j] = j < left ? p[j] : (T)0;
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> zero_group() {
+  Raw8<T> r;
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) r.e[j] = (T)0;
+  return r;
+}
+// Rounds to T (nearest even) and stores the elements that lie in the row.
+template <typename T>
+__device__ __forceinline__ void store_group(T* p, const float (&v)[kVec], int left) {
+  Raw8<T> r;
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) r.e[j] = (T)v[j];
+  if (left >= kVec) {
+    __builtin_memcpy(p, &r, sizeof(r));
+  } else {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      if (j < left) p[j] = r.e[j];
+  }
+}
+// v rounded to T and back: what a reader of the stored value sees.
+template <typename T>
+__device__ __forceinline__ float as_stored(float v) {
+  return (float)(T)v;
+}
+
+// Philox4x32-10 (Salmon et al., SC'11) of counter (group, row, site), the
+// generator and draw order of the rounding: draw j is 16-bit half (j mod 2)
+// of word j / 2.
+struct DropSite {
+  uint32_t s0, s1;
+};
+__device__ __forceinline__ DropSite drop_site(const DropArgs& d) {
+  uint64_t s = d.site;
+  if (d.d_site) s += *d.d_site;
+  return {(uint32_t)s, (uint32_t)(s >> 32)};
+}
+__device__ __forceinline__ uint32_t drop_xor3(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);   // truth table of a ^ b ^ c
+}
+// Applies the dropout to the group's eight values: dropped ones become 0
+// whatever they hold, NaN and infinities too.
+__device__ __forceinline__ void drop8(float (&v)[kVec], const DropArgs& d, DropSite s, uint32_t group, uint32_t row) {
+  // the product is rounded by itself in every operator (not fused with a sum that
+  // follows), so that an operator with a dropout inside gives the bits of the two
+  // operators one after the other
+#pragma clang fp contract(off)
+  uint32_t c0 = group, c1 = row, c2 = s.s0, c3 = s.s1, k0 = d.k0, k1 = d.k1;
+#pragma unroll
+  for (int r = 0; r < 10; ++r) {
+    const uint64_t p0 = (uint64_t)0xD2511F53u * c0;
+    const uint64_t p1 = (uint64_t)0xCD9E8D57u * c2;
+    const uint32_t n0 = drop_xor3((uint32_t)(p1 >> 32), c1, k0);
+    const uint32_t n2 = drop_xor3((uint32_t)(p0 >> 32), c3, k1);
+    c0 = n0;
+    c1 = (uint32_t)p1;
+    c2 = n2;
+    c3 = (uint32_t)p0;
+    k0 += 0x9E3779B9u;
+    k1 += 0xBB67AE85u;
+  }
+  const uint32_t x[4] = {c0, c1, c2, c3};
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) {
+    const uint32_t u = (j & 1) ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu;
+    v[j] = u < d.keep ? v[j] * d.scale : 0.0f;
+  }
+}
+
+// Sums and maxima over the kLanes threads of a row. Within 16 lanes by lane
+// permutations, over a wave by reading its four 16-lane rows, over more waves
+// through LDS. Every thread of the row gets the result, by one order of
+// additions that depends on kLanes alone.
+template <int kCtrl>
+__device__ __forceinline__ float dpp_move(float x) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), kCtrl, 0xf, 0xf, true));
+}
+struct OpSum {
+  __device__ __forceinline__ static float of(float a, float b) { return a + b; }
+};
+struct OpMax {
+  __device__ __forceinline__ static float of(float a, float b) { return fmaxf(a, b); }
+};
+template <typename Op>
+__device__ __forceinline__ float reduce16(float x) {
+  x = Op::of(x, dpp_move<0xB1>(x));    // lanes xor 1
+  x = Op::of(x, dpp_move<0x4E>(x));    // lanes xor 2
+  x = Op::of(x, dpp_move<0x141>(x));   // the other four of eight
+  x = Op::of(x, dpp_move<0x140>(x));   // the other eight of sixteen
+  return x;
+}
+__device__ __forceinline__ float lane_of(float x, int lane) {
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
+}
+template <typename Op>
+__device__ __forceinline__ float reduce64(float x) {
+  x = reduce16<Op>(x);
+  return Op::of(Op::of(lane_of(x, 0), lane_of(x, 16)), Op::of(lane_of(x, 32), lane_of(x, 48)));
+}
+// kLanes 16, 64, or a multiple of 64 that divides the block's kBlock threads.
+// lds: 2 kBlock / 64 floats per value; `turn` (0 or 1) picks the half, and a
+// kernel's reductions take turns: a wave can write a half again only after the
+// barrier of the reduction between, which every reader of it has reached. All
+// threads of the block take part.
+template <typename Op, int kLanes, int kBlock>
+__device__ __forceinline__ float reduce_row(float x, float* lds, int turn) {
+  if constexpr (kLanes == 16) {
+    return reduce16<Op>(x);
+  } else {
+    x = reduce64<Op>(x);
+    if constexpr (kLanes > 64) {
+      constexpr int kWaves = kLanes / 64;
+      float* at = lds + turn * (kBlock / 64);
+      if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
+      __syncthreads();
+      at += threadIdx.x / kLanes * kWaves;
+      x = at[0];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) x = Op::of(x, at[w]);
+    }
+    return x;
+  }
+}
+// Two sums at once, one barrier. lds: 4 kBlock / 64 floats.
+template <int kLanes, int kBlock>
+__device__ __forceinline__ void reduce_two(float& x, float& y, float* lds, int turn) {
+  if constexpr (kLanes == 16) {
+    x = reduce16<OpSum>(x);
+    y = reduce16<OpSum>(y);
+  } else {
+    x = reduce64<OpSum>(x);
+    y = reduce64<OpSum>(y);
+    if constexpr (kLanes > 64) {
+      constexpr int kWaves = kLanes / 64;
+      float* at = lds + turn * (2 * kBlock / 64);
+      if ((threadIdx.x & 63) == 0) {
+        at[2 * (threadIdx.x >> 6)] = x;
+        at[2 * (threadIdx.x >> 6) + 1] = y;
+      }
+      __syncthreads();
+      at += threadIdx.x / kLanes * (2 * kWaves);
+      x = at[0];
+      y = at[1];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) {
+        x += at[2 * w];
+        y += at[2 * w + 1];
+      }
+    }
+  }
+}
+
+}  // namespace ckm

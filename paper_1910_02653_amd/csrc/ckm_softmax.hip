@@ -1,0 +1,486 @@
+// Softmax of attention scores with scale, masks and dropout in one pass, and its
+// gradient.
+//
+//   forward   t = scale x + mask over the visible keys, m = max t, z = 1 / sum
+//             exp(t - m), y = D(exp(t - m) z); a row that sees nothing gives
+//             zeros and the statistics (0, 0)
+//   gradient  p = exp(t - m) z from the scores and the statistics, g = D(dy),
+//             dx = scale p (g - sum p g)
+//
+// Neither the probabilities before the dropout nor its mask are ever stored:
+// the gradient makes both again, the same bits as the forward pass made.
+// Logits, statistics and sums are in binary32; exp(v) is 2^(v log2 e), which is
+// off by 2^-24 |v log2 e| relative at most beside the unit's own last bit, and
+// v <= 0 is near 0 where the result counts.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "ckm_ops.h"
+
+namespace ckm {
+namespace {
+
+struct Strided {
+  const void* p;
+  int64_t s[3];   // elements between batches, heads, queries
+};
+
+struct SoftmaxArgs {
+  int64_t rows;
+  int32_t heads, queries, keys;
+  Strided x, dy;
+  void* y;          // probabilities, or the scores' gradient
+  int64_t ys[3];
+  float* stats;     // [rows][2]: m, z (read by the gradient)
+  float scale;
+  bool causal;
+  const int32_t* lengths;
+  int mask_kind;
+  Strided mask;
+  DropArgs drop;
+};
+
+struct Row {
+  int32_t b, h, i;
+  int32_t seen;     // keys seen are below this (masks aside)
+};
+__device__ __forceinline__ Row row_of(const SoftmaxArgs& a, int64_t row) {
+  Row r;
+  const uint32_t bh = (uint32_t)row / (uint32_t)a.queries;
+  r.i = (uint32_t)row - bh * a.queries;
+  r.b = bh / (uint32_t)a.heads;
+  r.h = bh - r.b * a.heads;
+  int32_t seen = a.keys;
+  if (a.lengths) seen = min(seen, a.lengths[r.b]);
+  if (a.causal) seen = min(seen, r.i + (a.keys - a.queries) + 1);
+  r.seen = max(seen, 0);
+  return r;
+}
+__device__ __forceinline__ int64_t offset_of(const int64_t (&s)[3], const Row& r) {
+  return r.b * s[0] + r.h * s[1] + r.i * s[2];
+}
+
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kLog2e = 1.44269504088896341f;
+__device__ __forceinline__ float exp_of(float t, float m) {
+  return __builtin_amdgcn_exp2f((t - m) * kLog2e);
+}
+
+// The logits of a group; -inf where a key is not seen. Scores there are not used,
+// whatever they hold. left: seen keys from the group's first on, 1 or more.
+template <typename T>
+__device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, const T* x, const Row& r, int col,
+                                        int left) {
+  const Raw8<T> v = load_group(x + col, left);
+  if (a.mask_kind == CKM_MASK_ADD) {
+    const Raw8<T> m = load_group((const T*)a.mask.p + offset_of(a.mask.s, r) + col, left);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) {
+      const float add = (float)m.e[j];
+      t[j] = j < left && add != -__builtin_inff() ? fmaf((float)v.e[j], a.scale, add) : -__builtin_inff();
+    }
+  } else if (a.mask_kind == CKM_MASK_BOOL) {
+    const Raw8<uint8_t> m = load_group((const uint8_t*)a.mask.p + offset_of(a.mask.s, r) + col, left);
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      t[j] = j < left && m.e[j] ? (float)v.e[j] * a.scale : -__builtin_inff();
+  } else {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) t[j] = j < left ? (float)v.e[j] * a.scale : -__builtin_inff();
+  }
+}
+
+// The gradient that reaches the probabilities of a group before the dropout; 0
+// where a key is not seen.
+template <typename T>
+__device__ __forceinline__ void grads8(float (&g)[kVec], const SoftmaxArgs& a, DropSite site, const T* dy,
+                                       const float (&t)[kVec], int64_t row, int col, int left) {
+  const Raw8<T> v = load_group(dy + col, left);
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) g[j] = (float)v.e[j];
+  if (a.drop.on) drop8(g, a.drop, site, col / kVec, (uint32_t)row);
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) g[j] = t[j] == -__builtin_inff() ? 0.0f : g[j];
+}
+
+constexpr int softmax_block(int lanes) { return lanes < 256 ? 256 : lanes; }
+
+// A row in the registers of kLanes threads, kPer groups each.
+template <typename T, int kLanes, int kPer, bool kBack>
+__global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(SoftmaxArgs a) {
+  constexpr int kBlock = softmax_block(kLanes), kRowsAt = kBlock / kLanes;
+  __shared__ float lds[kLanes > 64 ? 2 * kBlock / 64 : 1];
+  const int lane = threadIdx.x % kLanes;
+  const DropSite site = drop_site(a.drop);
+  int turn = 0;
+  for (int64_t first = (int64_t)blockIdx.x * kRowsAt; first < a.rows; first += (int64_t)gridDim.x * kRowsAt) {
+    const int64_t row = first + threadIdx.x / kLanes;
+    const bool live = row < a.rows;
+    const Row r = row_of(a, live ? row : a.rows - 1);
+    const T* x = (const T*)a.x.p + offset_of(a.x.s, r);
+    T* y = (T*)a.y + offset_of(a.ys, r);
+    const int seen = live ? r.seen : 0, keys = live ? a.keys : 0;
+    float t[kPer][kVec];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int col = (lane + i * kLanes) * kVec;
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) t[i][j] = -__builtin_inff();
+      if (col < seen) logits8(t[i], a, x, r, col, seen - col);
+    }
+    if constexpr (!kBack) {
+      float m = kLowest;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) m = fmaxf(m, t[i][j]);
+      m = reduce_row<OpMax, kLanes, kBlock>(m, lds, 0);
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) {
+          t[i][j] = exp_of(t[i][j], m);
+          sum += t[i][j];
+        }
+      sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, 1);
+      const float z = sum == 0.0f ? 0.0f : 1.0f / sum;
+      if (live && lane == 0 && a.stats) {
+        a.stats[2 * row] = sum == 0.0f ? 0.0f : m;
+        a.stats[2 * row + 1] = z;
+      }
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int group = lane + i * kLanes, col = group * kVec;
+        if (col >= keys) continue;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) t[i][j] *= z;
+        if (a.drop.on && col < seen) drop8(t[i], a.drop, site, group, (uint32_t)row);
+        store_group(y + col, t[i], keys - col);
+      }
+    } else {
+      const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
+      const float m = live ? a.stats[2 * row] : 0.0f, z = live ? a.stats[2 * row + 1] : 0.0f;
+      float g[kPer][kVec];
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int col = (lane + i * kLanes) * kVec;
+        if (col < seen) {
+          grads8(g[i], a, site, dy, t[i], row, col, seen - col);
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) {
+            t[i][j] = exp_of(t[i][j], m) * z;
+            sum += t[i][j] * g[i][j];
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) t[i][j] = g[i][j] = 0.0f;
+        }
+      }
+      sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, turn);
+      turn ^= 1;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        const int col = (lane + i * kLanes) * kVec;
+        if (col >= keys) continue;
+        float o[kVec];
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) o[j] = a.scale * (t[i][j] * (g[i][j] - sum));
+        store_group(y + col, o, keys - col);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Long rows, and few of them: a row is cut into `splits` shares of `chunk` keys
+// (a multiple of a block's 2048). The first launch leaves each share's maximum
+// and sum of exponentials (the gradient: its sum of p g); the second joins a row's
+// shares in each of its blocks and makes the share's outputs.
+// ---------------------------------------------------------------------------
+
+constexpr int kSplitBlock = 256, kSplitSpan = kSplitBlock * kVec, kMaxSplits = kSplitBlock;
+
+template <typename T, bool kBack>
+__global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxArgs a, int splits, int32_t chunk,
+                                                                        float2* part) {
+  __shared__ float lds[2 * kSplitBlock / 64];
+  const DropSite site = drop_site(a.drop);
+  int turn = 0;
+  for (int64_t item = blockIdx.x; item < a.rows * splits; item += gridDim.x) {
+    const int64_t row = item / splits;
+    const Row r = row_of(a, row);
+    const T* x = (const T*)a.x.p + offset_of(a.x.s, r);
+    const int from = (int)(item - row * splits) * chunk;
+    const int to = min(r.seen, from + chunk);
+    if constexpr (!kBack) {
+      float m = kLowest, sum = 0.0f;
+      for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
+        float t[kVec];
+        logits8(t, a, x, r, col, r.seen - col);
+        float top = m;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) top = fmaxf(top, t[j]);
+        sum *= exp_of(m, top);
+        m = top;
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) sum += exp_of(t[j], m);
+      }
+      const float top = reduce_row<OpMax, kSplitBlock, kSplitBlock>(m, lds, 0);
+      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum * exp_of(m, top), lds, 1);
+      if (threadIdx.x == 0) part[item] = {top, sum};
+    } else {
+      const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
+      const float m = a.stats[2 * row], z = a.stats[2 * row + 1];
+      float sum = 0.0f;
+      for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
+        float t[kVec], g[kVec];
+        logits8(t, a, x, r, col, r.seen - col);
+        grads8(g, a, site, dy, t, row, col, r.seen - col);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) sum += exp_of(t[j], m) * z * g[j];
+      }
+      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum, lds, turn);
+      turn ^= 1;
+      if (threadIdx.x == 0) part[item] = {0.0f, sum};
+    }
+  }
+}
+
+template <typename T, bool kBack>
+__global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxArgs a, int splits, int32_t chunk,
+                                                                       const float2* part) {
+  __shared__ float lds[2 * kSplitBlock / 64];
+  const DropSite site = drop_site(a.drop);
+  int turn = 0;
+  for (int64_t item = blockIdx.x; item < a.rows * splits; item += gridDim.x) {
+    const int64_t row = item / splits;
+    const Row r = row_of(a, row);
+    const T* x = (const T*)a.x.p + offset_of(a.x.s, r);
+    T* y = (T*)a.y + offset_of(a.ys, r);
+    const int share = (int)(item - row * splits);
+    const int from = share * chunk;
+    const int to = (int)min((int64_t)a.keys, (int64_t)from + chunk);
+    float2 mine = {kLowest, 0.0f};
+    if ((int)threadIdx.x < splits) mine = part[row * splits + threadIdx.x];
+    if constexpr (!kBack) {
+      const float m = reduce_row<OpMax, kSplitBlock, kSplitBlock>(mine.x, lds, 0);
+      const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y * exp_of(mine.x, m), lds, 1);
+      const float z = sum == 0.0f ? 0.0f : 1.0f / sum;
+      if (share == 0 && threadIdx.x == 0 && a.stats) {
+        a.stats[2 * row] = sum == 0.0f ? 0.0f : m;
+        a.stats[2 * row + 1] = z;
+      }
+      for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
+        float t[kVec] = {};
+        if (col < r.seen) {
+          logits8(t, a, x, r, col, r.seen - col);
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m) * z;
+          if (a.drop.on) drop8(t, a.drop, site, col / kVec, (uint32_t)row);
+        }
+        store_group(y + col, t, a.keys - col);
+      }
+    } else {
+      const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
+      const float m = a.stats[2 * row], z = a.stats[2 * row + 1];
+      const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, turn);
+      turn ^= 1;
+      for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
+        float o[kVec] = {};
+        if (col < r.seen) {
+          float t[kVec], g[kVec];
+          logits8(t, a, x, r, col, r.seen - col);
+          grads8(g, a, site, dy, t, row, col, r.seen - col);
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) o[j] = a.scale * (exp_of(t[j], m) * z * (g[j] - sum));
+        }
+        store_group(y + col, o, a.keys - col);
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// launch rules
+// ---------------------------------------------------------------------------
+
+// Shares of a row, 1 when a row stays whole in registers. The number fixes the
+// order of the sums, so it depends on the sizes alone.
+constexpr int kWholeKeys = 32768;
+int softmax_splits(int64_t rows, int64_t keys) {
+  if (keys <= kWholeKeys && (keys <= 4096 || rows > 64)) return 1;
+  const int64_t spans = (keys + kSplitSpan - 1) / kSplitSpan;
+  const int64_t wanted = std::max<int64_t>(2, (2048 + rows - 1) / std::max<int64_t>(rows, 1));
+  return (int)std::min<int64_t>(std::min<int64_t>(spans, wanted), kMaxSplits);
+}
+
+template <typename T, bool kBack, int kLanes, int kPer>
+void launch_whole_as(const SoftmaxArgs& a, hipStream_t s) {
+  constexpr int kBlock = softmax_block(kLanes), kRowsAt = kBlock / kLanes;
+  const int64_t blocks = std::min<int64_t>((a.rows + kRowsAt - 1) / kRowsAt, 1 << 20);
+  ckm_softmax_kernel<T, kLanes, kPer, kBack><<<dim3((uint32_t)blocks), kBlock, 0, s>>>(a);
+}
+
+template <typename T, bool kBack>
+void launch_softmax(const SoftmaxArgs& a, int splits, void* work, hipStream_t s) {
+  if (splits > 1) {
+    const int64_t spans = ((int64_t)a.keys + kSplitSpan - 1) / kSplitSpan;
+    const int32_t chunk = (int32_t)((spans + splits - 1) / splits * kSplitSpan);
+    const dim3 grid((uint32_t)std::min<int64_t>(a.rows * splits, 1 << 20));
+    ckm_softmax_share_kernel<T, kBack><<<grid, kSplitBlock, 0, s>>>(a, splits, chunk, (float2*)work);
+    ckm_softmax_join_kernel<T, kBack><<<grid, kSplitBlock, 0, s>>>(a, splits, chunk, (const float2*)work);
+    return;
+  }
+  const int groups = (a.keys + kVec - 1) / kVec;
+  if (groups <= 16) launch_whole_as<T, kBack, 16, 1>(a, s);
+  else if (groups <= 64) launch_whole_as<T, kBack, 64, 1>(a, s);
+  else if (groups <= 128) launch_whole_as<T, kBack, 64, 2>(a, s);
+  else if (groups <= 256) launch_whole_as<T, kBack, 64, 4>(a, s);
+  else if (groups <= 512) launch_whole_as<T, kBack, 256, 2>(a, s);
+  else if (groups <= 1024) launch_whole_as<T, kBack, 256, 4>(a, s);
+  else if (groups <= 2048) launch_whole_as<T, kBack, 1024, 2>(a, s);
+  else launch_whole_as<T, kBack, 1024, 4>(a, s);
+}
+
+template <bool kBack>
+void launch_typed(int type, const SoftmaxArgs& a, int splits, void* work, hipStream_t s) {
+  switch (type) {
+    case CKM_F32: launch_softmax<float, kBack>(a, splits, work, s); break;
+    case CKM_F16: launch_softmax<_Float16, kBack>(a, splits, work, s); break;
+    default: launch_softmax<__bf16, kBack>(a, splits, work, s); break;
+  }
+}
+
+// Strides of a [batch, heads, queries] array of rows of `keys` elements: not
+// negative, offsets within the address range, and for an output no two rows
+// that share an element (each stride spans everything with smaller ones).
+ckm_status check_strides(const char* name, const int64_t* stride, const ckm_scores& c, bool output) {
+  if (!stride) return set_error(CKM_E_INVALID_ARG, "%s strides are NULL", name);
+  const int64_t dim[3] = {c.batch, c.heads, c.queries};
+  int order[3] = {0, 1, 2};
+  __int128 last = 0;
+  for (int k = 0; k < 3; ++k) {
+    if (stride[k] < 0) return set_error(CKM_E_INVALID_ARG, "%s: negative stride %lld", name, (long long)stride[k]);
+    last += (__int128)(dim[k] - 1) * stride[k];
+  }
+  if (last > INT64_MAX / 8 - c.keys) return set_error(CKM_E_INVALID_ARG, "%s: strides pass the address range", name);
+  if (!output) return CKM_OK;
+  std::sort(order, order + 3, [&](int p, int q) { return stride[p] < stride[q]; });
+  int64_t span = c.keys;   // elements from the first to past the last one
+  for (const int k : order) {
+    if (dim[k] == 1) continue;
+    if (stride[k] < span) return set_error(CKM_E_INVALID_ARG, "%s: rows overlap (stride %lld)", name, (long long)stride[k]);
+    span += (dim[k] - 1) * stride[k];
+  }
+  return CKM_OK;
+}
+
+ckm_status check_scores(const ckm_scores* c, int64_t* rows) {
+  if (!c) return set_error(CKM_E_INVALID_ARG, "scores is NULL");
+  if (c->batch < 0 || c->heads < 0 || c->queries < 0 || c->keys < 0)
+    return set_error(CKM_E_INVALID_ARG, "scores of %lld x %lld x %lld x %lld", (long long)c->batch, (long long)c->heads,
+                     (long long)c->queries, (long long)c->keys);
+  if (c->batch > CKM_MAX_ROWS || c->heads > CKM_MAX_ROWS || c->queries > CKM_MAX_ROWS ||
+      (__int128)c->batch * c->heads * c->queries > CKM_MAX_ROWS || c->keys > CKM_MAX_COLS)
+    return set_error(CKM_E_UNSUPPORTED, "scores of %lld x %lld x %lld x %lld", (long long)c->batch, (long long)c->heads,
+                     (long long)c->queries, (long long)c->keys);
+  *rows = c->batch * c->heads * c->queries;
+  return CKM_OK;
+}
+
+ckm_status softmax(bool back, ckm_dtype type, const ckm_scores* c, const void* x, const int64_t* x_stride,
+                   const void* dy, const int64_t* dy_stride, const ckm_drop* drop, void* y, const int64_t* y_stride,
+                   float* stats, void* work, size_t work_bytes, void* stream) {
+  if (!dtype_ok(type)) return set_error(CKM_E_INVALID_ARG, "unknown type %d", (int)type);
+  SoftmaxArgs a = {};
+  ckm_status st = check_scores(c, &a.rows);
+  if (st != CKM_OK) return st;
+  if (!(c->scale >= -3.4e38f && c->scale <= 3.4e38f)) return set_error(CKM_E_INVALID_ARG, "scale = %g", (double)c->scale);
+  if (c->flags & ~CKM_SCORES_CAUSAL) return set_error(CKM_E_INVALID_ARG, "unknown flags 0x%x", c->flags);
+  if (c->mask_kind != CKM_MASK_NONE && c->mask_kind != CKM_MASK_BOOL && c->mask_kind != CKM_MASK_ADD)
+    return set_error(CKM_E_INVALID_ARG, "unknown mask kind %d", c->mask_kind);
+  if ((st = drop_args(drop, &a.drop)) != CKM_OK) return st;
+  if (a.rows == 0 || (back && c->keys == 0)) return CKM_OK;
+  const size_t elt = dtype_bytes(type);
+  // a NULL or misaligned array, then its strides
+  const auto check = [&](const void* p, const char* name, const int64_t* stride, size_t bytes, bool output) {
+    const ckm_status s = check_matrix(p, name, 1, c->keys, 0, bytes, false);
+    return s != CKM_OK ? s : check_strides(name, stride, *c, output);
+  };
+  if (c->keys > 0) {
+    if ((st = check(x, "x", x_stride, elt, false)) != CKM_OK) return st;
+    if (back && (st = check(dy, "dy", dy_stride, elt, false)) != CKM_OK) return st;
+    if ((st = check(y, back ? "dx" : "y", y_stride, elt, true)) != CKM_OK) return st;
+    if (c->mask_kind != CKM_MASK_NONE &&
+        (st = check(c->d_mask, "mask", c->mask_stride, c->mask_kind == CKM_MASK_ADD ? elt : 1, false)) != CKM_OK)
+      return st;
+  }
+  if (back && !stats) return set_error(CKM_E_INVALID_ARG, "stats is NULL");
+  if ((uintptr_t)stats % 4) return set_error(CKM_E_INVALID_ARG, "stats is not aligned to 4 bytes");
+  if ((uintptr_t)c->d_lengths % 4) return set_error(CKM_E_INVALID_ARG, "lengths is not aligned to 4 bytes");
+  const int splits = softmax_splits(a.rows, c->keys);
+  const size_t need = splits > 1 ? (size_t)a.rows * splits * sizeof(float2) : 0;
+  if (need > 0 && (!work || work_bytes < need))
+    return set_error(CKM_E_INVALID_ARG, "work buffer of %zu bytes, %zu needed", work ? work_bytes : (size_t)0, need);
+  if ((uintptr_t)work % 8) return set_error(CKM_E_INVALID_ARG, "work is not aligned to 8 bytes");
+  a.heads = (int32_t)c->heads;
+  a.queries = (int32_t)c->queries;
+  a.keys = (int32_t)c->keys;
+  const auto strided = [](const void* p, const int64_t* s) {
+    Strided v = {p, {0, 0, 0}};
+    if (s)
+      for (int k = 0; k < 3; ++k) v.s[k] = s[k];
+    return v;
+  };
+  a.x = strided(x, x_stride);
+  a.dy = strided(dy, dy_stride);
+  a.y = y;
+  for (int k = 0; k < 3; ++k) a.ys[k] = y_stride ? y_stride[k] : 0;
+  a.stats = stats;
+  a.scale = c->scale;
+  a.causal = c->flags & CKM_SCORES_CAUSAL;
+  a.lengths = c->d_lengths;
+  a.mask_kind = c->mask_kind;
+  a.mask = strided(c->d_mask, c->mask_stride);
+  if (back)
+    launch_typed<true>(type, a, splits, work, (hipStream_t)stream);
+  else
+    launch_typed<false>(type, a, splits, work, (hipStream_t)stream);
+  return launched(back ? "softmax gradient launch" : "softmax launch");
+}
+
+}  // namespace
+}  // namespace ckm
+
+extern "C" ckm_status ckm_softmax_workspace_size(const ckm_scores* scores, size_t* bytes) {
+  using namespace ckm;
+  if (!bytes) return set_error(CKM_E_INVALID_ARG, "bytes is NULL");
+  int64_t rows = 0;
+  const ckm_status st = check_scores(scores, &rows);
+  if (st != CKM_OK) return st;
+  const int splits = rows ? softmax_splits(rows, scores->keys) : 1;
+  *bytes = splits > 1 ? (size_t)rows * splits * sizeof(float2) : 0;
+  return CKM_OK;
+}
+
+extern "C" ckm_status ckm_softmax_async(ckm_dtype type, const ckm_scores* scores, const void* d_x,
+                                        const int64_t* x_stride, const ckm_drop* drop, void* d_y,
+                                        const int64_t* y_stride, float* d_stats, void* d_work, size_t work_bytes,
+                                        void* stream) {
+  return ckm::softmax(false, type, scores, d_x, x_stride, nullptr, nullptr, drop, d_y, y_stride, d_stats, d_work,
+                      work_bytes, stream);
+}
+
+extern "C" ckm_status ckm_softmax_backward_async(ckm_dtype type, const ckm_scores* scores, const void* d_dy,
+                                                 const int64_t* dy_stride, const void* d_x, const int64_t* x_stride,
+                                                 const float* d_stats, const ckm_drop* drop, void* d_dx,
+                                                 const int64_t* dx_stride, void* d_work, size_t work_bytes,
+                                                 void* stream) {
+  return ckm::softmax(true, type, scores, d_x, x_stride, d_dy, dy_stride, drop, d_dx, dx_stride,
+                      const_cast<float*>(d_stats), d_work, work_bytes, stream);
+}

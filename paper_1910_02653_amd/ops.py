@@ -1,0 +1,340 @@
+"""Training-node operators on device tensors: argument checks and marshalling only.
+
+The nodes of a transformer training graph that a rematerialization schedule
+computes again first, with their gradients as calls (nodes) of their own:
+
+  dropout, dropout_backward           counter-based, the mask never stored
+  layer_norm, layer_norm_backward     with the dropout and residual sum before it
+  softmax, softmax_backward           scale, masks, softmax and dropout of scores
+
+A call made again with the same inputs gives the same bits, in whatever stage
+of a plan it runs. Every computation is a HIP kernel of libckm (include/ckm.h
+states each operator's definition); there is no other implementation to fall
+back to. Tensors are float32, float16 or bfloat16 on the current device.
+
+Calls enqueue kernels on `stream` (a torch.cuda.Stream; None: the current one)
+and return at once. Results they allocate belong to that stream. No autograd
+graph is recorded: gradients are the *_backward calls.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+import math
+
+import torch
+
+from . import ckm
+
+F32, F16, BF16 = range(3)
+SCORES_CAUSAL = 1
+MASK_NONE, MASK_BOOL, MASK_ADD = range(3)
+MAX_ROWS, MAX_COLS, MAX_NORM_COLS = 0x7fffffff, 1 << 30, 32768
+_TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+
+
+class _Drop(C.Structure):
+    _fields_ = [("seed", C.c_uint64), ("site", C.c_uint64), ("d_site", C.c_void_p), ("keep", C.c_uint32)]
+
+
+class _Scores(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("heads", C.c_int64), ("queries", C.c_int64), ("keys", C.c_int64),
+                ("scale", C.c_float), ("flags", C.c_uint32), ("d_lengths", C.c_void_p), ("d_mask", C.c_void_p),
+                ("mask_kind", C.c_int32), ("mask_stride", C.c_int64 * 3)]
+
+
+_Stride = C.c_int64 * 3
+
+
+class Dropout:
+    """Which elements a dropout keeps, as a function of (seed, site, row, column) alone.
+
+    p: drop probability, kept to 16 bits (an element is kept with probability
+    keep / 65536, keep = floor((1 - p) 65536), and scaled by its inverse).
+    site: names the place and step; equal (seed, site) give equal masks.
+    d_site: an int64 device tensor of one element, added to site when a kernel
+    runs: the step counter of a captured graph."""
+
+    __slots__ = ("p", "seed", "site", "keep", "d_site", "_c")
+
+    def __init__(self, p: float, seed: int, site: int = 0, d_site=None):
+        if not 0.0 <= p <= 1.0:
+            raise ValueError("p must lie in [0, 1], got %r" % (p,))
+        if not 0 <= seed < 1 << 64 or not 0 <= site < 1 << 64:
+            raise ValueError("seed and site must be unsigned 64-bit numbers, got %r and %r" % (seed, site))
+        self.p, self.seed, self.site, self.d_site = float(p), int(seed), int(site), d_site
+        self.keep = math.floor((1.0 - self.p) * 65536.0)
+        ptr = None
+        if d_site is not None:
+            if not isinstance(d_site, torch.Tensor) or not d_site.is_cuda or d_site.dtype != torch.int64 or d_site.numel() != 1:
+                raise ValueError("d_site must be an int64 device tensor of one element")
+            ptr = d_site.data_ptr()
+        self._c = _Drop(self.seed, self.site, ptr, self.keep)
+
+
+def _tensor(t, name: str, dtype=None, device=None):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if dtype is None:
+        if t.dtype not in _TYPES:
+            raise ValueError("%s must be float32, float16 or bfloat16, got %s" % (name, t.dtype))
+    elif t.dtype != dtype:
+        raise ValueError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if device is None:
+        if t.get_device() != torch.cuda.current_device():
+            raise ValueError("%s is on %s, not on the current device" % (name, t.device))
+    elif t.get_device() != device:
+        raise ValueError("%s is on %s, not on device %d" % (name, t.device, device))
+    return t
+
+
+def _rows(t, name: str, shape, dtype, device):
+    """(pointer, row stride) of a tensor of `shape` seen as rows of its last dimension."""
+    _tensor(t, name, dtype, device)
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    if t.is_contiguous():
+        return t.data_ptr(), shape[-1]
+    if t.numel() == 0:
+        return t.data_ptr(), shape[-1]
+    if shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("%s: the last dimension must be contiguous, got strides %s" % (name, t.stride()))
+    # the other dimensions as one: each stride spans the next inner dimension
+    ld, span = None, 1
+    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+        if n == 1:
+            continue
+        if ld is None:
+            ld, span = s, n * s
+        elif s == span:
+            span = n * s
+        else:
+            raise ValueError("%s: rows must lie at one stride, got shape %s, strides %s (make it contiguous)"
+                             % (name, tuple(t.shape), t.stride()))
+    return t.data_ptr(), shape[-1] if ld is None else ld
+
+
+def _vector(t, name: str, cols: int, dtype, device):
+    if t is None:
+        return None
+    _tensor(t, name, dtype, device)
+    if t.dim() != 1 or t.shape[0] != cols or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous vector of %d elements, got shape %s" % (name, cols, tuple(t.shape)))
+    return t.data_ptr()
+
+
+def _drop_ptr(drop, device):
+    if drop is None:
+        return None
+    if not isinstance(drop, Dropout):
+        raise ValueError("drop must be an ops.Dropout, got %s" % type(drop).__name__)
+    if drop.d_site is not None and drop.d_site.get_device() != device:
+        raise ValueError("d_site is on %s, not on device %d" % (drop.d_site.device, device))
+    return C.byref(drop._c)
+
+
+def _stream(stream):
+    """(pointer, context in which results are allocated): results belong to the stream they are written on."""
+    if stream is None:
+        return torch.cuda.current_stream().cuda_stream, contextlib.nullcontext()
+    return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def _shape(t, name):
+    if t.dim() < 1:
+        raise ValueError("%s must have at least one dimension" % name)
+    return t.shape, t.shape[-1], (t.numel() // t.shape[-1] if t.shape[-1] else t.shape[:-1].numel())
+
+
+def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
+    """y = residual + D(x), rows by the last dimension (ckm_dropout_async). out may be x or residual."""
+    device = _tensor(x, "x").get_device()
+    shape, cols, rows = _shape(x, "x")
+    if drop is None:
+        raise ValueError("drop is needed")
+    sp, ctx = _stream(stream)
+    with ctx:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    xp, ldx = _rows(x, "x", shape, x.dtype, device)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", shape, x.dtype, device)
+    yp, ldy = _rows(y, "out", shape, x.dtype, device)
+    ckm._check(ckm.lib().ckm_dropout_async(_TYPES[x.dtype], rows, cols, xp, ldx, rp, ldr, _drop_ptr(drop, device), yp,
+                                           ldy, sp))
+    return y
+
+
+def dropout_backward(dy, drop: Dropout, out=None, stream=None):
+    """The gradient of x: D(dy). (The residual's gradient is dy.)"""
+    return dropout(dy, drop, out=out, stream=stream)
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop: Dropout = None, out=None,
+               stream=None):
+    """(y, h, stats) of the layer norm over the last dimension (ckm_layer_norm_async).
+
+    h = residual + D(x), rounded to x's type; x itself when neither is given.
+    weight, bias: vectors of x's type or float32, both of one type. stats:
+    float32 [..., 2], mean and 1 / standard deviation of each row of h.
+    out: for y; may be x or residual."""
+    device = _tensor(x, "x").get_device()
+    shape, cols, rows = _shape(x, "x")
+    wt = weight.dtype if weight is not None else bias.dtype if bias is not None else x.dtype
+    if wt not in (x.dtype, torch.float32):
+        raise ValueError("weights must be %s or float32, got %s" % (x.dtype, wt))
+    wp, bp = _vector(weight, "weight", cols, wt, device), _vector(bias, "bias", cols, wt, device)
+    sp, ctx = _stream(stream)
+    fused = residual is not None or drop is not None
+    with ctx:
+        y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+        h = torch.empty(shape, dtype=x.dtype, device=x.device) if fused else x
+        stats = torch.empty(shape[:-1] + (2,), dtype=torch.float32, device=x.device)
+    xp, ldx = _rows(x, "x", shape, x.dtype, device)
+    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", shape, x.dtype, device)
+    yp, ldy = _rows(y, "out", shape, x.dtype, device)
+    ckm._check(ckm.lib().ckm_layer_norm_async(_TYPES[x.dtype], _TYPES[wt], rows, cols, xp, ldx, rp, ldr,
+                                              _drop_ptr(drop, device), wp, bp, eps, h.data_ptr() if fused else None,
+                                              cols, yp, ldy, stats.data_ptr(), sp))
+    return y, h, stats
+
+
+def layer_norm_backward(dy, h, stats, weight=None, dres=None, drop: Dropout = None, wtype=None, out=None, work=None,
+                        stream=None):
+    """(dx, dh, dweight, dbias) of layer_norm (ckm_layer_norm_backward_async).
+
+    h, stats: what layer_norm returned. dres: a gradient that reaches h past the
+    norm, added to dh. drop: the forward call's; dx = D(dh), and without one dx
+    is dh. dweight and dbias are of weight's type (wtype when there is none:
+    x's type or float32). out: for dh; may be dy, h or dres. work: a uint8
+    device buffer of layer_norm_workspace(rows, cols) bytes to use."""
+    device = _tensor(dy, "dy").get_device()
+    shape, cols, rows = _shape(dy, "dy")
+    wt = weight.dtype if weight is not None else wtype or dy.dtype
+    if wt not in (dy.dtype, torch.float32):
+        raise ValueError("weights must be %s or float32, got %s" % (dy.dtype, wt))
+    wp = _vector(weight, "weight", cols, wt, device)
+    _tensor(stats, "stats", torch.float32, device)
+    if stats.shape != shape[:-1] + (2,) or not stats.is_contiguous():
+        raise ValueError("stats must be contiguous of shape %s, got %s" % (tuple(shape[:-1]) + (2,), tuple(stats.shape)))
+    dyp, lddy = _rows(dy, "dy", shape, dy.dtype, device)
+    hp, ldh = _rows(h, "h", shape, dy.dtype, device)
+    rp, ldr = (None, 0) if dres is None else _rows(dres, "dres", shape, dy.dtype, device)
+    need = layer_norm_workspace(rows, cols)
+    sp, ctx = _stream(stream)
+    with ctx:
+        dh = torch.empty(shape, dtype=dy.dtype, device=dy.device) if out is None else out
+        dx = torch.empty(shape, dtype=dy.dtype, device=dy.device) if drop is not None else dh
+        dw = torch.empty((2, cols), dtype=wt, device=dy.device)
+        if work is None:
+            work = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
+    wkp, wkb = (None, 0) if work is None else _work(work, device)
+    op, ldo = _rows(dh, "out", shape, dy.dtype, device)
+    dwp = dw.data_ptr()
+    ckm._check(ckm.lib().ckm_layer_norm_backward_async(
+        _TYPES[dy.dtype], _TYPES[wt], rows, cols, dyp, lddy, hp, ldh, stats.data_ptr(), wp, rp, ldr,
+        _drop_ptr(drop, device), op, ldo, dx.data_ptr() if drop is not None else None, cols, dwp,
+        dwp + cols * dw.element_size(), wkp, wkb, sp))
+    return dx, dh, dw[0], dw[1]
+
+
+def layer_norm_workspace(rows: int, cols: int) -> int:
+    """Bytes of work buffer that layer_norm_backward needs (ckm_layer_norm_workspace_size)."""
+    out = C.c_size_t()
+    ckm._check(ckm.lib().ckm_layer_norm_workspace_size(rows, cols, C.byref(out)))
+    return out.value
+
+
+def _work(work, device):
+    _tensor(work, "work", torch.uint8, device)
+    if not work.is_contiguous():
+        raise ValueError("work must be contiguous")
+    return work.data_ptr(), work.numel()
+
+
+def _strides(t, name: str, shape, dtype, device):
+    """(pointer, strides of batch, heads, queries) of a tensor of shape `shape`, up to four dimensions."""
+    _tensor(t, name, dtype, device)
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
+    s = t.stride()
+    if shape[-1] > 1 and s[-1] != 1 and t.numel():
+        raise ValueError("%s: the last dimension must be contiguous, got strides %s" % (name, s))
+    return t.data_ptr(), _Stride(*((0,) * (4 - len(s)) + s[:-1]))
+
+
+def _scores(scores, scale, causal, lengths, mask):
+    """The C struct of a call's shape, scale and masks, with the tensors it points to."""
+    device = _tensor(scores, "scores").get_device()
+    if not 1 <= scores.dim() <= 4:
+        raise ValueError("scores must have one to four dimensions, got shape %s" % (tuple(scores.shape),))
+    c = _Scores(*((1,) * (4 - scores.dim()) + tuple(scores.shape)))
+    c.scale = scale
+    c.flags = SCORES_CAUSAL if causal else 0
+    if lengths is not None:
+        _tensor(lengths, "lengths", torch.int32, device)
+        if lengths.numel() != c.batch or not lengths.is_contiguous():
+            raise ValueError("lengths must hold %d contiguous elements, got shape %s" % (c.batch, tuple(lengths.shape)))
+        c.d_lengths = lengths.data_ptr()
+    if mask is not None:
+        if not isinstance(mask, torch.Tensor) or mask.dtype not in (torch.bool, torch.uint8, scores.dtype):
+            raise ValueError("mask must be a bool, uint8 or %s device tensor" % scores.dtype)
+        _tensor(mask, "mask", mask.dtype, device)
+        try:
+            mask = mask.expand(scores.shape)
+        except RuntimeError:
+            raise ValueError("mask of shape %s does not broadcast to scores of shape %s"
+                             % (tuple(mask.shape), tuple(scores.shape))) from None
+        c.d_mask, c.mask_stride = _strides(mask, "mask", scores.shape, mask.dtype, device)
+        c.mask_kind = MASK_ADD if mask.dtype == scores.dtype else MASK_BOOL
+    return c, device
+
+
+def _scores_work(c, work, tensor, device):
+    need = C.c_size_t()
+    ckm._check(ckm.lib().ckm_softmax_workspace_size(C.byref(c), C.byref(need)))
+    if work is None and need.value:
+        work = torch.empty(need.value, dtype=torch.uint8, device=tensor.device)
+    return (work,) + ((None, 0) if work is None else _work(work, device))
+
+
+def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask=None, drop: Dropout = None, out=None,
+            work=None, stream=None):
+    """(probabilities, stats) of attention scores [batch, heads, queries, keys] (ckm_softmax_async).
+
+    Fewer dimensions stand for leading ones of 1. lengths: int32 [batch], the
+    keys that each sequence has. causal: query i sees key j iff j <= i + keys -
+    queries. mask: bool or uint8 (0 hides a key) or of the scores' type (added
+    after the scale; -inf hides), broadcast to the scores. A row that sees
+    nothing gives zeros. stats: float32 [..., queries, 2], the largest logit
+    and 1 / the sum of exponentials. out: for the probabilities; may be scores."""
+    c, device = _scores(scores, scale, causal, lengths, mask)
+    sp, ctx = _stream(stream)
+    with ctx:
+        y = torch.empty(scores.shape, dtype=scores.dtype, device=scores.device) if out is None else out
+        stats = torch.empty(scores.shape[:-1] + (2,), dtype=torch.float32, device=scores.device)
+        work, wp, wb = _scores_work(c, work, scores, device)
+    xp, xs = _strides(scores, "scores", scores.shape, scores.dtype, device)
+    yp, ys = _strides(y, "out", scores.shape, scores.dtype, device)
+    ckm._check(ckm.lib().ckm_softmax_async(_TYPES[scores.dtype], C.byref(c), xp, xs, _drop_ptr(drop, device), yp, ys,
+                                           stats.data_ptr(), wp, wb, sp))
+    return y, stats
+
+
+def softmax_backward(dy, scores, stats, scale: float = 1.0, causal: bool = False, lengths=None, mask=None,
+                     drop: Dropout = None, out=None, work=None, stream=None):
+    """The scores' gradient (ckm_softmax_backward_async): the forward call's scores, stats, masks and drop.
+    out: may be dy or scores."""
+    c, device = _scores(scores, scale, causal, lengths, mask)
+    _tensor(stats, "stats", torch.float32, device)
+    if stats.shape != scores.shape[:-1] + (2,) or not stats.is_contiguous():
+        raise ValueError("stats must be contiguous of shape %s, got %s"
+                         % (tuple(scores.shape[:-1]) + (2,), tuple(stats.shape)))
+    sp, ctx = _stream(stream)
+    with ctx:
+        dx = torch.empty(scores.shape, dtype=scores.dtype, device=scores.device) if out is None else out
+        work, wp, wb = _scores_work(c, work, scores, device)
+    gp, gs = _strides(dy, "dy", scores.shape, scores.dtype, device)
+    xp, xs = _strides(scores, "scores", scores.shape, scores.dtype, device)
+    op, os_ = _strides(dx, "out", scores.shape, scores.dtype, device)
+    ckm._check(ckm.lib().ckm_softmax_backward_async(_TYPES[scores.dtype], C.byref(c), gp, gs, xp, xs, stats.data_ptr(),
+                                                    _drop_ptr(drop, device), op, os_, wp, wb, sp))
+    return dx
