@@ -18,8 +18,8 @@ graph is recorded: gradients are the *_backward calls.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes as C
+import functools
 import math
 
 import torch
@@ -89,13 +89,13 @@ def _tensor(t, name: str, dtype=None, device=None):
 
 
 def _rows(t, name: str, shape, dtype, device):
-    """(pointer, row stride) of a tensor of `shape` seen as rows of its last dimension."""
+    """(pointer, row stride) of a tensor of `shape` seen as rows of its last dimension; (None, 0) for None."""
+    if t is None:
+        return None, 0
     _tensor(t, name, dtype, device)
     if t.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if t.is_contiguous():
-        return t.data_ptr(), shape[-1]
-    if t.numel() == 0:
+    if t.is_contiguous() or t.numel() == 0:
         return t.data_ptr(), shape[-1]
     if shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError("%s: the last dimension must be contiguous, got strides %s" % (name, t.stride()))
@@ -133,33 +133,53 @@ def _drop_ptr(drop, device):
     return C.byref(drop._c)
 
 
-def _stream(stream):
-    """(pointer, context in which results are allocated): results belong to the stream they are written on."""
-    if stream is None:
-        return torch.cuda.current_stream().cuda_stream, contextlib.nullcontext()
-    return stream.cuda_stream, torch.cuda.stream(stream)
+# the current stream's pointer without a torch.cuda.Stream object around it (0.1 us instead of 2.8)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _shape(t, name):
+def _on_stream(fn):
+    """A `stream` argument: the call is made with that stream as the current one, so that the results
+    it allocates belong to it."""
+    @functools.wraps(fn)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return fn(*args, **kw)
+        with torch.cuda.stream(stream):
+            return fn(*args, **kw)
+    return call
+
+
+def _like(t):
+    """A contiguous tensor of t's shape and type."""
+    return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def _row_count(t, name):
     if t.dim() < 1:
         raise ValueError("%s must have at least one dimension" % name)
-    return t.shape, t.shape[-1], (t.numel() // t.shape[-1] if t.shape[-1] else t.shape[:-1].numel())
+    cols = t.shape[-1]
+    return cols, (t.numel() // cols if cols else t.shape[:-1].numel())
 
 
-def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
+@_on_stream
+def dropout(x, drop: Dropout, residual=None, out=None):
     """y = residual + D(x), rows by the last dimension (ckm_dropout_async). out may be x or residual."""
     device = _tensor(x, "x").get_device()
-    shape, cols, rows = _shape(x, "x")
+    cols, rows = _row_count(x, "x")
     if drop is None:
         raise ValueError("drop is needed")
-    sp, ctx = _stream(stream)
-    with ctx:
-        y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
-    xp, ldx = _rows(x, "x", shape, x.dtype, device)
-    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", shape, x.dtype, device)
-    yp, ldy = _rows(y, "out", shape, x.dtype, device)
-    ckm._check(ckm.lib().ckm_dropout_async(_TYPES[x.dtype], rows, cols, xp, ldx, rp, ldr, _drop_ptr(drop, device), yp,
-                                           ldy, sp))
+    shape, dtype = x.shape, x.dtype
+    xp, ldx = _rows(x, "x", shape, dtype, device)
+    rp, ldr = _rows(residual, "residual", shape, dtype, device)
+    if out is None:
+        y = _like(x)
+        yp, ldy = y.data_ptr(), cols
+    else:
+        y = out
+        yp, ldy = _rows(y, "out", shape, dtype, device)
+    ckm._check(ckm.lib().ckm_dropout_async(_TYPES[dtype], rows, cols, xp, ldx, rp, ldr, _drop_ptr(drop, device), yp, ldy,
+                                           _raw_stream(device)))
     return y
 
 
@@ -168,8 +188,8 @@ def dropout_backward(dy, drop: Dropout, out=None, stream=None):
     return dropout(dy, drop, out=out, stream=stream)
 
 
-def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop: Dropout = None, out=None,
-               stream=None):
+@_on_stream
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop: Dropout = None, out=None):
     """(y, h, stats) of the layer norm over the last dimension (ckm_layer_norm_async).
 
     h = residual + D(x), rounded to x's type; x itself when neither is given.
@@ -177,28 +197,34 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop
     float32 [..., 2], mean and 1 / standard deviation of each row of h.
     out: for y; may be x or residual."""
     device = _tensor(x, "x").get_device()
-    shape, cols, rows = _shape(x, "x")
-    wt = weight.dtype if weight is not None else bias.dtype if bias is not None else x.dtype
-    if wt not in (x.dtype, torch.float32):
-        raise ValueError("weights must be %s or float32, got %s" % (x.dtype, wt))
+    cols, rows = _row_count(x, "x")
+    shape, dtype = x.shape, x.dtype
+    wt = weight.dtype if weight is not None else bias.dtype if bias is not None else dtype
+    if wt is not dtype and wt is not torch.float32:
+        raise ValueError("weights must be %s or float32, got %s" % (dtype, wt))
     wp, bp = _vector(weight, "weight", cols, wt, device), _vector(bias, "bias", cols, wt, device)
-    sp, ctx = _stream(stream)
-    fused = residual is not None or drop is not None
-    with ctx:
-        y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
-        h = torch.empty(shape, dtype=x.dtype, device=x.device) if fused else x
-        stats = torch.empty(shape[:-1] + (2,), dtype=torch.float32, device=x.device)
-    xp, ldx = _rows(x, "x", shape, x.dtype, device)
-    rp, ldr = (None, 0) if residual is None else _rows(residual, "residual", shape, x.dtype, device)
-    yp, ldy = _rows(y, "out", shape, x.dtype, device)
-    ckm._check(ckm.lib().ckm_layer_norm_async(_TYPES[x.dtype], _TYPES[wt], rows, cols, xp, ldx, rp, ldr,
-                                              _drop_ptr(drop, device), wp, bp, eps, h.data_ptr() if fused else None,
-                                              cols, yp, ldy, stats.data_ptr(), sp))
+    xp, ldx = _rows(x, "x", shape, dtype, device)
+    rp, ldr = _rows(residual, "residual", shape, dtype, device)
+    if out is None:
+        y = _like(x)
+        yp, ldy = y.data_ptr(), cols
+    else:
+        y = out
+        yp, ldy = _rows(y, "out", shape, dtype, device)
+    if residual is None and drop is None:
+        h, hp = x, None
+    else:
+        h = _like(x)
+        hp = h.data_ptr()
+    stats = torch.empty(shape[:-1] + (2,), dtype=torch.float32, device=x.device)
+    ckm._check(ckm.lib().ckm_layer_norm_async(_TYPES[dtype], _TYPES[wt], rows, cols, xp, ldx, rp, ldr,
+                                              _drop_ptr(drop, device), wp, bp, eps, hp, cols, yp, ldy,
+                                              stats.data_ptr(), _raw_stream(device)))
     return y, h, stats
 
 
-def layer_norm_backward(dy, h, stats, weight=None, dres=None, drop: Dropout = None, wtype=None, out=None, work=None,
-                        stream=None):
+@_on_stream
+def layer_norm_backward(dy, h, stats, weight=None, dres=None, drop: Dropout = None, wtype=None, out=None, work=None):
     """(dx, dh, dweight, dbias) of layer_norm (ckm_layer_norm_backward_async).
 
     h, stats: what layer_norm returned. dres: a gradient that reaches h past the
@@ -207,35 +233,39 @@ def layer_norm_backward(dy, h, stats, weight=None, dres=None, drop: Dropout = No
     x's type or float32). out: for dh; may be dy, h or dres. work: a uint8
     device buffer of layer_norm_workspace(rows, cols) bytes to use."""
     device = _tensor(dy, "dy").get_device()
-    shape, cols, rows = _shape(dy, "dy")
-    wt = weight.dtype if weight is not None else wtype or dy.dtype
-    if wt not in (dy.dtype, torch.float32):
-        raise ValueError("weights must be %s or float32, got %s" % (dy.dtype, wt))
+    cols, rows = _row_count(dy, "dy")
+    shape, dtype = dy.shape, dy.dtype
+    wt = weight.dtype if weight is not None else wtype or dtype
+    if wt is not dtype and wt is not torch.float32:
+        raise ValueError("weights must be %s or float32, got %s" % (dtype, wt))
     wp = _vector(weight, "weight", cols, wt, device)
-    _tensor(stats, "stats", torch.float32, device)
-    if stats.shape != shape[:-1] + (2,) or not stats.is_contiguous():
-        raise ValueError("stats must be contiguous of shape %s, got %s" % (tuple(shape[:-1]) + (2,), tuple(stats.shape)))
-    dyp, lddy = _rows(dy, "dy", shape, dy.dtype, device)
-    hp, ldh = _rows(h, "h", shape, dy.dtype, device)
-    rp, ldr = (None, 0) if dres is None else _rows(dres, "dres", shape, dy.dtype, device)
-    need = layer_norm_workspace(rows, cols)
-    sp, ctx = _stream(stream)
-    with ctx:
-        dh = torch.empty(shape, dtype=dy.dtype, device=dy.device) if out is None else out
-        dx = torch.empty(shape, dtype=dy.dtype, device=dy.device) if drop is not None else dh
-        dw = torch.empty((2, cols), dtype=wt, device=dy.device)
-        if work is None:
-            work = torch.empty(need, dtype=torch.uint8, device=dy.device) if need else None
-    wkp, wkb = (None, 0) if work is None else _work(work, device)
-    op, ldo = _rows(dh, "out", shape, dy.dtype, device)
-    dwp = dw.data_ptr()
+    _stats(stats, shape, device)
+    dyp, lddy = _rows(dy, "dy", shape, dtype, device)
+    hp, ldh = _rows(h, "h", shape, dtype, device)
+    rp, ldr = _rows(dres, "dres", shape, dtype, device)
+    if out is None:
+        dh = _like(dy)
+        op, ldo = dh.data_ptr(), cols
+    else:
+        dh = out
+        op, ldo = _rows(dh, "out", shape, dtype, device)
+    if drop is None:
+        dx, xp = dh, None
+    else:
+        dx = _like(dy)
+        xp = dx.data_ptr()
+    if weight is not None:
+        dw, db = torch.empty_like(weight), torch.empty_like(weight)
+    else:
+        dw, db = torch.empty((2, cols), dtype=wt, device=dy.device).unbind(0)
+    wkp, wkb, work = _work(work, layer_norm_workspace(rows, cols), dy)
     ckm._check(ckm.lib().ckm_layer_norm_backward_async(
-        _TYPES[dy.dtype], _TYPES[wt], rows, cols, dyp, lddy, hp, ldh, stats.data_ptr(), wp, rp, ldr,
-        _drop_ptr(drop, device), op, ldo, dx.data_ptr() if drop is not None else None, cols, dwp,
-        dwp + cols * dw.element_size(), wkp, wkb, sp))
-    return dx, dh, dw[0], dw[1]
+        _TYPES[dtype], _TYPES[wt], rows, cols, dyp, lddy, hp, ldh, stats.data_ptr(), wp, rp, ldr,
+        _drop_ptr(drop, device), op, ldo, xp, cols, dw.data_ptr(), db.data_ptr(), wkp, wkb, _raw_stream(device)))
+    return dx, dh, dw, db
 
 
+@functools.lru_cache(maxsize=1024)
 def layer_norm_workspace(rows: int, cols: int) -> int:
     """Bytes of work buffer that layer_norm_backward needs (ckm_layer_norm_workspace_size)."""
     out = C.c_size_t()
@@ -243,11 +273,31 @@ def layer_norm_workspace(rows: int, cols: int) -> int:
     return out.value
 
 
-def _work(work, device):
-    _tensor(work, "work", torch.uint8, device)
-    if not work.is_contiguous():
-        raise ValueError("work must be contiguous")
-    return work.data_ptr(), work.numel()
+@functools.lru_cache(maxsize=1024)
+def softmax_workspace(batch: int, heads: int, queries: int, keys: int) -> int:
+    """Bytes of work buffer that softmax and softmax_backward need (ckm_softmax_workspace_size)."""
+    out = C.c_size_t()
+    ckm._check(ckm.lib().ckm_softmax_workspace_size(C.byref(_Scores(batch, heads, queries, keys)), C.byref(out)))
+    return out.value
+
+
+def _stats(stats, shape, device):
+    _tensor(stats, "stats", torch.float32, device)
+    if stats.shape != shape[:-1] + (2,) or not stats.is_contiguous():
+        raise ValueError("stats must be contiguous of shape %s, got %s" % (tuple(shape[:-1]) + (2,), tuple(stats.shape)))
+
+
+def _work(work, need: int, like):
+    """(pointer, bytes, tensor) of the caller's work buffer, or of one made for the call on its stream."""
+    if work is None:
+        if not need:
+            return None, 0, None
+        work = torch.empty(need, dtype=torch.uint8, device=like.device)
+    else:
+        _tensor(work, "work", torch.uint8, like.get_device())
+        if not work.is_contiguous():
+            raise ValueError("work must be contiguous")
+    return work.data_ptr(), work.numel(), work
 
 
 def _strides(t, name: str, shape, dtype, device):
@@ -288,16 +338,9 @@ def _scores(scores, scale, causal, lengths, mask):
     return c, device
 
 
-def _scores_work(c, work, tensor, device):
-    need = C.c_size_t()
-    ckm._check(ckm.lib().ckm_softmax_workspace_size(C.byref(c), C.byref(need)))
-    if work is None and need.value:
-        work = torch.empty(need.value, dtype=torch.uint8, device=tensor.device)
-    return (work,) + ((None, 0) if work is None else _work(work, device))
-
-
+@_on_stream
 def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask=None, drop: Dropout = None, out=None,
-            work=None, stream=None):
+            work=None):
     """(probabilities, stats) of attention scores [batch, heads, queries, keys] (ckm_softmax_async).
 
     Fewer dimensions stand for leading ones of 1. lengths: int32 [batch], the
@@ -305,36 +348,41 @@ def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask
     queries. mask: bool or uint8 (0 hides a key) or of the scores' type (added
     after the scale; -inf hides), broadcast to the scores. A row that sees
     nothing gives zeros. stats: float32 [..., queries, 2], the largest logit
-    and 1 / the sum of exponentials. out: for the probabilities; may be scores."""
+    and 1 / the sum of exponentials. out: for the probabilities; may be scores.
+    work: a uint8 device buffer of softmax_workspace(...) bytes to use."""
     c, device = _scores(scores, scale, causal, lengths, mask)
-    sp, ctx = _stream(stream)
-    with ctx:
-        y = torch.empty(scores.shape, dtype=scores.dtype, device=scores.device) if out is None else out
-        stats = torch.empty(scores.shape[:-1] + (2,), dtype=torch.float32, device=scores.device)
-        work, wp, wb = _scores_work(c, work, scores, device)
-    xp, xs = _strides(scores, "scores", scores.shape, scores.dtype, device)
-    yp, ys = _strides(y, "out", scores.shape, scores.dtype, device)
-    ckm._check(ckm.lib().ckm_softmax_async(_TYPES[scores.dtype], C.byref(c), xp, xs, _drop_ptr(drop, device), yp, ys,
-                                           stats.data_ptr(), wp, wb, sp))
+    shape, dtype = scores.shape, scores.dtype
+    xp, xs = _strides(scores, "scores", shape, dtype, device)
+    if out is None:
+        y = _like(scores)
+        yp, ys = y.data_ptr(), _Stride(c.heads * c.queries * c.keys, c.queries * c.keys, c.keys)
+    else:
+        y = out
+        yp, ys = _strides(y, "out", shape, dtype, device)
+    stats = torch.empty(shape[:-1] + (2,), dtype=torch.float32, device=scores.device)
+    wp, wb, work = _work(work, softmax_workspace(c.batch, c.heads, c.queries, c.keys), scores)
+    ckm._check(ckm.lib().ckm_softmax_async(_TYPES[dtype], C.byref(c), xp, xs, _drop_ptr(drop, device), yp, ys,
+                                           stats.data_ptr(), wp, wb, _raw_stream(device)))
     return y, stats
 
 
+@_on_stream
 def softmax_backward(dy, scores, stats, scale: float = 1.0, causal: bool = False, lengths=None, mask=None,
-                     drop: Dropout = None, out=None, work=None, stream=None):
+                     drop: Dropout = None, out=None, work=None):
     """The scores' gradient (ckm_softmax_backward_async): the forward call's scores, stats, masks and drop.
     out: may be dy or scores."""
     c, device = _scores(scores, scale, causal, lengths, mask)
-    _tensor(stats, "stats", torch.float32, device)
-    if stats.shape != scores.shape[:-1] + (2,) or not stats.is_contiguous():
-        raise ValueError("stats must be contiguous of shape %s, got %s"
-                         % (tuple(scores.shape[:-1]) + (2,), tuple(stats.shape)))
-    sp, ctx = _stream(stream)
-    with ctx:
-        dx = torch.empty(scores.shape, dtype=scores.dtype, device=scores.device) if out is None else out
-        work, wp, wb = _scores_work(c, work, scores, device)
-    gp, gs = _strides(dy, "dy", scores.shape, scores.dtype, device)
-    xp, xs = _strides(scores, "scores", scores.shape, scores.dtype, device)
-    op, os_ = _strides(dx, "out", scores.shape, scores.dtype, device)
-    ckm._check(ckm.lib().ckm_softmax_backward_async(_TYPES[scores.dtype], C.byref(c), gp, gs, xp, xs, stats.data_ptr(),
-                                                    _drop_ptr(drop, device), op, os_, wp, wb, sp))
+    shape, dtype = scores.shape, scores.dtype
+    _stats(stats, shape, device)
+    gp, gs = _strides(dy, "dy", shape, dtype, device)
+    xp, xs = _strides(scores, "scores", shape, dtype, device)
+    if out is None:
+        dx = _like(scores)
+        op, os_ = dx.data_ptr(), _Stride(c.heads * c.queries * c.keys, c.queries * c.keys, c.keys)
+    else:
+        dx = out
+        op, os_ = _strides(dx, "out", shape, dtype, device)
+    wp, wb, work = _work(work, softmax_workspace(c.batch, c.heads, c.queries, c.keys), scores)
+    ckm._check(ckm.lib().ckm_softmax_backward_async(_TYPES[dtype], C.byref(c), gp, gs, xp, xs, stats.data_ptr(),
+                                                    _drop_ptr(drop, device), op, os_, wp, wb, _raw_stream(device)))
     return dx
