@@ -66,7 +66,7 @@ constexpr int norm_block(int lanes) { return lanes < 256 ? 256 : lanes; }
 // with four they are read again for each row (from the caches).
 constexpr bool keep_weights(int per) { return per <= 2; }
 
-template <typename T, int kLanes, int kPer, bool kFused>
+template <typename T, int kLanes, int kPer, bool kFused, bool kEven>
 __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a) {
   constexpr int kBlock = norm_block(kLanes), kRowsAt = kBlock / kLanes;   // rows of a block at a time
   __shared__ float lds[kLanes > 64 ? 2 * kBlock / 64 : 1];
@@ -85,25 +85,30 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
   for (int64_t first = (int64_t)blockIdx.x * kRowsAt; first < a.rows; first += (int64_t)gridDim.x * kRowsAt) {
     const int64_t row = first + threadIdx.x / kLanes;
     const bool live = row < a.rows;
+    // every load of the row first, then the arithmetic
+    Raw8<T> r[kPer], rr[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int col = (lane + i * kLanes) * kVec, left = live ? a.cols - col : 0;
+      r[i] = zero_group<T>();
+      if (left > 0) r[i] = load_part<kEven>((const T*)a.x + row * a.ld_x + col, left);
+      if constexpr (kFused) {
+        rr[i] = zero_group<T>();
+        if (a.res && left > 0) rr[i] = load_part<kEven>((const T*)a.res + row * a.ld_res + col, left);
+      }
+    }
     float v[kPer][kVec];
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int group = lane + i * kLanes, col = group * kVec;
-      const int left = live ? a.cols - col : 0;
-      Raw8<T> r = zero_group<T>(), rr = zero_group<T>();
-      if (left > 0) {
-        r = load_group((const T*)a.x + row * a.ld_x + col, left);
-        if constexpr (kFused)
-          if (a.res) rr = load_group((const T*)a.res + row * a.ld_res + col, left);
-      }
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) v[i][j] = (float)r.e[j];
+      for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].e[j];
       if constexpr (kFused) {
+        const int group = lane + i * kLanes, col = group * kVec, left = live ? a.cols - col : 0;
         if (a.drop.on) drop8(v[i], a.drop, site, group, (uint32_t)row);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) v[i][j] = as_stored<T>(v[i][j] + (float)rr.e[j]);
-        if (a.h && left > 0) store_group((T*)a.h + row * a.ld_h + col, v[i], left);
+        for (int j = 0; j < kVec; ++j) v[i][j] = as_stored<T>(v[i][j] + (float)rr[i].e[j]);
+        if (a.h && left > 0) store_part<kEven>((T*)a.h + row * a.ld_h + col, v[i], left);
       }
 #pragma unroll
       for (int j = 0; j < kVec; ++j) sum += v[i][j];
@@ -115,8 +120,8 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
       const int left = a.cols - (lane + i * kLanes) * kVec;
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const float d = j < left ? v[i][j] - mean : 0.0f;
-        sq += d * d;
+        const float d = (kEven ? left > 0 : j < left) ? v[i][j] - mean : 0.0f;
+        sq = fmaf(d, d, sq);
       }
     }
     const float rstd = 1.0f / sqrtf(reduce_row<OpSum, kLanes, kBlock>(sq, lds, 1) / (float)a.cols + a.eps);
@@ -136,8 +141,8 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
         }
         float o[kVec];
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) o[j] = (v[i][j] - mean) * rstd * w[k][j] + b[k][j];
-        store_group((T*)a.y + row * a.ld_y + col, o, left);
+        for (int j = 0; j < kVec; ++j) o[j] = fmaf((v[i][j] - mean) * rstd, w[k][j], b[k][j]);
+        store_part<kEven>((T*)a.y + row * a.ld_y + col, o, left);
       }
     }
   }
@@ -175,21 +180,21 @@ __device__ __forceinline__ void store_weight(void* p, bool w32, int col, float v
   if (w32)
     ((float*)p)[col] = v;
   else
-    ((T*)p)[col] = (T)v;
+    ((T*)p)[col] = rounded<T>(v);
 }
 
 // The gradient of the norm's input, o: rounds and stores it as dh
 // and, through the dropout, as dx (of the rounded dh, which other nodes see).
-template <typename T>
+template <typename T, bool kEven>
 __device__ __forceinline__ void finish_grad(const NormGradArgs& a, DropSite site, int64_t row, int group,
                                             float (&o)[kVec], int left) {
   const int col = group * kVec;
-  if (a.dh) store_group((T*)a.dh + row * a.ld_dh + col, o, left);
+  if (a.dh) store_part<kEven>((T*)a.dh + row * a.ld_dh + col, o, left);
   if (a.dx) {
 #pragma unroll
     for (int j = 0; j < kVec; ++j) o[j] = as_stored<T>(o[j]);
     if (a.drop.on) drop8(o, a.drop, site, group, (uint32_t)row);
-    store_group((T*)a.dx + row * a.ld_dx + col, o, left);
+    store_part<kEven>((T*)a.dx + row * a.ld_dx + col, o, left);
   }
 }
 // A block's sum over its rows for one column (which 0: dw, 1: db): the result
@@ -211,7 +216,7 @@ constexpr int grad_block(int lanes) { return lanes < 512 ? 512 : lanes; }
 // its columns' sums of dy xh and dy in registers; at the end its row sets join
 // through LDS in a fixed order, and ckm_norm_join_kernel adds the blocks' sums
 // in a fixed order, so the weights' gradients do not depend on scheduling.
-template <typename T, int kLanes, int kPer>
+template <typename T, int kLanes, int kPer, bool kEven>
 __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormGradArgs a) {
   constexpr int kBlock = grad_block(kLanes), kRowsAt = kBlock / kLanes;
   __shared__ float lds[kLanes > 64 ? 4 * kBlock / 64 : 1];
@@ -219,11 +224,13 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
   const int lane = threadIdx.x % kLanes;
   const DropSite site = drop_site(a.drop);
   int turn = 0;
-  float w[kPer][kVec], dw[kPer][kVec], db[kPer][kVec];
+  // a block of 1024 threads has no registers for two groups' weights
+  constexpr bool kKeep = kPer == 1 || kLanes < 1024;
+  float w[kKeep ? kPer : 1][kVec], dw[kPer][kVec], db[kPer][kVec];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int col = (lane + i * kLanes) * kVec;
-    weight_group<T>(w[i], a.w, a.w32, col, a.cols - col, 1.0f);
+    if constexpr (kKeep) weight_group<T>(w[i], a.w, a.w32, col, a.cols - col, 1.0f);
 #pragma unroll
     for (int j = 0; j < kVec; ++j) dw[i][j] = db[i][j] = 0.0f;
   }
@@ -231,28 +238,33 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
     const int64_t row = first + threadIdx.x / kLanes;
     const bool live = row < a.rows;
     const float mean = live ? a.stats[2 * row] : 0.0f, rstd = live ? a.stats[2 * row + 1] : 0.0f;
-    float g[kPer][kVec], xh[kPer][kVec];
-    Raw8<T> past[kPer];
-    float s1 = 0.0f, s2 = 0.0f;
+    // the row is held in its own type, and its products are made twice: registers
+    // are what limits the waves here
+    Raw8<T> rd[kPer], rh[kPer], past[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec, left = live ? a.cols - col : 0;
-      Raw8<T> rd = zero_group<T>(), rh = zero_group<T>();
-      past[i] = zero_group<T>();
+      rd[i] = rh[i] = past[i] = zero_group<T>();
       if (left > 0) {
-        rd = load_group((const T*)a.dy + row * a.ld_dy + col, left);
-        rh = load_group((const T*)a.h + row * a.ld_h + col, left);
-        if (a.dres) past[i] = load_group((const T*)a.dres + row * a.ld_dres + col, left);
+        rd[i] = load_part<kEven>((const T*)a.dy + row * a.ld_dy + col, left);
+        rh[i] = load_part<kEven>((const T*)a.h + row * a.ld_h + col, left);
+        if (a.dres) past[i] = load_part<kEven>((const T*)a.dres + row * a.ld_dres + col, left);
       }
+    }
+    float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int k = kKeep ? i : 0, left = live ? a.cols - (lane + i * kLanes) * kVec : 0;
+      if constexpr (!kKeep) weight_group<T>(w[0], a.w, a.w32, (lane + i * kLanes) * kVec, left, 1.0f);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const float d = (float)rd.e[j];
-        xh[i][j] = j < left ? ((float)rh.e[j] - mean) * rstd : 0.0f;
-        dw[i][j] += d * xh[i][j];
+        const float d = (float)rd[i].e[j];
+        const float xh = (kEven ? left > 0 : j < left) ? ((float)rh[i].e[j] - mean) * rstd : 0.0f;
+        const float g = d * w[k][j];
+        dw[i][j] = fmaf(d, xh, dw[i][j]);
         db[i][j] += d;
-        g[i][j] = d * w[i][j];
-        s1 += g[i][j];
-        s2 += g[i][j] * xh[i][j];
+        s1 += g;
+        s2 = fmaf(g, xh, s2);
       }
     }
     reduce_two<kLanes, kBlock>(s1, s2, lds, turn);
@@ -264,10 +276,15 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
     for (int i = 0; i < kPer; ++i) {
       const int group = lane + i * kLanes, col = group * kVec, left = a.cols - col;
       if (left <= 0) continue;
+      const int k = kKeep ? i : 0;
+      if constexpr (!kKeep) weight_group<T>(w[0], a.w, a.w32, col, left, 1.0f);
       float o[kVec];
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) o[j] = rstd * (g[i][j] - s1 - xh[i][j] * s2) + (float)past[i].e[j];
-      finish_grad<T>(a, site, row, group, o, left);
+      for (int j = 0; j < kVec; ++j) {
+        const float xh = ((float)rh[i].e[j] - mean) * rstd;
+        o[j] = fmaf(rstd, fmaf(-xh, s2, (float)rd[i].e[j] * w[k][j] - s1), (float)past[i].e[j]);
+      }
+      finish_grad<T, kEven>(a, site, row, group, o, left);
     }
   }
   if (!a.dw && !a.db) return;
@@ -353,7 +370,7 @@ __global__ void __launch_bounds__(1024) ckm_norm_wide_sums_kernel(NormGradArgs a
       for (int j = 0; j < kVec; ++j) {
         const float g = (float)rd.e[j] * w[j];
         s1 += g;
-        s2 += j < left ? g * (((float)rh.e[j] - mean) * rstd) : 0.0f;
+        s2 = j < left ? fmaf(g, ((float)rh.e[j] - mean) * rstd, s2) : s2;
       }
     }
     reduce_two<1024, 1024>(s1, s2, lds, turn);
@@ -382,11 +399,11 @@ __global__ void __launch_bounds__(256) ckm_norm_wide_grad_kernel(NormGradArgs a,
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
       const float d = (float)rd.e[j], xh = ((float)rh.e[j] - mean) * rstd;
-      dw[j] += d * xh;
+      dw[j] = fmaf(d, xh, dw[j]);
       db[j] += d;
-      o[j] = rstd * (d * w[j] - s1 - xh * s2) + (float)past.e[j];
+      o[j] = fmaf(rstd, fmaf(-xh, s2, d * w[j] - s1), (float)past.e[j]);
     }
-    finish_grad<T>(a, site, row, group, o, left);
+    finish_grad<T, false>(a, site, row, group, o, left);
   }
   if (!a.dw && !a.db) return;
   const int width = padded_cols(a.cols);
@@ -407,11 +424,12 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 template <typename T, int kLanes, int kPer>
 void launch_norm_as(const NormArgs& a, bool fused, hipStream_t s) {
   constexpr int kBlock = norm_block(kLanes), kRowsAt = kBlock / kLanes;
-  const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, kRowsAt), 256 * (2048 / kBlock));
-  if (fused)
-    ckm_norm_kernel<T, kLanes, kPer, true><<<dim3((uint32_t)blocks), kBlock, 0, s>>>(a);
-  else
-    ckm_norm_kernel<T, kLanes, kPer, false><<<dim3((uint32_t)blocks), kBlock, 0, s>>>(a);
+  const dim3 grid((uint32_t)std::min<int64_t>(ceil_div(a.rows, kRowsAt), 256 * (2048 / kBlock)));
+  const bool even = a.cols % kVec == 0;
+  if (fused && even) ckm_norm_kernel<T, kLanes, kPer, true, true><<<grid, kBlock, 0, s>>>(a);
+  else if (fused) ckm_norm_kernel<T, kLanes, kPer, true, false><<<grid, kBlock, 0, s>>>(a);
+  else if (even) ckm_norm_kernel<T, kLanes, kPer, false, true><<<grid, kBlock, 0, s>>>(a);
+  else ckm_norm_kernel<T, kLanes, kPer, false, false><<<grid, kBlock, 0, s>>>(a);
 }
 
 template <typename T>
@@ -422,7 +440,7 @@ void launch_norm(const NormArgs& a, bool fused, hipStream_t s) {
   else if (groups <= 128) launch_norm_as<T, 64, 2>(a, fused, s);
   else if (groups <= 256) launch_norm_as<T, 256, 1>(a, fused, s);
   else if (groups <= 512) launch_norm_as<T, 256, 2>(a, fused, s);
-  else if (groups <= 1024) launch_norm_as<T, 256, 4>(a, fused, s);
+  else if (groups <= 1024) launch_norm_as<T, 512, 2>(a, fused, s);
   else if (groups <= 2048) launch_norm_as<T, 1024, 2>(a, fused, s);
   else launch_norm_as<T, 1024, 4>(a, fused, s);
 }
@@ -460,23 +478,32 @@ size_t grad_workspace(int64_t rows, int64_t cols) {
   return bytes;
 }
 
+template <typename T, int kLanes, int kPer>
+void launch_grad_as(const NormGradArgs& a, int64_t blocks, hipStream_t s) {
+  constexpr int kBlock = grad_block(kLanes);
+  const dim3 grid((uint32_t)blocks);
+  if (a.cols % kVec == 0)
+    ckm_norm_grad_kernel<T, kLanes, kPer, true><<<grid, kBlock, 0, s>>>(a);
+  else
+    ckm_norm_grad_kernel<T, kLanes, kPer, false><<<grid, kBlock, 0, s>>>(a);
+}
+
 template <typename T>
 void launch_grad(NormGradArgs a, void* work, hipStream_t s) {
   const GradPlan p = grad_plan(a.rows, a.cols);
   a.part = (float*)work;
-  const dim3 grid((uint32_t)p.blocks);
   if (p.lanes == 0) {
     float* sums = (float*)work + (p.blocks > 1 ? (size_t)p.blocks * 2 * padded_cols(a.cols) : 0);
     if (a.rows > 0)
       ckm_norm_wide_sums_kernel<T><<<dim3((uint32_t)std::min<int64_t>(a.rows, 2048)), 1024, 0, s>>>(a, sums);
     ckm_norm_wide_grad_kernel<T><<<dim3((uint32_t)ceil_div(a.cols, 256 * kVec), (uint32_t)p.blocks), 256, 0, s>>>(a, sums);
-  } else if (p.lanes == 16) ckm_norm_grad_kernel<T, 16, 1><<<grid, grad_block(16), 0, s>>>(a);
-  else if (p.lanes == 64 && p.per == 1) ckm_norm_grad_kernel<T, 64, 1><<<grid, grad_block(64), 0, s>>>(a);
-  else if (p.lanes == 64) ckm_norm_grad_kernel<T, 64, 2><<<grid, grad_block(64), 0, s>>>(a);
-  else if (p.lanes == 256) ckm_norm_grad_kernel<T, 256, 1><<<grid, grad_block(256), 0, s>>>(a);
-  else if (p.lanes == 512) ckm_norm_grad_kernel<T, 512, 1><<<grid, grad_block(512), 0, s>>>(a);
-  else if (p.per == 1) ckm_norm_grad_kernel<T, 1024, 1><<<grid, grad_block(1024), 0, s>>>(a);
-  else ckm_norm_grad_kernel<T, 1024, 2><<<grid, grad_block(1024), 0, s>>>(a);
+  } else if (p.lanes == 16) launch_grad_as<T, 16, 1>(a, p.blocks, s);
+  else if (p.lanes == 64 && p.per == 1) launch_grad_as<T, 64, 1>(a, p.blocks, s);
+  else if (p.lanes == 64) launch_grad_as<T, 64, 2>(a, p.blocks, s);
+  else if (p.lanes == 256) launch_grad_as<T, 256, 1>(a, p.blocks, s);
+  else if (p.lanes == 512) launch_grad_as<T, 512, 1>(a, p.blocks, s);
+  else if (p.per == 1) launch_grad_as<T, 1024, 1>(a, p.blocks, s);
+  else launch_grad_as<T, 1024, 2>(a, p.blocks, s);
   if (p.blocks > 1 && (a.dw || a.db))
     ckm_norm_join_kernel<T><<<dim3((uint32_t)ceil_div(a.cols, 32), 2), 256, 0, s>>>(a.part, (int)p.blocks, a.cols, a.w32,
                                                                                    a.dw, a.db);

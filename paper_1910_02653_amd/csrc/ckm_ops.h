@@ -10,9 +10,15 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <type_traits>
 
 #include "ckm.h"
 #include "ckm_internal.h"
+
+// Products and sums are fused where the code says so (fmaf) and nowhere else: an
+// operator then gives the same bits in each of its kernels' forms, and one with a
+// dropout or a residual inside the bits of the operators one after the other.
+#pragma clang fp contract(off)
 
 namespace ckm {
 
@@ -71,12 +77,29 @@ __device__ __forceinline__ Raw8<T> zero_group() {
   for (int j = 0; j < kVec; ++j) r.e[j] = (T)0;
   return r;
 }
+// The same for rows whose length is a multiple of eight (kEven): a group lies in
+// the row whole or not at all.
+template <bool kEven, typename T>
+__device__ __forceinline__ Raw8<T> load_part(const T* p, int left) {
+  if constexpr (kEven)
+    return load8(p);
+  else
+    return load_group(p, left);
+}
+// v rounded to T, nearest even. For binary16 the empty statement keeps the compiler
+// from fusing the conversion with a product before it, which rounds once and not
+// twice: it does that for some elements of a kernel and not for others.
+template <typename T>
+__device__ __forceinline__ T rounded(float v) {
+  if constexpr (std::is_same<T, _Float16>::value) asm("" : "+v"(v));
+  return (T)v;
+}
 // Rounds to T (nearest even) and stores the elements that lie in the row.
 template <typename T>
 __device__ __forceinline__ void store_group(T* p, const float (&v)[kVec], int left) {
   Raw8<T> r;
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) r.e[j] = (T)v[j];
+  for (int j = 0; j < kVec; ++j) r.e[j] = rounded<T>(v[j]);
   if (left >= kVec) {
     __builtin_memcpy(p, &r, sizeof(r));
   } else {
@@ -85,10 +108,14 @@ __device__ __forceinline__ void store_group(T* p, const float (&v)[kVec], int le
       if (j < left) p[j] = r.e[j];
   }
 }
+template <bool kEven, typename T>
+__device__ __forceinline__ void store_part(T* p, const float (&v)[kVec], int left) {
+  store_group(p, v, kEven ? kVec : left);
+}
 // v rounded to T and back: what a reader of the stored value sees.
 template <typename T>
 __device__ __forceinline__ float as_stored(float v) {
-  return (float)(T)v;
+  return (float)rounded<T>(v);
 }
 
 // Philox4x32-10 (Salmon et al., SC'11) of counter (group, row, site), the
@@ -108,10 +135,6 @@ __device__ __forceinline__ uint32_t drop_xor3(uint32_t a, uint32_t b, uint32_t c
 // Applies the dropout to the group's eight values: dropped ones become 0
 // whatever they hold, NaN and infinities too.
 __device__ __forceinline__ void drop8(float (&v)[kVec], const DropArgs& d, DropSite s, uint32_t group, uint32_t row) {
-  // the product is rounded by itself in every operator (not fused with a sum that
-  // follows), so that an operator with a dropout inside gives the bits of the two
-  // operators one after the other
-#pragma clang fp contract(off)
   uint32_t c0 = group, c1 = row, c2 = s.s0, c3 = s.s1, k0 = d.k0, k1 = d.k1;
 #pragma unroll
   for (int r = 0; r < 10; ++r) {

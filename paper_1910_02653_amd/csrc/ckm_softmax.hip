@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
 #pragma unroll
           for (int j = 0; j < kVec; ++j) {
             t[i][j] = exp_of(t[i][j], m) * z;
-            sum += t[i][j] * g[i][j];
+            sum = fmaf(t[i][j], g[i][j], sum);
           }
         } else {
 #pragma unroll
@@ -242,7 +242,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxA
         logits8(t, a, x, r, col, r.seen - col);
         grads8(g, a, site, dy, t, row, col, r.seen - col);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) sum += exp_of(t[j], m) * z * g[j];
+        for (int j = 0; j < kVec; ++j) sum = fmaf(exp_of(t[j], m) * z, g[j], sum);
       }
       sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum, lds, turn);
       turn ^= 1;
