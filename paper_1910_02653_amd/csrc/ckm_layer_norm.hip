@@ -210,7 +210,7 @@ __device__ __forceinline__ void put_sum(const NormGradArgs& a, bool only, float*
   }
 }
 
-constexpr int grad_block(int lanes) { return lanes < 512 ? 512 : lanes; }
+constexpr int grad_block(int lanes) { return 1024; }
 
 // One pass over dy and h. A block takes every gridDim-th set of rows and keeps
 // its columns' sums of dy xh and dy in registers; at the end its row sets join
@@ -467,7 +467,7 @@ GradPlan grad_plan(int64_t rows, int64_t cols) {
   else if (groups <= 1024) p = {1024, 1, 0};
   else p = {1024, 2, 0};
   const int at = grad_block(p.lanes) / p.lanes;
-  p.blocks = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, at), 256 * (1024 / grad_block(p.lanes))));
+  p.blocks = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, at), 256));
   return p;
 }
 
