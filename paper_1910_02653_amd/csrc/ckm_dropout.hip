@@ -2,6 +2,12 @@
 // y = r + D(x), D(x) = x 65536 / keep where the element's draw is below keep,
 // else 0. Its gradient is the same map of dy, so one kernel serves both, and
 // the mask exists only in registers.
+//
+// Bound by memory: each element is read once and written once, and the draws,
+// about 50 instructions for eight elements, hide behind that. A thread takes one
+// group of eight; two and four groups a thread, their loads first, were slower at
+// every size (bf16 16384x8192: 91, 96, 100 us; f16 4096x4096 with a residual
+// 17, 20, 20). bf16 16384x8192 moves 5.9 TB/s, where a large copy moves 5.2.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -15,49 +21,43 @@ namespace {
 
 constexpr int kDropBlock = 256;
 
-// Groups are numbered row by row, `groups` to a row. A block takes kPer x 256
+// Groups are numbered row by row, `groups` to a row. A block takes 256
 // consecutive ones at a time; the division by `groups` is made once for the
 // block's first group, and a thread's place follows from it without one: with
 // magic = floor(2^32 / groups) + 1, q = hi(at * magic) is exact for at * groups
-// < 2^32 and groups > 1; where a row holds two shares or more, a share crosses one
-// row border at most (magic 0).
-template <typename T, int kPer, bool kRes>
+// < 2^32 and groups > 1; where a row holds 512 groups or more, a block crosses one
+// row border at most (magic 0). kFlat: rows of whole groups without gaps, so that
+// a group's number is its address and the loads need not wait for its place.
+template <typename T, bool kRes, bool kFlat>
 __global__ void __launch_bounds__(kDropBlock) ckm_dropout_kernel(int64_t total, uint32_t groups, uint32_t magic,
                                                                  int32_t cols, const T* x, int64_t ld_x, const T* res,
                                                                  int64_t ld_res, DropArgs drop, T* y, int64_t ld_y) {
   const DropSite site = drop_site(drop);
-  for (int64_t base = (int64_t)blockIdx.x * (kPer * kDropBlock); base < total;
-       base += (int64_t)gridDim.x * (kPer * kDropBlock)) {
+  for (int64_t base = (int64_t)blockIdx.x * kDropBlock; base < total; base += (int64_t)gridDim.x * kDropBlock) {
+    const int64_t g = base + threadIdx.x;
     const int64_t row0 = base / groups;
-    const uint32_t at0 = (uint32_t)(base - row0 * groups);
-    Raw8<T> vx[kPer], vr[kPer];
-    uint32_t col[kPer];
-    int64_t row[kPer];
+    const uint32_t at = (uint32_t)(base - row0 * groups) + threadIdx.x;
+    const uint32_t q = groups == 1 ? at : magic ? __umulhi(at, magic) : (at >= groups ? 1u : 0u);
+    const uint32_t group = at - q * groups;
+    const int64_t row = row0 + q;
+    if (g >= total) continue;
+    const int left = kFlat ? kVec : cols - (int)(group * kVec);
+    const int64_t ox = kFlat ? g * kVec : row * ld_x + group * kVec;
+    const Raw8<T> vx = load_part<kFlat>(x + ox, left);
+    float v[kVec];
+    if constexpr (kRes) {
+      const Raw8<T> vr = load_part<kFlat>(res + (kFlat ? ox : row * ld_res + group * kVec), left);
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const uint32_t at = at0 + i * kDropBlock + threadIdx.x;
-      const uint32_t q = groups == 1 ? at : magic ? __umulhi(at, magic) : (at >= groups ? 1u : 0u);
-      row[i] = row0 + q;
-      col[i] = at - q * groups;
-      if (base + i * kDropBlock + threadIdx.x < total) {
-        const int left = cols - (int)col[i] * kVec;
-        vx[i] = load_group(x + row[i] * ld_x + col[i] * kVec, left);
-        if constexpr (kRes) vr[i] = load_group(res + row[i] * ld_res + col[i] * kVec, left);
-      }
+      for (int j = 0; j < kVec; ++j) v[j] = (float)vx.e[j];
+      if (drop.on) drop8(v, drop, site, group, (uint32_t)row);
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) v[j] += (float)vr.e[j];
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) v[j] = (float)vx.e[j];
+      if (drop.on) drop8(v, drop, site, group, (uint32_t)row);
     }
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      if (base + i * kDropBlock + threadIdx.x >= total) continue;
-      float v[kVec];
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) v[j] = (float)vx[i].e[j];
-      if (drop.on) drop8(v, drop, site, col[i], (uint32_t)row[i]);
-      if constexpr (kRes) {
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) v[j] += (float)vr[i].e[j];
-      }
-      store_group(y + row[i] * ld_y + col[i] * kVec, v, cols - (int)col[i] * kVec);
-    }
+    store_part<kFlat>(y + (kFlat ? ox : row * ld_y + group * kVec), v, left);
   }
 }
 
@@ -66,26 +66,18 @@ void launch_dropout(int64_t rows, int64_t cols, const void* x, int64_t ld_x, con
                     const DropArgs& drop, void* y, int64_t ld_y, hipStream_t stream) {
   const uint32_t groups = (uint32_t)((cols + kVec - 1) / kVec);
   const int64_t total = rows * groups;
-  constexpr int64_t kMaxBlocks = 1 << 20;
-  const auto go = [&](auto per, auto with_res) {
-    constexpr int kPer = decltype(per)::value;
-    constexpr bool kRes = decltype(with_res)::value;
-    constexpr int64_t kShare = kPer * kDropBlock;
-    const uint32_t magic = groups == 1 || groups >= 2 * kShare ? 0u : (uint32_t)((((uint64_t)1 << 32) / groups) + 1);
-    const int64_t blocks = std::min<int64_t>((total + kShare - 1) / kShare, kMaxBlocks);
-    ckm_dropout_kernel<T, kPer, kRes><<<dim3((uint32_t)blocks), kDropBlock, 0, stream>>>(
+  const uint32_t magic = groups == 1 || groups >= 2 * kDropBlock ? 0u : (uint32_t)((((uint64_t)1 << 32) / groups) + 1);
+  const dim3 grid((uint32_t)std::min<int64_t>((total + kDropBlock - 1) / kDropBlock, 1 << 20));
+  const auto go = [&](auto with_res, auto flat) {
+    ckm_dropout_kernel<T, decltype(with_res)::value, decltype(flat)::value><<<grid, kDropBlock, 0, stream>>>(
         total, groups, magic, (int32_t)cols, (const T*)x, ld_x, (const T*)res, ld_res, drop, (T*)y, ld_y);
   };
-  const auto by_size = [&](auto with_res) {
-    if (total <= 4 * kDropBlock * 256)
-      go(std::integral_constant<int, 1>{}, with_res);
-    else
-      go(std::integral_constant<int, 4>{}, with_res);
-  };
-  if (res)
-    by_size(std::true_type{});
-  else
-    by_size(std::false_type{});
+  const bool flat =
+      cols % kVec == 0 && (rows == 1 || (ld_x == cols && ld_y == cols && (!res || ld_res == cols)));
+  if (res && flat) go(std::true_type{}, std::true_type{});
+  else if (res) go(std::true_type{}, std::false_type{});
+  else if (flat) go(std::false_type{}, std::true_type{});
+  else go(std::false_type{}, std::false_type{});
 }
 
 }  // namespace
