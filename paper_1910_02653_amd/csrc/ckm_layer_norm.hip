@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
     }
   }
   for (int64_t first = (int64_t)blockIdx.x * kRowsAt; first < a.rows; first += (int64_t)gridDim.x * kRowsAt) {
-    const int64_t row = first + threadIdx.x / kLanes;
+    const int64_t row = first + row_in_block<kLanes>();
     const bool live = row < a.rows;
     // every load of the row first, then the arithmetic
     Raw8<T> r[kPer], rr[kPer];
@@ -235,7 +235,7 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
     for (int j = 0; j < kVec; ++j) dw[i][j] = db[i][j] = 0.0f;
   }
   for (int64_t first = (int64_t)blockIdx.x * kRowsAt; first < a.rows; first += (int64_t)gridDim.x * kRowsAt) {
-    const int64_t row = first + threadIdx.x / kLanes;
+    const int64_t row = first + row_in_block<kLanes>();
     const bool live = row < a.rows;
     const float mean = live ? a.stats[2 * row] : 0.0f, rstd = live ? a.stats[2 * row + 1] : 0.0f;
     // the row is held in its own type, and its products are made twice: registers

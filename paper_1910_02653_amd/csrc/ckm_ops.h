@@ -132,9 +132,8 @@ __device__ __forceinline__ DropSite drop_site(const DropArgs& d) {
 __device__ __forceinline__ uint32_t drop_xor3(uint32_t a, uint32_t b, uint32_t c) {
   return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);   // truth table of a ^ b ^ c
 }
-// Applies the dropout to the group's eight values: dropped ones become 0
-// whatever they hold, NaN and infinities too.
-__device__ __forceinline__ void drop8(float (&v)[kVec], const DropArgs& d, DropSite s, uint32_t group, uint32_t row) {
+// The group's eight draws, two to a word, low half first.
+__device__ __forceinline__ void draws8(uint32_t (&x)[4], const DropArgs& d, DropSite s, uint32_t group, uint32_t row) {
   uint32_t c0 = group, c1 = row, c2 = s.s0, c3 = s.s1, k0 = d.k0, k1 = d.k1;
 #pragma unroll
   for (int r = 0; r < 10; ++r) {
@@ -149,12 +148,31 @@ __device__ __forceinline__ void drop8(float (&v)[kVec], const DropArgs& d, DropS
     k0 += 0x9E3779B9u;
     k1 += 0xBB67AE85u;
   }
-  const uint32_t x[4] = {c0, c1, c2, c3};
+  x[0] = c0;
+  x[1] = c1;
+  x[2] = c2;
+  x[3] = c3;
+}
+__device__ __forceinline__ bool kept(const uint32_t (&x)[4], int j, uint32_t keep) {
+  return ((j & 1) ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu) < keep;
+}
+// Applies the dropout to the group's eight values: dropped ones become 0
+// whatever they hold, NaN and infinities too.
+__device__ __forceinline__ void drop8(float (&v)[kVec], const DropArgs& d, DropSite s, uint32_t group, uint32_t row) {
+  uint32_t x[4];
+  draws8(x, d, s, group, row);
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) {
-    const uint32_t u = (j & 1) ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu;
-    v[j] = u < d.keep ? v[j] * d.scale : 0.0f;
-  }
+  for (int j = 0; j < kVec; ++j) v[j] = kept(x, j, d.keep) ? v[j] * d.scale : 0.0f;
+}
+
+// The row of a block's rows that this thread works on: the same for a whole wave
+// where a row has 64 threads or more, and then in a scalar register.
+template <int kLanes>
+__device__ __forceinline__ int row_in_block() {
+  if constexpr (kLanes >= 64)
+    return __builtin_amdgcn_readfirstlane(threadIdx.x) / kLanes;
+  else
+    return threadIdx.x / kLanes;
 }
 
 // Sums and maxima over the kLanes threads of a row. Within 16 lanes by lane

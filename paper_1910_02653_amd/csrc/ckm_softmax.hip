@@ -69,47 +69,69 @@ __device__ __forceinline__ float exp_of(float t, float m) {
   return __builtin_amdgcn_exp2f((t - m) * kLog2e);
 }
 
-// The logits of a group; -inf where a key is not seen. Scores there are not used,
-// whatever they hold. left: seen keys from the group's first on, 1 or more.
+// A group of a mask as it is stored: values of the scores' type, or bytes.
 template <typename T>
-__device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, const T* x, const Row& r, int col,
+union RawMask {
+  Raw8<T> add;
+  Raw8<uint8_t> seen;
+  __device__ RawMask() {}
+};
+template <bool kEven, typename T>
+__device__ __forceinline__ void load_mask(RawMask<T>& m, const SoftmaxArgs& a, const void* p, int col, int left) {
+  if (a.mask_kind == CKM_MASK_ADD)
+    m.add = load_part<kEven>((const T*)p + col, left);
+  else
+    m.seen = load_part<kEven>((const uint8_t*)p + col, left);
+}
+template <typename T>
+__device__ __forceinline__ const void* mask_row(const SoftmaxArgs& a, const Row& r) {
+  return (const char*)a.mask.p + offset_of(a.mask.s, r) * (a.mask_kind == CKM_MASK_ADD ? (int)sizeof(T) : 1);
+}
+
+// The logits of a group; -inf where a key is not seen. Scores there are not used,
+// whatever they hold. left: seen keys from the group's first on.
+template <bool kMask, typename T>
+__device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, const Raw8<T>& x, const RawMask<T>& m,
                                         int left) {
-  const Raw8<T> v = load_group(x + col, left);
-  if (a.mask_kind == CKM_MASK_ADD) {
-    const Raw8<T> m = load_group((const T*)a.mask.p + offset_of(a.mask.s, r) + col, left);
+  if constexpr (kMask) {
+    if (a.mask_kind == CKM_MASK_ADD) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const float add = (float)m.e[j];
-      t[j] = j < left && add != -__builtin_inff() ? fmaf((float)v.e[j], a.scale, add) : -__builtin_inff();
+      for (int j = 0; j < kVec; ++j) {
+        const float add = (float)m.add.e[j];
+        t[j] = j < left && add != -__builtin_inff() ? fmaf((float)x.e[j], a.scale, add) : -__builtin_inff();
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j)
+        t[j] = j < left && m.seen.e[j] ? (float)x.e[j] * a.scale : -__builtin_inff();
     }
-  } else if (a.mask_kind == CKM_MASK_BOOL) {
-    const Raw8<uint8_t> m = load_group((const uint8_t*)a.mask.p + offset_of(a.mask.s, r) + col, left);
-#pragma unroll
-    for (int j = 0; j < kVec; ++j)
-      t[j] = j < left && m.e[j] ? (float)v.e[j] * a.scale : -__builtin_inff();
   } else {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) t[j] = j < left ? (float)v.e[j] * a.scale : -__builtin_inff();
+    for (int j = 0; j < kVec; ++j) t[j] = j < left ? (float)x.e[j] * a.scale : -__builtin_inff();
   }
 }
 
-// The gradient that reaches the probabilities of a group before the dropout; 0
-// where a key is not seen.
+// The gradient that reaches a group's probabilities through the dropout, but for
+// its factor, which the row's sum and the result take together; 0 where a key
+// is not seen.
 template <typename T>
-__device__ __forceinline__ void grads8(float (&g)[kVec], const SoftmaxArgs& a, DropSite site, const T* dy,
-                                       const float (&t)[kVec], int64_t row, int col, int left) {
-  const Raw8<T> v = load_group(dy + col, left);
+__device__ __forceinline__ void grads8(float (&g)[kVec], const SoftmaxArgs& a, DropSite site, const Raw8<T>& dy,
+                                       const float (&t)[kVec], int64_t row, int col) {
+  uint32_t x[4];
+  if (a.drop.on) draws8(x, a.drop, site, col / kVec, (uint32_t)row);
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) g[j] = (float)v.e[j];
-  if (a.drop.on) drop8(g, a.drop, site, col / kVec, (uint32_t)row);
-#pragma unroll
-  for (int j = 0; j < kVec; ++j) g[j] = t[j] == -__builtin_inff() ? 0.0f : g[j];
+  for (int j = 0; j < kVec; ++j) {
+    bool use = t[j] != -__builtin_inff();
+    if (a.drop.on) use = use && kept(x, j, a.drop.keep);
+    g[j] = use ? (float)dy.e[j] : 0.0f;
+  }
 }
 
 constexpr int softmax_block(int lanes) { return lanes < 256 ? 256 : lanes; }
 
-// A row in the registers of kLanes threads, kPer groups each.
-template <typename T, int kLanes, int kPer, bool kBack>
+// A row in the registers of kLanes threads, kPer groups each. kEven: rows of
+// whole groups, so that a group with any key seen can be loaded whole.
+template <typename T, int kLanes, int kPer, bool kBack, bool kMask, bool kEven>
 __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(SoftmaxArgs a) {
   constexpr int kBlock = softmax_block(kLanes), kRowsAt = kBlock / kLanes;
   __shared__ float lds[kLanes > 64 ? 2 * kBlock / 64 : 1];
@@ -117,35 +139,51 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
   const DropSite site = drop_site(a.drop);
   int turn = 0;
   for (int64_t first = (int64_t)blockIdx.x * kRowsAt; first < a.rows; first += (int64_t)gridDim.x * kRowsAt) {
-    const int64_t row = first + threadIdx.x / kLanes;
+    const int64_t row = first + row_in_block<kLanes>();
     const bool live = row < a.rows;
     const Row r = row_of(a, live ? row : a.rows - 1);
     const T* x = (const T*)a.x.p + offset_of(a.x.s, r);
+    const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
+    const void* mask = kMask ? mask_row<T>(a, r) : nullptr;
     T* y = (T*)a.y + offset_of(a.ys, r);
     const int seen = live ? r.seen : 0, keys = live ? a.keys : 0;
-    float t[kPer][kVec];
+    // every load of the row first, then the arithmetic
+    Raw8<T> rx[kPer], rd[kBack ? kPer : 1];
+    RawMask<T> rm[kMask ? kPer : 1];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec;
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) t[i][j] = -__builtin_inff();
-      if (col < seen) logits8(t[i], a, x, r, col, seen - col);
+      if (col < seen) {
+        rx[i] = load_part<kEven>(x + col, seen - col);
+        if constexpr (kBack) rd[i] = load_part<kEven>(dy + col, seen - col);
+        if constexpr (kMask) load_mask<kEven>(rm[i], a, mask, col, seen - col);
+      }
     }
+    float t[kPer][kVec];
     if constexpr (!kBack) {
       float m = kLowest;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
+      for (int i = 0; i < kPer; ++i) {
+        const int col = (lane + i * kLanes) * kVec;
+        if (col < seen) {
+          logits8<kMask>(t[i], a, rx[i], rm[kMask ? i : 0], seen - col);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) m = fmaxf(m, t[i][j]);
+          for (int j = 0; j < kVec; ++j) m = fmaxf(m, t[i][j]);
+        }
+      }
       m = reduce_row<OpMax, kLanes, kBlock>(m, lds, 0);
       float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
+      for (int i = 0; i < kPer; ++i) {
+        const int col = (lane + i * kLanes) * kVec;
+        if (col < seen) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) {
-          t[i][j] = exp_of(t[i][j], m);
-          sum += t[i][j];
+          for (int j = 0; j < kVec; ++j) {
+            t[i][j] = exp_of(t[i][j], m);
+            sum += t[i][j];
+          }
         }
+      }
       sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, 1);
       const float z = sum == 0.0f ? 0.0f : 1.0f / sum;
       if (live && lane == 0 && a.stats) {
@@ -156,41 +194,45 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       for (int i = 0; i < kPer; ++i) {
         const int group = lane + i * kLanes, col = group * kVec;
         if (col >= keys) continue;
+        float o[kVec] = {};
+        if (col < seen) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) t[i][j] *= z;
-        if (a.drop.on && col < seen) drop8(t[i], a.drop, site, group, (uint32_t)row);
-        store_group(y + col, t[i], keys - col);
+          for (int j = 0; j < kVec; ++j) o[j] = t[i][j] * z;
+          if (a.drop.on) drop8(o, a.drop, site, group, (uint32_t)row);
+        }
+        store_part<kEven>(y + col, o, keys - col);
       }
     } else {
-      const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
       const float m = live ? a.stats[2 * row] : 0.0f, z = live ? a.stats[2 * row + 1] : 0.0f;
+      const float by = a.drop.on ? a.scale * a.drop.scale : a.scale;
       float g[kPer][kVec];
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int col = (lane + i * kLanes) * kVec;
         if (col < seen) {
-          grads8(g[i], a, site, dy, t[i], row, col, seen - col);
+          logits8<kMask>(t[i], a, rx[i], rm[kMask ? i : 0], seen - col);
+          grads8(g[i], a, site, rd[i], t[i], row, col);
 #pragma unroll
           for (int j = 0; j < kVec; ++j) {
             t[i][j] = exp_of(t[i][j], m) * z;
             sum = fmaf(t[i][j], g[i][j], sum);
           }
-        } else {
-#pragma unroll
-          for (int j = 0; j < kVec; ++j) t[i][j] = g[i][j] = 0.0f;
         }
       }
       sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, turn);
       turn ^= 1;
+      sum *= by;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int col = (lane + i * kLanes) * kVec;
         if (col >= keys) continue;
-        float o[kVec];
+        float o[kVec] = {};
+        if (col < seen) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) o[j] = a.scale * (t[i][j] * (g[i][j] - sum));
-        store_group(y + col, o, keys - col);
+          for (int j = 0; j < kVec; ++j) o[j] = t[i][j] * fmaf(g[i][j], by, -sum);
+        }
+        store_part<kEven>(y + col, o, keys - col);
       }
     }
   }
@@ -202,6 +244,19 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
 // and sum of exponentials (the gradient: its sum of p g); the second joins a row's
 // shares in each of its blocks and makes the share's outputs.
 // ---------------------------------------------------------------------------
+
+template <typename T>
+__device__ __forceinline__ void load_logits8(float (&t)[kVec], const SoftmaxArgs& a, const T* x, const Row& r, int col) {
+  const int left = r.seen - col;
+  const Raw8<T> v = load_group(x + col, left);
+  RawMask<T> m;
+  if (a.mask_kind != CKM_MASK_NONE) {
+    load_mask<false>(m, a, mask_row<T>(a, r), col, left);
+    logits8<true>(t, a, v, m, left);
+  } else {
+    logits8<false>(t, a, v, m, left);
+  }
+}
 
 constexpr int kSplitBlock = 256, kSplitSpan = kSplitBlock * kVec, kMaxSplits = kSplitBlock;
 
@@ -221,7 +276,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxA
       float m = kLowest, sum = 0.0f;
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
         float t[kVec];
-        logits8(t, a, x, r, col, r.seen - col);
+        load_logits8(t, a, x, r, col);
         float top = m;
 #pragma unroll
         for (int j = 0; j < kVec; ++j) top = fmaxf(top, t[j]);
@@ -239,8 +294,8 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxA
       float sum = 0.0f;
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
         float t[kVec], g[kVec];
-        logits8(t, a, x, r, col, r.seen - col);
-        grads8(g, a, site, dy, t, row, col, r.seen - col);
+        load_logits8(t, a, x, r, col);
+        grads8(g, a, site, load_group(dy + col, r.seen - col), t, row, col);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) sum = fmaf(exp_of(t[j], m) * z, g[j], sum);
       }
@@ -278,7 +333,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxAr
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
         float t[kVec] = {};
         if (col < r.seen) {
-          logits8(t, a, x, r, col, r.seen - col);
+          load_logits8(t, a, x, r, col);
 #pragma unroll
           for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m) * z;
           if (a.drop.on) drop8(t, a.drop, site, col / kVec, (uint32_t)row);
@@ -288,16 +343,17 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxAr
     } else {
       const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
       const float m = a.stats[2 * row], z = a.stats[2 * row + 1];
-      const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, turn);
+      const float by = a.drop.on ? a.scale * a.drop.scale : a.scale;
+      const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, turn) * by;
       turn ^= 1;
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
         float o[kVec] = {};
         if (col < r.seen) {
           float t[kVec], g[kVec];
-          logits8(t, a, x, r, col, r.seen - col);
-          grads8(g, a, site, dy, t, row, col, r.seen - col);
+          load_logits8(t, a, x, r, col);
+          grads8(g, a, site, load_group(dy + col, r.seen - col), t, row, col);
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) o[j] = a.scale * (exp_of(t[j], m) * z * (g[j] - sum));
+          for (int j = 0; j < kVec; ++j) o[j] = exp_of(t[j], m) * z * fmaf(g[j], by, -sum);
         }
         store_group(y + col, o, a.keys - col);
       }
@@ -323,7 +379,12 @@ template <typename T, bool kBack, int kLanes, int kPer>
 void launch_whole_as(const SoftmaxArgs& a, hipStream_t s) {
   constexpr int kBlock = softmax_block(kLanes), kRowsAt = kBlock / kLanes;
   const int64_t blocks = std::min<int64_t>((a.rows + kRowsAt - 1) / kRowsAt, 1 << 20);
-  ckm_softmax_kernel<T, kLanes, kPer, kBack><<<dim3((uint32_t)blocks), kBlock, 0, s>>>(a);
+  const dim3 grid((uint32_t)blocks);
+  const bool mask = a.mask_kind != CKM_MASK_NONE, even = a.keys % kVec == 0;
+  if (mask && even) ckm_softmax_kernel<T, kLanes, kPer, kBack, true, true><<<grid, kBlock, 0, s>>>(a);
+  else if (mask) ckm_softmax_kernel<T, kLanes, kPer, kBack, true, false><<<grid, kBlock, 0, s>>>(a);
+  else if (even) ckm_softmax_kernel<T, kLanes, kPer, kBack, false, true><<<grid, kBlock, 0, s>>>(a);
+  else ckm_softmax_kernel<T, kLanes, kPer, kBack, false, false><<<grid, kBlock, 0, s>>>(a);
 }
 
 template <typename T, bool kBack>
@@ -340,6 +401,7 @@ void launch_softmax(const SoftmaxArgs& a, int splits, void* work, hipStream_t s)
   if (groups <= 16) launch_whole_as<T, kBack, 16, 1>(a, s);
   else if (groups <= 64) launch_whole_as<T, kBack, 64, 1>(a, s);
   else if (groups <= 128) launch_whole_as<T, kBack, 64, 2>(a, s);
+  else if (groups <= 256 && kBack) launch_whole_as<T, kBack, 128, 2>(a, s);
   else if (groups <= 256) launch_whole_as<T, kBack, 64, 4>(a, s);
   else if (groups <= 512) launch_whole_as<T, kBack, 256, 2>(a, s);
   else if (groups <= 1024) launch_whole_as<T, kBack, 256, 4>(a, s);
