@@ -41,23 +41,26 @@ __global__ void __launch_bounds__(kDropBlock) ckm_dropout_kernel(int64_t total, 
     const uint32_t group = at - q * groups;
     const int64_t row = row0 + q;
     if (g >= total) continue;
-    const int left = kFlat ? kVec : cols - (int)(group * kVec);
-    const int64_t ox = kFlat ? g * kVec : row * ld_x + group * kVec;
-    const Raw8<T> vx = load_part<kFlat>(x + ox, left);
+    const int col = (int)(group * kVec);
+    Raw8<T> vx, vr;
+    if constexpr (kFlat) {
+      vx = load8(x + g * kVec);
+      if constexpr (kRes) vr = load8(res + g * kVec);
+    } else {
+      vx = load_cols<false>(x + row * ld_x, col, cols);
+      if constexpr (kRes) vr = load_cols<false>(res + row * ld_res, col, cols);
+    }
+    fix_tail<kFlat>(vx, col, cols);
     float v[kVec];
-    if constexpr (kRes) {
-      const Raw8<T> vr = load_part<kFlat>(res + (kFlat ? ox : row * ld_res + group * kVec), left);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) v[j] = (float)vx.e[j];
-      if (drop.on) drop8(v, drop, site, group, (uint32_t)row);
+    for (int j = 0; j < kVec; ++j) v[j] = (float)vx.e[j];
+    if (drop.on) drop8(v, drop, site, group, (uint32_t)row);
+    if constexpr (kRes) {
+      fix_tail<kFlat>(vr, col, cols);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) v[j] += (float)vr.e[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) v[j] = (float)vx.e[j];
-      if (drop.on) drop8(v, drop, site, group, (uint32_t)row);
     }
-    store_part<kFlat>(y + (kFlat ? ox : row * ld_y + group * kVec), v, left);
+    store_part<kFlat>(kFlat ? y + g * kVec : y + row * ld_y + col, v, cols - col);
   }
 }
 

@@ -91,21 +91,23 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec, left = live ? a.cols - col : 0;
       r[i] = zero_group<T>();
-      if (left > 0) r[i] = load_part<kEven>((const T*)a.x + row * a.ld_x + col, left);
+      if (left > 0) r[i] = load_cols<kEven>((const T*)a.x + row * a.ld_x, col, a.cols);
       if constexpr (kFused) {
         rr[i] = zero_group<T>();
-        if (a.res && left > 0) rr[i] = load_part<kEven>((const T*)a.res + row * a.ld_res + col, left);
+        if (a.res && left > 0) rr[i] = load_cols<kEven>((const T*)a.res + row * a.ld_res, col, a.cols);
       }
     }
     float v[kPer][kVec];
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
+      fix_tail<kEven>(r[i], (lane + i * kLanes) * kVec, a.cols);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].e[j];
       if constexpr (kFused) {
         const int group = lane + i * kLanes, col = group * kVec, left = live ? a.cols - col : 0;
         if (a.drop.on) drop8(v[i], a.drop, site, group, (uint32_t)row);
+        fix_tail<kEven>(rr[i], col, a.cols);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) v[i][j] = as_stored<T>(v[i][j] + (float)rr[i].e[j]);
         if (a.h && left > 0) store_part<kEven>((T*)a.h + row * a.ld_h + col, v[i], left);
@@ -246,15 +248,18 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
       const int col = (lane + i * kLanes) * kVec, left = live ? a.cols - col : 0;
       rd[i] = rh[i] = past[i] = zero_group<T>();
       if (left > 0) {
-        rd[i] = load_part<kEven>((const T*)a.dy + row * a.ld_dy + col, left);
-        rh[i] = load_part<kEven>((const T*)a.h + row * a.ld_h + col, left);
-        if (a.dres) past[i] = load_part<kEven>((const T*)a.dres + row * a.ld_dres + col, left);
+        rd[i] = load_cols<kEven>((const T*)a.dy + row * a.ld_dy, col, a.cols);
+        rh[i] = load_cols<kEven>((const T*)a.h + row * a.ld_h, col, a.cols);
+        if (a.dres) past[i] = load_cols<kEven>((const T*)a.dres + row * a.ld_dres, col, a.cols);
       }
     }
     float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int k = kKeep ? i : 0, left = live ? a.cols - (lane + i * kLanes) * kVec : 0;
+      fix_tail<kEven>(rd[i], (lane + i * kLanes) * kVec, a.cols);
+      fix_tail<kEven>(rh[i], (lane + i * kLanes) * kVec, a.cols);
+      fix_tail<kEven>(past[i], (lane + i * kLanes) * kVec, a.cols);
       if constexpr (!kKeep) weight_group<T>(w[0], a.w, a.w32, (lane + i * kLanes) * kVec, left, 1.0f);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
@@ -436,7 +441,8 @@ template <typename T>
 void launch_norm(const NormArgs& a, bool fused, hipStream_t s) {
   const int groups = padded_cols(a.cols) / kVec;
   if (groups <= 16) launch_norm_as<T, 16, 1>(a, fused, s);
-  else if (groups <= 64) launch_norm_as<T, 64, 1>(a, fused, s);
+  else if (groups <= 32) launch_norm_as<T, 16, 2>(a, fused, s);
+  else if (groups <= 64) launch_norm_as<T, 32, 2>(a, fused, s);
   else if (groups <= 128) launch_norm_as<T, 64, 2>(a, fused, s);
   else if (groups <= 256) launch_norm_as<T, 256, 1>(a, fused, s);
   else if (groups <= 512) launch_norm_as<T, 256, 2>(a, fused, s);
@@ -460,7 +466,8 @@ GradPlan grad_plan(int64_t rows, int64_t cols) {
     return p;
   }
   if (groups <= 16) p = {16, 1, 0};
-  else if (groups <= 64) p = {64, 1, 0};
+  else if (groups <= 32) p = {16, 2, 0};
+  else if (groups <= 64) p = {32, 2, 0};
   else if (groups <= 128) p = {64, 2, 0};
   else if (groups <= 256) p = {256, 1, 0};
   else if (groups <= 512) p = {512, 1, 0};
@@ -497,8 +504,9 @@ void launch_grad(NormGradArgs a, void* work, hipStream_t s) {
     if (a.rows > 0)
       ckm_norm_wide_sums_kernel<T><<<dim3((uint32_t)std::min<int64_t>(a.rows, 2048)), 1024, 0, s>>>(a, sums);
     ckm_norm_wide_grad_kernel<T><<<dim3((uint32_t)ceil_div(a.cols, 256 * kVec), (uint32_t)p.blocks), 256, 0, s>>>(a, sums);
-  } else if (p.lanes == 16) launch_grad_as<T, 16, 1>(a, p.blocks, s);
-  else if (p.lanes == 64 && p.per == 1) launch_grad_as<T, 64, 1>(a, p.blocks, s);
+  } else if (p.lanes == 16 && p.per == 1) launch_grad_as<T, 16, 1>(a, p.blocks, s);
+  else if (p.lanes == 16) launch_grad_as<T, 16, 2>(a, p.blocks, s);
+  else if (p.lanes == 32) launch_grad_as<T, 32, 2>(a, p.blocks, s);
   else if (p.lanes == 64) launch_grad_as<T, 64, 2>(a, p.blocks, s);
   else if (p.lanes == 256) launch_grad_as<T, 256, 1>(a, p.blocks, s);
   else if (p.lanes == 512) launch_grad_as<T, 512, 1>(a, p.blocks, s);

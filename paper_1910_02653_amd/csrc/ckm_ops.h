@@ -30,8 +30,8 @@ struct DropArgs {
   uint32_t k0 = 0, k1 = 0;            // Philox key: the seed
   uint64_t site = 0;                  // counter words 2 and 3, plus *d_site when given
   const uint64_t* d_site = nullptr;
-  uint32_t keep = 0;                  // a draw below this keeps the element
-  float scale = 0.0f;                 // 65536 / keep
+  uint32_t keep = 65536;              // a draw below this keeps the element
+  float scale = 1.0f;                 // 65536 / keep
   bool on = false;
 };
 
@@ -77,14 +77,32 @@ __device__ __forceinline__ Raw8<T> zero_group() {
   for (int j = 0; j < kVec; ++j) r.e[j] = (T)0;
   return r;
 }
-// The same for rows whose length is a multiple of eight (kEven): a group lies in
-// the row whole or not at all.
+// Column `col` on of a row of `cols` columns: one load for a whole group. In rows
+// that are not of whole groups (kEven false) the last one is loaded where it ends
+// with the row, and fix_tail moves its elements into place, after the loads that
+// a kernel wants in flight together. Rows of fewer than eight go by element.
 template <bool kEven, typename T>
-__device__ __forceinline__ Raw8<T> load_part(const T* p, int left) {
-  if constexpr (kEven)
-    return load8(p);
-  else
-    return load_group(p, left);
+__device__ __forceinline__ Raw8<T> load_cols(const T* row, int col, int cols) {
+  if constexpr (kEven) {
+    return load8(row + col);
+  } else {
+    if (cols < kVec) return load_group(row + col, cols - col);
+    return load8(row + min(col, cols - kVec));
+  }
+}
+template <bool kEven, typename T>
+__device__ __forceinline__ void fix_tail(Raw8<T>& r, int col, int cols) {
+  if constexpr (!kEven) {
+    if (cols >= kVec && col + kVec > cols) {
+      const int by = col + kVec - cols;
+#pragma unroll
+      for (int bit = 4; bit >= 1; bit >>= 1)
+        if (by & bit) {
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) r.e[j] = j + bit < kVec ? r.e[j + bit] : (T)0;
+        }
+    }
+  }
 }
 // v rounded to T, nearest even. For binary16 the empty statement keeps the compiler
 // from fusing the conversion with a product before it, which rounds once and not
@@ -197,6 +215,13 @@ __device__ __forceinline__ float reduce16(float x) {
   x = Op::of(x, dpp_move<0x140>(x));   // the other eight of sixteen
   return x;
 }
+template <typename Op>
+__device__ __forceinline__ float reduce32(float x) {
+  x = reduce16<Op>(x);
+  // both of the pair's rows of 16 lanes, in every lane of the two
+  const auto v = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return Op::of(__uint_as_float(v[0]), __uint_as_float(v[1]));
+}
 __device__ __forceinline__ float lane_of(float x, int lane) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), lane));
 }
@@ -205,7 +230,7 @@ __device__ __forceinline__ float reduce64(float x) {
   x = reduce16<Op>(x);
   return Op::of(Op::of(lane_of(x, 0), lane_of(x, 16)), Op::of(lane_of(x, 32), lane_of(x, 48)));
 }
-// kLanes 16, 64, or a multiple of 64 that divides the block's kBlock threads.
+// kLanes 16, 32, 64, or a multiple of 64 that divides the block's kBlock threads.
 // lds: 2 kBlock / 64 floats per value; `turn` (0 or 1) picks the half, and a
 // kernel's reductions take turns: a wave can write a half again only after the
 // barrier of the reduction between, which every reader of it has reached. All
@@ -214,6 +239,8 @@ template <typename Op, int kLanes, int kBlock>
 __device__ __forceinline__ float reduce_row(float x, float* lds, int turn) {
   if constexpr (kLanes == 16) {
     return reduce16<Op>(x);
+  } else if constexpr (kLanes == 32) {
+    return reduce32<Op>(x);
   } else {
     x = reduce64<Op>(x);
     if constexpr (kLanes > 64) {
@@ -235,6 +262,9 @@ __device__ __forceinline__ void reduce_two(float& x, float& y, float* lds, int t
   if constexpr (kLanes == 16) {
     x = reduce16<OpSum>(x);
     y = reduce16<OpSum>(y);
+  } else if constexpr (kLanes == 32) {
+    x = reduce32<OpSum>(x);
+    y = reduce32<OpSum>(y);
   } else {
     x = reduce64<OpSum>(x);
     y = reduce64<OpSum>(y);

@@ -23,17 +23,18 @@
 namespace ckm {
 namespace {
 
+// Rows in memory: elements between batches, heads, queries; where those make one
+// stride from row to row, that.
 struct Strided {
   const void* p;
-  int64_t s[3];   // elements between batches, heads, queries
+  int64_t s[3];
+  int64_t row;   // -1: there is no such stride
 };
 
 struct SoftmaxArgs {
   int64_t rows;
   int32_t heads, queries, keys;
-  Strided x, dy;
-  void* y;          // probabilities, or the scores' gradient
-  int64_t ys[3];
+  Strided x, dy, y; // y: probabilities, or the scores' gradient
   float* stats;     // [rows][2]: m, z (read by the gradient)
   float scale;
   bool causal;
@@ -41,14 +42,17 @@ struct SoftmaxArgs {
   int mask_kind;
   Strided mask;
   DropArgs drop;
+  bool places;      // a row's batch, head and query matter: masks, or rows without one stride
 };
 
 struct Row {
+  int64_t n;        // its number
   int32_t b, h, i;
   int32_t seen;     // keys seen are below this (masks aside)
 };
 __device__ __forceinline__ Row row_of(const SoftmaxArgs& a, int64_t row) {
-  Row r;
+  Row r = {row, 0, 0, 0, a.keys};
+  if (!a.places) return r;
   const uint32_t bh = (uint32_t)row / (uint32_t)a.queries;
   r.i = (uint32_t)row - bh * a.queries;
   r.b = bh / (uint32_t)a.heads;
@@ -59,8 +63,8 @@ __device__ __forceinline__ Row row_of(const SoftmaxArgs& a, int64_t row) {
   r.seen = max(seen, 0);
   return r;
 }
-__device__ __forceinline__ int64_t offset_of(const int64_t (&s)[3], const Row& r) {
-  return r.b * s[0] + r.h * s[1] + r.i * s[2];
+__device__ __forceinline__ int64_t offset_of(const Strided& t, const Row& r) {
+  return t.row >= 0 ? r.n * t.row : r.b * t.s[0] + r.h * t.s[1] + r.i * t.s[2];
 }
 
 constexpr float kLowest = -3.402823466e38f;
@@ -77,15 +81,22 @@ union RawMask {
   __device__ RawMask() {}
 };
 template <bool kEven, typename T>
-__device__ __forceinline__ void load_mask(RawMask<T>& m, const SoftmaxArgs& a, const void* p, int col, int left) {
+__device__ __forceinline__ void load_mask(RawMask<T>& m, const SoftmaxArgs& a, const void* p, int col) {
   if (a.mask_kind == CKM_MASK_ADD)
-    m.add = load_part<kEven>((const T*)p + col, left);
+    m.add = load_cols<kEven>((const T*)p, col, a.keys);
   else
-    m.seen = load_part<kEven>((const uint8_t*)p + col, left);
+    m.seen = load_cols<kEven>((const uint8_t*)p, col, a.keys);
+}
+template <bool kEven, typename T>
+__device__ __forceinline__ void fix_mask(RawMask<T>& m, const SoftmaxArgs& a, int col) {
+  if (a.mask_kind == CKM_MASK_ADD)
+    fix_tail<kEven>(m.add, col, a.keys);
+  else
+    fix_tail<kEven>(m.seen, col, a.keys);
 }
 template <typename T>
 __device__ __forceinline__ const void* mask_row(const SoftmaxArgs& a, const Row& r) {
-  return (const char*)a.mask.p + offset_of(a.mask.s, r) * (a.mask_kind == CKM_MASK_ADD ? (int)sizeof(T) : 1);
+  return (const char*)a.mask.p + offset_of(a.mask, r) * (a.mask_kind == CKM_MASK_ADD ? (int)sizeof(T) : 1);
 }
 
 // The logits of a group; -inf where a key is not seen. Scores there are not used,
@@ -117,14 +128,11 @@ __device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, 
 template <typename T>
 __device__ __forceinline__ void grads8(float (&g)[kVec], const SoftmaxArgs& a, DropSite site, const Raw8<T>& dy,
                                        const float (&t)[kVec], int64_t row, int col) {
-  uint32_t x[4];
+  uint32_t x[4] = {};   // without a dropout every draw is below keep
   if (a.drop.on) draws8(x, a.drop, site, col / kVec, (uint32_t)row);
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) {
-    bool use = t[j] != -__builtin_inff();
-    if (a.drop.on) use = use && kept(x, j, a.drop.keep);
-    g[j] = use ? (float)dy.e[j] : 0.0f;
-  }
+  for (int j = 0; j < kVec; ++j)
+    g[j] = (t[j] != -__builtin_inff()) & kept(x, j, a.drop.keep) ? (float)dy.e[j] : 0.0f;
 }
 
 constexpr int softmax_block(int lanes) { return lanes < 256 ? 256 : lanes; }
@@ -142,10 +150,10 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
     const int64_t row = first + row_in_block<kLanes>();
     const bool live = row < a.rows;
     const Row r = row_of(a, live ? row : a.rows - 1);
-    const T* x = (const T*)a.x.p + offset_of(a.x.s, r);
-    const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
+    const T* x = (const T*)a.x.p + offset_of(a.x, r);
+    const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
     const void* mask = kMask ? mask_row<T>(a, r) : nullptr;
-    T* y = (T*)a.y + offset_of(a.ys, r);
+    T* y = (T*)const_cast<void*>(a.y.p) + offset_of(a.y, r);
     const int seen = live ? r.seen : 0, keys = live ? a.keys : 0;
     // every load of the row first, then the arithmetic
     Raw8<T> rx[kPer], rd[kBack ? kPer : 1];
@@ -154,9 +162,9 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec;
       if (col < seen) {
-        rx[i] = load_part<kEven>(x + col, seen - col);
-        if constexpr (kBack) rd[i] = load_part<kEven>(dy + col, seen - col);
-        if constexpr (kMask) load_mask<kEven>(rm[i], a, mask, col, seen - col);
+        rx[i] = load_cols<kEven>(x, col, a.keys);
+        if constexpr (kBack) rd[i] = load_cols<kEven>(dy, col, a.keys);
+        if constexpr (kMask) load_mask<kEven>(rm[i], a, mask, col);
       }
     }
     float t[kPer][kVec];
@@ -166,6 +174,8 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       for (int i = 0; i < kPer; ++i) {
         const int col = (lane + i * kLanes) * kVec;
         if (col < seen) {
+          fix_tail<kEven>(rx[i], col, a.keys);
+          if constexpr (kMask) fix_mask<kEven>(rm[i], a, col);
           logits8<kMask>(t[i], a, rx[i], rm[kMask ? i : 0], seen - col);
 #pragma unroll
           for (int j = 0; j < kVec; ++j) m = fmaxf(m, t[i][j]);
@@ -204,13 +214,16 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       }
     } else {
       const float m = live ? a.stats[2 * row] : 0.0f, z = live ? a.stats[2 * row + 1] : 0.0f;
-      const float by = a.drop.on ? a.scale * a.drop.scale : a.scale;
+      const float by = a.scale * a.drop.scale;
       float g[kPer][kVec];
       float sum = 0.0f;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int col = (lane + i * kLanes) * kVec;
         if (col < seen) {
+          fix_tail<kEven>(rx[i], col, a.keys);
+          fix_tail<kEven>(rd[i], col, a.keys);
+          if constexpr (kMask) fix_mask<kEven>(rm[i], a, col);
           logits8<kMask>(t[i], a, rx[i], rm[kMask ? i : 0], seen - col);
           grads8(g[i], a, site, rd[i], t[i], row, col);
 #pragma unroll
@@ -246,14 +259,23 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
 // ---------------------------------------------------------------------------
 
 template <typename T>
+__device__ __forceinline__ Raw8<T> load_whole(const T* row, int col, int cols) {
+  Raw8<T> r = load_cols<false>(row, col, cols);
+  fix_tail<false>(r, col, cols);
+  return r;
+}
+template <typename T>
 __device__ __forceinline__ void load_logits8(float (&t)[kVec], const SoftmaxArgs& a, const T* x, const Row& r, int col) {
   const int left = r.seen - col;
-  const Raw8<T> v = load_group(x + col, left);
+  Raw8<T> v = load_cols<false>(x, col, a.keys);
   RawMask<T> m;
   if (a.mask_kind != CKM_MASK_NONE) {
-    load_mask<false>(m, a, mask_row<T>(a, r), col, left);
+    load_mask<false>(m, a, mask_row<T>(a, r), col);
+    fix_tail<false>(v, col, a.keys);
+    fix_mask<false>(m, a, col);
     logits8<true>(t, a, v, m, left);
   } else {
+    fix_tail<false>(v, col, a.keys);
     logits8<false>(t, a, v, m, left);
   }
 }
@@ -269,7 +291,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxA
   for (int64_t item = blockIdx.x; item < a.rows * splits; item += gridDim.x) {
     const int64_t row = item / splits;
     const Row r = row_of(a, row);
-    const T* x = (const T*)a.x.p + offset_of(a.x.s, r);
+    const T* x = (const T*)a.x.p + offset_of(a.x, r);
     const int from = (int)(item - row * splits) * chunk;
     const int to = min(r.seen, from + chunk);
     if constexpr (!kBack) {
@@ -289,13 +311,13 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxA
       sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum * exp_of(m, top), lds, 1);
       if (threadIdx.x == 0) part[item] = {top, sum};
     } else {
-      const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
+      const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
       const float m = a.stats[2 * row], z = a.stats[2 * row + 1];
       float sum = 0.0f;
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
         float t[kVec], g[kVec];
         load_logits8(t, a, x, r, col);
-        grads8(g, a, site, load_group(dy + col, r.seen - col), t, row, col);
+        grads8(g, a, site, load_whole(dy, col, a.keys), t, row, col);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) sum = fmaf(exp_of(t[j], m) * z, g[j], sum);
       }
@@ -315,8 +337,8 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxAr
   for (int64_t item = blockIdx.x; item < a.rows * splits; item += gridDim.x) {
     const int64_t row = item / splits;
     const Row r = row_of(a, row);
-    const T* x = (const T*)a.x.p + offset_of(a.x.s, r);
-    T* y = (T*)a.y + offset_of(a.ys, r);
+    const T* x = (const T*)a.x.p + offset_of(a.x, r);
+    T* y = (T*)const_cast<void*>(a.y.p) + offset_of(a.y, r);
     const int share = (int)(item - row * splits);
     const int from = share * chunk;
     const int to = (int)min((int64_t)a.keys, (int64_t)from + chunk);
@@ -341,9 +363,9 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxAr
         store_group(y + col, t, a.keys - col);
       }
     } else {
-      const T* dy = (const T*)a.dy.p + offset_of(a.dy.s, r);
+      const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
       const float m = a.stats[2 * row], z = a.stats[2 * row + 1];
-      const float by = a.drop.on ? a.scale * a.drop.scale : a.scale;
+      const float by = a.scale * a.drop.scale;
       const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, turn) * by;
       turn ^= 1;
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
@@ -351,7 +373,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxAr
         if (col < r.seen) {
           float t[kVec], g[kVec];
           load_logits8(t, a, x, r, col);
-          grads8(g, a, site, load_group(dy + col, r.seen - col), t, row, col);
+          grads8(g, a, site, load_whole(dy, col, a.keys), t, row, col);
 #pragma unroll
           for (int j = 0; j < kVec; ++j) o[j] = exp_of(t[j], m) * z * fmaf(g[j], by, -sum);
         }
@@ -399,7 +421,8 @@ void launch_softmax(const SoftmaxArgs& a, int splits, void* work, hipStream_t s)
   }
   const int groups = (a.keys + kVec - 1) / kVec;
   if (groups <= 16) launch_whole_as<T, kBack, 16, 1>(a, s);
-  else if (groups <= 64) launch_whole_as<T, kBack, 64, 1>(a, s);
+  else if (groups <= 32) launch_whole_as<T, kBack, 16, 2>(a, s);
+  else if (groups <= 64) launch_whole_as<T, kBack, 32, 2>(a, s);
   else if (groups <= 128) launch_whole_as<T, kBack, 64, 2>(a, s);
   else if (groups <= 256 && kBack) launch_whole_as<T, kBack, 128, 2>(a, s);
   else if (groups <= 256) launch_whole_as<T, kBack, 64, 4>(a, s);
@@ -493,22 +516,27 @@ ckm_status softmax(bool back, ckm_dtype type, const ckm_scores* c, const void* x
   a.heads = (int32_t)c->heads;
   a.queries = (int32_t)c->queries;
   a.keys = (int32_t)c->keys;
-  const auto strided = [](const void* p, const int64_t* s) {
-    Strided v = {p, {0, 0, 0}};
-    if (s)
-      for (int k = 0; k < 3; ++k) v.s[k] = s[k];
+  const auto strided = [&](const void* p, const int64_t* s) {
+    Strided v = {p, {0, 0, 0}, 0};
+    if (!s) return v;
+    for (int k = 0; k < 3; ++k) v.s[k] = s[k];
+    // one stride d for all rows: heads lie queries d apart, batches heads queries d
+    const int64_t d = c->queries > 1 ? s[2] : c->heads > 1 ? s[1] : s[0];
+    v.row = d;
+    if (c->queries > 1 && c->heads > 1 && s[1] != (__int128)c->queries * d) v.row = -1;
+    if (c->batch > 1 && c->heads * c->queries > 1 && s[0] != (__int128)c->heads * c->queries * d) v.row = -1;
     return v;
   };
   a.x = strided(x, x_stride);
   a.dy = strided(dy, dy_stride);
-  a.y = y;
-  for (int k = 0; k < 3; ++k) a.ys[k] = y_stride ? y_stride[k] : 0;
+  a.y = strided(y, y_stride);
   a.stats = stats;
   a.scale = c->scale;
   a.causal = c->flags & CKM_SCORES_CAUSAL;
   a.lengths = c->d_lengths;
   a.mask_kind = c->mask_kind;
-  a.mask = strided(c->d_mask, c->mask_stride);
+  a.mask = strided(c->d_mask, c->mask_kind == CKM_MASK_NONE ? nullptr : c->mask_stride);
+  a.places = a.causal || a.lengths || a.x.row < 0 || a.dy.row < 0 || a.y.row < 0 || a.mask.row < 0;
   if (back)
     launch_typed<true>(type, a, splits, work, (hipStream_t)stream);
   else
