@@ -51,16 +51,19 @@ __global__ void __launch_bounds__(kDropBlock) ckm_dropout_kernel(int64_t total, 
       if constexpr (kRes) vr = load_cols<false>(res + row * ld_res, col, cols);
     }
     fix_tail<kFlat>(vx, col, cols);
+    if (drop.on) drop_choice(vx, drop, site, group, (uint32_t)row);
     float v[kVec];
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = (float)vx.e[j];
-    if (drop.on) drop8(v, drop, site, group, (uint32_t)row);
+    for (int j = 0; j < kVec; ++j) v[j] = (float)vx.e[j] * drop.scale;
     if constexpr (kRes) {
       fix_tail<kFlat>(vr, col, cols);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) v[j] += (float)vr.e[j];
     }
-    store_part<kFlat>(kFlat ? y + g * kVec : y + row * ld_y + col, v, cols - col);
+    if constexpr (kFlat)
+      store_part<true>(y + g * kVec, rounded8<T>(v), 0, kVec);
+    else
+      store_part<false>(y + row * ld_y, rounded8<T>(v), col, cols);
   }
 }
 

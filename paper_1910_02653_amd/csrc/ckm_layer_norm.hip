@@ -101,16 +101,21 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      fix_tail<kEven>(r[i], (lane + i * kLanes) * kVec, a.cols);
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].e[j];
+      const int group = lane + i * kLanes, col = group * kVec;
+      fix_tail<kEven>(r[i], col, a.cols);
       if constexpr (kFused) {
-        const int group = lane + i * kLanes, col = group * kVec, left = live ? a.cols - col : 0;
-        if (a.drop.on) drop8(v[i], a.drop, site, group, (uint32_t)row);
+        const int left = live ? a.cols - col : 0;
+        if (a.drop.on) drop_choice(r[i], a.drop, site, group, (uint32_t)row);
         fix_tail<kEven>(rr[i], col, a.cols);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) v[i][j] = as_stored<T>(v[i][j] + (float)rr[i].e[j]);
-        if (a.h && left > 0) store_part<kEven>((T*)a.h + row * a.ld_h + col, v[i], left);
+        for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].e[j] * a.drop.scale + (float)rr[i].e[j];
+        const Raw8<T> h = rounded8<T>(v[i]);
+        if (a.h && left > 0) store_part<kEven>((T*)a.h + row * a.ld_h, h, col, a.cols);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) v[i][j] = (float)h.e[j];
+      } else {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].e[j];
       }
 #pragma unroll
       for (int j = 0; j < kVec; ++j) sum += v[i][j];
@@ -144,7 +149,7 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
         float o[kVec];
 #pragma unroll
         for (int j = 0; j < kVec; ++j) o[j] = fmaf((v[i][j] - mean) * rstd, w[k][j], b[k][j]);
-        store_part<kEven>((T*)a.y + row * a.ld_y + col, o, left);
+        store_part<kEven>((T*)a.y + row * a.ld_y, rounded8<T>(o), col, a.cols);
       }
     }
   }
@@ -189,14 +194,14 @@ __device__ __forceinline__ void store_weight(void* p, bool w32, int col, float v
 // and, through the dropout, as dx (of the rounded dh, which other nodes see).
 template <typename T, bool kEven>
 __device__ __forceinline__ void finish_grad(const NormGradArgs& a, DropSite site, int64_t row, int group,
-                                            float (&o)[kVec], int left) {
+                                            float (&o)[kVec]) {
   const int col = group * kVec;
-  if (a.dh) store_part<kEven>((T*)a.dh + row * a.ld_dh + col, o, left);
+  const Raw8<T> r = rounded8<T>(o);
+  if (a.dh) store_part<kEven>((T*)a.dh + row * a.ld_dh, r, col, a.cols);
   if (a.dx) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) o[j] = as_stored<T>(o[j]);
-    if (a.drop.on) drop8(o, a.drop, site, group, (uint32_t)row);
-    store_part<kEven>((T*)a.dx + row * a.ld_dx + col, o, left);
+    for (int j = 0; j < kVec; ++j) o[j] = (float)r.e[j];
+    store_part<kEven>((T*)a.dx + row * a.ld_dx, dropped8<T>(o, a.drop, site, group, (uint32_t)row), col, a.cols);
   }
 }
 // A block's sum over its rows for one column (which 0: dw, 1: db): the result
@@ -289,7 +294,7 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
         const float xh = ((float)rh[i].e[j] - mean) * rstd;
         o[j] = fmaf(rstd, fmaf(-xh, s2, (float)rd[i].e[j] * w[k][j] - s1), (float)past[i].e[j]);
       }
-      finish_grad<T, kEven>(a, site, row, group, o, left);
+      finish_grad<T, kEven>(a, site, row, group, o);
     }
   }
   if (!a.dw && !a.db) return;
@@ -408,7 +413,7 @@ __global__ void __launch_bounds__(256) ckm_norm_wide_grad_kernel(NormGradArgs a,
       db[j] += d;
       o[j] = fmaf(rstd, fmaf(-xh, s2, d * w[j] - s1), (float)past.e[j]);
     }
-    finish_grad<T, false>(a, site, row, group, o, left);
+    finish_grad<T, false>(a, site, row, group, o);
   }
   if (!a.dw && !a.db) return;
   const int width = padded_cols(a.cols);

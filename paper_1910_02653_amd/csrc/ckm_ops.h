@@ -94,13 +94,28 @@ template <bool kEven, typename T>
 __device__ __forceinline__ void fix_tail(Raw8<T>& r, int col, int cols) {
   if constexpr (!kEven) {
     if (cols >= kVec && col + kVec > cols) {
-      const int by = col + kVec - cols;
+      const int by = kVec - cols % kVec;   // elements to move down, the same for every such group
+      constexpr int kWords = sizeof(r) / 4;
+      uint32_t w[kWords];
+      __builtin_memcpy(w, &r, sizeof(r));
+      const auto down = [&](int n) {       // by n words
 #pragma unroll
-      for (int bit = 4; bit >= 1; bit >>= 1)
-        if (by & bit) {
+        for (int k = 0; k < kWords; ++k) w[k] = k + n < kWords ? w[k + n] : 0u;
+      };
+      constexpr int kIn = 4 / sizeof(T);   // elements in a word
+      if (by & 4) down(4 / kIn);
+      if constexpr (kIn <= 2) {
+        if (by & 2) down(2 / kIn);
+      }
+      if constexpr (kIn == 1) {
+        if (by & 1) down(1);
+      } else {
+        const uint32_t bits = by % kIn * (32 / kIn);
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) r.e[j] = j + bit < kVec ? r.e[j + bit] : (T)0;
-        }
+        for (int k = 0; k < kWords; ++k)
+          w[k] = __builtin_amdgcn_alignbit(k + 1 < kWords ? w[k + 1] : 0u, w[k], bits);
+      }
+      __builtin_memcpy(&r, w, sizeof(r));
     }
   }
 }
@@ -112,28 +127,54 @@ __device__ __forceinline__ T rounded(float v) {
   if constexpr (std::is_same<T, _Float16>::value) asm("" : "+v"(v));
   return (T)v;
 }
-// Rounds to T (nearest even) and stores the elements that lie in the row.
 template <typename T>
-__device__ __forceinline__ void store_group(T* p, const float (&v)[kVec], int left) {
+__device__ __forceinline__ Raw8<T> rounded8(const float (&v)[kVec]) {
   Raw8<T> r;
+  if constexpr (sizeof(T) == 2) {   // two at a time
+    typedef float Two __attribute__((ext_vector_type(2)));
+    typedef T Half2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) r.e[j] = rounded<T>(v[j]);
-  if (left >= kVec) {
-    __builtin_memcpy(p, &r, sizeof(r));
+    for (int j = 0; j < kVec; j += 2) {
+      float lo = v[j], hi = v[j + 1];
+      if constexpr (std::is_same<T, _Float16>::value) asm("" : "+v"(lo), "+v"(hi));   // as in rounded()
+      const Half2 p = __builtin_convertvector((Two{lo, hi}), Half2);
+      r.e[j] = p.x;
+      r.e[j + 1] = p.y;
+    }
   } else {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j)
-      if (j < left) p[j] = r.e[j];
+    for (int j = 0; j < kVec; ++j) r.e[j] = v[j];
   }
+  return r;
+}
+// Stores a group at column `col` of a row: the last one of a row that is not of
+// whole groups in up to three pieces, of four, two and one elements.
+template <typename T, int kFrom, int kCount>
+__device__ __forceinline__ void store_piece(T* p, const Raw8<T>& r) {
+  __builtin_memcpy(p + kFrom, &r.e[kFrom], kCount * sizeof(T));
 }
 template <bool kEven, typename T>
-__device__ __forceinline__ void store_part(T* p, const float (&v)[kVec], int left) {
-  store_group(p, v, kEven ? kVec : left);
-}
-// v rounded to T and back: what a reader of the stored value sees.
-template <typename T>
-__device__ __forceinline__ float as_stored(float v) {
-  return (float)rounded<T>(v);
+__device__ __forceinline__ void store_part(T* row, const Raw8<T>& r, int col, int cols) {
+  T* p = row + col;
+  if (kEven || col + kVec <= cols) {
+    store_piece<T, 0, kVec>(p, r);
+    return;
+  }
+  const int n = cols % kVec;
+  if (n & 4) {
+    store_piece<T, 0, 4>(p, r);
+    if (n & 2) {
+      store_piece<T, 4, 2>(p, r);
+      if (n & 1) store_piece<T, 6, 1>(p, r);
+    } else if (n & 1) {
+      store_piece<T, 4, 1>(p, r);
+    }
+  } else if (n & 2) {
+    store_piece<T, 0, 2>(p, r);
+    if (n & 1) store_piece<T, 2, 1>(p, r);
+  } else {
+    store_piece<T, 0, 1>(p, r);
+  }
 }
 
 // Philox4x32-10 (Salmon et al., SC'11) of counter (group, row, site), the
@@ -171,16 +212,43 @@ __device__ __forceinline__ void draws8(uint32_t (&x)[4], const DropArgs& d, Drop
   x[2] = c2;
   x[3] = c3;
 }
-__device__ __forceinline__ bool kept(const uint32_t (&x)[4], int j, uint32_t keep) {
-  return ((j & 1) ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu) < keep;
+// All ones in the halves whose draw is below keep (keep < 65536), by saturating
+// differences of the two 16-bit halves at once: no lane masks, whose use right
+// after a comparison stalls.
+__device__ __forceinline__ uint32_t kept_halves(uint32_t draws, uint32_t keep) {
+  typedef uint16_t Half2 __attribute__((ext_vector_type(2)));
+  const Half2 k = {(uint16_t)keep, (uint16_t)keep}, one = {1, 1};
+  const Half2 below = __builtin_elementwise_min(__builtin_elementwise_sub_sat(k, __builtin_bit_cast(Half2, draws)), one);
+  return __builtin_bit_cast(uint32_t, (Half2)-below);
 }
-// Applies the dropout to the group's eight values: dropped ones become 0
-// whatever they hold, NaN and infinities too.
-__device__ __forceinline__ void drop8(float (&v)[kVec], const DropArgs& d, DropSite s, uint32_t group, uint32_t row) {
+// Applies the dropout's choice to a group as it is stored, before or after the
+// factor: dropped elements become 0 whatever they hold, NaN and infinities too.
+template <typename T>
+__device__ __forceinline__ void drop_choice(Raw8<T>& r, const DropArgs& d, DropSite s, uint32_t group, uint32_t row) {
   uint32_t x[4];
   draws8(x, d, s, group, row);
+  if constexpr (sizeof(T) == 2) {
+    uint32_t w[4];
+    __builtin_memcpy(w, &r, sizeof(w));
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) v[j] = kept(x, j, d.keep) ? v[j] * d.scale : 0.0f;
+    for (int k = 0; k < 4; ++k) w[k] &= kept_halves(x[k], d.keep);
+    __builtin_memcpy(&r, w, sizeof(w));
+  } else {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j)
+      r.e[j] = ((j & 1) ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu) < d.keep ? r.e[j] : (T)0;
+  }
+}
+// D of eight values, rounded to T.
+template <typename T>
+__device__ __forceinline__ Raw8<T> dropped8(const float (&v)[kVec], const DropArgs& d, DropSite s, uint32_t group,
+                                            uint32_t row) {
+  float o[kVec];
+#pragma unroll
+  for (int j = 0; j < kVec; ++j) o[j] = v[j] * d.scale;
+  Raw8<T> r = rounded8<T>(o);
+  if (d.on) drop_choice(r, d, s, group, row);
+  return r;
 }
 
 // The row of a block's rows that this thread works on: the same for a whole wave

@@ -73,6 +73,54 @@ __device__ __forceinline__ float exp_of(float t, float m) {
   return __builtin_amdgcn_exp2f((t - m) * kLog2e);
 }
 
+// A row's largest logit as its exponentials use it. Without a mask an
+// exponential is one fused multiply-add and 2^v: 2^(x scale log2 e - m log2 e).
+// Where those products could pass the range, at logits beyond 1e37, they are
+// formed by difference instead.
+struct Top {
+  float m, ml, sl;
+  bool far;
+};
+__device__ __forceinline__ Top top_of(float m, float scale) {
+  const float sl = scale * kLog2e;
+  return {m, m * kLog2e, sl, !(fabsf(m) < 1e37f) || !(fabsf(sl) < 1e37f)};
+}
+// exp(scale x - m) of a group's scores.
+template <typename T>
+__device__ __forceinline__ void exps8(float (&e)[kVec], const Raw8<T>& x, const Top& top, float scale) {
+  if (!top.far) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf((float)x.e[j], top.sl, -top.ml));
+  } else {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) e[j] = exp_of((float)x.e[j] * scale, top.m);
+  }
+}
+// The largest of a group's scores.
+template <typename T>
+__device__ __forceinline__ float top8(const Raw8<T>& x) {
+  if constexpr (std::is_same<T, _Float16>::value) {   // two at a time
+    typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
+    const Half2 a = __builtin_elementwise_max(Half2{x.e[0], x.e[1]}, Half2{x.e[2], x.e[3]});
+    const Half2 b = __builtin_elementwise_max(Half2{x.e[4], x.e[5]}, Half2{x.e[6], x.e[7]});
+    const Half2 m = __builtin_elementwise_max(a, b);
+    return fmaxf((float)m.x, (float)m.y);
+  } else {
+    float m = (float)x.e[0];
+#pragma unroll
+    for (int j = 1; j < kVec; ++j) m = fmaxf(m, (float)x.e[j]);
+    return m;
+  }
+}
+// Puts `value` in the place of a group's elements past the first `left`.
+template <typename T>
+__device__ __forceinline__ void hide(Raw8<T>& r, int left, T value) {
+  if (left < kVec) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) r.e[j] = j < left ? r.e[j] : value;
+  }
+}
+
 // A group of a mask as it is stored: values of the scores' type, or bytes.
 template <typename T>
 union RawMask {
@@ -84,14 +132,14 @@ template <bool kEven, typename T>
 __device__ __forceinline__ void load_mask(RawMask<T>& m, const SoftmaxArgs& a, const void* p, int col) {
   if (a.mask_kind == CKM_MASK_ADD)
     m.add = load_cols<kEven>((const T*)p, col, a.keys);
-  else
+  else if (a.mask_kind == CKM_MASK_BOOL)
     m.seen = load_cols<kEven>((const uint8_t*)p, col, a.keys);
 }
 template <bool kEven, typename T>
 __device__ __forceinline__ void fix_mask(RawMask<T>& m, const SoftmaxArgs& a, int col) {
   if (a.mask_kind == CKM_MASK_ADD)
     fix_tail<kEven>(m.add, col, a.keys);
-  else
+  else if (a.mask_kind == CKM_MASK_BOOL)
     fix_tail<kEven>(m.seen, col, a.keys);
 }
 template <typename T>
@@ -101,21 +149,18 @@ __device__ __forceinline__ const void* mask_row(const SoftmaxArgs& a, const Row&
 
 // The logits of a group; -inf where a key is not seen. Scores there are not used,
 // whatever they hold. left: seen keys from the group's first on.
-template <bool kMask, typename T>
+template <typename T>
 __device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, const Raw8<T>& x, const RawMask<T>& m,
                                         int left) {
-  if constexpr (kMask) {
-    if (a.mask_kind == CKM_MASK_ADD) {
+  if (a.mask_kind == CKM_MASK_ADD) {
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const float add = (float)m.add.e[j];
-        t[j] = j < left && add != -__builtin_inff() ? fmaf((float)x.e[j], a.scale, add) : -__builtin_inff();
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j)
-        t[j] = j < left && m.seen.e[j] ? (float)x.e[j] * a.scale : -__builtin_inff();
+    for (int j = 0; j < kVec; ++j) {
+      const float add = (float)m.add.e[j];
+      t[j] = (j < left) & (add != -__builtin_inff()) ? fmaf((float)x.e[j], a.scale, add) : -__builtin_inff();
     }
+  } else if (a.mask_kind == CKM_MASK_BOOL) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) t[j] = (j < left) & (m.seen.e[j] != 0) ? (float)x.e[j] * a.scale : -__builtin_inff();
   } else {
 #pragma unroll
     for (int j = 0; j < kVec; ++j) t[j] = j < left ? (float)x.e[j] * a.scale : -__builtin_inff();
@@ -123,130 +168,142 @@ __device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, 
 }
 
 // The gradient that reaches a group's probabilities through the dropout, but for
-// its factor, which the row's sum and the result take together; 0 where a key
-// is not seen.
-template <typename T>
-__device__ __forceinline__ void grads8(float (&g)[kVec], const SoftmaxArgs& a, DropSite site, const Raw8<T>& dy,
-                                       const float (&t)[kVec], int64_t row, int col) {
-  uint32_t x[4] = {};   // without a dropout every draw is below keep
-  if (a.drop.on) draws8(x, a.drop, site, col / kVec, (uint32_t)row);
+// its factor, which the row's sum and the result take together; 0 where a mask
+// left the exponential 0.
+template <bool kMask, typename T>
+__device__ __forceinline__ void grads8(float (&g)[kVec], const SoftmaxArgs& a, DropSite site, Raw8<T> dy,
+                                       const float (&e)[kVec], int64_t row, int col) {
+  if (a.drop.on) drop_choice(dy, a.drop, site, col / kVec, (uint32_t)row);
 #pragma unroll
-  for (int j = 0; j < kVec; ++j)
-    g[j] = (t[j] != -__builtin_inff()) & kept(x, j, a.drop.keep) ? (float)dy.e[j] : 0.0f;
+  for (int j = 0; j < kVec; ++j) g[j] = kMask && e[j] == 0.0f ? 0.0f : (float)dy.e[j];
 }
 
 constexpr int softmax_block(int lanes) { return lanes < 256 ? 256 : lanes; }
 
 // A row in the registers of kLanes threads, kPer groups each. kEven: rows of
-// whole groups, so that a group with any key seen can be loaded whole.
+// whole groups. kMask: a mask, or a scale that is not positive; without it the
+// unseen scores of a row's last group are set to -inf once, and the logits are
+// never formed.
 template <typename T, int kLanes, int kPer, bool kBack, bool kMask, bool kEven>
 __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(SoftmaxArgs a) {
   constexpr int kBlock = softmax_block(kLanes), kRowsAt = kBlock / kLanes;
   __shared__ float lds[kLanes > 64 ? 2 * kBlock / 64 : 1];
   const int lane = threadIdx.x % kLanes;
   const DropSite site = drop_site(a.drop);
-  int turn = 0;
-  for (int64_t first = (int64_t)blockIdx.x * kRowsAt; first < a.rows; first += (int64_t)gridDim.x * kRowsAt) {
-    const int64_t row = first + row_in_block<kLanes>();
-    const bool live = row < a.rows;
-    const Row r = row_of(a, live ? row : a.rows - 1);
-    const T* x = (const T*)a.x.p + offset_of(a.x, r);
-    const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
-    const void* mask = kMask ? mask_row<T>(a, r) : nullptr;
-    T* y = (T*)const_cast<void*>(a.y.p) + offset_of(a.y, r);
-    const int seen = live ? r.seen : 0, keys = live ? a.keys : 0;
-    // every load of the row first, then the arithmetic
-    Raw8<T> rx[kPer], rd[kBack ? kPer : 1];
-    RawMask<T> rm[kMask ? kPer : 1];
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kRowsAt + row_in_block<kLanes>();
+  const bool live = row < a.rows;
+  const Row r = row_of(a, live ? row : a.rows - 1);
+  const T* x = (const T*)a.x.p + offset_of(a.x, r);
+  const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
+  const void* mask = kMask ? mask_row<T>(a, r) : nullptr;
+  T* y = (T*)const_cast<void*>(a.y.p) + offset_of(a.y, r);
+  const int seen = live ? r.seen : 0, keys = live ? a.keys : 0;
+  // every load of the row first, then the arithmetic
+  Raw8<T> rx[kPer], rd[kBack ? kPer : 1];
+  RawMask<T> rm[kMask ? kPer : 1];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int col = (lane + i * kLanes) * kVec;
+    if (col < seen) {
+      rx[i] = load_cols<kEven>(x, col, a.keys);
+      if constexpr (kBack) rd[i] = load_cols<kEven>(dy, col, a.keys);
+      if constexpr (kMask) load_mask<kEven>(rm[i], a, mask, col);
+    }
+  }
+  float t[kPer][kVec];   // logits, then exponentials
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int col = (lane + i * kLanes) * kVec;
+    if (col < seen) {
+      fix_tail<kEven>(rx[i], col, a.keys);
+      if constexpr (kBack) fix_tail<kEven>(rd[i], col, a.keys);
+      if constexpr (kMask) {
+        fix_mask<kEven>(rm[i], a, col);
+        logits8(t[i], a, rx[i], rm[i], seen - col);
+      } else {
+        hide(rx[i], seen - col, (T)-__builtin_inff());
+        if constexpr (kBack) hide(rd[i], seen - col, (T)0);
+      }
+    }
+  }
+  if constexpr (!kBack) {
+    float m = kLowest;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec;
-      if (col < seen) {
-        rx[i] = load_cols<kEven>(x, col, a.keys);
-        if constexpr (kBack) rd[i] = load_cols<kEven>(dy, col, a.keys);
-        if constexpr (kMask) load_mask<kEven>(rm[i], a, mask, col);
+      if (col >= seen) continue;
+      if constexpr (kMask) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) m = fmaxf(m, t[i][j]);
+      } else {
+        m = fmaxf(m, top8(rx[i]));
       }
     }
-    float t[kPer][kVec];
-    if constexpr (!kBack) {
-      float m = kLowest;
+    m = reduce_row<OpMax, kLanes, kBlock>(m, lds, 0);
+    if constexpr (!kMask) m = fmaxf(m * a.scale, kLowest);
+    const Top top = top_of(m, a.scale);
+    float sum = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int col = (lane + i * kLanes) * kVec;
-        if (col < seen) {
-          fix_tail<kEven>(rx[i], col, a.keys);
-          if constexpr (kMask) fix_mask<kEven>(rm[i], a, col);
-          logits8<kMask>(t[i], a, rx[i], rm[kMask ? i : 0], seen - col);
+    for (int i = 0; i < kPer; ++i) {
+      const int col = (lane + i * kLanes) * kVec;
+      if (col >= seen) continue;
+      if constexpr (!kMask) exps8(t[i], rx[i], top, a.scale);
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) m = fmaxf(m, t[i][j]);
-        }
+      for (int j = 0; j < kVec; ++j) {
+        if constexpr (kMask) t[i][j] = exp_of(t[i][j], m);
+        sum += t[i][j];
       }
-      m = reduce_row<OpMax, kLanes, kBlock>(m, lds, 0);
-      float sum = 0.0f;
+    }
+    sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, 1);
+    const float z = sum == 0.0f ? 0.0f : 1.0f / sum;
+    if (live && lane == 0 && a.stats) {
+      a.stats[2 * row] = sum == 0.0f ? 0.0f : m;
+      a.stats[2 * row + 1] = z;
+    }
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int col = (lane + i * kLanes) * kVec;
-        if (col < seen) {
+    for (int i = 0; i < kPer; ++i) {
+      const int group = lane + i * kLanes, col = group * kVec;
+      if (col >= keys) continue;
+      Raw8<T> o = zero_group<T>();
+      if (col < seen) {
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) {
-            t[i][j] = exp_of(t[i][j], m);
-            sum += t[i][j];
-          }
-        }
+        for (int j = 0; j < kVec; ++j) t[i][j] *= z;
+        o = dropped8<T>(t[i], a.drop, site, group, (uint32_t)row);
       }
-      sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, 1);
-      const float z = sum == 0.0f ? 0.0f : 1.0f / sum;
-      if (live && lane == 0 && a.stats) {
-        a.stats[2 * row] = sum == 0.0f ? 0.0f : m;
-        a.stats[2 * row + 1] = z;
+      store_part<kEven>(y, o, col, keys);
+    }
+  } else {
+    const float m = live ? a.stats[2 * row] : 0.0f, z = live ? a.stats[2 * row + 1] : 0.0f;
+    const Top top = top_of(m, a.scale);
+    float g[kPer][kVec];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int col = (lane + i * kLanes) * kVec;
+      if (col >= seen) continue;
+      if constexpr (kMask) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) t[i][j] = exp_of(t[i][j], m);
+      } else {
+        exps8(t[i], rx[i], top, a.scale);
       }
+      grads8<kMask>(g[i], a, site, rd[i], t[i], row, col);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int group = lane + i * kLanes, col = group * kVec;
-        if (col >= keys) continue;
-        float o[kVec] = {};
-        if (col < seen) {
+      for (int j = 0; j < kVec; ++j) sum = fmaf(t[i][j], g[i][j], sum);
+    }
+    // p = e z: the row's z goes into its two factors
+    const float by = a.scale * a.drop.scale * z;
+    sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, 0) * z * by;
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) o[j] = t[i][j] * z;
-          if (a.drop.on) drop8(o, a.drop, site, group, (uint32_t)row);
-        }
-        store_part<kEven>(y + col, o, keys - col);
+    for (int i = 0; i < kPer; ++i) {
+      const int col = (lane + i * kLanes) * kVec;
+      if (col >= keys) continue;
+      float o[kVec] = {};
+      if (col < seen) {
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) o[j] = t[i][j] * fmaf(g[i][j], by, -sum);
       }
-    } else {
-      const float m = live ? a.stats[2 * row] : 0.0f, z = live ? a.stats[2 * row + 1] : 0.0f;
-      const float by = a.scale * a.drop.scale;
-      float g[kPer][kVec];
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int col = (lane + i * kLanes) * kVec;
-        if (col < seen) {
-          fix_tail<kEven>(rx[i], col, a.keys);
-          fix_tail<kEven>(rd[i], col, a.keys);
-          if constexpr (kMask) fix_mask<kEven>(rm[i], a, col);
-          logits8<kMask>(t[i], a, rx[i], rm[kMask ? i : 0], seen - col);
-          grads8(g[i], a, site, rd[i], t[i], row, col);
-#pragma unroll
-          for (int j = 0; j < kVec; ++j) {
-            t[i][j] = exp_of(t[i][j], m) * z;
-            sum = fmaf(t[i][j], g[i][j], sum);
-          }
-        }
-      }
-      sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, turn);
-      turn ^= 1;
-      sum *= by;
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const int col = (lane + i * kLanes) * kVec;
-        if (col >= keys) continue;
-        float o[kVec] = {};
-        if (col < seen) {
-#pragma unroll
-          for (int j = 0; j < kVec; ++j) o[j] = t[i][j] * fmaf(g[i][j], by, -sum);
-        }
-        store_part<kEven>(y + col, o, keys - col);
-      }
+      store_part<kEven>(y, rounded8<T>(o), col, keys);
     }
   }
 }
@@ -266,18 +323,14 @@ __device__ __forceinline__ Raw8<T> load_whole(const T* row, int col, int cols) {
 }
 template <typename T>
 __device__ __forceinline__ void load_logits8(float (&t)[kVec], const SoftmaxArgs& a, const T* x, const Row& r, int col) {
-  const int left = r.seen - col;
   Raw8<T> v = load_cols<false>(x, col, a.keys);
   RawMask<T> m;
   if (a.mask_kind != CKM_MASK_NONE) {
     load_mask<false>(m, a, mask_row<T>(a, r), col);
-    fix_tail<false>(v, col, a.keys);
     fix_mask<false>(m, a, col);
-    logits8<true>(t, a, v, m, left);
-  } else {
-    fix_tail<false>(v, col, a.keys);
-    logits8<false>(t, a, v, m, left);
   }
+  fix_tail<false>(v, col, a.keys);
+  logits8(t, a, v, m, r.seen - col);
 }
 
 constexpr int kSplitBlock = 256, kSplitSpan = kSplitBlock * kVec, kMaxSplits = kSplitBlock;
@@ -312,14 +365,16 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxA
       if (threadIdx.x == 0) part[item] = {top, sum};
     } else {
       const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
-      const float m = a.stats[2 * row], z = a.stats[2 * row + 1];
+      const float m = a.stats[2 * row];
       float sum = 0.0f;
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
         float t[kVec], g[kVec];
         load_logits8(t, a, x, r, col);
-        grads8(g, a, site, load_whole(dy, col, a.keys), t, row, col);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) sum = fmaf(exp_of(t[j], m) * z, g[j], sum);
+        for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m);
+        grads8<true>(g, a, site, load_whole(dy, col, a.keys), t, row, col);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) sum = fmaf(t[j], g[j], sum);
       }
       sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum, lds, turn);
       turn ^= 1;
@@ -353,31 +408,34 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxAr
         a.stats[2 * row + 1] = z;
       }
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
-        float t[kVec] = {};
+        Raw8<T> o = zero_group<T>();
         if (col < r.seen) {
+          float t[kVec];
           load_logits8(t, a, x, r, col);
 #pragma unroll
           for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m) * z;
-          if (a.drop.on) drop8(t, a.drop, site, col / kVec, (uint32_t)row);
+          o = dropped8<T>(t, a.drop, site, col / kVec, (uint32_t)row);
         }
-        store_group(y + col, t, a.keys - col);
+        store_part<false>(y, o, col, a.keys);
       }
     } else {
       const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
       const float m = a.stats[2 * row], z = a.stats[2 * row + 1];
-      const float by = a.scale * a.drop.scale;
-      const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, turn) * by;
+      const float by = a.scale * a.drop.scale * z;
+      const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, turn) * z * by;
       turn ^= 1;
       for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
         float o[kVec] = {};
         if (col < r.seen) {
           float t[kVec], g[kVec];
           load_logits8(t, a, x, r, col);
-          grads8(g, a, site, load_whole(dy, col, a.keys), t, row, col);
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) o[j] = exp_of(t[j], m) * z * fmaf(g[j], by, -sum);
+          for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m);
+          grads8<true>(g, a, site, load_whole(dy, col, a.keys), t, row, col);
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) o[j] = t[j] * fmaf(g[j], by, -sum);
         }
-        store_group(y + col, o, a.keys - col);
+        store_part<false>(y, rounded8<T>(o), col, a.keys);
       }
     }
   }
@@ -400,9 +458,11 @@ int softmax_splits(int64_t rows, int64_t keys) {
 template <typename T, bool kBack, int kLanes, int kPer>
 void launch_whole_as(const SoftmaxArgs& a, hipStream_t s) {
   constexpr int kBlock = softmax_block(kLanes), kRowsAt = kBlock / kLanes;
-  const int64_t blocks = std::min<int64_t>((a.rows + kRowsAt - 1) / kRowsAt, 1 << 20);
-  const dim3 grid((uint32_t)blocks);
-  const bool mask = a.mask_kind != CKM_MASK_NONE, even = a.keys % kVec == 0;
+  // one set of rows to a block, in two dimensions: a launch has fewer than 2^32
+  // threads in each
+  const int64_t blocks = (a.rows + kRowsAt - 1) / kRowsAt, wide = std::min<int64_t>(blocks, 1 << 20);
+  const dim3 grid((uint32_t)wide, (uint32_t)((blocks + wide - 1) / wide));
+  const bool mask = a.mask_kind != CKM_MASK_NONE || !(a.scale > 0.0f), even = a.keys % kVec == 0;
   if (mask && even) ckm_softmax_kernel<T, kLanes, kPer, kBack, true, true><<<grid, kBlock, 0, s>>>(a);
   else if (mask) ckm_softmax_kernel<T, kLanes, kPer, kBack, true, false><<<grid, kBlock, 0, s>>>(a);
   else if (even) ckm_softmax_kernel<T, kLanes, kPer, kBack, false, true><<<grid, kBlock, 0, s>>>(a);
