@@ -54,11 +54,11 @@ __global__ void __launch_bounds__(kDropBlock) ckm_dropout_kernel(int64_t total, 
     if (drop.on) drop_choice(vx, drop, site, group, (uint32_t)row);
     float v[kVec];
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = (float)vx.e[j] * drop.scale;
+    for (int j = 0; j < kVec; ++j) v[j] = (float)vx.get(j) * drop.scale;
     if constexpr (kRes) {
       fix_tail<kFlat>(vr, col, cols);
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) v[j] += (float)vr.e[j];
+      for (int j = 0; j < kVec; ++j) v[j] += (float)vr.get(j);
     }
     if constexpr (kFlat)
       store_part<true>(y + g * kVec, rounded8<T>(v), 0, kVec);

@@ -51,13 +51,13 @@ __device__ __forceinline__ void weight_group(float (&v)[kVec], const void* p, bo
 #pragma unroll
     for (int j = 0; j < kVec; ++j) v[j] = absent;
   } else if (w32) {
-    const Raw8<float> r = load_group((const float*)p + col, left);
+    const Raw8<float> r = load_left((const float*)p + col, left);
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = r.e[j];
+    for (int j = 0; j < kVec; ++j) v[j] = r.get(j);
   } else {
-    const Raw8<T> r = load_group((const T*)p + col, left);
+    const Raw8<T> r = load_left((const T*)p + col, left);
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = (float)r.e[j];
+    for (int j = 0; j < kVec; ++j) v[j] = (float)r.get(j);
   }
 }
 
@@ -108,14 +108,14 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
         if (a.drop.on) drop_choice(r[i], a.drop, site, group, (uint32_t)row);
         fix_tail<kEven>(rr[i], col, a.cols);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].e[j] * a.drop.scale + (float)rr[i].e[j];
+        for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].get(j) * a.drop.scale + (float)rr[i].get(j);
         const Raw8<T> h = rounded8<T>(v[i]);
         if (a.h && left > 0) store_part<kEven>((T*)a.h + row * a.ld_h, h, col, a.cols);
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) v[i][j] = (float)h.e[j];
+        for (int j = 0; j < kVec; ++j) v[i][j] = (float)h.get(j);
       } else {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].e[j];
+        for (int j = 0; j < kVec; ++j) v[i][j] = (float)r[i].get(j);
       }
 #pragma unroll
       for (int j = 0; j < kVec; ++j) sum += v[i][j];
@@ -200,7 +200,7 @@ __device__ __forceinline__ void finish_grad(const NormGradArgs& a, DropSite site
   if (a.dh) store_part<kEven>((T*)a.dh + row * a.ld_dh, r, col, a.cols);
   if (a.dx) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) o[j] = (float)r.e[j];
+    for (int j = 0; j < kVec; ++j) o[j] = (float)r.get(j);
     store_part<kEven>((T*)a.dx + row * a.ld_dx, dropped8<T>(o, a.drop, site, group, (uint32_t)row), col, a.cols);
   }
 }
@@ -268,8 +268,8 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
       if constexpr (!kKeep) weight_group<T>(w[0], a.w, a.w32, (lane + i * kLanes) * kVec, left, 1.0f);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const float d = (float)rd[i].e[j];
-        const float xh = (kEven ? left > 0 : j < left) ? ((float)rh[i].e[j] - mean) * rstd : 0.0f;
+        const float d = (float)rd[i].get(j);
+        const float xh = (kEven ? left > 0 : j < left) ? ((float)rh[i].get(j) - mean) * rstd : 0.0f;
         const float g = d * w[k][j];
         dw[i][j] = fmaf(d, xh, dw[i][j]);
         db[i][j] += d;
@@ -291,8 +291,8 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
       float o[kVec];
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const float xh = ((float)rh[i].e[j] - mean) * rstd;
-        o[j] = fmaf(rstd, fmaf(-xh, s2, (float)rd[i].e[j] * w[k][j] - s1), (float)past[i].e[j]);
+        const float xh = ((float)rh[i].get(j) - mean) * rstd;
+        o[j] = fmaf(rstd, fmaf(-xh, s2, (float)rd[i].get(j) * w[k][j] - s1), (float)past[i].get(j));
       }
       finish_grad<T, kEven>(a, site, row, group, o);
     }
@@ -372,15 +372,15 @@ __global__ void __launch_bounds__(1024) ckm_norm_wide_sums_kernel(NormGradArgs a
     float s1 = 0.0f, s2 = 0.0f;
     for (int col = threadIdx.x * kVec; col < a.cols; col += 1024 * kVec) {
       const int left = a.cols - col;
-      const Raw8<T> rd = load_group((const T*)a.dy + row * a.ld_dy + col, left);
-      const Raw8<T> rh = load_group((const T*)a.h + row * a.ld_h + col, left);
+      const Raw8<T> rd = load_left((const T*)a.dy + row * a.ld_dy + col, left);
+      const Raw8<T> rh = load_left((const T*)a.h + row * a.ld_h + col, left);
       float w[kVec];
       weight_group<T>(w, a.w, a.w32, col, left, 1.0f);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const float g = (float)rd.e[j] * w[j];
+        const float g = (float)rd.get(j) * w[j];
         s1 += g;
-        s2 = j < left ? fmaf(g, ((float)rh.e[j] - mean) * rstd, s2) : s2;
+        s2 = j < left ? fmaf(g, ((float)rh.get(j) - mean) * rstd, s2) : s2;
       }
     }
     reduce_two<1024, 1024>(s1, s2, lds, turn);
@@ -401,17 +401,17 @@ __global__ void __launch_bounds__(256) ckm_norm_wide_grad_kernel(NormGradArgs a,
   weight_group<T>(w, a.w, a.w32, col, left, 1.0f);
   for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
     const float mean = a.stats[2 * row], rstd = a.stats[2 * row + 1], s1 = sums[2 * row], s2 = sums[2 * row + 1];
-    const Raw8<T> rd = load_group((const T*)a.dy + row * a.ld_dy + col, left);
-    const Raw8<T> rh = load_group((const T*)a.h + row * a.ld_h + col, left);
+    const Raw8<T> rd = load_left((const T*)a.dy + row * a.ld_dy + col, left);
+    const Raw8<T> rh = load_left((const T*)a.h + row * a.ld_h + col, left);
     Raw8<T> past = zero_group<T>();
-    if (a.dres) past = load_group((const T*)a.dres + row * a.ld_dres + col, left);
+    if (a.dres) past = load_left((const T*)a.dres + row * a.ld_dres + col, left);
     float o[kVec];
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      const float d = (float)rd.e[j], xh = ((float)rh.e[j] - mean) * rstd;
+      const float d = (float)rd.get(j), xh = ((float)rh.get(j) - mean) * rstd;
       dw[j] = fmaf(d, xh, dw[j]);
       db[j] += d;
-      o[j] = fmaf(rstd, fmaf(-xh, s2, d * w[j] - s1), (float)past.e[j]);
+      o[j] = fmaf(rstd, fmaf(-xh, s2, d * w[j] - s1), (float)past.get(j));
     }
     finish_grad<T, false>(a, site, row, group, o);
   }

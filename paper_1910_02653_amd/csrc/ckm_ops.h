@@ -49,11 +49,22 @@ ckm_status launched(const char* what);
 
 // ---- device side ----------------------------------------------------------
 
-// Eight elements at p, which need only be aligned to their own size: rows of
-// odd length or stride start anywhere, and the hardware takes such addresses.
+// A group as it is stored, in whole words: joined and moved as words, it stays in
+// the registers it was loaded into, and a load need not be waited for to take it
+// apart. Rows of odd length or stride start anywhere: addresses need only be
+// aligned to an element, which the hardware's loads and stores take.
 template <typename T>
 struct Raw8 {
-  T e[kVec];
+  static constexpr int kWords = kVec * sizeof(T) / 4, kIn = 4 / sizeof(T);   // words, elements in one
+  uint32_t w[kWords];
+  __device__ __forceinline__ T get(int j) const {
+    if constexpr (sizeof(T) == 4)
+      return __builtin_bit_cast(T, w[j]);
+    else if constexpr (sizeof(T) == 2)
+      return __builtin_bit_cast(T, (uint16_t)(w[j / 2] >> (16 * (j % 2))));
+    else
+      return (T)(w[j / 4] >> (8 * (j % 4)));
+  }
 };
 template <typename T>
 __device__ __forceinline__ Raw8<T> load8(const T* p) {
@@ -61,61 +72,128 @@ __device__ __forceinline__ Raw8<T> load8(const T* p) {
   __builtin_memcpy(&r, p, sizeof(r));
   return r;
 }
-// The group's elements that lie in the row (left of them, 1 or more); zeros past it.
-template <typename T>
-__device__ __forceinline__ Raw8<T> load_group(const T* p, int left) {
-  if (left >= kVec) return load8(p);
-  Raw8<T> r;
-#pragma unroll
-  for (int j = 0; j < kVec; ++j) r.e[j] = j < left ? p[j] : (T)0;
-  return r;
-}
 template <typename T>
 __device__ __forceinline__ Raw8<T> zero_group() {
   Raw8<T> r;
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) r.e[j] = (T)0;
+  for (int k = 0; k < Raw8<T>::kWords; ++k) r.w[k] = 0u;
   return r;
+}
+// kCount elements from kFrom on.
+template <typename T, int kFrom, int kCount>
+__device__ __forceinline__ void load_piece(Raw8<T>& r, const T* p) {
+  constexpr int kBytes = kCount * sizeof(T), kAt = kFrom * sizeof(T);
+  if constexpr (kBytes >= 4) {
+    __builtin_memcpy(&r.w[kAt / 4], p + kFrom, kBytes);
+  } else if constexpr (kBytes == 2) {
+    uint16_t v;
+    __builtin_memcpy(&v, p + kFrom, 2);
+    r.w[kAt / 4] |= (uint32_t)v << (kAt % 4 * 8);
+  } else {
+    r.w[kAt / 4] |= (uint32_t)(uint8_t)p[kFrom] << (kAt % 4 * 8);
+  }
+}
+template <typename T, int kFrom, int kCount>
+__device__ __forceinline__ void store_piece(T* p, const Raw8<T>& r) {
+  constexpr int kBytes = kCount * sizeof(T), kAt = kFrom * sizeof(T);
+  if constexpr (kBytes >= 4) {
+    __builtin_memcpy(p + kFrom, &r.w[kAt / 4], kBytes);
+  } else {
+    const uint16_t v = (uint16_t)(r.w[kAt / 4] >> (kAt % 4 * 8));
+    __builtin_memcpy(p + kFrom, &v, 2);
+  }
+}
+// Calls f(from, count) for the pieces of four, two and one elements of n < 8.
+template <typename F>
+__device__ __forceinline__ void pieces(int n, F&& f) {
+  using std::integral_constant;
+  if (n & 4) {
+    f(integral_constant<int, 0>{}, integral_constant<int, 4>{});
+    if (n & 2) {
+      f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
+      if (n & 1) f(integral_constant<int, 6>{}, integral_constant<int, 1>{});
+    } else if (n & 1) {
+      f(integral_constant<int, 4>{}, integral_constant<int, 1>{});
+    }
+  } else if (n & 2) {
+    f(integral_constant<int, 0>{}, integral_constant<int, 2>{});
+    if (n & 1) f(integral_constant<int, 2>{}, integral_constant<int, 1>{});
+  } else if (n & 1) {
+    f(integral_constant<int, 0>{}, integral_constant<int, 1>{});
+  }
 }
 // Column `col` on of a row of `cols` columns: one load for a whole group. In rows
 // that are not of whole groups (kEven false) the last one is loaded where it ends
 // with the row, and fix_tail moves its elements into place, after the loads that
-// a kernel wants in flight together. Rows of fewer than eight go by element.
+// a kernel wants in flight together. Rows of fewer than eight go by pieces.
 template <bool kEven, typename T>
 __device__ __forceinline__ Raw8<T> load_cols(const T* row, int col, int cols) {
   if constexpr (kEven) {
     return load8(row + col);
   } else {
-    if (cols < kVec) return load_group(row + col, cols - col);
-    return load8(row + min(col, cols - kVec));
+    if (cols >= kVec) return load8(row + min(col, cols - kVec));
+    Raw8<T> r = zero_group<T>();
+    pieces(cols, [&](auto from, auto count) { load_piece<T, decltype(from)::value, decltype(count)::value>(r, row); });
+    return r;
   }
 }
 template <bool kEven, typename T>
 __device__ __forceinline__ void fix_tail(Raw8<T>& r, int col, int cols) {
   if constexpr (!kEven) {
     if (cols >= kVec && col + kVec > cols) {
+      constexpr int kWords = Raw8<T>::kWords, kIn = Raw8<T>::kIn;
       const int by = kVec - cols % kVec;   // elements to move down, the same for every such group
-      constexpr int kWords = sizeof(r) / 4;
-      uint32_t w[kWords];
-      __builtin_memcpy(w, &r, sizeof(r));
       const auto down = [&](int n) {       // by n words
 #pragma unroll
-        for (int k = 0; k < kWords; ++k) w[k] = k + n < kWords ? w[k + n] : 0u;
+        for (int k = 0; k < kWords; ++k) r.w[k] = k + n < kWords ? r.w[k + n] : 0u;
       };
-      constexpr int kIn = 4 / sizeof(T);   // elements in a word
       if (by & 4) down(4 / kIn);
-      if constexpr (kIn <= 2) {
+      if constexpr (kIn <= 2)
         if (by & 2) down(2 / kIn);
-      }
       if constexpr (kIn == 1) {
         if (by & 1) down(1);
       } else {
         const uint32_t bits = by % kIn * (32 / kIn);
 #pragma unroll
         for (int k = 0; k < kWords; ++k)
-          w[k] = __builtin_amdgcn_alignbit(k + 1 < kWords ? w[k + 1] : 0u, w[k], bits);
+          r.w[k] = __builtin_amdgcn_alignbit(k + 1 < kWords ? r.w[k + 1] : 0u, r.w[k], bits);
       }
-      __builtin_memcpy(&r, w, sizeof(r));
+    }
+  }
+}
+// Stores a group at column `col` of a row, the last one of a row that is not of
+// whole groups in pieces.
+template <bool kEven, typename T>
+__device__ __forceinline__ void store_part(T* row, const Raw8<T>& r, int col, int cols) {
+  T* p = row + col;
+  if (kEven || col + kVec <= cols) {
+    __builtin_memcpy(p, &r, sizeof(r));
+  } else {
+    pieces(cols % kVec,
+           [&](auto from, auto count) { store_piece<T, decltype(from)::value, decltype(count)::value>(p, r); });
+  }
+}
+// The first `left` elements of eight in memory, 1 or more; zeros past them.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_left(const T* p, int left) {
+  if (left >= kVec) return load8(p);
+  Raw8<T> r = zero_group<T>();
+  pieces(left, [&](auto from, auto count) { load_piece<T, decltype(from)::value, decltype(count)::value>(r, p); });
+  return r;
+}
+// Puts `value` in the place of a group's elements past the first `left`.
+template <typename T>
+__device__ __forceinline__ void hide(Raw8<T>& r, int left, T value) {
+  if (left >= kVec) return;
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < kVec; ++j) r.w[j] = j < left ? r.w[j] : __builtin_bit_cast(uint32_t, value);
+  } else {
+    const uint32_t v = __builtin_bit_cast(uint16_t, value) * 0x10001u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t keep = left >= 2 * k + 2 ? ~0u : left > 2 * k ? 0xFFFFu : 0u;
+      r.w[k] = (r.w[k] & keep) | (v & ~keep);
     }
   }
 }
@@ -134,47 +212,16 @@ __device__ __forceinline__ Raw8<T> rounded8(const float (&v)[kVec]) {
     typedef float Two __attribute__((ext_vector_type(2)));
     typedef T Half2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int j = 0; j < kVec; j += 2) {
-      float lo = v[j], hi = v[j + 1];
+    for (int k = 0; k < 4; ++k) {
+      float lo = v[2 * k], hi = v[2 * k + 1];
       if constexpr (std::is_same<T, _Float16>::value) asm("" : "+v"(lo), "+v"(hi));   // as in rounded()
-      const Half2 p = __builtin_convertvector((Two{lo, hi}), Half2);
-      r.e[j] = p.x;
-      r.e[j + 1] = p.y;
+      r.w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((Two{lo, hi}), Half2));
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) r.e[j] = v[j];
+    for (int j = 0; j < kVec; ++j) r.w[j] = __float_as_uint(v[j]);
   }
   return r;
-}
-// Stores a group at column `col` of a row: the last one of a row that is not of
-// whole groups in up to three pieces, of four, two and one elements.
-template <typename T, int kFrom, int kCount>
-__device__ __forceinline__ void store_piece(T* p, const Raw8<T>& r) {
-  __builtin_memcpy(p + kFrom, &r.e[kFrom], kCount * sizeof(T));
-}
-template <bool kEven, typename T>
-__device__ __forceinline__ void store_part(T* row, const Raw8<T>& r, int col, int cols) {
-  T* p = row + col;
-  if (kEven || col + kVec <= cols) {
-    store_piece<T, 0, kVec>(p, r);
-    return;
-  }
-  const int n = cols % kVec;
-  if (n & 4) {
-    store_piece<T, 0, 4>(p, r);
-    if (n & 2) {
-      store_piece<T, 4, 2>(p, r);
-      if (n & 1) store_piece<T, 6, 1>(p, r);
-    } else if (n & 1) {
-      store_piece<T, 4, 1>(p, r);
-    }
-  } else if (n & 2) {
-    store_piece<T, 0, 2>(p, r);
-    if (n & 1) store_piece<T, 2, 1>(p, r);
-  } else {
-    store_piece<T, 0, 1>(p, r);
-  }
 }
 
 // Philox4x32-10 (Salmon et al., SC'11) of counter (group, row, site), the
@@ -228,15 +275,12 @@ __device__ __forceinline__ void drop_choice(Raw8<T>& r, const DropArgs& d, DropS
   uint32_t x[4];
   draws8(x, d, s, group, row);
   if constexpr (sizeof(T) == 2) {
-    uint32_t w[4];
-    __builtin_memcpy(w, &r, sizeof(w));
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w[k] &= kept_halves(x[k], d.keep);
-    __builtin_memcpy(&r, w, sizeof(w));
+    for (int k = 0; k < 4; ++k) r.w[k] &= kept_halves(x[k], d.keep);
   } else {
 #pragma unroll
     for (int j = 0; j < kVec; ++j)
-      r.e[j] = ((j & 1) ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu) < d.keep ? r.e[j] : (T)0;
+      r.w[j] = ((j & 1) ? x[j >> 1] >> 16 : x[j >> 1] & 0xFFFFu) < d.keep ? r.w[j] : 0u;
   }
 }
 // D of eight values, rounded to T.

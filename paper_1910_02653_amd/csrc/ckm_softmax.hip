@@ -90,10 +90,10 @@ template <typename T>
 __device__ __forceinline__ void exps8(float (&e)[kVec], const Raw8<T>& x, const Top& top, float scale) {
   if (!top.far) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf((float)x.e[j], top.sl, -top.ml));
+    for (int j = 0; j < kVec; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf((float)x.get(j), top.sl, -top.ml));
   } else {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) e[j] = exp_of((float)x.e[j] * scale, top.m);
+    for (int j = 0; j < kVec; ++j) e[j] = exp_of((float)x.get(j) * scale, top.m);
   }
 }
 // The largest of a group's scores.
@@ -101,26 +101,17 @@ template <typename T>
 __device__ __forceinline__ float top8(const Raw8<T>& x) {
   if constexpr (std::is_same<T, _Float16>::value) {   // two at a time
     typedef _Float16 Half2 __attribute__((ext_vector_type(2)));
-    const Half2 a = __builtin_elementwise_max(Half2{x.e[0], x.e[1]}, Half2{x.e[2], x.e[3]});
-    const Half2 b = __builtin_elementwise_max(Half2{x.e[4], x.e[5]}, Half2{x.e[6], x.e[7]});
-    const Half2 m = __builtin_elementwise_max(a, b);
+    const auto two = [&](int k) { return __builtin_bit_cast(Half2, x.w[k]); };
+    const Half2 m = __builtin_elementwise_max(__builtin_elementwise_max(two(0), two(1)),
+                                              __builtin_elementwise_max(two(2), two(3)));
     return fmaxf((float)m.x, (float)m.y);
   } else {
-    float m = (float)x.e[0];
+    float m = (float)x.get(0);
 #pragma unroll
-    for (int j = 1; j < kVec; ++j) m = fmaxf(m, (float)x.e[j]);
+    for (int j = 1; j < kVec; ++j) m = fmaxf(m, (float)x.get(j));
     return m;
   }
 }
-// Puts `value` in the place of a group's elements past the first `left`.
-template <typename T>
-__device__ __forceinline__ void hide(Raw8<T>& r, int left, T value) {
-  if (left < kVec) {
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) r.e[j] = j < left ? r.e[j] : value;
-  }
-}
-
 // A group of a mask as it is stored: values of the scores' type, or bytes.
 template <typename T>
 union RawMask {
@@ -155,15 +146,15 @@ __device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, 
   if (a.mask_kind == CKM_MASK_ADD) {
 #pragma unroll
     for (int j = 0; j < kVec; ++j) {
-      const float add = (float)m.add.e[j];
-      t[j] = (j < left) & (add != -__builtin_inff()) ? fmaf((float)x.e[j], a.scale, add) : -__builtin_inff();
+      const float add = (float)m.add.get(j);
+      t[j] = (j < left) & (add != -__builtin_inff()) ? fmaf((float)x.get(j), a.scale, add) : -__builtin_inff();
     }
   } else if (a.mask_kind == CKM_MASK_BOOL) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) t[j] = (j < left) & (m.seen.e[j] != 0) ? (float)x.e[j] * a.scale : -__builtin_inff();
+    for (int j = 0; j < kVec; ++j) t[j] = (j < left) & (m.seen.get(j) != 0) ? (float)x.get(j) * a.scale : -__builtin_inff();
   } else {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) t[j] = j < left ? (float)x.e[j] * a.scale : -__builtin_inff();
+    for (int j = 0; j < kVec; ++j) t[j] = j < left ? (float)x.get(j) * a.scale : -__builtin_inff();
   }
 }
 
@@ -175,7 +166,7 @@ __device__ __forceinline__ void grads8(float (&g)[kVec], const SoftmaxArgs& a, D
                                        const float (&e)[kVec], int64_t row, int col) {
   if (a.drop.on) drop_choice(dy, a.drop, site, col / kVec, (uint32_t)row);
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) g[j] = kMask && e[j] == 0.0f ? 0.0f : (float)dy.e[j];
+  for (int j = 0; j < kVec; ++j) g[j] = kMask && e[j] == 0.0f ? 0.0f : (float)dy.get(j);
 }
 
 constexpr int softmax_block(int lanes) { return lanes < 256 ? 256 : lanes; }
