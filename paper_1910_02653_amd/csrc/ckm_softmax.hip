@@ -112,70 +112,57 @@ __device__ __forceinline__ float top8(const Raw8<T>& x) {
     return m;
   }
 }
-// A group of a mask as it is stored: values of the scores' type, or bytes.
-template <typename T>
-union RawMask {
-  Raw8<T> add;
-  Raw8<uint8_t> seen;
-  __device__ RawMask() {}
-};
-template <bool kEven, typename T>
-__device__ __forceinline__ void load_mask(RawMask<T>& m, const SoftmaxArgs& a, const void* p, int col) {
-  if (a.mask_kind == CKM_MASK_ADD)
-    m.add = load_cols<kEven>((const T*)p, col, a.keys);
-  else if (a.mask_kind == CKM_MASK_BOOL)
-    m.seen = load_cols<kEven>((const uint8_t*)p, col, a.keys);
-}
-template <bool kEven, typename T>
-__device__ __forceinline__ void fix_mask(RawMask<T>& m, const SoftmaxArgs& a, int col) {
-  if (a.mask_kind == CKM_MASK_ADD)
-    fix_tail<kEven>(m.add, col, a.keys);
-  else if (a.mask_kind == CKM_MASK_BOOL)
-    fix_tail<kEven>(m.seen, col, a.keys);
-}
-template <typename T>
-__device__ __forceinline__ const void* mask_row(const SoftmaxArgs& a, const Row& r) {
-  return (const char*)a.mask.p + offset_of(a.mask, r) * (a.mask_kind == CKM_MASK_ADD ? (int)sizeof(T) : 1);
-}
 
+// What a row's logits are made of: the scores alone (kPlain: with a scale that is
+// not positive), a mask of truth values or of values to add. Without a mask and
+// with a positive scale (kNoMask) no logits are formed.
+enum : int { kNoMask = 0, kBool = 1, kAdd = 2, kPlain = 3 };
+int mask_form(int mask_kind, float scale) {
+  return mask_kind == CKM_MASK_BOOL ? kBool : mask_kind == CKM_MASK_ADD ? kAdd : scale > 0.0f ? kNoMask : kPlain;
+}
+template <int kMask, typename T>
+using MaskType = std::conditional_t<kMask == kBool, uint8_t, T>;
+
+template <int kMask, typename T>
+__device__ __forceinline__ const MaskType<kMask, T>* mask_row(const SoftmaxArgs& a, const Row& r) {
+  return (const MaskType<kMask, T>*)a.mask.p + offset_of(a.mask, r);
+}
 // The logits of a group; -inf where a key is not seen. Scores there are not used,
 // whatever they hold. left: seen keys from the group's first on.
-template <typename T>
-__device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, const Raw8<T>& x, const RawMask<T>& m,
-                                        int left) {
-  if (a.mask_kind == CKM_MASK_ADD) {
+template <int kMask, typename T>
+__device__ __forceinline__ void logits8(float (&t)[kVec], const SoftmaxArgs& a, const Raw8<T>& x,
+                                        const Raw8<MaskType<kMask, T>>& m, int left) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) {
-      const float add = (float)m.add.get(j);
-      t[j] = (j < left) & (add != -__builtin_inff()) ? fmaf((float)x.get(j), a.scale, add) : -__builtin_inff();
+  for (int j = 0; j < kVec; ++j) {
+    bool seen = j < left;
+    float add = 0.0f;
+    if constexpr (kMask == kAdd) {
+      add = (float)m.get(j);
+      seen &= add != -__builtin_inff();
     }
-  } else if (a.mask_kind == CKM_MASK_BOOL) {
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) t[j] = (j < left) & (m.seen.get(j) != 0) ? (float)x.get(j) * a.scale : -__builtin_inff();
-  } else {
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) t[j] = j < left ? (float)x.get(j) * a.scale : -__builtin_inff();
+    if constexpr (kMask == kBool) seen &= m.get(j) != 0;
+    const float v = kMask == kAdd ? fmaf((float)x.get(j), a.scale, add) : (float)x.get(j) * a.scale;
+    t[j] = seen ? v : -__builtin_inff();
   }
 }
 
 // The gradient that reaches a group's probabilities through the dropout, but for
 // its factor, which the row's sum and the result take together; 0 where a mask
 // left the exponential 0.
-template <bool kMask, typename T>
+template <int kMask, typename T>
 __device__ __forceinline__ void grads8(float (&g)[kVec], const SoftmaxArgs& a, DropSite site, Raw8<T> dy,
                                        const float (&e)[kVec], int64_t row, int col) {
   if (a.drop.on) drop_choice(dy, a.drop, site, col / kVec, (uint32_t)row);
 #pragma unroll
-  for (int j = 0; j < kVec; ++j) g[j] = kMask && e[j] == 0.0f ? 0.0f : (float)dy.get(j);
+  for (int j = 0; j < kVec; ++j) g[j] = kMask != kNoMask && e[j] == 0.0f ? 0.0f : (float)dy.get(j);
 }
 
 constexpr int softmax_block(int lanes) { return lanes < 256 ? 256 : lanes; }
 
 // A row in the registers of kLanes threads, kPer groups each. kEven: rows of
-// whole groups. kMask: a mask, or a scale that is not positive; without it the
-// unseen scores of a row's last group are set to -inf once, and the logits are
-// never formed.
-template <typename T, int kLanes, int kPer, bool kBack, bool kMask, bool kEven>
+// whole groups. With kNoMask the unseen scores of a row's last group are set to
+// -inf once.
+template <typename T, int kLanes, int kPer, bool kBack, int kMask, bool kEven>
 __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(SoftmaxArgs a) {
   constexpr int kBlock = softmax_block(kLanes), kRowsAt = kBlock / kLanes;
   __shared__ float lds[kLanes > 64 ? 2 * kBlock / 64 : 1];
@@ -186,19 +173,20 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
   const Row r = row_of(a, live ? row : a.rows - 1);
   const T* x = (const T*)a.x.p + offset_of(a.x, r);
   const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
-  const void* mask = kMask ? mask_row<T>(a, r) : nullptr;
+  constexpr bool kMasked = kMask == kBool || kMask == kAdd;
+  const MaskType<kMask, T>* mask = kMasked ? mask_row<kMask, T>(a, r) : nullptr;
   T* y = (T*)const_cast<void*>(a.y.p) + offset_of(a.y, r);
   const int seen = live ? r.seen : 0, keys = live ? a.keys : 0;
   // every load of the row first, then the arithmetic
   Raw8<T> rx[kPer], rd[kBack ? kPer : 1];
-  RawMask<T> rm[kMask ? kPer : 1];
+  Raw8<MaskType<kMask, T>> rm[kMasked ? kPer : 1];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int col = (lane + i * kLanes) * kVec;
     if (col < seen) {
       rx[i] = load_cols<kEven>(x, col, a.keys);
       if constexpr (kBack) rd[i] = load_cols<kEven>(dy, col, a.keys);
-      if constexpr (kMask) load_mask<kEven>(rm[i], a, mask, col);
+      if constexpr (kMasked) rm[i] = load_cols<kEven>(mask, col, a.keys);
     }
   }
   float t[kPer][kVec];   // logits, then exponentials
@@ -208,9 +196,9 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
     if (col < seen) {
       fix_tail<kEven>(rx[i], col, a.keys);
       if constexpr (kBack) fix_tail<kEven>(rd[i], col, a.keys);
-      if constexpr (kMask) {
-        fix_mask<kEven>(rm[i], a, col);
-        logits8(t[i], a, rx[i], rm[i], seen - col);
+      if constexpr (kMask != kNoMask) {
+        if constexpr (kMasked) fix_tail<kEven>(rm[i], col, a.keys);
+        logits8<kMask>(t[i], a, rx[i], rm[kMasked ? i : 0], seen - col);
       } else {
         hide(rx[i], seen - col, (T)-__builtin_inff());
         if constexpr (kBack) hide(rd[i], seen - col, (T)0);
@@ -223,7 +211,7 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec;
       if (col >= seen) continue;
-      if constexpr (kMask) {
+      if constexpr (kMask != kNoMask) {
 #pragma unroll
         for (int j = 0; j < kVec; ++j) m = fmaxf(m, t[i][j]);
       } else {
@@ -231,17 +219,17 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       }
     }
     m = reduce_row<OpMax, kLanes, kBlock>(m, lds, 0);
-    if constexpr (!kMask) m = fmaxf(m * a.scale, kLowest);
+    if constexpr (kMask == kNoMask) m = fmaxf(m * a.scale, kLowest);
     const Top top = top_of(m, a.scale);
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec;
       if (col >= seen) continue;
-      if constexpr (!kMask) exps8(t[i], rx[i], top, a.scale);
+      if constexpr (kMask == kNoMask) exps8(t[i], rx[i], top, a.scale);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        if constexpr (kMask) t[i][j] = exp_of(t[i][j], m);
+        if constexpr (kMask != kNoMask) t[i][j] = exp_of(t[i][j], m);
         sum += t[i][j];
       }
     }
@@ -272,7 +260,7 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec;
       if (col >= seen) continue;
-      if constexpr (kMask) {
+      if constexpr (kMask != kNoMask) {
 #pragma unroll
         for (int j = 0; j < kVec; ++j) t[i][j] = exp_of(t[i][j], m);
       } else {
@@ -314,14 +302,20 @@ __device__ __forceinline__ Raw8<T> load_whole(const T* row, int col, int cols) {
 }
 template <typename T>
 __device__ __forceinline__ void load_logits8(float (&t)[kVec], const SoftmaxArgs& a, const T* x, const Row& r, int col) {
+  const int left = r.seen - col;
   Raw8<T> v = load_cols<false>(x, col, a.keys);
-  RawMask<T> m;
-  if (a.mask_kind != CKM_MASK_NONE) {
-    load_mask<false>(m, a, mask_row<T>(a, r), col);
-    fix_mask<false>(m, a, col);
+  if (a.mask_kind == CKM_MASK_BOOL) {
+    const Raw8<uint8_t> m = load_whole(mask_row<kBool, T>(a, r), col, a.keys);
+    fix_tail<false>(v, col, a.keys);
+    logits8<kBool>(t, a, v, m, left);
+  } else if (a.mask_kind == CKM_MASK_ADD) {
+    const Raw8<T> m = load_whole(mask_row<kAdd, T>(a, r), col, a.keys);
+    fix_tail<false>(v, col, a.keys);
+    logits8<kAdd>(t, a, v, m, left);
+  } else {
+    fix_tail<false>(v, col, a.keys);
+    logits8<kPlain>(t, a, v, v, left);
   }
-  fix_tail<false>(v, col, a.keys);
-  logits8(t, a, v, m, r.seen - col);
 }
 
 constexpr int kSplitBlock = 256, kSplitSpan = kSplitBlock * kVec, kMaxSplits = kSplitBlock;
@@ -363,7 +357,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxA
         load_logits8(t, a, x, r, col);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m);
-        grads8<true>(g, a, site, load_whole(dy, col, a.keys), t, row, col);
+        grads8<kPlain>(g, a, site, load_whole(dy, col, a.keys), t, row, col);
 #pragma unroll
         for (int j = 0; j < kVec; ++j) sum = fmaf(t[j], g[j], sum);
       }
@@ -422,7 +416,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxAr
           load_logits8(t, a, x, r, col);
 #pragma unroll
           for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m);
-          grads8<true>(g, a, site, load_whole(dy, col, a.keys), t, row, col);
+          grads8<kPlain>(g, a, site, load_whole(dy, col, a.keys), t, row, col);
 #pragma unroll
           for (int j = 0; j < kVec; ++j) o[j] = t[j] * fmaf(g[j], by, -sum);
         }
@@ -453,11 +447,16 @@ void launch_whole_as(const SoftmaxArgs& a, hipStream_t s) {
   // threads in each
   const int64_t blocks = (a.rows + kRowsAt - 1) / kRowsAt, wide = std::min<int64_t>(blocks, 1 << 20);
   const dim3 grid((uint32_t)wide, (uint32_t)((blocks + wide - 1) / wide));
-  const bool mask = a.mask_kind != CKM_MASK_NONE || !(a.scale > 0.0f), even = a.keys % kVec == 0;
-  if (mask && even) ckm_softmax_kernel<T, kLanes, kPer, kBack, true, true><<<grid, kBlock, 0, s>>>(a);
-  else if (mask) ckm_softmax_kernel<T, kLanes, kPer, kBack, true, false><<<grid, kBlock, 0, s>>>(a);
-  else if (even) ckm_softmax_kernel<T, kLanes, kPer, kBack, false, true><<<grid, kBlock, 0, s>>>(a);
-  else ckm_softmax_kernel<T, kLanes, kPer, kBack, false, false><<<grid, kBlock, 0, s>>>(a);
+  switch (mask_form(a.mask_kind, a.scale)) {
+    case kBool: ckm_softmax_kernel<T, kLanes, kPer, kBack, kBool, false><<<grid, kBlock, 0, s>>>(a); break;
+    case kAdd: ckm_softmax_kernel<T, kLanes, kPer, kBack, kAdd, false><<<grid, kBlock, 0, s>>>(a); break;
+    case kPlain: ckm_softmax_kernel<T, kLanes, kPer, kBack, kPlain, false><<<grid, kBlock, 0, s>>>(a); break;
+    default:
+      if (a.keys % kVec == 0)
+        ckm_softmax_kernel<T, kLanes, kPer, kBack, kNoMask, true><<<grid, kBlock, 0, s>>>(a);
+      else
+        ckm_softmax_kernel<T, kLanes, kPer, kBack, kNoMask, false><<<grid, kBlock, 0, s>>>(a);
+  }
 }
 
 template <typename T, bool kBack>
