@@ -290,137 +290,166 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
 // ---------------------------------------------------------------------------
 // Long rows, and few of them: a row is cut into `splits` shares of `chunk` keys
 // (a multiple of a block's 2048). The first launch leaves each share's maximum
-// and sum of exponentials (the gradient: its sum of p g); the second joins a row's
+// and sum of exponentials (the gradient: its sum of e g); the second joins a row's
 // shares in each of its blocks and makes the share's outputs.
 // ---------------------------------------------------------------------------
 
-template <typename T>
-__device__ __forceinline__ Raw8<T> load_whole(const T* row, int col, int cols) {
-  Raw8<T> r = load_cols<false>(row, col, cols);
-  fix_tail<false>(r, col, cols);
-  return r;
-}
-template <typename T>
-__device__ __forceinline__ void load_logits8(float (&t)[kVec], const SoftmaxArgs& a, const T* x, const Row& r, int col) {
-  const int left = r.seen - col;
-  Raw8<T> v = load_cols<false>(x, col, a.keys);
-  if (a.mask_kind == CKM_MASK_BOOL) {
-    const Raw8<uint8_t> m = load_whole(mask_row<kBool, T>(a, r), col, a.keys);
-    fix_tail<false>(v, col, a.keys);
-    logits8<kBool>(t, a, v, m, left);
-  } else if (a.mask_kind == CKM_MASK_ADD) {
-    const Raw8<T> m = load_whole(mask_row<kAdd, T>(a, r), col, a.keys);
-    fix_tail<false>(v, col, a.keys);
-    logits8<kAdd>(t, a, v, m, left);
-  } else {
-    fix_tail<false>(v, col, a.keys);
-    logits8<kPlain>(t, a, v, v, left);
-  }
-}
-
 constexpr int kSplitBlock = 256, kSplitSpan = kSplitBlock * kVec, kMaxSplits = kSplitBlock;
+constexpr int kSplitPer = 2;   // spans loaded together
 
-template <typename T, bool kBack>
-__global__ void __launch_bounds__(kSplitBlock) ckm_softmax_share_kernel(SoftmaxArgs a, int splits, int32_t chunk,
-                                                                        float2* part) {
-  __shared__ float lds[2 * kSplitBlock / 64];
-  const DropSite site = drop_site(a.drop);
-  int turn = 0;
-  for (int64_t item = blockIdx.x; item < a.rows * splits; item += gridDim.x) {
-    const int64_t row = item / splits;
-    const Row r = row_of(a, row);
-    const T* x = (const T*)a.x.p + offset_of(a.x, r);
-    const int from = (int)(item - row * splits) * chunk;
-    const int to = min(r.seen, from + chunk);
-    if constexpr (!kBack) {
-      float m = kLowest, sum = 0.0f;
-      for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
-        float t[kVec];
-        load_logits8(t, a, x, r, col);
-        float top = m;
+// The groups of a share that a thread holds at a time: kSplitPer from `col` on, a
+// span apart.
+template <typename T, bool kBack, int kMask>
+struct Span {
+  static constexpr bool kMasked = kMask == kBool || kMask == kAdd;
+  Raw8<T> x[kSplitPer], dy[kBack ? kSplitPer : 1];
+  Raw8<MaskType<kMask, T>> m[kMasked ? kSplitPer : 1];
+  float t[kSplitPer][kVec];   // logits (not with kNoMask), then exponentials
+
+  __device__ __forceinline__ void load(const SoftmaxArgs& a, const T* px, const T* pdy, const MaskType<kMask, T>* pm,
+                                       int col, int to) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) top = fmaxf(top, t[j]);
-        sum *= exp_of(m, top);
-        m = top;
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) sum += exp_of(t[j], m);
+    for (int i = 0; i < kSplitPer; ++i) {
+      const int c = col + i * kSplitSpan;
+      if (c < to) {
+        x[i] = load_cols<false>(px, c, a.keys);
+        if constexpr (kBack) dy[i] = load_cols<false>(pdy, c, a.keys);
+        if constexpr (kMasked) m[i] = load_cols<false>(pm, c, a.keys);
       }
-      const float top = reduce_row<OpMax, kSplitBlock, kSplitBlock>(m, lds, 0);
-      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum * exp_of(m, top), lds, 1);
-      if (threadIdx.x == 0) part[item] = {top, sum};
-    } else {
-      const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
-      const float m = a.stats[2 * row];
-      float sum = 0.0f;
-      for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
-        float t[kVec], g[kVec];
-        load_logits8(t, a, x, r, col);
+    }
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m);
-        grads8<kPlain>(g, a, site, load_whole(dy, col, a.keys), t, row, col);
-#pragma unroll
-        for (int j = 0; j < kVec; ++j) sum = fmaf(t[j], g[j], sum);
+    for (int i = 0; i < kSplitPer; ++i) {
+      const int c = col + i * kSplitSpan;
+      if (c < to) {
+        fix_tail<false>(x[i], c, a.keys);
+        if constexpr (kBack) fix_tail<false>(dy[i], c, a.keys);
+        if constexpr (kMasked) fix_tail<false>(m[i], c, a.keys);
+        if constexpr (kMask == kNoMask) {
+          hide(x[i], to - c, (T)-__builtin_inff());
+          if constexpr (kBack) hide(dy[i], to - c, (T)0);
+        } else {
+          logits8<kMask>(t[i], a, x[i], m[kMasked ? i : 0], to - c);
+        }
       }
-      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum, lds, turn);
-      turn ^= 1;
-      if (threadIdx.x == 0) part[item] = {0.0f, sum};
     }
   }
-}
+  __device__ __forceinline__ float largest(const SoftmaxArgs& a, int i) const {
+    if constexpr (kMask == kNoMask) return top8(x[i]) * a.scale;
+    float v = t[i][0];
+#pragma unroll
+    for (int j = 1; j < kVec; ++j) v = fmaxf(v, t[i][j]);
+    return v;
+  }
+  __device__ __forceinline__ void exps(const SoftmaxArgs& a, const Top& top, int i) {
+    if constexpr (kMask == kNoMask) {
+      exps8(t[i], x[i], top, a.scale);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kVec; ++j) t[i][j] = exp_of(t[i][j], top.m);
+    }
+  }
+};
 
-template <typename T, bool kBack>
-__global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxArgs a, int splits, int32_t chunk,
-                                                                       const float2* part) {
+template <typename T, bool kBack, int kMask, bool kJoin>
+__global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxArgs a, int splits, int32_t chunk,
+                                                                        float2* part) {
   __shared__ float lds[2 * kSplitBlock / 64];
+  const int64_t item = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  if (item >= a.rows * splits) return;
+  const int64_t row = item / splits;
+  const int share = (int)(item - row * splits);
   const DropSite site = drop_site(a.drop);
-  int turn = 0;
-  for (int64_t item = blockIdx.x; item < a.rows * splits; item += gridDim.x) {
-    const int64_t row = item / splits;
-    const Row r = row_of(a, row);
-    const T* x = (const T*)a.x.p + offset_of(a.x, r);
+  const Row r = row_of(a, row);
+  const T* x = (const T*)a.x.p + offset_of(a.x, r);
+  const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
+  const MaskType<kMask, T>* mask = nullptr;
+  if constexpr (kMask == kBool || kMask == kAdd) mask = mask_row<kMask, T>(a, r);
+  const int from = share * chunk, first = from + (int)threadIdx.x * kVec;
+  const int seen = min(r.seen, from + chunk);   // below 2^31: chunk holds at most 2^30 keys and a block's
+  Span<T, kBack, kMask> s;
+  if constexpr (!kJoin) {
+    const float m = kBack ? a.stats[2 * row] : 0.0f;
+    const Top given = top_of(m, a.scale);
+    float top = kLowest, sum = 0.0f;
+    for (int col = first; col < seen; col += kSplitPer * kSplitSpan) {
+      s.load(a, x, dy, mask, col, seen);
+      float now = top;
+      if constexpr (!kBack) {
+#pragma unroll
+        for (int i = 0; i < kSplitPer; ++i)
+          if (col + i * kSplitSpan < seen) now = fmaxf(now, s.largest(a, i));
+        sum *= exp_of(top, now);
+        top = now;
+      }
+      const Top at = kBack ? given : top_of(now, a.scale);
+#pragma unroll
+      for (int i = 0; i < kSplitPer; ++i) {
+        const int c = col + i * kSplitSpan;
+        if (c >= seen) continue;
+        s.exps(a, at, i);
+        if constexpr (kBack) {
+          float g[kVec];
+          grads8<kMask>(g, a, site, s.dy[i], s.t[i], row, c);
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) sum = fmaf(s.t[i][j], g[j], sum);
+        } else {
+#pragma unroll
+          for (int j = 0; j < kVec; ++j) sum += s.t[i][j];
+        }
+      }
+    }
+    if constexpr (!kBack) {
+      const float all = reduce_row<OpMax, kSplitBlock, kSplitBlock>(top, lds, 0);
+      sum *= exp_of(top, all);
+      top = all;
+    }
+    sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum, lds, 1);
+    if (threadIdx.x == 0) part[item] = {top, sum};
+  } else {
     T* y = (T*)const_cast<void*>(a.y.p) + offset_of(a.y, r);
-    const int share = (int)(item - row * splits);
-    const int from = share * chunk;
     const int to = (int)min((int64_t)a.keys, (int64_t)from + chunk);
+    // the share's first groups, which do not wait for the shares' sums
+    if (first < seen) s.load(a, x, dy, mask, first, seen);
     float2 mine = {kLowest, 0.0f};
     if ((int)threadIdx.x < splits) mine = part[row * splits + threadIdx.x];
+    float m, z, sum, by = 1.0f;
     if constexpr (!kBack) {
-      const float m = reduce_row<OpMax, kSplitBlock, kSplitBlock>(mine.x, lds, 0);
-      const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y * exp_of(mine.x, m), lds, 1);
-      const float z = sum == 0.0f ? 0.0f : 1.0f / sum;
+      m = reduce_row<OpMax, kSplitBlock, kSplitBlock>(mine.x, lds, 0);
+      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y * exp_of(mine.x, m), lds, 1);
+      z = sum == 0.0f ? 0.0f : 1.0f / sum;
       if (share == 0 && threadIdx.x == 0 && a.stats) {
         a.stats[2 * row] = sum == 0.0f ? 0.0f : m;
         a.stats[2 * row + 1] = z;
       }
-      for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
-        Raw8<T> o = zero_group<T>();
-        if (col < r.seen) {
-          float t[kVec];
-          load_logits8(t, a, x, r, col);
-#pragma unroll
-          for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m) * z;
-          o = dropped8<T>(t, a.drop, site, col / kVec, (uint32_t)row);
-        }
-        store_part<false>(y, o, col, a.keys);
-      }
     } else {
-      const T* dy = (const T*)a.dy.p + offset_of(a.dy, r);
-      const float m = a.stats[2 * row], z = a.stats[2 * row + 1];
-      const float by = a.scale * a.drop.scale * z;
-      const float sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, turn) * z * by;
-      turn ^= 1;
-      for (int col = from + threadIdx.x * kVec; col < to; col += kSplitSpan) {
-        float o[kVec] = {};
-        if (col < r.seen) {
-          float t[kVec], g[kVec];
-          load_logits8(t, a, x, r, col);
+      m = a.stats[2 * row];
+      z = a.stats[2 * row + 1];
+      by = a.scale * a.drop.scale * z;
+      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, 0) * z * by;
+    }
+    const Top top = top_of(m, a.scale);
+    for (int col = first; col < to; col += kSplitPer * kSplitSpan) {
+      if (col != first && col < seen) s.load(a, x, dy, mask, col, seen);
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) t[j] = exp_of(t[j], m);
-          grads8<kPlain>(g, a, site, load_whole(dy, col, a.keys), t, row, col);
+      for (int i = 0; i < kSplitPer; ++i) {
+        const int c = col + i * kSplitSpan;
+        if (c >= to) continue;
+        Raw8<T> o = zero_group<T>();
+        if (c < seen) {
+          s.exps(a, top, i);
+          if constexpr (kBack) {
+            float g[kVec];
+            grads8<kMask>(g, a, site, s.dy[i], s.t[i], row, c);
 #pragma unroll
-          for (int j = 0; j < kVec; ++j) o[j] = t[j] * fmaf(g[j], by, -sum);
+            for (int j = 0; j < kVec; ++j) s.t[i][j] *= fmaf(g[j], by, -sum);
+            o = rounded8<T>(s.t[i]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) s.t[i][j] *= z;
+            o = dropped8<T>(s.t[i], a.drop, site, c / kVec, (uint32_t)row);
+          }
         }
-        store_part<false>(y, rounded8<T>(o), col, a.keys);
+        store_part<false>(y, o, c, a.keys);
       }
     }
   }
@@ -434,19 +463,22 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_join_kernel(SoftmaxAr
 // order of the sums, so it depends on the sizes alone.
 constexpr int kWholeKeys = 32768;
 int softmax_splits(int64_t rows, int64_t keys) {
-  if (keys <= kWholeKeys && (keys <= 4096 || rows > 64)) return 1;
+  if (keys <= kWholeKeys) return 1;
   const int64_t spans = (keys + kSplitSpan - 1) / kSplitSpan;
-  const int64_t wanted = std::max<int64_t>(2, (2048 + rows - 1) / std::max<int64_t>(rows, 1));
-  return (int)std::min<int64_t>(std::min<int64_t>(spans, wanted), kMaxSplits);
+  const int64_t wanted = std::max<int64_t>(2, (1024 + rows - 1) / std::max<int64_t>(rows, 1));
+  return (int)std::min<int64_t>(std::min<int64_t>((spans + kSplitPer - 1) / kSplitPer, wanted), kMaxSplits);
+}
+// One set of work to a block, in two dimensions: a launch has fewer than 2^32
+// threads in each.
+dim3 grid_of(int64_t blocks) {
+  const int64_t wide = std::min<int64_t>(blocks, 1 << 20);
+  return dim3((uint32_t)wide, (uint32_t)((blocks + wide - 1) / wide));
 }
 
 template <typename T, bool kBack, int kLanes, int kPer>
 void launch_whole_as(const SoftmaxArgs& a, hipStream_t s) {
   constexpr int kBlock = softmax_block(kLanes), kRowsAt = kBlock / kLanes;
-  // one set of rows to a block, in two dimensions: a launch has fewer than 2^32
-  // threads in each
-  const int64_t blocks = (a.rows + kRowsAt - 1) / kRowsAt, wide = std::min<int64_t>(blocks, 1 << 20);
-  const dim3 grid((uint32_t)wide, (uint32_t)((blocks + wide - 1) / wide));
+  const dim3 grid = grid_of((a.rows + kRowsAt - 1) / kRowsAt);
   switch (mask_form(a.mask_kind, a.scale)) {
     case kBool: ckm_softmax_kernel<T, kLanes, kPer, kBack, kBool, false><<<grid, kBlock, 0, s>>>(a); break;
     case kAdd: ckm_softmax_kernel<T, kLanes, kPer, kBack, kAdd, false><<<grid, kBlock, 0, s>>>(a); break;
@@ -459,15 +491,24 @@ void launch_whole_as(const SoftmaxArgs& a, hipStream_t s) {
   }
 }
 
+template <typename T, bool kBack, int kMask>
+void launch_split_as(const SoftmaxArgs& a, int splits, void* work, hipStream_t s) {
+  const int64_t spans = ((int64_t)a.keys + kSplitSpan - 1) / kSplitSpan;
+  const int32_t chunk = (int32_t)((spans + splits - 1) / splits * kSplitSpan);
+  const dim3 grid = grid_of(a.rows * splits);
+  ckm_softmax_split_kernel<T, kBack, kMask, false><<<grid, kSplitBlock, 0, s>>>(a, splits, chunk, (float2*)work);
+  ckm_softmax_split_kernel<T, kBack, kMask, true><<<grid, kSplitBlock, 0, s>>>(a, splits, chunk, (float2*)work);
+}
+
 template <typename T, bool kBack>
 void launch_softmax(const SoftmaxArgs& a, int splits, void* work, hipStream_t s) {
   if (splits > 1) {
-    const int64_t spans = ((int64_t)a.keys + kSplitSpan - 1) / kSplitSpan;
-    const int32_t chunk = (int32_t)((spans + splits - 1) / splits * kSplitSpan);
-    const dim3 grid((uint32_t)std::min<int64_t>(a.rows * splits, 1 << 20));
-    ckm_softmax_share_kernel<T, kBack><<<grid, kSplitBlock, 0, s>>>(a, splits, chunk, (float2*)work);
-    ckm_softmax_join_kernel<T, kBack><<<grid, kSplitBlock, 0, s>>>(a, splits, chunk, (const float2*)work);
-    return;
+    switch (mask_form(a.mask_kind, a.scale)) {
+      case kBool: return launch_split_as<T, kBack, kBool>(a, splits, work, s);
+      case kAdd: return launch_split_as<T, kBack, kAdd>(a, splits, work, s);
+      case kPlain: return launch_split_as<T, kBack, kPlain>(a, splits, work, s);
+      default: return launch_split_as<T, kBack, kNoMask>(a, splits, work, s);
+    }
   }
   const int groups = (a.keys + kVec - 1) / kVec;
   if (groups <= 16) launch_whole_as<T, kBack, 16, 1>(a, s);
