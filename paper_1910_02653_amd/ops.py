@@ -92,11 +92,13 @@ def _rows(t, name: str, shape, dtype, device):
     """(pointer, row stride) of a tensor of `shape` seen as rows of its last dimension; (None, 0) for None."""
     if t is None:
         return None, 0
-    _tensor(t, name, dtype, device)
-    if t.shape != shape:
+    # the common case first: what is a tensor, and on which device, one call tells
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape:
+        if t.is_contiguous() or t.numel() == 0:
+            return t.data_ptr(), shape[-1]
+    else:
+        _tensor(t, name, dtype, device)
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-    if t.is_contiguous() or t.numel() == 0:
-        return t.data_ptr(), shape[-1]
     if shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError("%s: the last dimension must be contiguous, got strides %s" % (name, t.stride()))
     # the other dimensions as one: each stride spans the next inner dimension
@@ -117,6 +119,8 @@ def _rows(t, name: str, shape, dtype, device):
 def _vector(t, name: str, cols: int, dtype, device):
     if t is None:
         return None
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == (cols,) and t.is_contiguous():
+        return t.data_ptr()
     _tensor(t, name, dtype, device)
     if t.dim() != 1 or t.shape[0] != cols or not t.is_contiguous():
         raise ValueError("%s must be a contiguous vector of %d elements, got shape %s" % (name, cols, tuple(t.shape)))
@@ -216,7 +220,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop
     else:
         h = _like(x)
         hp = h.data_ptr()
-    stats = torch.empty(shape[:-1] + (2,), dtype=torch.float32, device=x.device)
+    stats = x.new_empty(shape[:-1] + (2,), dtype=torch.float32)
     ckm._check(ckm.lib().ckm_layer_norm_async(_TYPES[dtype], _TYPES[wt], rows, cols, xp, ldx, rp, ldr,
                                               _drop_ptr(drop, device), wp, bp, eps, hp, cols, yp, ldy,
                                               stats.data_ptr(), _raw_stream(device)))
@@ -292,7 +296,7 @@ def _work(work, need: int, like):
     if work is None:
         if not need:
             return None, 0, None
-        work = torch.empty(need, dtype=torch.uint8, device=like.device)
+        work = like.new_empty(need, dtype=torch.uint8)
     else:
         _tensor(work, "work", torch.uint8, like.get_device())
         if not work.is_contiguous():
@@ -302,8 +306,8 @@ def _work(work, need: int, like):
 
 def _strides(t, name: str, shape, dtype, device):
     """(pointer, strides of batch, heads, queries) of a tensor of shape `shape`, up to four dimensions."""
-    _tensor(t, name, dtype, device)
-    if t.shape != shape:
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape):
+        _tensor(t, name, dtype, device)
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
     s = t.stride()
     if shape[-1] > 1 and s[-1] != 1 and t.numel():
@@ -359,7 +363,7 @@ def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask
     else:
         y = out
         yp, ys = _strides(y, "out", shape, dtype, device)
-    stats = torch.empty(shape[:-1] + (2,), dtype=torch.float32, device=scores.device)
+    stats = scores.new_empty(shape[:-1] + (2,), dtype=torch.float32)
     wp, wb, work = _work(work, softmax_workspace(c.batch, c.heads, c.queries, c.keys), scores)
     ckm._check(ckm.lib().ckm_softmax_async(_TYPES[dtype], C.byref(c), xp, xs, _drop_ptr(drop, device), yp, ys,
                                            stats.data_ptr(), wp, wb, _raw_stream(device)))
