@@ -217,82 +217,93 @@ __device__ __forceinline__ void put_sum(const NormGradArgs& a, bool only, float*
   }
 }
 
-constexpr int grad_block(int lanes) { return 1024; }
+constexpr int kGradBlock = 1024;
 
-// One pass over dy and h. A block takes every gridDim-th set of rows and keeps
-// its columns' sums of dy xh and dy in registers; at the end its row sets join
-// through LDS in a fixed order, and ckm_norm_join_kernel adds the blocks' sums
-// in a fixed order, so the weights' gradients do not depend on scheduling.
+// A row of the gradient's inputs as a thread holds it, in its own type: its
+// products are made twice, since registers are what limits the waves here.
+template <typename T, int kPer>
+struct GradRow {
+  Raw8<T> dy[kPer], h[kPer], past[kPer];
+  float mean, rstd;
+};
+template <int kLanes, bool kEven, typename T, int kPer>
+__device__ __forceinline__ void load_grad_row(GradRow<T, kPer>& r, const NormGradArgs& a, int64_t row, int lane) {
+  const bool live = row < a.rows;
+  r.mean = live ? a.stats[2 * row] : 0.0f;
+  r.rstd = live ? a.stats[2 * row + 1] : 0.0f;
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int col = (lane + i * kLanes) * kVec, left = live ? a.cols - col : 0;
+    r.dy[i] = r.h[i] = r.past[i] = zero_group<T>();
+    if (left > 0) {
+      r.dy[i] = load_cols<kEven>((const T*)a.dy + row * a.ld_dy, col, a.cols);
+      r.h[i] = load_cols<kEven>((const T*)a.h + row * a.ld_h, col, a.cols);
+      if (a.dres) r.past[i] = load_cols<kEven>((const T*)a.dres + row * a.ld_dres, col, a.cols);
+    }
+  }
+}
+
+// One pass over dy and h. A block takes every gridDim-th set of rows, one in each
+// of its row places, and keeps its columns' sums of dy xh and dy in registers; at
+// the end its places join through LDS in a fixed order, and
+// ckm_norm_join_kernel adds the blocks' sums in a fixed order, so the weights'
+// gradients do not depend on scheduling.
 template <typename T, int kLanes, int kPer, bool kEven>
-__global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormGradArgs a) {
-  constexpr int kBlock = grad_block(kLanes), kRowsAt = kBlock / kLanes;
-  __shared__ float lds[kLanes > 64 ? 4 * kBlock / 64 : 1];
-  __shared__ __align__(16) float join[kRowsAt > 1 ? kRowsAt * 2 * kLanes * kVec : 1];
+__global__ void __launch_bounds__(kGradBlock) ckm_norm_grad_kernel(NormGradArgs a) {
+  constexpr int kPlaces = kGradBlock / kLanes;
+  __shared__ float lds[kLanes > 64 ? 4 * kGradBlock / 64 : 1];
+  __shared__ __align__(16) float join[kPlaces > 1 ? kPlaces * 2 * kLanes * kVec : 1];
   const int lane = threadIdx.x % kLanes;
   const DropSite site = drop_site(a.drop);
   int turn = 0;
-  // a block of 1024 threads has no registers for two groups' weights
-  constexpr bool kKeep = kPer == 1 || kLanes < 1024;
-  float w[kKeep ? kPer : 1][kVec], dw[kPer][kVec], db[kPer][kVec];
+  // two groups' weights are read again for each row: no registers for them
+  constexpr bool kKeep = kPer == 1;
+  float w[kVec], dw[kPer][kVec], db[kPer][kVec];
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
     const int col = (lane + i * kLanes) * kVec;
-    if constexpr (kKeep) weight_group<T>(w[i], a.w, a.w32, col, a.cols - col, 1.0f);
+    if constexpr (kKeep) weight_group<T>(w, a.w, a.w32, col, a.cols - col, 1.0f);
 #pragma unroll
     for (int j = 0; j < kVec; ++j) dw[i][j] = db[i][j] = 0.0f;
   }
-  for (int64_t first = (int64_t)blockIdx.x * kRowsAt; first < a.rows; first += (int64_t)gridDim.x * kRowsAt) {
+  for (int64_t first = (int64_t)blockIdx.x * kPlaces; first < a.rows; first += (int64_t)gridDim.x * kPlaces) {
     const int64_t row = first + row_in_block<kLanes>();
     const bool live = row < a.rows;
-    const float mean = live ? a.stats[2 * row] : 0.0f, rstd = live ? a.stats[2 * row + 1] : 0.0f;
-    // the row is held in its own type, and its products are made twice: registers
-    // are what limits the waves here
-    Raw8<T> rd[kPer], rh[kPer], past[kPer];
+    GradRow<T, kPer> r;
+    load_grad_row<kLanes, kEven>(r, a, row, lane);
+    float s[2] = {};   // sum g, sum g xh
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec, left = live ? a.cols - col : 0;
-      rd[i] = rh[i] = past[i] = zero_group<T>();
-      if (left > 0) {
-        rd[i] = load_cols<kEven>((const T*)a.dy + row * a.ld_dy, col, a.cols);
-        rh[i] = load_cols<kEven>((const T*)a.h + row * a.ld_h, col, a.cols);
-        if (a.dres) past[i] = load_cols<kEven>((const T*)a.dres + row * a.ld_dres, col, a.cols);
-      }
-    }
-    float s1 = 0.0f, s2 = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-      const int k = kKeep ? i : 0, left = live ? a.cols - (lane + i * kLanes) * kVec : 0;
-      fix_tail<kEven>(rd[i], (lane + i * kLanes) * kVec, a.cols);
-      fix_tail<kEven>(rh[i], (lane + i * kLanes) * kVec, a.cols);
-      fix_tail<kEven>(past[i], (lane + i * kLanes) * kVec, a.cols);
-      if constexpr (!kKeep) weight_group<T>(w[0], a.w, a.w32, (lane + i * kLanes) * kVec, left, 1.0f);
+      fix_tail<kEven>(r.dy[i], col, a.cols);
+      fix_tail<kEven>(r.h[i], col, a.cols);
+      fix_tail<kEven>(r.past[i], col, a.cols);
+      if constexpr (!kKeep) weight_group<T>(w, a.w, a.w32, col, left, 1.0f);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const float d = (float)rd[i].get(j);
-        const float xh = (kEven ? left > 0 : j < left) ? ((float)rh[i].get(j) - mean) * rstd : 0.0f;
-        const float g = d * w[k][j];
+        const float d = (float)r.dy[i].get(j);
+        const float xh = (kEven ? left > 0 : j < left) ? ((float)r.h[i].get(j) - r.mean) * r.rstd : 0.0f;
+        const float g = d * w[j];
         dw[i][j] = fmaf(d, xh, dw[i][j]);
         db[i][j] += d;
-        s1 += g;
-        s2 = fmaf(g, xh, s2);
+        s[0] += g;
+        s[1] = fmaf(g, xh, s[1]);
       }
     }
-    reduce_two<kLanes, kBlock>(s1, s2, lds, turn);
+    reduce_rows<OpSum, kLanes, kGradBlock>(s, lds, turn);
     turn ^= 1;
-    s1 /= (float)a.cols;
-    s2 /= (float)a.cols;
     if (!live) continue;
+    const float s1 = s[0] / (float)a.cols, s2 = s[1] / (float)a.cols;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int group = lane + i * kLanes, col = group * kVec, left = a.cols - col;
       if (left <= 0) continue;
-      const int k = kKeep ? i : 0;
-      if constexpr (!kKeep) weight_group<T>(w[0], a.w, a.w32, col, left, 1.0f);
+      if constexpr (!kKeep) weight_group<T>(w, a.w, a.w32, col, left, 1.0f);
       float o[kVec];
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        const float xh = ((float)rh[i].get(j) - mean) * rstd;
-        o[j] = fmaf(rstd, fmaf(-xh, s2, (float)rd[i].get(j) * w[k][j] - s1), (float)past[i].get(j));
+        const float xh = ((float)r.h[i].get(j) - r.mean) * r.rstd;
+        o[j] = fmaf(r.rstd, fmaf(-xh, s2, (float)r.dy[i].get(j) * w[j] - s1), (float)r.past[i].get(j));
       }
       finish_grad<T, kEven>(a, site, row, group, o);
     }
@@ -303,7 +314,7 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
   float* part = a.part + (size_t)blockIdx.x * 2 * width;
 #pragma unroll
   for (int i = 0; i < kPer; ++i) {
-    if constexpr (kRowsAt == 1) {
+    if constexpr (kPlaces == 1) {
       const int col = (lane + i * kLanes) * kVec;
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
@@ -320,9 +331,9 @@ __global__ void __launch_bounds__(grad_block(kLanes)) ckm_norm_grad_kernel(NormG
         at[kSpan + j] = db[i][j];
       }
       __syncthreads();
-      for (int k = threadIdx.x; k < 2 * kSpan; k += kBlock) {
+      for (int k = threadIdx.x; k < 2 * kSpan; k += kGradBlock) {
         float s = join[k];
-        for (int r = 1; r < kRowsAt; ++r) s += join[r * (2 * kSpan) + k];
+        for (int r = 1; r < kPlaces; ++r) s += join[r * (2 * kSpan) + k];
         put_sum<T>(a, only, part, width, k / kSpan, i * kSpan + k % kSpan, s);
       }
     }
@@ -383,11 +394,12 @@ __global__ void __launch_bounds__(1024) ckm_norm_wide_sums_kernel(NormGradArgs a
         s2 = j < left ? fmaf(g, ((float)rh.get(j) - mean) * rstd, s2) : s2;
       }
     }
-    reduce_two<1024, 1024>(s1, s2, lds, turn);
+    float s[2] = {s1, s2};
+    reduce_rows<OpSum, 1024, 1024>(s, lds, turn);
     turn ^= 1;
     if (threadIdx.x == 0) {
-      sums[2 * row] = s1 / (float)a.cols;
-      sums[2 * row + 1] = s2 / (float)a.cols;
+      sums[2 * row] = s[0] / (float)a.cols;
+      sums[2 * row + 1] = s[1] / (float)a.cols;
     }
   }
 }
@@ -470,16 +482,11 @@ GradPlan grad_plan(int64_t rows, int64_t cols) {
     p.blocks = std::max<int64_t>(1, std::min<int64_t>(rows, 256));
     return p;
   }
-  if (groups <= 16) p = {16, 1, 0};
-  else if (groups <= 32) p = {16, 2, 0};
-  else if (groups <= 64) p = {32, 2, 0};
-  else if (groups <= 128) p = {64, 2, 0};
-  else if (groups <= 256) p = {256, 1, 0};
-  else if (groups <= 512) p = {512, 1, 0};
-  else if (groups <= 1024) p = {1024, 1, 0};
-  else p = {1024, 2, 0};
-  const int at = grad_block(p.lanes) / p.lanes;
-  p.blocks = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, at), 256));
+  int lanes = 16;
+  while (lanes < 1024 && lanes < groups) lanes *= 2;
+  p.lanes = lanes;
+  p.per = groups <= 1024 ? 1 : 2;
+  p.blocks = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, kGradBlock / lanes), 256));
   return p;
 }
 
@@ -492,12 +499,11 @@ size_t grad_workspace(int64_t rows, int64_t cols) {
 
 template <typename T, int kLanes, int kPer>
 void launch_grad_as(const NormGradArgs& a, int64_t blocks, hipStream_t s) {
-  constexpr int kBlock = grad_block(kLanes);
   const dim3 grid((uint32_t)blocks);
   if (a.cols % kVec == 0)
-    ckm_norm_grad_kernel<T, kLanes, kPer, true><<<grid, kBlock, 0, s>>>(a);
+    ckm_norm_grad_kernel<T, kLanes, kPer, true><<<grid, kGradBlock, 0, s>>>(a);
   else
-    ckm_norm_grad_kernel<T, kLanes, kPer, false><<<grid, kBlock, 0, s>>>(a);
+    ckm_norm_grad_kernel<T, kLanes, kPer, false><<<grid, kGradBlock, 0, s>>>(a);
 }
 
 template <typename T>
@@ -509,14 +515,21 @@ void launch_grad(NormGradArgs a, void* work, hipStream_t s) {
     if (a.rows > 0)
       ckm_norm_wide_sums_kernel<T><<<dim3((uint32_t)std::min<int64_t>(a.rows, 2048)), 1024, 0, s>>>(a, sums);
     ckm_norm_wide_grad_kernel<T><<<dim3((uint32_t)ceil_div(a.cols, 256 * kVec), (uint32_t)p.blocks), 256, 0, s>>>(a, sums);
-  } else if (p.lanes == 16 && p.per == 1) launch_grad_as<T, 16, 1>(a, p.blocks, s);
-  else if (p.lanes == 16) launch_grad_as<T, 16, 2>(a, p.blocks, s);
-  else if (p.lanes == 32) launch_grad_as<T, 32, 2>(a, p.blocks, s);
-  else if (p.lanes == 64) launch_grad_as<T, 64, 2>(a, p.blocks, s);
-  else if (p.lanes == 256) launch_grad_as<T, 256, 1>(a, p.blocks, s);
-  else if (p.lanes == 512) launch_grad_as<T, 512, 1>(a, p.blocks, s);
-  else if (p.per == 1) launch_grad_as<T, 1024, 1>(a, p.blocks, s);
-  else launch_grad_as<T, 1024, 2>(a, p.blocks, s);
+  } else {
+    switch (p.lanes) {
+      case 16: launch_grad_as<T, 16, 1>(a, p.blocks, s); break;
+      case 32: launch_grad_as<T, 32, 1>(a, p.blocks, s); break;
+      case 64: launch_grad_as<T, 64, 1>(a, p.blocks, s); break;
+      case 128: launch_grad_as<T, 128, 1>(a, p.blocks, s); break;
+      case 256: launch_grad_as<T, 256, 1>(a, p.blocks, s); break;
+      case 512: launch_grad_as<T, 512, 1>(a, p.blocks, s); break;
+      default:
+        if (p.per == 1)
+          launch_grad_as<T, 1024, 1>(a, p.blocks, s);
+        else
+          launch_grad_as<T, 1024, 2>(a, p.blocks, s);
+    }
+  }
   if (p.blocks > 1 && (a.dw || a.db))
     ckm_norm_join_kernel<T><<<dim3((uint32_t)ceil_div(a.cols, 32), 2), 256, 0, s>>>(a.part, (int)p.blocks, a.cols, a.w32,
                                                                                    a.dw, a.db);

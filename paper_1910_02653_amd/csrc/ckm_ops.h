@@ -342,62 +342,45 @@ __device__ __forceinline__ float reduce64(float x) {
   x = reduce16<Op>(x);
   return Op::of(Op::of(lane_of(x, 0), lane_of(x, 16)), Op::of(lane_of(x, 32), lane_of(x, 48)));
 }
-// kLanes 16, 32, 64, or a multiple of 64 that divides the block's kBlock threads.
-// lds: 2 kBlock / 64 floats per value; `turn` (0 or 1) picks the half, and a
-// kernel's reductions take turns: a wave can write a half again only after the
-// barrier of the reduction between, which every reader of it has reached. All
-// threads of the block take part.
-template <typename Op, int kLanes, int kBlock>
-__device__ __forceinline__ float reduce_row(float x, float* lds, int turn) {
-  if constexpr (kLanes == 16) {
-    return reduce16<Op>(x);
-  } else if constexpr (kLanes == 32) {
-    return reduce32<Op>(x);
-  } else {
-    x = reduce64<Op>(x);
-    if constexpr (kLanes > 64) {
-      constexpr int kWaves = kLanes / 64;
-      float* at = lds + turn * (kBlock / 64);
-      if ((threadIdx.x & 63) == 0) at[threadIdx.x >> 6] = x;
-      __syncthreads();
-      at += threadIdx.x / kLanes * kWaves;
-      x = at[0];
+// Over kWaves (a power of two up to 16) values in LDS, `step` apart: each lane
+// reads one.
+template <typename Op, int kWaves>
+__device__ __forceinline__ float reduce_waves(const float* at, int step) {
+  float x = at[(threadIdx.x % kWaves) * step];
+  if constexpr (kWaves > 1) x = Op::of(x, dpp_move<0xB1>(x));
+  if constexpr (kWaves > 2) x = Op::of(x, dpp_move<0x4E>(x));
+  if constexpr (kWaves > 4) x = Op::of(x, dpp_move<0x141>(x));
+  if constexpr (kWaves > 8) x = Op::of(x, dpp_move<0x140>(x));
+  return lane_of(x, 0);
+}
+// kCount values at once, one barrier. kLanes 16, 32, 64, or a power of two of waves
+// that divides the block's kBlock threads. lds: 2 kCount kBlock / 64 floats; `turn`
+// (0 or 1) picks the half, and a kernel's reductions take turns: a wave can write a
+// half again only after the barrier of the reduction between, which every reader of
+// it has reached. All threads of the block take part.
+template <typename Op, int kLanes, int kBlock, int kCount>
+__device__ __forceinline__ void reduce_rows(float (&v)[kCount], float* lds, int turn) {
 #pragma unroll
-      for (int w = 1; w < kWaves; ++w) x = Op::of(x, at[w]);
+  for (int k = 0; k < kCount; ++k)
+    v[k] = kLanes == 16 ? reduce16<Op>(v[k]) : kLanes == 32 ? reduce32<Op>(v[k]) : reduce64<Op>(v[k]);
+  if constexpr (kLanes > 64) {
+    constexpr int kWaves = kLanes / 64;
+    float* at = lds + turn * (kCount * kBlock / 64);
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int k = 0; k < kCount; ++k) at[kCount * (threadIdx.x >> 6) + k] = v[k];
     }
-    return x;
+    __syncthreads();
+    at += row_in_block<kLanes>() * (kCount * kWaves);
+#pragma unroll
+    for (int k = 0; k < kCount; ++k) v[k] = reduce_waves<Op, kWaves>(at + k, kCount);
   }
 }
-// Two sums at once, one barrier. lds: 4 kBlock / 64 floats.
-template <int kLanes, int kBlock>
-__device__ __forceinline__ void reduce_two(float& x, float& y, float* lds, int turn) {
-  if constexpr (kLanes == 16) {
-    x = reduce16<OpSum>(x);
-    y = reduce16<OpSum>(y);
-  } else if constexpr (kLanes == 32) {
-    x = reduce32<OpSum>(x);
-    y = reduce32<OpSum>(y);
-  } else {
-    x = reduce64<OpSum>(x);
-    y = reduce64<OpSum>(y);
-    if constexpr (kLanes > 64) {
-      constexpr int kWaves = kLanes / 64;
-      float* at = lds + turn * (2 * kBlock / 64);
-      if ((threadIdx.x & 63) == 0) {
-        at[2 * (threadIdx.x >> 6)] = x;
-        at[2 * (threadIdx.x >> 6) + 1] = y;
-      }
-      __syncthreads();
-      at += threadIdx.x / kLanes * (2 * kWaves);
-      x = at[0];
-      y = at[1];
-#pragma unroll
-      for (int w = 1; w < kWaves; ++w) {
-        x += at[2 * w];
-        y += at[2 * w + 1];
-      }
-    }
-  }
+template <typename Op, int kLanes, int kBlock>
+__device__ __forceinline__ float reduce_row(float x, float* lds, int turn) {
+  float v[1] = {x};
+  reduce_rows<Op, kLanes, kBlock>(v, lds, turn);
+  return v[0];
 }
 
 }  // namespace ckm
