@@ -9,14 +9,14 @@ from __future__ import annotations
 import numpy as np
 
 
-def draws(rows: int, cols: int, seed: int, site: int) -> np.ndarray:
+def draws(rows: int, cols: int, seed: int, site: int, row0: int = 0, group0: int = 0) -> np.ndarray:
     """16-bit draws [rows][cols]: half col % 2 of word col % 8 / 2 of Philox4x32-10 (key = seed, counter =
-    (col / 8, row, site low, site high))."""
+    (col / 8, row, site low, site high)); from row row0 and column 8 group0 on."""
     mask = np.uint64(0xFFFFFFFF)
     sh = np.uint64(32)
     groups = (cols + 7) // 8
-    c = [np.broadcast_to(np.arange(groups, dtype=np.uint64), (rows, groups)),
-         np.broadcast_to(np.arange(rows, dtype=np.uint64)[:, None], (rows, groups)),
+    c = [np.broadcast_to(group0 + np.arange(groups, dtype=np.uint64), (rows, groups)),
+         np.broadcast_to(row0 + np.arange(rows, dtype=np.uint64)[:, None], (rows, groups)),
          np.full((rows, groups), site & 0xFFFFFFFF, np.uint64), np.full((rows, groups), site >> 32, np.uint64)]
     k0, k1 = seed & 0xFFFFFFFF, seed >> 32
     for _ in range(10):

@@ -491,3 +491,91 @@ def test_binding_refusals():
         with pytest.raises(ckm.CkmError) as e:
             call()
         assert e.value.status in (ckm.E_INVALID_ARG, ckm.E_UNSUPPORTED)
+
+
+# ---------------------------------------------------------------------------
+# both sides of each launch rule, and the largest calls
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("cols", [9, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1024, 1025, 2047, 2049, 4096, 4097, 8191,
+                                  8193, 16383, 32761])
+def test_layer_norm_at_its_launch_rules(cols):
+    test_layer_norm_and_gradient("f16", "f32", 5, cols)
+    test_layer_norm_and_gradient("f32", "f32", 2, cols)
+
+
+@pytest.mark.parametrize("keys", [8, 9, 127, 129, 256, 257, 511, 513, 1024, 1025, 2047, 2049, 4096, 8191, 8193, 16385, 32767,
+                                  32768, 32769, 34817])
+@pytest.mark.parametrize("kind,causal,ragged", [("none", False, False), ("none", True, True), ("bool", True, False),
+                                                ("add", False, True)])
+def test_softmax_at_its_launch_rules(keys, kind, causal, ragged):
+    test_softmax_and_gradient("f16", (2, 1, 3, keys), kind, causal, ragged)
+    test_softmax_and_gradient("f32", (1, 2, 2, keys), kind, causal, ragged)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("keys", [13, 2000, 40000])
+@pytest.mark.parametrize("scale", [-0.25, 0.0, 1e-30])
+def test_softmax_other_scales(dtype, keys, scale):
+    T = TYPES[dtype]
+    x, dy = randn((3, keys), dtype, 31, gain=3.0), randn((3, keys), dtype, 32)
+    y, stats = ops.softmax(x, scale)
+    t = host(x) * scale
+    p, m, z = nodes.softmax(t)
+    # as in test_softmax_and_gradient: the logit, the difference, the factor, the last bit
+    rel = 5 * U * np.abs(t) + 4 * U * np.abs(t - m[:, None]) + 8 * U
+    d_p = p * (rel + (p * rel).sum(-1, keepdims=True) + 2 * U * np.abs(m)[:, None] + (DEPTH + 8) * U)
+    check(y, p, d_p + 2.0 ** -126, T, "y")
+    g = host(dy)
+    s = (p * g).sum(-1, keepdims=True)
+    d_s = (np.abs(p * g) * (2 * d_p / p + (DEPTH + 8) * U)).sum(-1, keepdims=True)
+    tol = np.abs(scale) * (2 * d_p * np.abs(g - s) + p * (d_s + 6 * U * np.abs(g) + 6 * U * np.abs(s))) + 2.0 ** -120
+    check(ops.softmax_backward(dy, x, stats, scale), nodes.softmax_backward(g, p, scale), tol, T, "dx")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("keys", [30, 3000, 40000])
+def test_softmax_logits_near_the_range(dtype, keys):
+    """Scores of 1e38 and more: the largest takes all, equal ones share, and gradients stay finite."""
+    x = torch.full((4, keys), -3e38, dtype=TYPES[dtype], device="cuda")
+    x[0, 7] = 3e38
+    x[1, 3], x[1, 20] = 2e38, 2e38
+    x[2] = 3e38
+    x[3] = 0.0
+    y, stats = ops.softmax(x, 1.1)
+    assert y[0, 7] == 1 and y[0].float().sum() == 1 and y[1, 3] == 0.5 and y[1, 20] == 0.5
+    for r in (2, 3):
+        assert torch.allclose(y[r].float(), torch.full((keys,), 1.0 / keys, device="cuda"), rtol=2.0 ** -7)
+    assert torch.isfinite(ops.softmax_backward(torch.ones_like(x), x, stats, 1.1)).all()
+
+
+def test_more_rows_than_a_launch_has_blocks_in_one_dimension():
+    rows = (1 << 24) + 37
+    x = torch.ones((rows, 2), dtype=torch.float16, device="cuda")
+    d = ops.Dropout(0.5, SEED, SITE)
+    y, stats = ops.softmax(x, drop=d)
+    want = 0.5 * np.where(nodes.draws(100, 2, SEED, SITE, row0=rows - 100) < d.keep, 65536.0 / d.keep, 0.0)
+    assert np.array_equal(host(y[-100:]), want) and torch.all(stats[:, 1] == 0.5)
+    assert torch.isfinite(ops.softmax_backward(x, x, stats, drop=d)).all()
+    y, _, stats = ops.layer_norm(x)
+    assert torch.all(y == 0) and torch.all(stats[:, 0] == 1)
+    dx, _, dw, db = ops.layer_norm_backward(x, x, stats, wtype=torch.float32)
+    assert torch.all(dw == 0)
+    # a sum of ones, exact in 32 bits up to 2^24, then off by the roundings of its few largest partial sums
+    assert torch.all((db - rows).abs() <= rows * 256 * U)
+
+
+def test_largest_dropouts():
+    d = ops.Dropout(0.25, SEED, SITE)
+    scale = 65536.0 / d.keep
+    rows = (1 << 28) + 1003
+    y = ops.dropout(torch.ones((rows, 1), dtype=torch.float16, device="cuda"), d)
+    u = nodes.draws(2000, 1, SEED, SITE, row0=rows - 2000)
+    assert np.array_equal(host(y[-2000:]) > 0, u < d.keep) and float(y.max()) == float(torch.tensor(scale).half())
+    del y
+    cols = 1 << 30
+    y = ops.dropout(torch.ones((1, cols), dtype=torch.float16, device="cuda"), d)
+    u = nodes.draws(1, 800, SEED, SITE, group0=cols // 8 - 100)
+    assert np.array_equal(host(y[:, -800:]) > 0, u < d.keep)
+    with pytest.raises(ckm.CkmError):
+        ops.dropout(y.expand(2, cols).reshape(1, 2 * cols)[:, :cols + 8], d)
