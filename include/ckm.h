@@ -32,6 +32,11 @@
  * ckm_last_error() gives a thread-local message for the last non-OK status
  * of the calling thread. On a non-OK return the outputs are unspecified.
  *
+ * Beside the evaluation the library has the training-graph nodes that a
+ * schedule computes again first, as operators on device tensors: dropout from the
+ * same counter-based generator, layer norm and the attention softmax, with their
+ * gradients (the section before ckm_last_error).
+ *
  * Exact-arithmetic range: every memory level and cost the method forms is
  * at most M_in + 2 M_param + sum(M), or n * sum(C); a graph for which either
  * exceeds INT64_MAX is rejected with CKM_E_OVERFLOW, and every other graph is
@@ -55,7 +60,8 @@ typedef enum {
   CKM_E_INVALID_ARG = 1, /* bad argument: NULL, K < 1, ld < n, negative budget, NaN in S* */
   CKM_E_GRAPH = 2,       /* not topologically numbered, duplicate edge, users != transpose */
   CKM_E_OVERFLOW = 3,    /* M_in + 2 M_param + sum(M) or n * sum(C) exceeds INT64_MAX */
-  CKM_E_UNSUPPORTED = 4, /* n > CKM_MAX_NODES, K > CKM_MAX_CANDIDATES (CKM_MAX_THRESHOLDS) */
+  CKM_E_UNSUPPORTED = 4, /* n > CKM_MAX_NODES, K > CKM_MAX_CANDIDATES (CKM_MAX_THRESHOLDS), sizes past
+                            CKM_MAX_ROWS, CKM_MAX_COLS or CKM_MAX_NORM_COLS */
   CKM_E_NOMEM = 5,       /* host or device allocation failed */
   CKM_E_DEVICE = 6       /* a HIP runtime call failed (message has the HIP error) */
 } ckm_status;
@@ -359,8 +365,9 @@ ckm_status ckm_round_eval_noalloc(const ckm_graph* g, const double* d_s_frac, in
  *
  * All pointers are device memory of the current HIP device except the structs
  * and stride arrays, which are read before the call returns. Calls enqueue
- * kernel launches on `stream` (NULL: the null stream) and nothing else, so they can be captured
- * into a HIP graph. Rows start anywhere (pointers need only their element's
+ * kernel launches on `stream` (NULL: the null stream) and nothing else, so they
+ * can be captured into a HIP graph. A work buffer must not be used by two calls
+ * that may run concurrently. Rows start anywhere (pointers need only their element's
  * alignment, rows any stride of at least 0); an output's rows must not overlap
  * each other. An output may be an input itself (the same pointer and strides)
  * but must not overlap one otherwise. */
@@ -440,8 +447,9 @@ typedef struct ckm_scores {
 } ckm_scores;
 
 /* y = D(softmax(scale x + mask)) over the seen keys, 0 at the others; a row that
- * sees nothing (or only scores of -inf) is all 0. The dropout's row is (b heads + h) queries + i. x_stride,
- * y_stride: elements between batches, heads and queries. stats (may be NULL):
+ * sees nothing (or only scores of -inf) is all 0. The dropout's row is (b heads +
+ * h) queries + i. x_stride, y_stride: elements between batches, heads and queries,
+ * at least 0; y's rows must not overlap. stats (may be NULL):
  * float [batch][heads][queries][2], the largest logit and 1 / the sum of
  * exponentials; 0 and 0 for a row that sees nothing. work:
  * ckm_softmax_workspace_size bytes (0 unless rows are long), aligned to 8. */

@@ -12,6 +12,14 @@
 // Logits, statistics and sums are in binary32; exp(v) is 2^(v log2 e), which is
 // off by 2^-24 |v log2 e| relative at most beside the unit's own last bit, and
 // v <= 0 is near 0 where the result counts.
+//
+// Bound by memory, the dropout's draws a close second: f16 16x2048x2048 without
+// causal mask moves 269 MB in 50 us (5.4 TB/s, where a large copy moves 5.2), causal
+// 202 MB in 43 us, its gradient 269 MB in 54 us. What it took: a row's loads all in
+// flight before its arithmetic; the arithmetic of a score down to a maximum, one
+// fused multiply-add, 2^v, a sum and two products; the dropout's choice on packed
+// halves; one row set a block and no loop, whose invariants had cost a third of the
+// registers (gradient 72 -> 55 us); scores held as the words they were loaded as.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -459,8 +467,11 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxA
 // launch rules
 // ---------------------------------------------------------------------------
 
-// Shares of a row, 1 when a row stays whole in registers. The number fixes the
-// order of the sums, so it depends on the sizes alone.
+// Shares of a row, 1 when a row stays whole in registers, which is faster wherever
+// it fits, for few rows too: f16, 16 rows of 16384 keys 4.3 us whole, 6.8 in eight
+// shares; 8 of 32768 5.3, 8 of 33000 in shares 6.6. Shares fill the chip with about
+// 1024 blocks (32 rows of 131072: 9.9 us; with twice as many, half as long, 14.5).
+// The number fixes the order of the sums, so it depends on the sizes alone.
 constexpr int kWholeKeys = 32768;
 int softmax_splits(int64_t rows, int64_t keys) {
   if (keys <= kWholeKeys) return 1;
@@ -500,6 +511,14 @@ void launch_split_as(const SoftmaxArgs& a, int splits, void* work, hipStream_t s
   ckm_softmax_split_kernel<T, kBack, kMask, true><<<grid, kSplitBlock, 0, s>>>(a, splits, chunk, (float2*)work);
 }
 
+// Threads and groups a thread for whole rows. Forward: four groups a thread, so that
+// what a row costs once (its place, two sums, its statistics) is shared by more
+// columns. Measured against two groups on twice the threads, with dropout (us):
+// bf16 64x16x256x300 73.6 / 88.6, 4x16x1024x1024 causal 41.8 / 44.5, f16
+// 16x2048x2048 causal 43.1 / 45.7 (one group 66.3), bf16 4x4096x4096 causal 41.4 /
+// 44.0 (one 64.3), 4096x16384 causal 51.1 / 58.0; against it 16x16x512x512 causal 49.3 /
+// 46.2. The gradient holds a row's exponentials and gradients, and is faster with two
+// groups: f16 16x2048x2048 54.1, four 55.0, one 60.3; bf16 2x4096x8192 64.9, four 65.8.
 template <typename T, bool kBack>
 void launch_softmax(const SoftmaxArgs& a, int splits, void* work, hipStream_t s) {
   if (splits > 1) {
@@ -511,16 +530,25 @@ void launch_softmax(const SoftmaxArgs& a, int splits, void* work, hipStream_t s)
     }
   }
   const int groups = (a.keys + kVec - 1) / kVec;
-  if (groups <= 16) launch_whole_as<T, kBack, 16, 1>(a, s);
-  else if (groups <= 32) launch_whole_as<T, kBack, 16, 2>(a, s);
-  else if (groups <= 64) launch_whole_as<T, kBack, 32, 2>(a, s);
-  else if (groups <= 128) launch_whole_as<T, kBack, 64, 2>(a, s);
-  else if (groups <= 256 && kBack) launch_whole_as<T, kBack, 128, 2>(a, s);
-  else if (groups <= 256) launch_whole_as<T, kBack, 64, 4>(a, s);
-  else if (groups <= 512) launch_whole_as<T, kBack, 256, 2>(a, s);
-  else if (groups <= 1024) launch_whole_as<T, kBack, 256, 4>(a, s);
-  else if (groups <= 2048) launch_whole_as<T, kBack, 1024, 2>(a, s);
-  else launch_whole_as<T, kBack, 1024, 4>(a, s);
+  if (groups <= 16) return launch_whole_as<T, kBack, 16, 1>(a, s);
+  if (groups <= 32) return launch_whole_as<T, kBack, 16, 2>(a, s);
+  if constexpr (kBack) {
+    if (groups <= 64) launch_whole_as<T, true, 32, 2>(a, s);
+    else if (groups <= 128) launch_whole_as<T, true, 64, 2>(a, s);
+    else if (groups <= 256) launch_whole_as<T, true, 128, 2>(a, s);
+    else if (groups <= 512) launch_whole_as<T, true, 256, 2>(a, s);
+    else if (groups <= 1024) launch_whole_as<T, true, 512, 2>(a, s);
+    else if (groups <= 2048) launch_whole_as<T, true, 1024, 2>(a, s);
+    else launch_whole_as<T, true, 1024, 4>(a, s);
+  } else {
+    if (groups <= 64) launch_whole_as<T, false, 16, 4>(a, s);
+    else if (groups <= 128) launch_whole_as<T, false, 32, 4>(a, s);
+    else if (groups <= 256) launch_whole_as<T, false, 64, 4>(a, s);
+    else if (groups <= 512) launch_whole_as<T, false, 128, 4>(a, s);
+    else if (groups <= 1024) launch_whole_as<T, false, 256, 4>(a, s);
+    else if (groups <= 2048) launch_whole_as<T, false, 512, 4>(a, s);
+    else launch_whole_as<T, false, 1024, 4>(a, s);
+  }
 }
 
 template <bool kBack>
