@@ -10,7 +10,9 @@
 //             db = sum over rows of dy
 //
 // Statistics and sums are in binary32; the variance is summed from the
-// centred values, in registers, so that a large mean costs no digits.
+// centred values, in registers, so that a large mean costs no digits. The
+// gradient's products are rounded on their own: in rows of few columns, where dh is
+// a small difference of them, opposite elements then stay opposite.
 //
 // The forward pass reads and writes each element once: a row lives in the
 // registers of 16 to 1024 threads, which hold one to four groups of eight columns
@@ -294,7 +296,7 @@ __global__ void __launch_bounds__(kGradBlock) ckm_norm_grad_kernel(NormGradArgs 
         dw[i][j] = fmaf(d, xh, dw[i][j]);
         db[i][j] += d;
         s[0] += g;
-        s[1] = fmaf(g, xh, s[1]);
+        s[1] += g * xh;
       }
     }
     reduce_rows<OpSum, kLanes, kGradBlock>(s, lds, turn);
@@ -310,7 +312,7 @@ __global__ void __launch_bounds__(kGradBlock) ckm_norm_grad_kernel(NormGradArgs 
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
         const float xh = ((float)r.h[i].get(j) - r.mean) * r.rstd;
-        o[j] = fmaf(r.rstd, fmaf(-xh, s2, (float)r.dy[i].get(j) * w[j] - s1), (float)r.past[i].get(j));
+        o[j] = r.rstd * ((float)r.dy[i].get(j) * w[j] - s1 - xh * s2) + (float)r.past[i].get(j);
       }
       finish_grad<T, kEven>(a, site, row, group, o);
     }
@@ -400,7 +402,7 @@ __global__ void __launch_bounds__(1024) ckm_norm_wide_sums_kernel(NormGradArgs a
       for (int j = 0; j < kVec; ++j) {
         const float g = (float)rd.get(j) * w[j];
         s1 += g;
-        s2 = j < left ? fmaf(g, ((float)rh.get(j) - mean) * rstd, s2) : s2;
+        s2 += j < left ? g * (((float)rh.get(j) - mean) * rstd) : 0.0f;
       }
     }
     float s[2] = {s1, s2};
@@ -432,7 +434,7 @@ __global__ void __launch_bounds__(256) ckm_norm_wide_grad_kernel(NormGradArgs a,
       const float d = (float)rd.get(j), xh = ((float)rh.get(j) - mean) * rstd;
       dw[j] = fmaf(d, xh, dw[j]);
       db[j] += d;
-      o[j] = fmaf(rstd, fmaf(-xh, s2, d * w[j] - s1), (float)past.get(j));
+      o[j] = rstd * (d * w[j] - s1 - xh * s2) + (float)past.get(j);
     }
     finish_grad<T, false>(a, site, row, group, o);
   }

@@ -16,9 +16,8 @@
 // Bound by memory, the dropout's draws a close second: f16 16x2048x2048 without
 // causal mask moves 269 MB in 50 us (5.4 TB/s, where a large copy moves 5.2), causal
 // 202 MB in 43 us, its gradient 269 MB in 54 us. What it took: a row's loads all in
-// flight before its arithmetic; the arithmetic of a score down to a maximum, one
-// fused multiply-add, 2^v, a sum and two products; the dropout's choice on packed
-// halves; one row set a block and no loop, whose invariants had cost a third of the
+// flight before its arithmetic; the arithmetic of a score down to a maximum, a
+// difference, 2^v, a sum and three products; the dropout's choice on packed halves; one row set a block and no loop, whose invariants had cost a third of the
 // registers (gradient 72 -> 55 us); scores held as the words they were loaded as.
 #include <hip/hip_runtime.h>
 
@@ -81,27 +80,31 @@ __device__ __forceinline__ float exp_of(float t, float m) {
   return __builtin_amdgcn_exp2f((t - m) * kLog2e);
 }
 
-// A row's largest logit as its exponentials use it. Without a mask an
-// exponential is one fused multiply-add and 2^v: 2^(x scale log2 e - m log2 e).
-// Where those products could pass the range, at logits beyond 1e37, they are
-// formed by difference instead.
+// A row's largest logit m as its exponentials use it, where no logits are formed. In
+// the 16-bit types exp(scale x - m) is 2^((x - top) scale log2 e), top the largest
+// score: exactly 1 there, as where t - m is formed, so that a row that sees one
+// key has probability 1 and gradient 0. The gradient finds top from m: the score
+// next to m / scale, which lies within a few 2^-24 of one (or is taken as it is).
+template <typename T>
 struct Top {
-  float m, ml, sl;
-  bool far;
+  float m, top, sl;
+  __device__ __forceinline__ Top(float m_, float top_, float scale) : m(m_), top(top_), sl(scale * kLog2e) {}
+  __device__ __forceinline__ Top(float m_, float scale) : m(m_), top(0.0f), sl(scale * kLog2e) {
+    if constexpr (sizeof(T) == 2) {
+      const float q = fmaxf(m / scale, kLowest), near = (float)rounded<T>(q);
+      top = fabsf(q - near) <= 0x1p-20f * fabsf(q) ? near : q;
+    }
+  }
 };
-__device__ __forceinline__ Top top_of(float m, float scale) {
-  const float sl = scale * kLog2e;
-  return {m, m * kLog2e, sl, !(fabsf(m) < 1e37f) || !(fabsf(sl) < 1e37f)};
-}
 // exp(scale x - m) of a group's scores.
 template <typename T>
-__device__ __forceinline__ void exps8(float (&e)[kVec], const Raw8<T>& x, const Top& top, float scale) {
-  if (!top.far) {
+__device__ __forceinline__ void exps8(float (&e)[kVec], const Raw8<T>& x, const Top<T>& top, float scale) {
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf((float)x.get(j), top.sl, -top.ml));
-  } else {
-#pragma unroll
-    for (int j = 0; j < kVec; ++j) e[j] = exp_of((float)x.get(j) * scale, top.m);
+  for (int j = 0; j < kVec; ++j) {
+    if constexpr (sizeof(T) == 2)
+      e[j] = __builtin_amdgcn_exp2f(((float)x.get(j) - top.top) * top.sl);
+    else
+      e[j] = exp_of((float)x.get(j) * scale, top.m);
   }
 }
 // The largest of a group's scores.
@@ -122,11 +125,13 @@ __device__ __forceinline__ float top8(const Raw8<T>& x) {
 }
 
 // What a row's logits are made of: the scores alone (kPlain: with a scale that is
-// not positive), a mask of truth values or of values to add. Without a mask and
-// with a positive scale (kNoMask) no logits are formed.
+// not positive, or near the range's end), a mask of truth values or of values to
+// add. Without a mask and with an ordinary scale (kNoMask) no logits are formed.
 enum : int { kNoMask = 0, kBool = 1, kAdd = 2, kPlain = 3 };
 int mask_form(int mask_kind, float scale) {
-  return mask_kind == CKM_MASK_BOOL ? kBool : mask_kind == CKM_MASK_ADD ? kAdd : scale > 0.0f ? kNoMask : kPlain;
+  return mask_kind == CKM_MASK_BOOL  ? kBool
+         : mask_kind == CKM_MASK_ADD ? kAdd
+         : scale > 1e-30f && scale < 1e30f ? kNoMask : kPlain;
 }
 template <int kMask, typename T>
 using MaskType = std::conditional_t<kMask == kBool, uint8_t, T>;
@@ -227,8 +232,9 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       }
     }
     m = reduce_row<OpMax, kLanes, kBlock>(m, lds, 0);
+    const float most = m;   // a score, with kNoMask
     if constexpr (kMask == kNoMask) m = fmaxf(m * a.scale, kLowest);
-    const Top top = top_of(m, a.scale);
+    const Top<T> top(m, most, a.scale);
     float sum = 0.0f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
@@ -261,7 +267,7 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
     }
   } else {
     const float m = live ? a.stats[2 * row] : 0.0f, z = live ? a.stats[2 * row + 1] : 0.0f;
-    const Top top = top_of(m, a.scale);
+    const Top<T> top(m, a.scale);
     float g[kPer][kVec];
     float sum = 0.0f;
 #pragma unroll
@@ -278,9 +284,9 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
 #pragma unroll
       for (int j = 0; j < kVec; ++j) sum = fmaf(t[i][j], g[i][j], sum);
     }
-    // p = e z: the row's z goes into its two factors
+    // p = e z: the row's z goes into its sum and its factor
     const float by = a.scale * a.drop.scale * z;
-    sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, 0) * z * by;
+    sum = reduce_row<OpSum, kLanes, kBlock>(sum, lds, 0) * z;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int col = (lane + i * kLanes) * kVec;
@@ -288,7 +294,7 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       float o[kVec] = {};
       if (col < seen) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) o[j] = t[i][j] * fmaf(g[i][j], by, -sum);
+        for (int j = 0; j < kVec; ++j) o[j] = t[i][j] * ((g[i][j] - sum) * by);
       }
       store_part<kEven>(y, rounded8<T>(o), col, keys);
     }
@@ -348,7 +354,7 @@ struct Span {
     for (int j = 1; j < kVec; ++j) v = fmaxf(v, t[i][j]);
     return v;
   }
-  __device__ __forceinline__ void exps(const SoftmaxArgs& a, const Top& top, int i) {
+  __device__ __forceinline__ void exps(const SoftmaxArgs& a, const Top<T>& top, int i) {
     if constexpr (kMask == kNoMask) {
       exps8(t[i], x[i], top, a.scale);
     } else {
@@ -377,7 +383,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxA
   Span<T, kBack, kMask> s;
   if constexpr (!kJoin) {
     const float m = kBack ? a.stats[2 * row] : 0.0f;
-    const Top given = top_of(m, a.scale);
+    const Top<T> given(m, a.scale);
     float top = kLowest, sum = 0.0f;
     for (int col = first; col < seen; col += kSplitPer * kSplitSpan) {
       s.load(a, x, dy, mask, col, seen);
@@ -389,7 +395,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxA
         sum *= exp_of(top, now);
         top = now;
       }
-      const Top at = kBack ? given : top_of(now, a.scale);
+      const Top<T> at = kBack ? given : Top<T>(now, a.scale);
 #pragma unroll
       for (int i = 0; i < kSplitPer; ++i) {
         const int c = col + i * kSplitSpan;
@@ -433,9 +439,9 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxA
       m = a.stats[2 * row];
       z = a.stats[2 * row + 1];
       by = a.scale * a.drop.scale * z;
-      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, 0) * z * by;
+      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y, lds, 0) * z;
     }
-    const Top top = top_of(m, a.scale);
+    const Top<T> top(m, a.scale);
     for (int col = first; col < to; col += kSplitPer * kSplitSpan) {
       if (col != first && col < seen) s.load(a, x, dy, mask, col, seen);
 #pragma unroll
@@ -449,7 +455,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxA
             float g[kVec];
             grads8<kMask>(g, a, site, s.dy[i], s.t[i], row, c);
 #pragma unroll
-            for (int j = 0; j < kVec; ++j) s.t[i][j] *= fmaf(g[j], by, -sum);
+            for (int j = 0; j < kVec; ++j) s.t[i][j] *= (g[j] - sum) * by;
             o = rounded8<T>(s.t[i]);
           } else {
 #pragma unroll

@@ -66,7 +66,8 @@ class Dropout:
         self.keep = math.floor((1.0 - self.p) * 65536.0)
         ptr = None
         if d_site is not None:
-            if not isinstance(d_site, torch.Tensor) or not d_site.is_cuda or d_site.dtype != torch.int64 or d_site.numel() != 1:
+            if (not isinstance(d_site, torch.Tensor) or not d_site.is_cuda or d_site.dtype != torch.int64
+                    or d_site.numel() != 1):
                 raise ValueError("d_site must be an int64 device tensor of one element")
             ptr = d_site.data_ptr()
         self._c = _Drop(self.seed, self.site, ptr, self.keep)
@@ -119,7 +120,8 @@ def _rows(t, name: str, shape, dtype, device):
 def _vector(t, name: str, cols: int, dtype, device):
     if t is None:
         return None
-    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == (cols,) and t.is_contiguous():
+    if (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == (cols,)
+            and t.is_contiguous()):
         return t.data_ptr()
     _tensor(t, name, dtype, device)
     if t.dim() != 1 or t.shape[0] != cols or not t.is_contiguous():
@@ -137,21 +139,13 @@ def _drop_ptr(drop, device):
     return C.byref(drop._c)
 
 
-# the current stream's pointer without a torch.cuda.Stream object around it (0.1 us instead of 2.8)
+# the current stream's pointer without a torch.cuda.Stream object around it (0.1 us instead of 2.8), and
+# the current device's number
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _on_stream(fn):
-    """A `stream` argument: the call is made with that stream as the current one, so that the results
-    it allocates belong to it."""
-    @functools.wraps(fn)
-    def call(*args, stream=None, **kw):
-        if stream is None:
-            return fn(*args, **kw)
-        with torch.cuda.stream(stream):
-            return fn(*args, **kw)
-    return call
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _like(t):
@@ -159,22 +153,27 @@ def _like(t):
     return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
-def _row_count(t, name):
-    if t.dim() < 1:
+def _first(t, name: str):
+    """(device, shape, type, columns, rows, pointer, row stride) of an operator's first tensor."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in _TYPES or t.get_device() != _current_device():
+        _tensor(t, name)
+    shape = t.shape
+    if not shape:
         raise ValueError("%s must have at least one dimension" % name)
-    cols = t.shape[-1]
-    return cols, (t.numel() // cols if cols else t.shape[:-1].numel())
+    cols, device = shape[-1], t.get_device()
+    rows = t.numel() // cols if cols else shape[:-1].numel()
+    p, ld = (t.data_ptr(), cols) if t.is_contiguous() else _rows(t, name, shape, t.dtype, device)
+    return device, shape, t.dtype, cols, rows, p, ld
 
 
-@_on_stream
-def dropout(x, drop: Dropout, residual=None, out=None):
+def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
     """y = residual + D(x), rows by the last dimension (ckm_dropout_async). out may be x or residual."""
-    device = _tensor(x, "x").get_device()
-    cols, rows = _row_count(x, "x")
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return dropout(x, drop, residual, out)
+    device, shape, dtype, cols, rows, xp, ldx = _first(x, "x")
     if drop is None:
         raise ValueError("drop is needed")
-    shape, dtype = x.shape, x.dtype
-    xp, ldx = _rows(x, "x", shape, dtype, device)
     rp, ldr = _rows(residual, "residual", shape, dtype, device)
     if out is None:
         y = _like(x)
@@ -192,22 +191,22 @@ def dropout_backward(dy, drop: Dropout, out=None, stream=None):
     return dropout(dy, drop, out=out, stream=stream)
 
 
-@_on_stream
-def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop: Dropout = None, out=None):
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop: Dropout = None, out=None,
+               stream=None):
     """(y, h, stats) of the layer norm over the last dimension (ckm_layer_norm_async).
 
     h = residual + D(x), rounded to x's type; x itself when neither is given.
     weight, bias: vectors of x's type or float32, both of one type. stats:
     float32 [..., 2], mean and 1 / standard deviation of each row of h.
     out: for y; may be x or residual."""
-    device = _tensor(x, "x").get_device()
-    cols, rows = _row_count(x, "x")
-    shape, dtype = x.shape, x.dtype
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return layer_norm(x, weight, bias, eps, residual, drop, out)
+    device, shape, dtype, cols, rows, xp, ldx = _first(x, "x")
     wt = weight.dtype if weight is not None else bias.dtype if bias is not None else dtype
     if wt is not dtype and wt is not torch.float32:
         raise ValueError("weights must be %s or float32, got %s" % (dtype, wt))
     wp, bp = _vector(weight, "weight", cols, wt, device), _vector(bias, "bias", cols, wt, device)
-    xp, ldx = _rows(x, "x", shape, dtype, device)
     rp, ldr = _rows(residual, "residual", shape, dtype, device)
     if out is None:
         y = _like(x)
@@ -227,8 +226,8 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop
     return y, h, stats
 
 
-@_on_stream
-def layer_norm_backward(dy, h, stats, weight=None, dres=None, drop: Dropout = None, wtype=None, out=None, work=None):
+def layer_norm_backward(dy, h, stats, weight=None, dres=None, drop: Dropout = None, wtype=None, out=None, work=None,
+                        stream=None):
     """(dx, dh, dweight, dbias) of layer_norm (ckm_layer_norm_backward_async).
 
     h, stats: what layer_norm returned. dres: a gradient that reaches h past the
@@ -236,15 +235,15 @@ def layer_norm_backward(dy, h, stats, weight=None, dres=None, drop: Dropout = No
     is dh. dweight and dbias are of weight's type (wtype when there is none:
     x's type or float32). out: for dh; may be dy, h or dres. work: a uint8
     device buffer of layer_norm_workspace(rows, cols) bytes to use."""
-    device = _tensor(dy, "dy").get_device()
-    cols, rows = _row_count(dy, "dy")
-    shape, dtype = dy.shape, dy.dtype
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return layer_norm_backward(dy, h, stats, weight, dres, drop, wtype, out, work)
+    device, shape, dtype, cols, rows, dyp, lddy = _first(dy, "dy")
     wt = weight.dtype if weight is not None else wtype or dtype
     if wt is not dtype and wt is not torch.float32:
         raise ValueError("weights must be %s or float32, got %s" % (dtype, wt))
     wp = _vector(weight, "weight", cols, wt, device)
     _stats(stats, shape, device)
-    dyp, lddy = _rows(dy, "dy", shape, dtype, device)
     hp, ldh = _rows(h, "h", shape, dtype, device)
     rp, ldr = _rows(dres, "dres", shape, dtype, device)
     if out is None:
@@ -317,12 +316,13 @@ def _strides(t, name: str, shape, dtype, device):
 
 def _scores(scores, scale, causal, lengths, mask):
     """The C struct of a call's shape, scale and masks, with the tensors it points to."""
-    device = _tensor(scores, "scores").get_device()
-    if not 1 <= scores.dim() <= 4:
-        raise ValueError("scores must have one to four dimensions, got shape %s" % (tuple(scores.shape),))
-    c = _Scores(*((1,) * (4 - scores.dim()) + tuple(scores.shape)))
-    c.scale = scale
-    c.flags = SCORES_CAUSAL if causal else 0
+    if (not isinstance(scores, torch.Tensor) or not scores.is_cuda or scores.dtype not in _TYPES
+            or scores.get_device() != _current_device()):
+        _tensor(scores, "scores")
+    device, shape = scores.get_device(), scores.shape
+    if not 1 <= len(shape) <= 4:
+        raise ValueError("scores must have one to four dimensions, got shape %s" % (tuple(shape),))
+    c = _Scores(*(1,) * (4 - len(shape)), *shape, scale, SCORES_CAUSAL if causal else 0)
     if lengths is not None:
         _tensor(lengths, "lengths", torch.int32, device)
         if lengths.numel() != c.batch or not lengths.is_contiguous():
@@ -342,9 +342,8 @@ def _scores(scores, scale, causal, lengths, mask):
     return c, device
 
 
-@_on_stream
 def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask=None, drop: Dropout = None, out=None,
-            work=None):
+            work=None, stream=None):
     """(probabilities, stats) of attention scores [batch, heads, queries, keys] (ckm_softmax_async).
 
     Fewer dimensions stand for leading ones of 1. lengths: int32 [batch], the
@@ -354,6 +353,9 @@ def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask
     nothing gives zeros. stats: float32 [..., queries, 2], the largest logit
     and 1 / the sum of exponentials. out: for the probabilities; may be scores.
     work: a uint8 device buffer of softmax_workspace(...) bytes to use."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return softmax(scores, scale, causal, lengths, mask, drop, out, work)
     c, device = _scores(scores, scale, causal, lengths, mask)
     shape, dtype = scores.shape, scores.dtype
     xp, xs = _strides(scores, "scores", shape, dtype, device)
@@ -370,11 +372,13 @@ def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask
     return y, stats
 
 
-@_on_stream
 def softmax_backward(dy, scores, stats, scale: float = 1.0, causal: bool = False, lengths=None, mask=None,
-                     drop: Dropout = None, out=None, work=None):
+                     drop: Dropout = None, out=None, work=None, stream=None):
     """The scores' gradient (ckm_softmax_backward_async): the forward call's scores, stats, masks and drop.
     out: may be dy or scores."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return softmax_backward(dy, scores, stats, scale, causal, lengths, mask, drop, out, work)
     c, device = _scores(scores, scale, causal, lengths, mask)
     shape, dtype = scores.shape, scores.dtype
     _stats(stats, shape, device)

@@ -579,3 +579,28 @@ def test_largest_dropouts():
     assert np.array_equal(host(y[:, -800:]) > 0, u < d.keep)
     with pytest.raises(ckm.CkmError):
         ops.dropout(y.expand(2, cols).reshape(1, 2 * cols)[:, :cols + 8], d)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("shape,kw", [((3, 2, 40, 1), {}), ((2, 3, 5, 300), {"lengths": [1, 1]}), ((1, 1, 1, 50000), {"lengths": [1]}),
+                                      ((1, 2, 1, 7), {"mask": True}), ((2, 1, 3, 1), {"scale": -0.7})])
+def test_softmax_of_one_seen_key_is_one_and_its_gradient_zero(dtype, shape, kw):
+    """A row that sees one key: probability 1 and gradient 0, exactly, whatever the score."""
+    B, H, Q, K = shape
+    scale = kw.get("scale", 0.0883883)
+    args = dict(scale=scale)
+    if "lengths" in kw:
+        args["lengths"] = torch.tensor(kw["lengths"], dtype=torch.int32, device="cuda")
+    if "mask" in kw:
+        args["mask"] = torch.arange(K, device="cuda").expand(Q, K) == 0
+    x, dy = randn(shape, dtype, 41, gain=20.0), randn(shape, dtype, 42)
+    d = ops.Dropout(0.25, SEED, SITE)
+    for drop in (None, d):
+        y, stats = ops.softmax(x, drop=drop, **args)
+        if drop is None:
+            assert torch.all(y[..., 0] == 1) and torch.all(y[..., 1:] == 0)
+        assert torch.all(stats[..., 1] == 1)
+        assert torch.all(ops.softmax_backward(dy, x, stats, drop=drop, **args) == 0)
+        # statistics from elsewhere, their maximum rounded to binary32 once
+        other = torch.stack([(x[..., 0].float() * scale), torch.ones_like(x[..., 0], dtype=torch.float32)], -1)
+        assert torch.all(ops.softmax_backward(dy, x, other, drop=drop, **args) == 0)
