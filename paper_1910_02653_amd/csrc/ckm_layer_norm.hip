@@ -21,9 +21,9 @@
 //
 // Bound by memory on large inputs: the fused forward pass of bf16 8192x8192 moves
 // 537 MB in 100 us (5.4 TB/s, where a large copy moves 5.2), the fused gradient of
-// bf16 16384x4096 671 MB in 130 us. Small ones are bound by the launch and one
-// row's chain of load, two sums and store: f16 2048x2048 6.5 us forward, 14 us
-// gradient (10.5 and 3.6 for joining the blocks' sums).
+// bf16 16384x4096 671 MB in 133 us. Small ones are bound by the launch and one
+// row's chain of load, two sums and store: f16 2048x2048 6.6 us forward, 14.6 us
+// gradient (10.8 and 4 for joining the blocks' sums).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -7,18 +7,18 @@
 //   gradient  p = exp(t - m) z from the scores and the statistics, g = D(dy),
 //             dx = scale p (g - sum p g)
 //
-// Neither the probabilities before the dropout nor its mask are ever stored:
-// the gradient makes both again, the same bits as the forward pass made.
+// Neither the probabilities before the dropout nor its mask are ever stored: the
+// gradient makes both again from the scores and the statistics, the mask bit for bit.
 // Logits, statistics and sums are in binary32; exp(v) is 2^(v log2 e), which is
 // off by 2^-24 |v log2 e| relative at most beside the unit's own last bit, and
 // v <= 0 is near 0 where the result counts.
 //
 // Bound by memory, the dropout's draws a close second: f16 16x2048x2048 without
 // causal mask moves 269 MB in 50 us (5.4 TB/s, where a large copy moves 5.2), causal
-// 202 MB in 43 us, its gradient 269 MB in 54 us. What it took: a row's loads all in
+// 202 MB in 44 us, its gradient 269 MB in 55 us. What it took: a row's loads all in
 // flight before its arithmetic; the arithmetic of a score down to a maximum, a
 // difference, 2^v, a sum and three products; the dropout's choice on packed halves; one row set a block and no loop, whose invariants had cost a third of the
-// registers (gradient 72 -> 55 us); scores held as the words they were loaded as.
+// registers (gradient 73 -> 56 us); scores held as the words they were loaded as.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
