@@ -604,3 +604,10 @@ def test_softmax_of_one_seen_key_is_one_and_its_gradient_zero(dtype, shape, kw):
         # statistics from elsewhere, their maximum rounded to binary32 once
         other = torch.stack([(x[..., 0].float() * scale), torch.ones_like(x[..., 0], dtype=torch.float32)], -1)
         assert torch.all(ops.softmax_backward(dy, x, other, drop=drop, **args) == 0)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 500), (16, 500), (64, 500), (65, 500), (4, 8000), (5, 8000), (256, 100), (257, 100)])
+def test_layer_norm_gradient_of_few_rows(rows, cols):
+    """Both sides of the rule that gives few rows to one block, which has no sums to join."""
+    assert (ops.layer_norm_workspace(rows, cols) == 0) == (rows not in (65, 5, 257))
+    test_layer_norm_and_gradient("bf16", "f32", rows, cols)
