@@ -13,8 +13,15 @@ states each operator's definition); there is no other implementation to fall
 back to. Tensors are float32, float16 or bfloat16 on the current device.
 
 Calls enqueue kernels on `stream` (a torch.cuda.Stream; None: the current one)
-and return at once. Results they allocate belong to that stream. No autograd
-graph is recorded: gradients are the *_backward calls.
+and return at once. With a stream other than the current one, that stream first
+waits for what the current stream holds at the call, so arguments made on the
+current stream are whole when they are read, and their memory is not given out
+again before the call is through with it: they may be dropped at once. Work on
+any third stream is the caller's to order, as are later uses of the arguments
+on other streams. Results that a call allocates belong to its stream. (To order
+everything oneself, make the stream the current one and leave `stream` out.)
+
+No autograd graph is recorded: gradients are the *_backward calls.
 """
 from __future__ import annotations
 
@@ -148,6 +155,21 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
+def _on(stream, drop, *tensors):
+    """The context of a call on `stream`, once that stream waits for the current one and holds the call's tensors."""
+    here = torch.cuda.current_stream(stream.device)
+    if stream != here:
+        within = torch.cuda.is_current_stream_capturing()
+        with torch.cuda.stream(stream):
+            # a capture cannot wait for work that is not part of it
+            if within or not torch.cuda.is_current_stream_capturing():
+                stream.wait_stream(here)
+        for t in (*tensors, drop.d_site if isinstance(drop, Dropout) else None):
+            if isinstance(t, torch.Tensor) and t.device == stream.device:
+                t.record_stream(stream)
+    return torch.cuda.stream(stream)
+
+
 def _like(t):
     """A contiguous tensor of t's shape and type."""
     return torch.empty_like(t) if t.is_contiguous() else torch.empty(t.shape, dtype=t.dtype, device=t.device)
@@ -169,7 +191,7 @@ def _first(t, name: str):
 def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
     """y = residual + D(x), rows by the last dimension (ckm_dropout_async). out may be x or residual."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, drop, x, residual, out):
             return dropout(x, drop, residual, out)
     device, shape, dtype, cols, rows, xp, ldx = _first(x, "x")
     if drop is None:
@@ -200,7 +222,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop
     float32 [..., 2], mean and 1 / standard deviation of each row of h.
     out: for y; may be x or residual."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, drop, x, weight, bias, residual, out):
             return layer_norm(x, weight, bias, eps, residual, drop, out)
     device, shape, dtype, cols, rows, xp, ldx = _first(x, "x")
     wt = weight.dtype if weight is not None else bias.dtype if bias is not None else dtype
@@ -236,7 +258,7 @@ def layer_norm_backward(dy, h, stats, weight=None, dres=None, drop: Dropout = No
     x's type or float32). out: for dh; may be dy, h or dres. work: a uint8
     device buffer of layer_norm_workspace(rows, cols) bytes to use."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, drop, dy, h, stats, weight, dres, out, work):
             return layer_norm_backward(dy, h, stats, weight, dres, drop, wtype, out, work)
     device, shape, dtype, cols, rows, dyp, lddy = _first(dy, "dy")
     wt = weight.dtype if weight is not None else wtype or dtype
@@ -354,7 +376,7 @@ def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask
     and 1 / the sum of exponentials. out: for the probabilities; may be scores.
     work: a uint8 device buffer of softmax_workspace(...) bytes to use."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, drop, scores, lengths, mask, out, work):
             return softmax(scores, scale, causal, lengths, mask, drop, out, work)
     c, device = _scores(scores, scale, causal, lengths, mask)
     shape, dtype = scores.shape, scores.dtype
@@ -377,7 +399,7 @@ def softmax_backward(dy, scores, stats, scale: float = 1.0, causal: bool = False
     """The scores' gradient (ckm_softmax_backward_async): the forward call's scores, stats, masks and drop.
     out: may be dy or scores."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, drop, dy, scores, stats, lengths, mask, out, work):
             return softmax_backward(dy, scores, stats, scale, causal, lengths, mask, drop, out, work)
     c, device = _scores(scores, scale, causal, lengths, mask)
     shape, dtype = scores.shape, scores.dtype

@@ -611,3 +611,22 @@ def test_layer_norm_gradient_of_few_rows(rows, cols):
     """Both sides of the rule that gives few rows to one block, which has no sums to join."""
     assert (ops.layer_norm_workspace(rows, cols) == 0) == (rows not in (65, 5, 257))
     test_layer_norm_and_gradient("bf16", "f32", rows, cols)
+
+
+def test_arguments_made_on_the_current_stream_and_dropped_after_the_call():
+    """A call on another stream reads what the current stream has yet to make, from memory that is not given out again
+    before it has."""
+    q = torch.cuda.Stream()
+    d = ops.Dropout(0.1, SEED, SITE)
+    x, s = randn((512, 1024), "f16", 51), randn((2, 3, 256, 512), "f16", 52)
+    want = ops.layer_norm(x, residual=x * 2.0, drop=d)[0], ops.softmax(s, mask=s > 0.0)[0]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        torch.cuda._sleep(20_000_000)   # the current stream is busy for some milliseconds
+        got = [ops.layer_norm(x, residual=x * 2.0, drop=d, stream=q)[0]]
+        torch.cuda._sleep(20_000_000)
+        got.append(ops.softmax(s, mask=s > 0.0, stream=q)[0])
+        junk = [torch.zeros_like(x) for _ in range(4)] + [torch.zeros_like(s, dtype=torch.bool) for _ in range(4)]
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        del junk

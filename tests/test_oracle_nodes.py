@@ -213,3 +213,61 @@ def test_binding_refuses_host_tensors_and_bad_dropouts():
         with pytest.raises(ValueError):
             ops.Dropout(**{"seed": 1, **bad})
     assert ops.Dropout(0.0, 1).keep == 65536 and ops.Dropout(1.0, 1).keep == 0 and ops.Dropout(0.1, 1).keep == 58982
+
+
+@pytest.mark.parametrize("within,captured,waits", [(False, False, True), (True, False, True), (True, True, True),
+                                                   (False, True, False)])
+def test_calls_on_another_stream_wait_for_the_current_one_and_hold_their_tensors(monkeypatch, within, captured, waits):
+    """Every operator with stream=: what happens to the streams and tensors before the call's checks refuse the host
+    tensors. within, captured: whether the current stream and the other one are being captured."""
+    import contextlib
+
+    import torch
+    events, current = [], []
+
+    class Stream:
+        device = torch.device("cpu")
+
+        def wait_stream(self, other):
+            events.append(("wait", self, other))
+
+    class Held(torch.Tensor):
+        def record_stream(self, stream):
+            events.append(("hold", id(self), stream))
+
+    @contextlib.contextmanager
+    def use(stream):
+        current.append(stream)
+        try:
+            yield
+        finally:
+            current.pop()
+
+    here, there = Stream(), Stream()
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current[-1] if current else here)
+    monkeypatch.setattr(torch.cuda, "stream", use)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: captured if current else within)
+    t = [torch.zeros(4, 8).as_subclass(Held) for _ in range(7)]
+    drop = ops.Dropout(0.1, 1)
+    drop.d_site = t[6]
+    calls = [
+        (lambda q: ops.dropout(t[0], drop, residual=t[1], out=t[2], stream=q), (0, 1, 2, 6)),
+        (lambda q: ops.dropout_backward(t[0], drop, out=t[1], stream=q), (0, 1, 6)),
+        (lambda q: ops.layer_norm(t[0], t[1], t[2], residual=t[3], drop=drop, out=t[4], stream=q), (0, 1, 2, 3, 4, 6)),
+        (lambda q: ops.layer_norm_backward(t[0], t[1], t[2], t[3], dres=t[4], out=t[5], work=t[6], stream=q), range(7)),
+        (lambda q: ops.softmax(t[0], lengths=t[1], mask=t[2], drop=drop, out=t[3], work=t[4], stream=q),
+         (0, 1, 2, 3, 4, 6)),
+        (lambda q: ops.softmax_backward(t[0], t[1], t[2], lengths=t[3], mask=t[4], out=t[5], work=t[6], stream=q),
+         range(7)),
+    ]
+    for call, held in calls:
+        for stream in (there, here, None):
+            events.clear()
+            with pytest.raises(ValueError):
+                call(stream)
+            if stream is not there:
+                assert not events
+                continue
+            assert [e for e in events if e[0] == "wait"] == ([("wait", there, here)] if waits else [])
+            assert sorted(e[1] for e in events if e[0] == "hold") == sorted(id(t[k]) for k in held)
+            assert all(e[2] is there for e in events if e[0] == "hold")
