@@ -91,6 +91,8 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
       weight_group<T>(b[i], a.b, a.w32, col, a.cols - col, 0.0f);
     }
   }
+  // a residual that is not there adds -0, which leaves a kept zero its sign
+  const uint32_t absent = a.res ? 0u : sizeof(T) == 4 ? 0x80000000u : 0x80008000u;
   for (int64_t first = (int64_t)blockIdx.x * kRowsAt; first < a.rows; first += (int64_t)gridDim.x * kRowsAt) {
     const int64_t row = first + row_in_block<kLanes>();
     const bool live = row < a.rows;
@@ -102,7 +104,7 @@ __global__ void __launch_bounds__(norm_block(kLanes)) ckm_norm_kernel(NormArgs a
       r[i] = zero_group<T>();
       if (left > 0) r[i] = load_cols<kEven>((const T*)a.x + row * a.ld_x, col, a.cols);
       if constexpr (kFused) {
-        rr[i] = zero_group<T>();
+        rr[i] = group_of<T>(absent);
         if (a.res && left > 0) rr[i] = load_cols<kEven>((const T*)a.res + row * a.ld_res, col, a.cols);
       }
     }

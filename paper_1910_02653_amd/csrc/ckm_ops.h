@@ -73,11 +73,15 @@ __device__ __forceinline__ Raw8<T> load8(const T* p) {
   return r;
 }
 template <typename T>
-__device__ __forceinline__ Raw8<T> zero_group() {
+__device__ __forceinline__ Raw8<T> group_of(uint32_t word) {
   Raw8<T> r;
 #pragma unroll
-  for (int k = 0; k < Raw8<T>::kWords; ++k) r.w[k] = 0u;
+  for (int k = 0; k < Raw8<T>::kWords; ++k) r.w[k] = word;
   return r;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> zero_group() {
+  return group_of<T>(0u);
 }
 // kCount elements from kFrom on.
 template <typename T, int kFrom, int kCount>

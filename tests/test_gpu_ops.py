@@ -630,3 +630,18 @@ def test_arguments_made_on_the_current_stream_and_dropped_after_the_call():
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
         del junk
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("cols", [5, 64, 300, 2048, 8193, 20000])
+@pytest.mark.parametrize("p", [0.25, 0.0])
+def test_a_kept_zero_keeps_its_sign(dtype, cols, p):
+    """The norm with a dropout and no residual before it: the bits of the two calls, zeros of both signs among them."""
+    x = randn((6, cols), dtype, 81)
+    x[0], x[1], x[2, ::2] = -0.0, 0.0, -0.0
+    d = ops.Dropout(p, SEED, SITE)
+    h = ops.dropout(x, d)
+    y, _, stats = ops.layer_norm(h)
+    for got, want in zip(ops.layer_norm(x, drop=d), (y, h, stats)):
+        bits = torch.int16 if got.element_size() == 2 else torch.int32
+        assert torch.equal(got.view(bits), want.view(bits))
