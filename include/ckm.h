@@ -433,7 +433,10 @@ ckm_status ckm_layer_norm_backward_async(ckm_dtype type, ckm_dtype wtype, int64_
  * the mask lets it: CKM_MASK_BOOL: uint8, 0 hides; CKM_MASK_ADD: values of the
  * scores' type added after the scale, -inf hides. mask_stride: elements between
  * batches, heads and queries, 0 to share one; keys are contiguous. Scores and
- * gradients where a key is not seen are never used. */
+ * gradients where a key is not seen are never used. The logits scale x + mask are
+ * binary32: one past its range is an infinite one, in a gradient too: -inf counts
+ * for nothing, and a row that sees +inf or NaN is NaN where it sees keys (elsewhere
+ * it is 0 or NaN), as is its 1 / the sum of exponentials. */
 enum { CKM_SCORES_CAUSAL = 1u };
 enum { CKM_MASK_NONE = 0, CKM_MASK_BOOL = 1, CKM_MASK_ADD = 2 };
 typedef struct ckm_scores {

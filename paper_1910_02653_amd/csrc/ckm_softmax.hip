@@ -232,8 +232,14 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       }
     }
     m = reduce_row<OpMax, kLanes, kBlock>(m, lds, 0);
-    const float most = m;   // a score, with kNoMask
-    if constexpr (kMask == kNoMask) m = fmaxf(m * a.scale, kLowest);
+    float most = m;   // a score, with kNoMask
+    if constexpr (kMask == kNoMask) {
+      m *= a.scale;
+      // a logit past the range is an infinite one, as where logits are formed
+      if constexpr (sizeof(T) == 2)
+        most = m == __builtin_inff() ? __builtin_nanf("") : m == -__builtin_inff() ? __builtin_inff() : most;
+      m = fmaxf(m, kLowest);
+    }
     const Top<T> top(m, most, a.scale);
     float sum = 0.0f;
 #pragma unroll

@@ -645,3 +645,35 @@ def test_a_kept_zero_keeps_its_sign(dtype, cols, p):
     for got, want in zip(ops.layer_norm(x, drop=d), (y, h, stats)):
         bits = torch.int16 if got.element_size() == 2 else torch.int32
         assert torch.equal(got.view(bits), want.view(bits))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("keys", [30, 3000, 40000])
+@pytest.mark.parametrize("form", ["none", "bool", "add", "negative"])
+def test_softmax_logits_past_the_range(dtype, keys, form):
+    """A logit that binary32 cannot hold is an infinite score, in every kernel and in both directions: below the range
+    it counts for nothing, above it the row is NaN."""
+    T = TYPES[dtype]
+    x = torch.full((4, keys), -3e38, dtype=T, device="cuda")   # row 0: all below
+    x[1, 7] = 1.0                                              # all below but one
+    x[2] = 0.0
+    x[2, :2] = 3e38                                            # two above
+    x[3, 5], x[3, 6] = 1e38, 1e38                              # in range, two alike
+    scale, kw = 2.0, {}
+    if form == "negative":
+        x, scale = -x, -2.0
+    if form == "bool":
+        kw["mask"] = torch.ones((4, keys), dtype=torch.bool, device="cuda")
+    if form == "add":
+        kw["mask"] = torch.zeros((4, keys), dtype=T, device="cuda")
+    y, stats = ops.softmax(x, scale, **kw)
+    assert torch.all(y[0] == 0) and torch.all(stats[0] == 0)
+    assert y[1, 7] == 1 and torch.all(y[1, :7] == 0) and torch.all(y[1, 8:] == 0)
+    assert stats[1, 0] == 2 and stats[1, 1] == 1
+    assert torch.isnan(y[2]).all() and stats[2, 0] == float("inf") and torch.isnan(stats[2, 1])
+    assert y[3, 5] == 0.5 and y[3, 6] == 0.5 and y[3].float().sum() == 1
+    dy = torch.linspace(-1, 1, 4 * keys, device="cuda").view(4, keys).to(T)
+    dy[3, 5], dy[3, 6] = 1.0, -1.0
+    dx = ops.softmax_backward(dy, x, stats, scale, **kw)
+    assert torch.all(dx[:2] == 0) and torch.isnan(dx[2]).all()
+    assert torch.all(dx[3, 7:] == 0) and dx[3, 5] == scale / 2 and dx[3, 6] == -scale / 2
