@@ -220,7 +220,8 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop
     h = residual + D(x), rounded to x's type; x itself when neither is given.
     weight, bias: vectors of x's type or float32, both of one type. stats:
     float32 [..., 2], mean and 1 / standard deviation of each row of h.
-    out: for y; may be x or residual."""
+    out: for y; may be x or residual. With y in the place of an x that would be
+    h, h is None: keep x for layer_norm_backward."""
     if stream is not None:
         with _on(stream, drop, x, weight, bias, residual, out):
             return layer_norm(x, weight, bias, eps, residual, drop, out)
@@ -237,7 +238,7 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop
         y = out
         yp, ldy = _rows(y, "out", shape, dtype, device)
     if residual is None and drop is None:
-        h, hp = x, None
+        h, hp = None if yp == xp and rows else x, None
     else:
         h = _like(x)
         hp = h.data_ptr()

@@ -677,3 +677,17 @@ def test_softmax_logits_past_the_range(dtype, keys, form):
     dx = ops.softmax_backward(dy, x, stats, scale, **kw)
     assert torch.all(dx[:2] == 0) and torch.isnan(dx[2]).all()
     assert torch.all(dx[3, 7:] == 0) and dx[3, 5] == scale / 2 and dx[3, 6] == -scale / 2
+
+
+def test_layer_norm_in_place_of_its_only_input_has_no_h():
+    """y in the place of x, which would have been h: the call says that there is none, and the gradient refuses."""
+    x, dy = randn((6, 48), "f16", 82), randn((6, 48), "f16", 83)
+    for out in (x, x.view(6, 48)):
+        y, h, stats = ops.layer_norm(x, out=out)
+        assert y is out and h is None
+        with pytest.raises((ValueError, ckm.CkmError)):
+            ops.layer_norm_backward(dy, h, stats)
+    r = randn((6, 48), "f16", 84)
+    assert ops.layer_norm(x, residual=r, out=x)[1] is not None and ops.layer_norm(r, out=x)[1] is r
+    empty = x[:0]
+    assert ops.layer_norm(empty)[1] is empty and ops.layer_norm(empty, out=empty)[1] is empty
