@@ -60,24 +60,67 @@ class Dropout:
     keep / 65536, keep = floor((1 - p) 65536), and scaled by its inverse).
     site: names the place and step; equal (seed, site) give equal masks.
     d_site: an int64 device tensor of one element, added to site when a kernel
-    runs: the step counter of a captured graph."""
+    runs: the step counter of a captured graph.
+    p, seed, site and d_site can be assigned; later calls go by the new values."""
 
-    __slots__ = ("p", "seed", "site", "keep", "d_site", "_c")
+    __slots__ = ("_p", "_d_site", "_c")
 
     def __init__(self, p: float, seed: int, site: int = 0, d_site=None):
         if not 0.0 <= p <= 1.0:
             raise ValueError("p must lie in [0, 1], got %r" % (p,))
         if not 0 <= seed < 1 << 64 or not 0 <= site < 1 << 64:
             raise ValueError("seed and site must be unsigned 64-bit numbers, got %r and %r" % (seed, site))
-        self.p, self.seed, self.site, self.d_site = float(p), int(seed), int(site), d_site
-        self.keep = math.floor((1.0 - self.p) * 65536.0)
-        ptr = None
+        self._p, self._d_site = float(p), None
+        self._c = _Drop(int(seed), int(site), None, math.floor((1.0 - self._p) * 65536.0))
         if d_site is not None:
-            if (not isinstance(d_site, torch.Tensor) or not d_site.is_cuda or d_site.dtype != torch.int64
-                    or d_site.numel() != 1):
-                raise ValueError("d_site must be an int64 device tensor of one element")
-            ptr = d_site.data_ptr()
-        self._c = _Drop(self.seed, self.site, ptr, self.keep)
+            self.d_site = d_site
+
+    @property
+    def p(self) -> float:
+        return self._p
+
+    @p.setter
+    def p(self, p: float):
+        if not 0.0 <= p <= 1.0:
+            raise ValueError("p must lie in [0, 1], got %r" % (p,))
+        self._p = float(p)
+        self._c.keep = math.floor((1.0 - self._p) * 65536.0)
+
+    @property
+    def keep(self) -> int:
+        return self._c.keep
+
+    @property
+    def seed(self) -> int:
+        return self._c.seed
+
+    @seed.setter
+    def seed(self, seed: int):
+        if not 0 <= seed < 1 << 64:
+            raise ValueError("seed must be an unsigned 64-bit number, got %r" % (seed,))
+        self._c.seed = int(seed)
+
+    @property
+    def site(self) -> int:
+        return self._c.site
+
+    @site.setter
+    def site(self, site: int):
+        if not 0 <= site < 1 << 64:
+            raise ValueError("site must be an unsigned 64-bit number, got %r" % (site,))
+        self._c.site = int(site)
+
+    @property
+    def d_site(self):
+        return self._d_site
+
+    @d_site.setter
+    def d_site(self, d_site):
+        if d_site is not None and (not isinstance(d_site, torch.Tensor) or not d_site.is_cuda
+                                   or d_site.dtype != torch.int64 or d_site.numel() != 1):
+            raise ValueError("d_site must be an int64 device tensor of one element")
+        self._d_site = d_site
+        self._c.d_site = None if d_site is None else d_site.data_ptr()
 
 
 def _tensor(t, name: str, dtype=None, device=None):
@@ -141,8 +184,8 @@ def _drop_ptr(drop, device):
         return None
     if not isinstance(drop, Dropout):
         raise ValueError("drop must be an ops.Dropout, got %s" % type(drop).__name__)
-    if drop.d_site is not None and drop.d_site.get_device() != device:
-        raise ValueError("d_site is on %s, not on device %d" % (drop.d_site.device, device))
+    if drop._d_site is not None and drop._d_site.get_device() != device:
+        raise ValueError("d_site is on %s, not on device %d" % (drop._d_site.device, device))
     return C.byref(drop._c)
 
 

@@ -691,3 +691,15 @@ def test_layer_norm_in_place_of_its_only_input_has_no_h():
     assert ops.layer_norm(x, residual=r, out=x)[1] is not None and ops.layer_norm(r, out=x)[1] is r
     empty = x[:0]
     assert ops.layer_norm(empty)[1] is empty and ops.layer_norm(empty, out=empty)[1] is empty
+
+
+def test_a_dropout_whose_site_is_assigned_draws_another_mask():
+    x = randn((16, 100), "f16", 85)
+    d = ops.Dropout(0.5, SEED, SITE)
+    first = ops.dropout(x, d)
+    d.site += 1
+    assert torch.equal(ops.dropout(x, d), ops.dropout(x, ops.Dropout(0.5, SEED, SITE + 1)))
+    d.site, d.d_site = 3, torch.tensor([SITE - 3], device="cuda")
+    assert torch.equal(ops.dropout(x, d), first)
+    d.d_site, d.p = None, 0.0
+    assert torch.equal(ops.dropout(x, d), x)

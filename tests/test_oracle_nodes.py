@@ -249,7 +249,7 @@ def test_calls_on_another_stream_wait_for_the_current_one_and_hold_their_tensors
     monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: captured if current else within)
     t = [torch.zeros(4, 8).as_subclass(Held) for _ in range(7)]
     drop = ops.Dropout(0.1, 1)
-    drop.d_site = t[6]
+    drop._d_site = t[6]   # past the check that it is on a device
     calls = [
         (lambda q: ops.dropout(t[0], drop, residual=t[1], out=t[2], stream=q), (0, 1, 2, 6)),
         (lambda q: ops.dropout_backward(t[0], drop, out=t[1], stream=q), (0, 1, 6)),
@@ -271,3 +271,17 @@ def test_calls_on_another_stream_wait_for_the_current_one_and_hold_their_tensors
             assert [e for e in events if e[0] == "wait"] == ([("wait", there, here)] if waits else [])
             assert sorted(e[1] for e in events if e[0] == "hold") == sorted(id(t[k]) for k in held)
             assert all(e[2] is there for e in events if e[0] == "hold")
+
+
+def test_a_dropout_goes_by_what_it_is_assigned():
+    d = ops.Dropout(0.25, 3, 4)
+    d.p, d.seed, d.site = 0.5, (1 << 64) - 1, 5
+    d.site += 1
+    assert (d.p, d.keep, d.seed, d.site, d.d_site) == (0.5, 32768, (1 << 64) - 1, 6, None)
+    assert (d._c.keep, d._c.seed, d._c.site, d._c.d_site) == (32768, (1 << 64) - 1, 6, None)
+    for name, value in (("p", 1.5), ("p", float("nan")), ("seed", -1), ("site", 1 << 64), ("d_site", 3)):
+        with pytest.raises(ValueError):
+            setattr(d, name, value)
+    with pytest.raises(AttributeError):
+        d.keep = 1
+    assert (d._c.keep, d._c.seed, d._c.site, d._c.d_site) == (32768, (1 << 64) - 1, 6, None)
