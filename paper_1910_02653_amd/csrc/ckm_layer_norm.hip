@@ -228,6 +228,16 @@ __device__ __forceinline__ void put_sum(const NormGradArgs& a, bool only, float*
   }
 }
 
+// The sum of kCount floats `step` apart, as a tree: a small term is not lost beside a
+// large one, as in a chain of as many additions.
+template <int kCount>
+__device__ __forceinline__ float tree_sum(const float* at, int step) {
+  if constexpr (kCount == 1)
+    return *at;
+  else
+    return tree_sum<kCount / 2>(at, step) + tree_sum<kCount / 2>(at + kCount / 2 * step, step);
+}
+
 constexpr int kGradBlock = 1024;
 
 // A row of the gradient's inputs as a thread holds it, in its own type: its
@@ -343,8 +353,7 @@ __global__ void __launch_bounds__(kGradBlock) ckm_norm_grad_kernel(NormGradArgs 
       }
       __syncthreads();
       for (int k = threadIdx.x; k < 2 * kSpan; k += kGradBlock) {
-        float s = join[k];
-        for (int r = 1; r < kPlaces; ++r) s += join[r * (2 * kSpan) + k];
+        const float s = tree_sum<kPlaces>(join + k, 2 * kSpan);
         put_sum<T>(a, only, part, width, k / kSpan, i * kSpan + k % kSpan, s);
       }
     }
@@ -374,8 +383,7 @@ __global__ void __launch_bounds__(256) ckm_norm_join_kernel(const float* __restr
   __syncthreads();
   if (threadIdx.x < 32) {
     const float* f = (const float*)&lds[0][0];
-    float t = 0.0f;
-    for (int r = 0; r < 32; ++r) t += f[r * 32 + threadIdx.x];
+    const float t = tree_sum<32>(f + threadIdx.x, 32);
     const int c = blockIdx.x * 32 + threadIdx.x;
     if (c < cols) store_weight<T>(out, w32, c, t);
   }

@@ -703,3 +703,20 @@ def test_a_dropout_whose_site_is_assigned_draws_another_mask():
     assert torch.equal(ops.dropout(x, d), first)
     d.d_site, d.p = None, 0.0
     assert torch.equal(ops.dropout(x, d), x)
+
+
+@pytest.mark.parametrize("rows,cols,at", [(4000, 30, 1), (4000, 30, 64), (300, 100, 1), (60000, 2, 64), (64, 1000, 1),
+                                          (2048, 2048, 4), (2048, 30, 64)])
+def test_weight_gradients_are_summed_in_trees(rows, cols, at):
+    """One large term and many small ones, every `at`-th row: a chain of additions past the large one would lose them
+    all. Depth: the rows of a thread (4 at most), trees over a block's rows (6) and over 32 slots of the blocks' sums
+    (5) of 8 blocks each, and the result's rounding: 24."""
+    dy = torch.zeros((rows, cols), device="cuda")
+    dy[::at] = 1.0
+    dy[0] = 2.0 ** 24
+    h = torch.ones((rows, cols), device="cuda")
+    stats = torch.tensor([0.0, 1.0], device="cuda").expand(rows, 2).contiguous()   # xh = 1: both sums are of dy
+    _, _, dw, db = ops.layer_norm_backward(dy, h, stats)
+    want = host(dy[:, 0]).sum()
+    for got in (dw, db):
+        assert np.all(np.abs(host(got) - want) <= 24 * U * want), (float(got[0]) - want)
