@@ -9,16 +9,21 @@
 //
 // Neither the probabilities before the dropout nor its mask are ever stored: the
 // gradient makes both again from the scores and the statistics, the mask bit for bit.
-// Logits, statistics and sums are in binary32; exp(v) is 2^(v log2 e), which is
-// off by 2^-24 |v log2 e| relative at most beside the unit's own last bit, and
-// v <= 0 is near 0 where the result counts.
+// Logits, statistics and sums are in binary32. exp(v), v = t - m <= 0, is 2^(v log2 e).
+// Its relative error beside the unit's last place, with u = 2^-24: in binary32 u,
+// since what the product's rounding loses is made good (four more operations a score:
+// f32 16x1024x1024 27 us with and without, single queries on 32768 keys 9.6 -> 10.1); in
+// the 16-bit types, whose own rounding is far coarser, 1.3 u |v| where logits are formed
+// (the factor and the product) and 3.3 u |v| where they are not (scale log2 e, the
+// difference of the scores, the product).
 //
 // Bound by memory, the dropout's draws a close second: f16 16x2048x2048 without
 // causal mask moves 269 MB in 50 us (5.4 TB/s, where a large copy moves 5.2), causal
 // 202 MB in 44 us, its gradient 269 MB in 55 us. What it took: a row's loads all in
 // flight before its arithmetic; the arithmetic of a score down to a maximum, a
-// difference, 2^v, a sum and three products; the dropout's choice on packed halves; one row set a block and no loop, whose invariants had cost a third of the
-// registers (gradient 73 -> 56 us); scores held as the words they were loaded as.
+// difference, 2^v, a sum and three products; the dropout's choice on packed halves; one
+// row set a block and no loop, whose invariants had cost a third of the registers
+// (gradient 73 -> 56 us); scores held as the words they were loaded as.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -76,8 +81,14 @@ __device__ __forceinline__ int64_t offset_of(const Strided& t, const Row& r) {
 
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0x1.62e43p-1f, kLn2Low = (float)(0.693147180559945309 - (double)kLn2);
+// exp(t - m), t <= m. In binary32, what the rounding of p = v log2 e lost goes in as a
+// factor 1 + (v - p ln 2); for v = -inf that is NaN, and the 0 before it stays.
+template <typename T>
 __device__ __forceinline__ float exp_of(float t, float m) {
-  return __builtin_amdgcn_exp2f((t - m) * kLog2e);
+  const float v = t - m, p = v * kLog2e, e = __builtin_amdgcn_exp2f(p);
+  if constexpr (sizeof(T) == 2) return e;
+  return fmaf(e, fmaxf(fmaf(-p, kLn2Low, fmaf(-p, kLn2, v)), -1.0f), e);
 }
 
 // A row's largest logit m as its exponentials use it, where no logits are formed. In
@@ -104,7 +115,7 @@ __device__ __forceinline__ void exps8(float (&e)[kVec], const Raw8<T>& x, const 
     if constexpr (sizeof(T) == 2)
       e[j] = __builtin_amdgcn_exp2f(((float)x.get(j) - top.top) * top.sl);
     else
-      e[j] = exp_of((float)x.get(j) * scale, top.m);
+      e[j] = exp_of<T>((float)x.get(j) * scale, top.m);
   }
 }
 // The largest of a group's scores.
@@ -249,7 +260,7 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       if constexpr (kMask == kNoMask) exps8(t[i], rx[i], top, a.scale);
 #pragma unroll
       for (int j = 0; j < kVec; ++j) {
-        if constexpr (kMask != kNoMask) t[i][j] = exp_of(t[i][j], m);
+        if constexpr (kMask != kNoMask) t[i][j] = exp_of<T>(t[i][j], m);
         sum += t[i][j];
       }
     }
@@ -282,7 +293,7 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
       if (col >= seen) continue;
       if constexpr (kMask != kNoMask) {
 #pragma unroll
-        for (int j = 0; j < kVec; ++j) t[i][j] = exp_of(t[i][j], m);
+        for (int j = 0; j < kVec; ++j) t[i][j] = exp_of<T>(t[i][j], m);
       } else {
         exps8(t[i], rx[i], top, a.scale);
       }
@@ -365,7 +376,7 @@ struct Span {
       exps8(t[i], x[i], top, a.scale);
     } else {
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) t[i][j] = exp_of(t[i][j], top.m);
+      for (int j = 0; j < kVec; ++j) t[i][j] = exp_of<T>(t[i][j], top.m);
     }
   }
 };
@@ -398,7 +409,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxA
 #pragma unroll
         for (int i = 0; i < kSplitPer; ++i)
           if (col + i * kSplitSpan < seen) now = fmaxf(now, s.largest(a, i));
-        sum *= exp_of(top, now);
+        sum *= exp_of<T>(top, now);
         top = now;
       }
       const Top<T> at = kBack ? given : Top<T>(now, a.scale);
@@ -420,7 +431,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxA
     }
     if constexpr (!kBack) {
       const float all = reduce_row<OpMax, kSplitBlock, kSplitBlock>(top, lds, 0);
-      sum *= exp_of(top, all);
+      sum *= exp_of<T>(top, all);
       top = all;
     }
     sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(sum, lds, 1);
@@ -435,7 +446,7 @@ __global__ void __launch_bounds__(kSplitBlock) ckm_softmax_split_kernel(SoftmaxA
     float m, z, sum, by = 1.0f;
     if constexpr (!kBack) {
       m = reduce_row<OpMax, kSplitBlock, kSplitBlock>(mine.x, lds, 0);
-      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y * exp_of(mine.x, m), lds, 1);
+      sum = reduce_row<OpSum, kSplitBlock, kSplitBlock>(mine.y * exp_of<T>(mine.x, m), lds, 1);
       z = sum == 0.0f ? 0.0f : 1.0f / sum;
       if (share == 0 && threadIdx.x == 0 && a.stats) {
         a.stats[2 * row] = sum == 0.0f ? 0.0f : m;

@@ -720,3 +720,33 @@ def test_weight_gradients_are_summed_in_trees(rows, cols, at):
     want = host(dy[:, 0]).sum()
     for got in (dw, db):
         assert np.all(np.abs(host(got) - want) <= 24 * U * want), (float(got[0]) - want)
+
+
+@pytest.mark.parametrize("keys", [500, 3000, 40000])
+@pytest.mark.parametrize("form", ["none", "bool", "add"])
+def test_small_probabilities_in_binary32(keys, form):
+    """exp(v) for v down to -80, with the largest logit 0 and the sum 1, is right to the exponential unit's last place
+    (2 U), the correction's rounding (U) and the product with 1 / sum: 4 U; the rounding of v log2 e alone would be up
+    to 2^-18, 64 U. The gradient adds a difference and two products."""
+    rng = np.random.default_rng(keys)
+    v = np.float32(rng.uniform(-80.0, -45.0, (3, keys)))
+    v[:, keys // 3] = 0.0
+    x = torch.from_numpy(v).cuda()
+    kw = {}
+    if form == "bool":
+        kw["mask"] = torch.ones((3, keys), dtype=torch.bool, device="cuda")
+    if form == "add":
+        kw["mask"] = torch.zeros((3, keys), device="cuda")
+    y, stats = ops.softmax(x, **kw)
+    assert torch.all(stats[:, 0] == 0) and torch.all(stats[:, 1] == 1)
+    want = np.exp(v.astype(np.float64))
+    off = np.abs(host(y) - want) / want
+    assert off.max() <= 4 * U, off.max() / U
+    dy = torch.from_numpy(np.float32(rng.uniform(1.0, 2.0, (3, keys)))).cuda()
+    dy[:, keys // 3] = 0.0
+    dx = host(ops.softmax_backward(dy, x, stats, **kw))
+    g = host(dy)
+    full = want * (g - (want * g).sum(1, keepdims=True))
+    seen = g > 0
+    off = np.abs(dx - full)[seen] / np.abs(full)[seen]
+    assert off.max() <= 8 * U, off.max() / U
