@@ -499,8 +499,13 @@ void launch_norm(const NormArgs& a, bool fused, hipStream_t s) {
 // 140 and 132). One group a thread up to 8192 columns, over as many threads as a row
 // needs: two groups on half the threads leave no registers (f16 16384x1024 48 us, 42
 // so), and two rows at a time neither (bf16 16384x4096 159 us, 130 so). Rows that four
-// blocks take in one turn are one block's, in four, which has no sums to join: a
-// call on f16 16x2048 10.9 us, 15.5 in four blocks; 32x2048 17.3, 15.5 in eight.
+// blocks take in one turn (two, with two groups a thread) are one block's, in as many
+// turns, which has no sums to join: a call on f16 256x128 10.6 us, 15.2 in four blocks;
+// 64x512 10.7, 15.3; 16x2048 10.7, 15.3; 4x8192 12.4, 15.9 (f32 14.7, 15.3); 2x16384 17.9,
+// 23.3 (f32 26.3, 24.9); 4x16384 25.9, 23.3 (f32 34.9, 24.9). That is the host's second
+// launch: in a graph the joined blocks are faster from three turns on (16x2048 6.6 us,
+// 9.9 in one block; of two turns, 8x2048 6.6, 6.3). f16 32x2048 as calls 17.3, 15.5 in
+// eight blocks.
 struct GradPlan {
   int lanes, per;       // 0, 0: by columns
   int64_t blocks;       // sets of column sums
@@ -518,7 +523,7 @@ GradPlan grad_plan(int64_t rows, int64_t cols) {
   p.lanes = lanes;
   p.per = groups <= 1024 ? 1 : 2;
   p.blocks = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, kGradBlock / lanes), 256));
-  if (p.blocks <= 4) p.blocks = 1;
+  if (p.blocks <= (p.per == 1 ? 4 : 2)) p.blocks = 1;
   return p;
 }
 

@@ -750,3 +750,9 @@ def test_small_probabilities_in_binary32(keys, form):
     seen = g > 0
     off = np.abs(dx - full)[seen] / np.abs(full)[seen]
     assert off.max() <= 8 * U, off.max() / U
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4])
+@pytest.mark.parametrize("dtype,cols", [("f16", 16384), ("f32", 8199)])
+def test_layer_norm_gradient_of_few_wide_rows(dtype, rows, cols):
+    test_layer_norm_and_gradient(dtype, "f32", rows, cols)

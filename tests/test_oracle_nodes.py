@@ -285,3 +285,11 @@ def test_a_dropout_goes_by_what_it_is_assigned():
     with pytest.raises(AttributeError):
         d.keep = 1
     assert (d._c.keep, d._c.seed, d._c.site, d._c.d_site) == (32768, (1 << 64) - 1, 6, None)
+
+
+def test_wide_rows_of_one_block_are_few():
+    """Rows of two groups a thread take a block's whole turn twice over: no more than two of them share one."""
+    for cols in (8193, 16384):
+        assert ops.layer_norm_workspace(2, cols) == 0
+        assert ops.layer_norm_workspace(3, cols) >= 3 * 2 * cols * 4 and ops.layer_norm_workspace(4, cols) >= 4 * 2 * cols * 4
+    assert ops.layer_norm_workspace(4, 8192) == 0
