@@ -403,6 +403,9 @@ def _scores(scores, scale, causal, lengths, mask):
         except RuntimeError:
             raise ValueError("mask of shape %s does not broadcast to scores of shape %s"
                              % (tuple(mask.shape), tuple(scores.shape))) from None
+        if shape[-1] > 1 and mask.stride(-1) == 0:
+            raise ValueError("mask must have each of the %d keys in its last dimension: it is broadcast over queries, "
+                             "heads and batches alone" % shape[-1])
         c.d_mask, c.mask_stride = _strides(mask, "mask", scores.shape, mask.dtype, device)
         c.mask_kind = MASK_ADD if mask.dtype == scores.dtype else MASK_BOOL
     return c, device
@@ -415,10 +418,12 @@ def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask
     Fewer dimensions stand for leading ones of 1. lengths: int32 [batch], the
     keys that each sequence has. causal: query i sees key j iff j <= i + keys -
     queries. mask: bool or uint8 (0 hides a key) or of the scores' type (added
-    after the scale; -inf hides), broadcast to the scores. A row that sees
-    nothing gives zeros. stats: float32 [..., queries, 2], the largest logit
-    and 1 / the sum of exponentials. out: for the probabilities; may be scores.
-    work: a uint8 device buffer of softmax_workspace(...) bytes to use."""
+    after the scale; -inf hides), with every key in its last dimension and
+    broadcast over queries, heads and batches. A row that sees nothing gives
+    zeros. stats: float32 [..., queries, 2], the largest logit and 1 / the sum
+    of exponentials. out: for the probabilities; may be scores (which the
+    gradient needs). work: a uint8 device buffer of softmax_workspace(...)
+    bytes to use."""
     if stream is not None:
         with _on(stream, drop, scores, lengths, mask, out, work):
             return softmax(scores, scale, causal, lengths, mask, drop, out, work)

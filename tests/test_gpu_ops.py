@@ -756,3 +756,15 @@ def test_small_probabilities_in_binary32(keys, form):
 @pytest.mark.parametrize("dtype,cols", [("f16", 16384), ("f32", 8199)])
 def test_layer_norm_gradient_of_few_wide_rows(dtype, rows, cols):
     test_layer_norm_and_gradient(dtype, "f32", rows, cols)
+
+
+def test_a_mask_of_one_key_is_refused_by_its_name():
+    x = torch.zeros((2, 3, 5, 8), device="cuda")
+    for shape in ((), (1,), (5, 1), (2, 1, 1, 1)):
+        for dtype in (torch.bool, torch.float32):
+            with pytest.raises(ValueError, match="mask must have each of the 8 keys"):
+                ops.softmax(x, mask=torch.ones(shape, dtype=dtype, device="cuda"))
+    for shape in ((8,), (1, 8), (5, 8), (2, 1, 1, 8), (1, 3, 5, 8)):
+        assert torch.all(ops.softmax(x, mask=torch.ones(shape, dtype=torch.bool, device="cuda"))[0] == 0.125)
+    one = x[..., :1]   # one key: any mask has it
+    assert torch.all(ops.softmax(one, mask=torch.ones((5, 1), dtype=torch.bool, device="cuda"))[0] == 1)
