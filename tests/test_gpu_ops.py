@@ -758,6 +758,151 @@ def test_layer_norm_gradient_of_few_wide_rows(dtype, rows, cols):
     test_layer_norm_and_gradient(dtype, "f32", rows, cols)
 
 
+# ---------------------------------------------------------------------------
+# rows and keys past what a launch takes in one turn
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype,wtype,rows,cols", [("f16", "f32", 2500, 2048), ("bf16", "bf16", 1100, 4104),
+                                                   ("f16", "f16", 600, 16384), ("f32", "f32", 40000, 72),
+                                                   ("f16", "f32", 300, 16392), ("bf16", "f32", 2100, 16392)])
+def test_layer_norm_rows_past_one_turn(dtype, wtype, rows, cols):
+    """More rows than a launch's blocks take at once: each block goes on to other rows, and the blocks' column sums are
+    joined. DEPTH holds: a thread sums 9 rows at most."""
+    test_layer_norm_and_gradient(dtype, wtype, rows, cols)
+
+
+@pytest.mark.parametrize("dtype,shape", [("f16", (2, 150, 1, 50001)), ("f32", (1, 260, 1, 33001)), ("bf16", (1, 1, 1, 1100003))])
+@pytest.mark.parametrize("kind,causal,ragged", [("none", False, True), ("bool", False, False), ("add", True, False)])
+def test_softmax_shares_past_one_turn(dtype, shape, kind, causal, ragged):
+    """Shares of more keys than a block holds at a time. DEPTH holds: a thread sums 80 keys in groups of 16 at most."""
+    test_softmax_and_gradient(dtype, shape, kind, causal, ragged)
+
+
+def test_rows_past_one_dimension_of_a_launch_by_value():
+    """Every row its own: none skipped, none taken for another, at the start, around the launch's dimensions, the end."""
+    rows, cols = (1 << 24) + 37, 3
+    place = torch.arange(rows, device="cuda")
+    x = torch.stack([((place * k) % 251).half() / 64 for k in (1, 5, 7)], -1)
+    dy = torch.stack([((place * k) % 241).half() / 64 for k in (11, 13, 3)], -1)
+    d = ops.Dropout(0.5, SEED, SITE)
+    parts = [(0, 200), ((1 << 20) - 100, 200), ((1 << 24) - 100, 137)]
+
+    def filled():
+        return torch.full_like(x, float("nan"))
+
+    y, stats = ops.softmax(x, drop=d, out=filled())
+    dx = ops.softmax_backward(dy, x, stats, drop=d, out=filled())
+    ny, _, nstats = ops.layer_norm(x, out=filled())
+    ndx, _, dw, db = ops.layer_norm_backward(dy, x, nstats, wtype=torch.float32, out=filled())
+    drop = ops.dropout(x, d, out=filled())
+    for t in (y, stats, dx, ny, nstats, ndx, drop):
+        assert torch.isfinite(t).all()
+    for at, n in parts:
+        f = np.where(nodes.draws(n, cols, SEED, SITE, row0=at) < d.keep, 65536.0 / d.keep, 0.0)
+        hx, hg = host(x[at:at + n]), host(dy[at:at + n])
+        p, m, z = nodes.softmax(hx)
+        rel = 4 * U * np.abs(hx - m[:, None]) + 32 * U
+        check(y[at:at + n], p * f, p * f * 3 * rel, torch.float16, "y")
+        check(stats[at:at + n, 0], m, 0.0, torch.float32, "max")
+        g = nodes.dropout(hg, f)
+        tol = p * (np.abs(g) + np.abs(p * g).sum(1, keepdims=True)) * 8 * rel
+        check(dx[at:at + n], nodes.softmax_backward(g, p, 1.0), tol, torch.float16, "dx")
+        check(drop[at:at + n], nodes.dropout(hx, f), 0.0, torch.float16, "dropout")
+        want, mean, rstd = nodes.layer_norm(hx, 1.0, 0.0, 1e-5)
+        _, d_rstd, d_y = norm_bounds(hx, np.ones(cols), 1e-5)
+        check(ny[at:at + n], want, d_y, torch.float16, "norm")
+        check(nstats[at:at + n, 1], rstd, d_rstd * rstd, torch.float32, "rstd")
+        hs = host(nstats[at:at + n])
+        want, _, _ = nodes.layer_norm_backward(hg, hx, hs[:, 0], hs[:, 1], 1.0)
+        xh = np.abs(hx - hs[:, :1]) * hs[:, 1:]
+        tol = hs[:, 1:] * (DEPTH + 16) * U * (np.abs(hg) + np.abs(hg).mean(1, keepdims=True)
+                                              + xh * (np.abs(hg) * xh).mean(1, keepdims=True))
+        check(ndx[at:at + n], want, tol, torch.float16, "norm dx")
+    # a thread sums 1025 rows, one after another
+    g, xh = dy.double(), (x.double() - nstats[:, :1].double()) * nstats[:, 1:].double()
+    depth = (1025 + DEPTH) * U
+    check(dw, host((g * xh).sum(0)), depth * host((g * xh).abs().sum(0)), torch.float32, "dweight")
+    check(db, host(g.sum(0)), depth * host(g.abs().sum(0)), torch.float32, "dbias")
+
+
+# ---------------------------------------------------------------------------
+# outputs in place of inputs, the caller's work buffers
+# ---------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols", [(70, 40), (300, 1000), (9, 4096), (5, 12345), (300, 16400), (4, 30001)])
+def test_layer_norm_in_place_of_its_inputs(dtype, rows, cols):
+    x, r, dy = (randn((rows, cols), dtype, k, offset=1, pad=2) for k in (61, 62, 63))
+    w, b = randn((cols,), dtype, 64, shift=1.0), randn((cols,), dtype, 65)
+    d = ops.Dropout(0.25, SEED, SITE)
+    y, h, stats = ops.layer_norm(x, w, b, residual=r, drop=d)
+    for which in (0, 1):
+        a = [x.clone(), r.clone()]
+        got = ops.layer_norm(a[0], w, b, residual=a[1], drop=d, out=a[which])
+        assert got[0] is a[which] and all(torch.equal(p, q) for p, q in zip(got, (y, h, stats)))
+    a = x.clone()
+    got = ops.layer_norm(a, w, b, out=a)
+    want = ops.layer_norm(x, w, b)
+    assert got[0] is a and torch.equal(a, want[0]) and torch.equal(got[2], want[2])
+    want = ops.layer_norm_backward(dy, h, stats, w, dres=r, drop=d)
+    for which in (0, 1, 2):
+        a = [dy.clone(), h.clone(), r.clone()]
+        got = ops.layer_norm_backward(a[0], a[1], stats, w, dres=a[2], drop=d, out=a[which])
+        assert got[1] is a[which] and all(torch.equal(p, q) for p, q in zip(got, want))
+    a = r.clone()
+    assert ops.dropout(x, d, residual=a, out=a) is a and torch.equal(a, h)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("keys", [13, 300, 2048, 20001, 40001])
+@pytest.mark.parametrize("kind", ["none", "bool", "add"])
+def test_softmax_gradient_in_place_of_the_scores(dtype, keys, kind):
+    shape = (1, 2, 5, keys)
+    x, dy = randn(shape, dtype, 66, gain=3.0, offset=1, pad=2), randn(shape, dtype, 67)
+    mask, _ = masks(kind, shape, dtype, 68)
+    d = ops.Dropout(0.25, SEED, SITE)
+    kw = dict(scale=0.5, causal=True, mask=mask, drop=d)
+    _, stats = ops.softmax(x, **kw)
+    want = ops.softmax_backward(dy, x, stats, **kw)
+    a = x.clone()
+    assert ops.softmax_backward(dy, a, stats, out=a, **kw) is a and torch.equal(a, want)
+
+
+def test_work_buffers_of_the_caller():
+    """The bits of the calls that make their own, whatever the buffer held; one that is too small is refused."""
+    d = ops.Dropout(0.25, SEED, SITE)
+
+    def buffers(need):
+        assert need > 0
+        return [torch.full((n,), 255, dtype=torch.uint8, device="cuda") for n in (need, need + 4096)]
+
+    for rows, cols in ((300, 1000), (5000, 40), (9, 20000)):
+        h, dy = randn((rows, cols), "f16", 71), randn((rows, cols), "f16", 72)
+        _, _, stats = ops.layer_norm(h)
+        want = ops.layer_norm_backward(dy, h, stats, drop=d)
+        need = ops.layer_norm_workspace(rows, cols)
+        for work in buffers(need):
+            got = ops.layer_norm_backward(dy, h, stats, drop=d, work=work)
+            assert all(torch.equal(p, q) for p, q in zip(got, want))
+        with pytest.raises(ckm.CkmError):
+            ops.layer_norm_backward(dy, h, stats, drop=d, work=work[:need - 1])
+    shape = (1, 2, 3, 40001)
+    x, dy = randn(shape, "bf16", 73), randn(shape, "bf16", 74)
+    want, stats = ops.softmax(x, drop=d)
+    dx = ops.softmax_backward(dy, x, stats, drop=d)
+    need = ops.softmax_workspace(*shape)
+    for work in buffers(need):
+        got = ops.softmax(x, drop=d, work=work)
+        assert torch.equal(got[0], want) and torch.equal(got[1], stats)
+        work.fill_(255)
+        assert torch.equal(ops.softmax_backward(dy, x, stats, drop=d, work=work), dx)
+    for call in (lambda w: ops.softmax(x, work=w), lambda w: ops.softmax_backward(dy, x, stats, work=w)):
+        with pytest.raises(ckm.CkmError):
+            call(work[:need - 1])
+    work = torch.zeros(16, dtype=torch.uint8, device="cuda")   # not needed: any will do
+    assert torch.equal(ops.softmax(x[..., :100], work=work)[0], ops.softmax(x[..., :100])[0])
+
+
 def test_a_mask_of_one_key_is_refused_by_its_name():
     x = torch.zeros((2, 3, 5, 8), device="cuda")
     for shape in ((), (1,), (5, 1), (2, 1, 1, 1)):
