@@ -12,7 +12,7 @@
 // Logits, statistics and sums are in binary32. exp(v), v = t - m <= 0, is 2^(v log2 e).
 // Its relative error beside the unit's last place, with u = 2^-24: in binary32 u,
 // since what the product's rounding loses is made good (four more operations a score:
-// f32 16x1024x1024 27 us with and without, single queries on 32768 keys 9.6 -> 10.1); in
+// f32 16x1024x1024 27 us with and without, 128 single queries on 32768 keys 11.1 -> 12); in
 // the 16-bit types, whose own rounding is far coarser, 1.3 u |v| where logits are formed
 // (the factor and the product) and 3.3 u |v| where they are not (scale log2 e, the
 // difference of the scores, the product).
@@ -246,8 +246,9 @@ __global__ void __launch_bounds__(softmax_block(kLanes)) ckm_softmax_kernel(Soft
     float most = m;   // a score, with kNoMask
     if constexpr (kMask == kNoMask) {
       m *= a.scale;
-      // a logit past the range is an infinite one, as where logits are formed
-      if constexpr (sizeof(T) == 2)
+      // a logit past the range (binary16 scores have none) is an infinite one, as where
+      // logits are formed
+      if constexpr (std::is_same<T, __bf16>::value)
         most = m == __builtin_inff() ? __builtin_nanf("") : m == -__builtin_inff() ? __builtin_inff() : most;
       m = fmaxf(m, kLowest);
     }
