@@ -75,6 +75,9 @@ class Dropout:
         if d_site is not None:
             self.d_site = d_site
 
+    def __reduce__(self):   # a copy has values of its own
+        return Dropout, (self.p, self.seed, self.site, self.d_site)
+
     @property
     def p(self) -> float:
         return self._p

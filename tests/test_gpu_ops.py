@@ -913,3 +913,29 @@ def test_a_mask_of_one_key_is_refused_by_its_name():
         assert torch.all(ops.softmax(x, mask=torch.ones(shape, dtype=torch.bool, device="cuda"))[0] == 0.125)
     one = x[..., :1]   # one key: any mask has it
     assert torch.all(ops.softmax(one, mask=torch.ones((5, 1), dtype=torch.bool, device="cuda"))[0] == 1)
+
+
+def test_calls_on_another_stream_in_a_capture():
+    """A captured call on another stream joins the capture; the caller joins back. Replays give the eager bits."""
+    x, s = randn((300, 1000), "f16", 91), randn((1, 4, 60, 700), "f16", 92)
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    d = ops.Dropout(0.1, SEED, SITE, step)
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        all_ops(x, s, d)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = all_ops(x, s, d, stream=other)
+        torch.cuda.current_stream().wait_stream(other)
+    for n in range(3):
+        step.fill_(n)
+        for t in got:
+            t.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        want = all_ops(x, s, ops.Dropout(0.1, SEED, SITE + n))
+        assert all(torch.equal(p, q) for p, q in zip(got, want)), n

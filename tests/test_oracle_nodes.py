@@ -293,3 +293,13 @@ def test_wide_rows_of_one_block_are_few():
         assert ops.layer_norm_workspace(2, cols) == 0
         assert ops.layer_norm_workspace(3, cols) >= 3 * 2 * cols * 4 and ops.layer_norm_workspace(4, cols) >= 4 * 2 * cols * 4
     assert ops.layer_norm_workspace(4, 8192) == 0
+
+
+def test_a_copied_dropout_is_its_own():
+    import copy
+    import pickle
+    d = ops.Dropout(0.25, 3, 4)
+    for other in (copy.copy(d), copy.deepcopy(d), pickle.loads(pickle.dumps(d))):
+        assert (other.p, other.seed, other.site, other.d_site, other.keep) == (0.25, 3, 4, None, d.keep)
+        other.site = 9
+        assert d.site == 4 and other.site == 9
