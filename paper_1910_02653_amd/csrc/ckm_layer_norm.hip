@@ -22,7 +22,7 @@
 // Bound by memory on large inputs: the fused forward pass of bf16 8192x8192 moves
 // 537 MB in 100 us (5.4 TB/s, where a large copy moves 5.2), the fused gradient of
 // bf16 16384x4096 671 MB in 133 us. Small ones are bound by the launch and one
-// row's chain of load, two sums and store: f16 2048x2048 6.6 us forward, 14.6 us
+// row's chain of load, two sums and store: f16 2048x2048 6.6 us forward, 14.5 us
 // gradient (10.8 and 4 for joining the blocks' sums).
 #include <hip/hip_runtime.h>
 
@@ -497,8 +497,8 @@ void launch_norm(const NormArgs& a, bool fused, hipStream_t s) {
 // sums, so it depends on the sizes alone. 256 blocks of 1024 threads: blocks of 512,
 // twice as many, write twice the sums (f16 2048x2048 17.4 us, 13.7 so; bf16 16384x4096
 // 140 and 132). One group a thread up to 8192 columns, over as many threads as a row
-// needs: two groups on half the threads leave no registers (f16 16384x1024 48 us, 42
-// so), and two rows at a time neither (bf16 16384x4096 159 us, 130 so). Rows that four
+// needs: two groups on half the threads leave no registers (f16 16384x1024 fused 48
+// us, 43 so), and two rows at a time neither (bf16 16384x4096 159 us, 130 so). Rows that four
 // blocks take in one turn (two, with two groups a thread) are one block's, in as many
 // turns, which has no sums to join: a call on f16 256x128 10.6 us, 15.2 in four blocks;
 // 64x512 10.7, 15.3; 16x2048 10.7, 15.3; 4x8192 12.4, 15.9 (f32 14.7, 15.3); 2x16384 17.9,

@@ -21,7 +21,8 @@ any third stream is the caller's to order, as are later uses of the arguments
 on other streams. Results that a call allocates belong to its stream. (To order
 everything oneself, make the stream the current one and leave `stream` out.)
 
-No autograd graph is recorded: gradients are the *_backward calls.
+No call records an autograd graph, whatever its tensors require: results that it
+allocates require no gradient, and gradients are the *_backward calls.
 """
 from __future__ import annotations
 
@@ -235,7 +236,8 @@ def _first(t, name: str):
 
 
 def dropout(x, drop: Dropout, residual=None, out=None, stream=None):
-    """y = residual + D(x), rows by the last dimension (ckm_dropout_async). out may be x or residual."""
+    """y = residual + D(x), rows by the last dimension (ckm_dropout_async). out may be x or residual.
+    Outside autograd: the gradient is dropout_backward."""
     if stream is not None:
         with _on(stream, drop, x, residual, out):
             return dropout(x, drop, residual, out)
@@ -267,7 +269,8 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, residual=None, drop
     weight, bias: vectors of x's type or float32, both of one type. stats:
     float32 [..., 2], mean and 1 / standard deviation of each row of h.
     out: for y; may be x or residual. With y in the place of an x that would be
-    h, h is None: keep x for layer_norm_backward."""
+    h, h is None: keep x for layer_norm_backward, which is the gradient (the
+    call is outside autograd)."""
     if stream is not None:
         with _on(stream, drop, x, weight, bias, residual, out):
             return layer_norm(x, weight, bias, eps, residual, drop, out)
@@ -424,9 +427,9 @@ def softmax(scores, scale: float = 1.0, causal: bool = False, lengths=None, mask
     after the scale; -inf hides), with every key in its last dimension and
     broadcast over queries, heads and batches. A row that sees nothing gives
     zeros. stats: float32 [..., queries, 2], the largest logit and 1 / the sum
-    of exponentials. out: for the probabilities; may be scores (which the
-    gradient needs). work: a uint8 device buffer of softmax_workspace(...)
-    bytes to use."""
+    of exponentials. out: for the probabilities; may be scores (which
+    softmax_backward, the gradient, needs: the call is outside autograd). work:
+    a uint8 device buffer of softmax_workspace(...) bytes to use."""
     if stream is not None:
         with _on(stream, drop, scores, lengths, mask, out, work):
             return softmax(scores, scale, causal, lengths, mask, drop, out, work)
