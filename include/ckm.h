@@ -468,6 +468,97 @@ ckm_status ckm_softmax_backward_async(ckm_dtype type, const ckm_scores* scores, 
                                       const float* d_stats, const ckm_drop* drop, void* d_dx,
                                       const int64_t* dx_stride, void* d_work, size_t work_bytes, void* stream);
 
+/* ---- matrix operators of a training step -------------------------------
+ * The feed-forward block and the loss of a transformer, whose large values
+ * never exist in memory, and the step's end. Pointers, streams, work buffers,
+ * alignment and strides as above, except that no output may overlap an input
+ * (ckm_clip_async: but its own). Operands of rows that do not start on 16 bytes,
+ * or do not end on them, are first copied into the work buffer; the sizes of work
+ * buffers go by the struct's pointers and strides too. Products are summed in
+ * binary32, in an order that the sizes fix. */
+#define CKM_MAX_MATRIX_ROWS (1 << 30) /* rows of x */
+#define CKM_MAX_MATRIX_COLS (1 << 20) /* hidden and inner width */
+#define CKM_MAX_VOCAB (1 << 30)       /* rows of a vocabulary's table */
+#define CKM_MAX_TENSORS (1 << 20)     /* of a norm */
+
+/* act(z): z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2; max(z, 0), whose
+ * derivative at 0 is 0. */
+enum { CKM_ACT_SILU = 0, CKM_ACT_GELU = 1, CKM_ACT_RELU = 2 };
+
+/* h = act(x Wg) (x Wu), elementwise: x [rows][hidden], Wg and Wu (gate and up)
+ * [hidden][inner] with row strides ld_*. rows may be 0. */
+typedef struct ckm_gated {
+  int64_t rows, hidden, inner;
+  int32_t act;
+  const void* d_x;
+  int64_t ld_x;
+  const void* d_gate;
+  int64_t ld_gate;
+  const void* d_up;
+  int64_t ld_up;
+} ckm_gated;
+
+/* work: ckm_gated_workspace_size bytes of the same struct (backward: 0 or 1),
+ * aligned to 16. */
+ckm_status ckm_gated_workspace_size(ckm_dtype type, const ckm_gated* gated, int32_t backward, size_t* bytes);
+ckm_status ckm_gated_async(ckm_dtype type, const ckm_gated* gated, void* d_h, int64_t ld_h, void* d_work,
+                           size_t work_bytes, void* stream);
+
+/* Its gradient from dh: with g = x Wg, u = x Wu (computed again), dg = dh u
+ * act'(g) and du = dh act(g), both rounded to `type`: dx = dg Wg' + du Wu', dWg =
+ * x' dg, dWu = x' du. dx may be NULL, and dWg and dWu together. rows = 0 gives
+ * zero weight gradients. */
+ckm_status ckm_gated_backward_async(ckm_dtype type, const ckm_gated* gated, const void* d_dh, int64_t ld_dh,
+                                    void* d_dx, int64_t ld_dx, void* d_dgate, int64_t ld_dgate, void* d_dup,
+                                    int64_t ld_dup, void* d_work, size_t work_bytes, void* stream);
+
+/* Cross entropy of hidden states x [rows][hidden] against a vocabulary's table
+ * W [vocab][hidden]: logits l = x W' (binary32, never stored), lse = log of the
+ * sum over the vocabulary of exp(l), loss = lse - l[target]. A row whose target
+ * lies outside [0, vocab) has loss 0 and no part in a gradient, whatever it
+ * holds. A logit of +inf or NaN makes its row's lse NaN. */
+typedef struct ckm_vocab {
+  int64_t rows, hidden, vocab;
+  const void* d_x;
+  int64_t ld_x;
+  const void* d_weight;
+  int64_t ld_weight;
+  const int64_t* d_targets;   /* [rows] */
+} ckm_vocab;
+
+/* loss, lse: float [rows], either may be NULL. work as for ckm_gated_async. */
+ckm_status ckm_cross_entropy_workspace_size(ckm_dtype type, const ckm_vocab* vocab, int32_t backward, size_t* bytes);
+ckm_status ckm_cross_entropy_async(ckm_dtype type, const ckm_vocab* vocab, float* d_loss, float* d_lse, void* d_work,
+                                   size_t work_bytes, void* stream);
+
+/* Its gradient from dloss [rows] and the forward call's lse: d = (exp(l - lse) -
+ * 1[v = target]) dloss, rounded to `type`, dx = d W, dW = d' x. In binary16, d is
+ * held relative to the largest |dloss|: rows whose dloss is less than 2^-12 of it
+ * lose digits. dx or dW may be NULL. rows = 0 gives a zero dW. */
+ckm_status ckm_cross_entropy_backward_async(ckm_dtype type, const ckm_vocab* vocab, const float* d_dloss,
+                                            const float* d_lse, void* d_dx, int64_t ld_dx, void* d_dweight,
+                                            int64_t ld_dweight, void* d_work, size_t work_bytes, void* stream);
+
+/* One of many tensors: count elements of type `type` one after another. */
+typedef struct ckm_tensor {
+  const void* d_in;
+  void* d_out;    /* ckm_clip_async: may be d_in */
+  int64_t count;
+  int64_t type;   /* ckm_dtype */
+} ckm_tensor;
+
+/* norm = the square root of the sum over all elements of all tensors of their
+ * squares (binary64, rounded once); 0 for none. ckm_clip_async also writes every
+ * element times min(1, max_norm / (norm + eps)) to its tensor's d_out; outputs must
+ * overlap neither each other nor another tensor. A norm of inf gives 0 for finite
+ * elements, a norm of NaN gives NaN. norm: one float. work:
+ * ckm_norm_workspace_size bytes, aligned to 8. */
+ckm_status ckm_norm_workspace_size(int64_t count, size_t* bytes);
+ckm_status ckm_norm_async(int64_t count, const ckm_tensor* tensors, float* d_norm, void* d_work, size_t work_bytes,
+                          void* stream);
+ckm_status ckm_clip_async(int64_t count, const ckm_tensor* tensors, double max_norm, double eps, float* d_norm,
+                          void* d_work, size_t work_bytes, void* stream);
+
 /* Thread-local text describing the calling thread's last non-OK status. */
 const char* ckm_last_error(void);
 

@@ -1,10 +1,13 @@
 """The training-node operators in 64 bits (numpy), from their definitions: test infrastructure only.
 
-Dropout by counter, layer norm and the attention softmax with their gradients,
+Dropout by counter, layer norm, the attention softmax, the gated feed-forward and the
+vocabulary's cross entropy with their gradients, and the norm over many arrays,
 written as the formulas read, one array operation after another. Nothing here
 is rounded to the operators' types.
 """
 from __future__ import annotations
+
+import math
 
 import numpy as np
 
@@ -90,3 +93,49 @@ def softmax(t):
 def softmax_backward(g, p, scale):
     """The scores' gradient from the gradient g that reaches the probabilities p."""
     return scale * p * (g - (p * g).sum(-1, keepdims=True))
+
+
+def activation(z, act):
+    """(act(z), its derivative); act: silu, gelu or relu."""
+    if act == "silu":
+        s = 1.0 / (1.0 + np.exp(-z))
+        return z * s, s * (1.0 + z * (1.0 - s))
+    if act == "gelu":
+        c = 0.5 * (1.0 + np.vectorize(math.erf, otypes=[float])(z / math.sqrt(2.0)))
+        return z * c, c + z * np.exp(-0.5 * z * z) / math.sqrt(2.0 * math.pi)
+    return np.maximum(z, 0.0), (z > 0.0).astype(float)
+
+
+def gated(x, w_gate, w_up, act):
+    """h = act(x w_gate) * (x w_up)"""
+    return activation(x @ w_gate, act)[0] * (x @ w_up)
+
+
+def gated_backward(dh, x, w_gate, w_up, act):
+    """(dx, dw_gate, dw_up)"""
+    a, da = activation(x @ w_gate, act)
+    dg, du = dh * (x @ w_up) * da, dh * a
+    return dg @ w_gate.T + du @ w_up.T, x.T @ dg, x.T @ du
+
+
+def cross_entropy(x, w, targets):
+    """(loss, lse) of each row of x against the table w; a target outside it has loss 0."""
+    t = x @ w.T
+    m = t.max(1)
+    lse = m + np.log(np.exp(t - m[:, None]).sum(1))
+    some = (targets >= 0) & (targets < len(w))
+    return np.where(some, lse - t[np.arange(len(x)), np.where(some, targets, 0)], 0.0), lse
+
+
+def cross_entropy_backward(dloss, x, w, targets, lse):
+    """(dx, dw)"""
+    some = (targets >= 0) & (targets < len(w))
+    d = np.exp(x @ w.T - lse[:, None])
+    d[np.arange(len(x))[some], targets[some]] -= 1.0
+    d = np.where(some[:, None], d * np.where(some, dloss, 0.0)[:, None], 0.0)
+    return d @ w, d.T @ x
+
+
+def norm(arrays):
+    """The 2-norm over all elements of all arrays."""
+    return math.sqrt(math.fsum(math.fsum(float(v) * float(v) for v in a.ravel()) for a in arrays))

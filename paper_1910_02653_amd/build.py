@@ -14,7 +14,9 @@ SOURCES = [os.path.join(HERE, "csrc", "ckm_kernels.hip"), os.path.join(HERE, "cs
            os.path.join(HERE, "csrc", "ckm_noalloc.hip"), os.path.join(HERE, "csrc", "ckm_tiles.hip"),
            os.path.join(HERE, "csrc", "ckm_tiles.cpp"),
            os.path.join(HERE, "csrc", "ckm_dropout.hip"), os.path.join(HERE, "csrc", "ckm_layer_norm.hip"),
-           os.path.join(HERE, "csrc", "ckm_softmax.hip"),
+           os.path.join(HERE, "csrc", "ckm_softmax.hip"), os.path.join(HERE, "csrc", "ckm_matrix.hip"),
+           os.path.join(HERE, "csrc", "ckm_gated.hip"), os.path.join(HERE, "csrc", "ckm_cross_entropy.hip"),
+           os.path.join(HERE, "csrc", "ckm_clip.hip"),
            os.path.join(HERE, "csrc", "ckm_host.cpp")]
 ARCH = "gfx950"
 

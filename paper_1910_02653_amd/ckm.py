@@ -31,7 +31,9 @@ EXPORTS = (
     "ckm_max_batch_async", "ckm_round_eval_noalloc", "ckm_last_error",
     "ckm_dropout_async", "ckm_layer_norm_async", "ckm_layer_norm_workspace_size",
     "ckm_layer_norm_backward_async", "ckm_softmax_workspace_size", "ckm_softmax_async",
-    "ckm_softmax_backward_async",   # bound by ops.py
+    "ckm_softmax_backward_async", "ckm_gated_workspace_size", "ckm_gated_async", "ckm_gated_backward_async",
+    "ckm_cross_entropy_workspace_size", "ckm_cross_entropy_async", "ckm_cross_entropy_backward_async",
+    "ckm_norm_workspace_size", "ckm_norm_async", "ckm_clip_async",   # bound by ops.py
 )
 NOALLOC_SCRATCH_BYTES = 256 << 20
 PLAN_EARLY_FREE = 1
@@ -116,6 +118,24 @@ def lib():
         L.ckm_softmax_async.restype = C.c_int
         L.ckm_softmax_backward_async.argtypes = [t, p, p, p, p, p, p, p, p, p, p, sz, p]
         L.ckm_softmax_backward_async.restype = C.c_int
+        L.ckm_gated_workspace_size.argtypes = [t, p, i32, p]
+        L.ckm_gated_workspace_size.restype = C.c_int
+        L.ckm_gated_async.argtypes = [t, p, p, i64, p, sz, p]
+        L.ckm_gated_async.restype = C.c_int
+        L.ckm_gated_backward_async.argtypes = [t, p, p, i64, p, i64, p, i64, p, i64, p, sz, p]
+        L.ckm_gated_backward_async.restype = C.c_int
+        L.ckm_cross_entropy_workspace_size.argtypes = [t, p, i32, p]
+        L.ckm_cross_entropy_workspace_size.restype = C.c_int
+        L.ckm_cross_entropy_async.argtypes = [t, p, p, p, p, sz, p]
+        L.ckm_cross_entropy_async.restype = C.c_int
+        L.ckm_cross_entropy_backward_async.argtypes = [t, p, p, p, p, i64, p, i64, p, sz, p]
+        L.ckm_cross_entropy_backward_async.restype = C.c_int
+        L.ckm_norm_workspace_size.argtypes = [i64, p]
+        L.ckm_norm_workspace_size.restype = C.c_int
+        L.ckm_norm_async.argtypes = [i64, p, p, p, sz, p]
+        L.ckm_norm_async.restype = C.c_int
+        L.ckm_clip_async.argtypes = [i64, p, C.c_double, C.c_double, p, p, sz, p]
+        L.ckm_clip_async.restype = C.c_int
         L.ckm_last_error.argtypes = []
         L.ckm_last_error.restype = C.c_char_p
         _lib = L

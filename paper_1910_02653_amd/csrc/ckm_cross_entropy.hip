@@ -1,0 +1,395 @@
+// Softmax cross entropy of hidden states against a vocabulary's table, without the
+// logits, and its gradient.
+//
+//   forward   l = x W', lse = log sum over v of exp l, loss = lse - l_target
+//   gradient  d = (exp(l - lse) - 1[v = target]) dloss, dx = d W, dW = d' x
+//
+// Forward: a tile of the logits stays in registers; of each of its rows remain the
+// largest logit and the sum of exponentials, which a second launch joins over the
+// tiles in their order. Gradient: the vocabulary in pieces; a piece's logits are
+// computed again, d is written for that piece alone, in the tensors' type, and the two
+// products after it read it from the caches; dx is summed over pieces in binary32.
+//
+// binary16 has too few exponents for d: exp(l - lse) is about 1 / vocab and dloss 1 /
+// rows. It holds d 2^15 / s, s the largest |dloss|, of at most 32768, and the
+// products' results are multiplied by s / 2^15.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "ckm_matrix.h"
+
+namespace ckm {
+namespace {
+
+constexpr float kLog2e = 1.44269504f;
+constexpr float kLog2eRest = 1.92596299e-8f;   // log2(e) = the sum of both
+constexpr float kHalfGain = 32768.0f;          // binary16's factor
+
+struct LossArgs {
+  ProductArgs p;            // n: of the vocabulary, or of a piece of it
+  int32_t tiles_m, tiles_n;
+  const int64_t* targets;
+  float2* parts;            // [rows][tiles_n]: largest logit, sum of exponentials
+  float* hit;               // [rows]: the target's logit
+  float* loss;
+  float* lse;               // written, or the gradient's input
+  const float* dloss;
+  const float* most;        // binary16: the largest |dloss|
+  void* d;                  // [rows][ld_d]
+  int64_t ld_d, first;      // first: the piece's first column
+  int64_t vocab;
+};
+
+// e^v for v <= 0 or so, to a few units in the last place: 2^(v log2 e) with what the product loses.
+__device__ __forceinline__ float exp_of(float v) {
+  const float t = v * kLog2e;
+  const float rest = fmaf(v, kLog2eRest, fmaf(v, kLog2e, -t));
+  const float e = __builtin_amdgcn_exp2f(t);
+  return t > -126.0f && t < 126.0f ? fmaf(e, rest * 0.69314718f, e) : e;
+}
+
+template <class P>
+__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_kernel(LossArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+  const P p;
+  int tm, tn;
+  tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
+  F4 acc[P::kFN][P::kFM];
+  p.run(acc, a.p, tm * P::kM, tn * P::kN, 0, (a.p.k + P::kStep - 1) / P::kStep, (LdsChar*)lds);
+  float2* joined = (float2*)lds;   // [waves of n][rows of the tile]
+#pragma unroll
+  for (int i = 0; i < P::kFM; ++i) {
+    const int m = tm * P::kM + p.row(i);
+    const int64_t target = m < a.p.m ? a.targets[m] : -1;
+    float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < P::kFN; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int n = tn * P::kN + p.col(j) + k;
+        if (n < a.p.n) {
+          most = fmaxf(most, acc[j][i][k]);
+          if (n == target) a.hit[m] = acc[j][i][k];
+        }
+      }
+    // the four lanes that hold a row
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const float base = most == -INFINITY ? 0.0f : most;
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < P::kFN; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (tn * P::kN + p.col(j) + k < a.p.n) sum += exp_of(acc[j][i][k] - base);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (p.lane < 16) joined[p.wn * P::kM + p.row(i)] = make_float2(most, sum);
+  }
+  __syncthreads();
+  for (int r = threadIdx.x; r < P::kM; r += P::kThreads) {
+    const int m = tm * P::kM + r;
+    if (m >= a.p.m) continue;
+    float most = joined[r].x;
+#pragma unroll
+    for (int w = 1; w < P::kWavesN; ++w) most = fmaxf(most, joined[w * P::kM + r].x);
+    const float base = most == -INFINITY ? 0.0f : most;
+    float sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < P::kWavesN; ++w)
+      sum += joined[w * P::kM + r].y * (joined[w * P::kM + r].x == -INFINITY ? 1.0f : exp_of(joined[w * P::kM + r].x - base));
+    a.parts[(int64_t)m * a.tiles_n + tn] = make_float2(most, sum);
+  }
+}
+
+// A wave a row: the tiles' parts in their order (each lane every 64th, then the lanes).
+__global__ void __launch_bounds__(256) ckm_loss_join_kernel(LossArgs a) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  if (row >= a.p.m) return;
+  const float2* parts = a.parts + row * a.tiles_n;
+  float most = -INFINITY;
+  for (int k = lane; k < a.tiles_n; k += 64) most = fmaxf(most, parts[k].x);
+  most = reduce64<OpMax>(most);
+  const float base = most == -INFINITY ? 0.0f : most;
+  float sum = 0.0f;
+  for (int k = lane; k < a.tiles_n; k += 64) {
+    const float2 v = parts[k];
+    sum += v.y * (v.x == -INFINITY ? 1.0f : exp_of(v.x - base));
+  }
+  sum = reduce64<OpSum>(sum);
+  if (lane == 0) {
+    const float lse = base + logf(sum);
+    const int64_t target = a.targets[row];
+    if (a.lse) a.lse[row] = lse;
+    if (a.loss) a.loss[row] = target >= 0 && target < a.vocab ? lse - a.hit[row] : 0.0f;
+  }
+}
+
+// The largest finite |dloss| of rows that have a target; 1 if that is 0.
+__global__ void __launch_bounds__(1024) ckm_loss_most_kernel(LossArgs a, float* out) {
+  __shared__ float lds[2 * 16];
+  float most = 0.0f;
+  for (int64_t r = threadIdx.x; r < a.p.m; r += 1024) {
+    const float v = fabsf(a.dloss[r]);
+    if (a.targets[r] >= 0 && a.targets[r] < a.vocab && v < INFINITY) most = fmaxf(most, v);
+  }
+  most = reduce_row<OpMax, 1024, 1024>(most, lds, 0);
+  if (threadIdx.x == 0) *out = most > 0.0f ? most : 1.0f;
+}
+
+template <class P>
+__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_back_kernel(LossArgs a) {
+  using T = typename P::T;
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+  const P p;
+  int tm, tn;
+  tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
+  F4 acc[P::kFN][P::kFM];
+  p.run(acc, a.p, tm * P::kM, tn * P::kN, 0, (a.p.k + P::kStep - 1) / P::kStep, (LdsChar*)lds);
+  const int width = (int)whole(a.p.n, 16 / sizeof(T));   // zeros to the end of a group
+#pragma unroll
+  for (int i = 0; i < P::kFM; ++i) {
+    const int m = tm * P::kM + p.row(i);
+    if (m >= a.p.m) continue;
+    int64_t target = a.targets[m];
+    const bool some = target >= 0 && target < a.vocab;
+    target -= a.first;
+    const float lse = a.lse[m];
+    float by = a.dloss[m];
+    if constexpr (std::is_same<T, _Float16>::value) by = by / *a.most * kHalfGain;
+#pragma unroll
+    for (int j = 0; j < P::kFN; ++j) {
+      const int n = tn * P::kN + p.col(j);
+      F4 v;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float e = exp_of(acc[j][i][k] - lse);
+        v[k] = some && n + k < a.p.n ? (n + k == target ? e - 1.0f : e) * by : 0.0f;
+      }
+      store4((T*)a.d + (int64_t)m * a.ld_d, n, width, v);
+    }
+  }
+}
+
+template <typename T, bool kBack>
+void launch_logits(LossArgs a, const Cut& cut, hipStream_t s) {
+  a.tiles_m = cut.tiles_m;
+  a.tiles_n = cut.tiles_n;
+  const auto go = [&](auto p) {
+    using P = typename decltype(p)::Shape;
+    const uint32_t blocks = (uint32_t)(cut.tiles_m * cut.tiles_n);
+    if constexpr (kBack) ckm_loss_back_kernel<P><<<blocks, P::kThreads, 0, s>>>(a);
+    else ckm_loss_kernel<P><<<blocks, P::kThreads, 0, s>>>(a);
+  };
+  if (cut.rows == 256) go(Tag<Product<T, 256, 256, 2, 4, 2, true, true, 1>>());
+  else go(Tag<Product<T, 128, 128, 2, 2, 2, true, true, 1>>());
+}
+
+// Bytes of a piece's d: what stays in the caches between its writer and its readers;
+// never less than 8192 columns, so that dx, summed over pieces in memory, is read and
+// written seldom.
+constexpr int64_t kPieceBytes = (int64_t)128 << 20, kLeastPiece = 8192;
+
+struct LossPlan {
+  bool pack_x, pack_w;
+  int64_t ld_x, ld_w;
+  int64_t piece;             // columns
+  Cut logits, dx, dw, last;  // last: logits of the last piece
+  size_t x, w, parts, hit, most, d, slab, dw_slab, total;
+};
+
+LossPlan plan_of(int type, const ckm_vocab& c, bool back) {
+  const size_t elt = dtype_bytes(type);
+  const int64_t group = 16 / elt, step = kStepBytes / elt;
+  LossPlan p = {};
+  // the gradient takes a copy whose rows without a target are zeros: in d' x they are
+  // multiplied by d's zeros, and may hold anything
+  p.pack_x = back || !loadable(c.d_x, c.rows, c.hidden, c.ld_x, elt, true);
+  p.pack_w = !loadable(c.d_weight, c.vocab, c.hidden, c.ld_weight, elt, true);
+  p.ld_x = p.pack_x || c.rows == 1 ? whole(c.hidden, group) : c.ld_x;
+  p.ld_w = p.pack_w || c.vocab == 1 ? whole(c.hidden, group) : c.ld_weight;
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at = whole(at + bytes, 256);
+    return here;
+  };
+  if (p.pack_x) p.x = take(c.rows * p.ld_x * elt);
+  if (p.pack_w) p.w = take(c.vocab * p.ld_w * elt);
+  if (!back) {
+    p.logits = cut_product(c.rows, c.vocab, 1, 1, 0);
+    p.parts = take((size_t)c.rows * p.logits.tiles_n * sizeof(float2));
+    p.hit = take(c.rows * sizeof(float));
+  } else {
+    p.piece = std::min(c.vocab, std::max(kLeastPiece, kPieceBytes / (int64_t)(c.rows * elt) / 256 * 256));
+    p.logits = cut_product(c.rows, p.piece, 1, 1, 0);
+    const int64_t tail = c.vocab - (c.vocab - 1) / p.piece * p.piece;
+    p.last = cut_product(c.rows, tail, 1, 1, 0);
+    p.dx = cut_product(c.rows, c.hidden, 1, (p.piece + step - 1) / step, 0);
+    p.dw = cut_product(p.piece, c.hidden, 1, (c.rows + step - 1) / step, 0);
+    p.most = take(sizeof(float));
+    p.d = take((size_t)c.rows * whole(p.piece, 64) * elt);
+    if (p.dx.splits > 1 || p.piece < c.vocab) p.slab = take((size_t)p.dx.splits * c.rows * whole(c.hidden, 4) * 4);
+    if (p.dw.splits > 1) p.dw_slab = take((size_t)p.dw.splits * p.piece * whole(c.hidden, 4) * 4);
+  }
+  p.total = at;
+  return p;
+}
+
+template <typename T>
+void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, const float* dloss, float* loss,
+                 float* lse, void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, char* work, hipStream_t s) {
+  const T *x = (const T*)c.d_x, *w = (const T*)c.d_weight;
+  if (plan.pack_x) {
+    launch_pack(type, x, c.rows, c.hidden, c.ld_x, work + plan.x, plan.ld_x, s, back ? c.d_targets : nullptr,
+                c.vocab);
+    x = (const T*)(work + plan.x);
+  }
+  if (plan.pack_w) {
+    launch_pack(type, w, c.vocab, c.hidden, c.ld_weight, work + plan.w, plan.ld_w, s);
+    w = (const T*)(work + plan.w);
+  }
+  LossArgs a = {};
+  a.p = {{{x, x}, plan.ld_x}, {{w, w}, plan.ld_w}, (int32_t)c.rows, (int32_t)c.vocab, (int32_t)c.hidden, 1};
+  a.targets = c.d_targets;
+  a.vocab = c.vocab;
+  a.lse = lse;
+  if (!back) {
+    a.parts = (float2*)(work + plan.parts);
+    a.hit = (float*)(work + plan.hit);
+    a.loss = loss;
+    launch_logits<T, false>(a, plan.logits, s);
+    a.tiles_n = plan.logits.tiles_n;
+    ckm_loss_join_kernel<<<(uint32_t)((c.rows + 3) / 4), 256, 0, s>>>(a);
+    return;
+  }
+  a.dloss = dloss;
+  constexpr bool kHalf = std::is_same<T, _Float16>::value;
+  float* most = (float*)(work + plan.most);
+  if (kHalf) {
+    ckm_loss_most_kernel<<<1, 1024, 0, s>>>(a, most);
+    a.most = most;
+  }
+  a.d = work + plan.d;
+  a.ld_d = whole(plan.piece, 64);
+  ResultArgs rx = {}, rw = {};
+  rx.alpha = rw.alpha = a.most;
+  rx.factor = rw.factor = kHalf ? 1.0f / kHalfGain : 1.0f;
+  const bool slab = plan.dx.splits > 1 || plan.piece < c.vocab;
+  if (slab) rx.slab = (float*)(work + plan.slab);
+  rx.ld_slab = rw.ld_slab = whole(c.hidden, 4);
+  rx.c[0] = dx;
+  rx.ld_c[0] = ld_dx;
+  rx.halves = rw.halves = 1;
+  if (plan.dw.splits > 1) rw.slab = (float*)(work + plan.dw_slab);
+  rw.ld_c[0] = ld_dw;
+  for (int64_t v = 0; v < c.vocab; v += plan.piece) {
+    const int32_t width = (int32_t)std::min(plan.piece, c.vocab - v);
+    const bool tail = width < plan.piece;
+    const T* wv = w + v * plan.ld_w;
+    a.first = v;
+    a.p.b.p[0] = a.p.b.p[1] = wv;
+    a.p.n = width;
+    launch_logits<T, true>(a, tail ? plan.last : plan.logits, s);
+    if (dx) {   // d W; a short last piece leaves shares at the end of k with nothing to add
+      rx.p = {{{a.d, a.d}, a.ld_d}, {{wv, wv}, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, width, 1};
+      launch_product<T, true, false>(rx, plan.dx, s);
+      rx.add = true;
+    }
+    if (dw) {   // d' x
+      rw.p = {{{a.d, a.d}, a.ld_d}, {{x, x}, plan.ld_x}, width, (int32_t)c.hidden, (int32_t)c.rows, 1};
+      rw.c[0] = (T*)dw + v * ld_dw;
+      Cut cut = plan.dw;
+      cut.tiles_m = (width + cut.rows - 1) / cut.rows;
+      launch_product<T, false, false>(rw, cut, s);
+      if (cut.splits > 1) launch_join(type, rw, cut.splits, s);
+    }
+  }
+  if (dx && slab) launch_join(type, rx, plan.dx.splits, s);
+}
+
+ckm_status check_vocab(ckm_dtype type, const ckm_vocab* c) {
+  if (!dtype_ok(type)) return set_error(CKM_E_INVALID_ARG, "unknown type %d", (int)type);
+  if (!c) return set_error(CKM_E_INVALID_ARG, "vocab is NULL");
+  if (c->rows < 0 || c->hidden < 1 || c->vocab < 1)
+    return set_error(CKM_E_INVALID_ARG, "%lld rows, hidden width %lld, vocabulary of %lld", (long long)c->rows,
+                     (long long)c->hidden, (long long)c->vocab);
+  if (c->rows > CKM_MAX_MATRIX_ROWS || c->hidden > CKM_MAX_MATRIX_COLS || c->vocab > CKM_MAX_VOCAB)
+    return set_error(CKM_E_UNSUPPORTED, "%lld rows, hidden width %lld, vocabulary of %lld", (long long)c->rows,
+                     (long long)c->hidden, (long long)c->vocab);
+  const size_t elt = dtype_bytes(type);
+  ckm_status st;
+  if ((st = check_matrix(c->d_weight, "weight", c->vocab, c->hidden, c->ld_weight, elt, false)) != CKM_OK) return st;
+  if (!c->rows) return CKM_OK;
+  if ((st = check_matrix(c->d_x, "x", c->rows, c->hidden, c->ld_x, elt, false)) != CKM_OK) return st;
+  return check_matrix(c->d_targets, "targets", 1, c->rows, 0, 8, false);
+}
+
+ckm_status loss(ckm_dtype type, const ckm_vocab* c, bool back, const float* dloss, float* loss_out, float* lse,
+                void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, void* work, size_t work_bytes, void* stream) {
+  ckm_status st = check_vocab(type, c);
+  if (st != CKM_OK) return st;
+  const size_t elt = dtype_bytes(type);
+  const hipStream_t s = (hipStream_t)stream;
+  if (dw && (st = check_matrix(dw, "dweight", c->vocab, c->hidden, ld_dw, elt, true)) != CKM_OK) return st;
+  if (c->rows == 0) {
+    if (!dw) return CKM_OK;
+    launch_zero(type, dw, c->vocab, c->hidden, ld_dw, s);
+    return launched("cross entropy gradient launch");
+  }
+  if (back) {
+    if ((st = check_matrix(dloss, "dloss", 1, c->rows, 0, 4, false)) != CKM_OK) return st;
+    if ((st = check_matrix(lse, "lse", 1, c->rows, 0, 4, false)) != CKM_OK) return st;
+    if (dx && (st = check_matrix(dx, "dx", c->rows, c->hidden, ld_dx, elt, true)) != CKM_OK) return st;
+    if (!dx && !dw) return CKM_OK;
+  } else {
+    if ((uintptr_t)loss_out % 4 || (uintptr_t)lse % 4)
+      return set_error(CKM_E_INVALID_ARG, "loss or lse is not aligned to 4 bytes");
+    if (!loss_out && !lse) return CKM_OK;
+  }
+  const LossPlan plan = plan_of(type, *c, back);
+  if ((st = check_blocks(plan.logits)) != CKM_OK) return st;
+  if (back && ((st = check_blocks(plan.dx)) != CKM_OK || (st = check_blocks(plan.dw)) != CKM_OK)) return st;
+  if (plan.total && (!work || work_bytes < plan.total))
+    return set_error(CKM_E_INVALID_ARG, "work buffer of %zu bytes, %zu needed", work ? work_bytes : (size_t)0,
+                     plan.total);
+  if ((uintptr_t)work % 16) return set_error(CKM_E_INVALID_ARG, "work is not aligned to 16 bytes");
+  const auto go = [&](auto t) {
+    launch_loss<decltype(t)>(type, *c, plan, back, dloss, loss_out, lse, dx, ld_dx, dw, ld_dw, (char*)work, s);
+  };
+  switch (type) {
+    case CKM_F32: go(0.0f); break;
+    case CKM_F16: go((_Float16)0); break;
+    default: go((__bf16)0.0f); break;
+  }
+  return launched(back ? "cross entropy gradient launch" : "cross entropy launch");
+}
+
+}  // namespace
+}  // namespace ckm
+
+extern "C" ckm_status ckm_cross_entropy_workspace_size(ckm_dtype type, const ckm_vocab* vocab, int32_t backward,
+                                                       size_t* bytes) {
+  using namespace ckm;
+  if (!bytes) return set_error(CKM_E_INVALID_ARG, "bytes is NULL");
+  const ckm_status st = check_vocab(type, vocab);
+  if (st != CKM_OK) return st;
+  *bytes = vocab->rows ? plan_of(type, *vocab, backward != 0).total : 0;
+  return CKM_OK;
+}
+
+extern "C" ckm_status ckm_cross_entropy_async(ckm_dtype type, const ckm_vocab* vocab, float* d_loss, float* d_lse,
+                                              void* d_work, size_t work_bytes, void* stream) {
+  return ckm::loss(type, vocab, false, nullptr, d_loss, d_lse, nullptr, 0, nullptr, 0, d_work, work_bytes, stream);
+}
+
+extern "C" ckm_status ckm_cross_entropy_backward_async(ckm_dtype type, const ckm_vocab* vocab, const float* d_dloss,
+                                                       const float* d_lse, void* d_dx, int64_t ld_dx, void* d_dweight,
+                                                       int64_t ld_dweight, void* d_work, size_t work_bytes,
+                                                       void* stream) {
+  return ckm::loss(type, vocab, true, d_dloss, nullptr, const_cast<float*>(d_lse), d_dx, ld_dx, d_dweight, ld_dweight,
+                   d_work, work_bytes, stream);
+}

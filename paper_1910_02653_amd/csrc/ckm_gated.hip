@@ -1,0 +1,358 @@
+// Gated feed-forward: h = act(x Wg) (x Wu), both projections, the activation and the
+// product in one kernel, and its gradient.
+//
+//   forward   g = x Wg, u = x Wu (binary32, in registers), h = act(g) u
+//   gradient  g and u again, dg = dh u act'(g), du = dh act(g), dx = dg Wg' + du Wu',
+//             dWg = x' dg, dWu = x' du
+//
+// A tile of the forward product has as many columns of Wg as of Wu, the same ones,
+// and a wave holds both of an element. The gradient writes dg and du, side by side in
+// a row and rounded to the tensors' type, which the products after it multiply (a
+// rounding more than the formulas': one part in 2^9 of each term in bfloat16,
+// independent of one another); dx is one product over both, dWg and dWu one launch.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+
+#include "ckm_matrix.h"
+
+namespace ckm {
+namespace {
+
+enum { kForward, kBackward, kShares };   // what a kernel makes of g and u
+
+struct GatedArgs {
+  ProductArgs p;
+  int32_t act;
+  int32_t tiles_m, tiles_n, steps;
+  const void* dh;
+  int64_t ld_dh;
+  void* out;         // h, or dg | du
+  int64_t ld_out;    // of dg | du: of one of them
+  float* slab;       // [split][g, u][m][ld_slab]
+  int64_t ld_slab;
+};
+
+// act(z) and its derivative.
+template <typename T>
+__device__ __forceinline__ void activation(int act, float z, float& a, float& da) {
+  if (act == CKM_ACT_SILU) {
+    float s;
+    if constexpr (std::is_same<T, float>::value) {
+      s = 1.0f / (1.0f + expf(-z));
+    } else {   // to some 2^-21: the product's rounding to 16 bits is far above
+      s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
+    }
+    a = z * s;
+    da = s * (1.0f + z * (1.0f - s));
+  } else if (act == CKM_ACT_GELU) {
+    const float c = 0.5f * (1.0f + erff(z * 0.70710678f));
+    a = z * c;
+    da = c + z * (0.39894228f * expf(-0.5f * z * z));
+  } else {
+    a = z > 0.0f ? z : z != z ? z : 0.0f;
+    da = z > 0.0f ? 1.0f : z != z ? z : 0.0f;
+  }
+}
+
+template <typename T>
+__device__ __forceinline__ F4 gated4(int act, F4 g, F4 u) {
+  F4 h;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float a, da;
+    activation<T>(act, g[k], a, da);
+    h[k] = a * u[k];
+  }
+  return h;
+}
+template <typename T>
+__device__ __forceinline__ void gated4_back(int act, F4 dh, F4& g, F4& u) {   // dg, du in their places
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float a, da;
+    activation<T>(act, g[k], a, da);
+    g[k] = dh[k] * u[k] * da;
+    u[k] = dh[k] * a;
+  }
+}
+
+template <class P, int kMode>
+__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(GatedArgs a) {
+  using T = typename P::T;
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+  const P p;
+  const int tiles = a.tiles_m * a.tiles_n, split = blockIdx.x / tiles;
+  int tm, tn;
+  tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n, tm, tn);
+  const int all = (a.p.k + P::kStep - 1) / P::kStep, from = split * a.steps;
+  F4 acc[P::kFN][P::kFM];
+  p.run(acc, a.p, tm * P::kM, tn * P::kSubN, from, min(all, from + a.steps), (LdsChar*)lds);
+#pragma unroll
+  for (int i = 0; i < P::kFM; ++i) {
+    const int m = tm * P::kM + p.row(i);
+    if (m >= a.p.m) continue;
+#pragma unroll
+    for (int j = 0; j < P::kFS; ++j) {
+      const int n = tn * P::kSubN + p.col(j);
+      F4 g = acc[j][i], u = acc[j + P::kFS][i];
+      if constexpr (kMode == kForward) {
+        store4((T*)a.out + (int64_t)m * a.ld_out, n, a.p.n, gated4<T>(a.act, g, u));
+      } else if constexpr (kMode == kBackward) {
+        gated4_back<T>(a.act, read4((const T*)a.dh + (int64_t)m * a.ld_dh, n, a.p.n), g, u);
+        T* row = (T*)a.out + (int64_t)m * 2 * a.ld_out;
+        store4(row, n, (int)a.ld_out, g);
+        store4(row + a.ld_out, n, (int)a.ld_out, u);
+      } else if (n < a.p.n) {
+        float* at = a.slab + ((int64_t)split * 2 * a.p.m + m) * a.ld_slab + n;
+        *(F4*)at = g;
+        *(F4*)(at + a.p.m * a.ld_slab) = u;
+      }
+    }
+  }
+}
+
+// The shares of g and u added in their order, and what kMode makes of them; a thread
+// four columns.
+template <typename T, int kMode>
+__global__ void __launch_bounds__(256) ckm_gated_join_kernel(GatedArgs a, int splits, int64_t total, uint32_t fours) {
+  const int64_t one = (int64_t)a.p.m * a.ld_slab;
+  for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
+    const int64_t m = at / fours;
+    const int n = (int)(at - m * fours) * 4;
+    F4 g = {0.0f, 0.0f, 0.0f, 0.0f}, u = g;
+    if (n < a.p.n) {
+      const float* p = a.slab + m * a.ld_slab + n;
+      g = *(const F4*)p;
+      u = *(const F4*)(p + one);
+      for (int k = 1; k < splits; ++k) {
+        g += *(const F4*)(p + 2 * k * one);
+        u += *(const F4*)(p + (2 * k + 1) * one);
+      }
+    }
+    if constexpr (kMode == kForward) {
+      store4((T*)a.out + m * a.ld_out, n, a.p.n, gated4<T>(a.act, g, u));
+    } else {
+      gated4_back<T>(a.act, read4((const T*)a.dh + m * a.ld_dh, n, a.p.n), g, u);
+      T* row = (T*)a.out + m * 2 * a.ld_out;
+      store4(row, n, (int)a.ld_out, g);
+      store4(row + a.ld_out, n, (int)a.ld_out, u);
+    }
+  }
+}
+
+template <typename T, int kMode>
+void launch_both(GatedArgs a, const Cut& cut, hipStream_t s) {
+  a.tiles_m = cut.tiles_m;
+  a.tiles_n = cut.tiles_n;
+  a.steps = cut.steps;
+  const auto go = [&](auto p) {
+    using P = typename decltype(p)::Shape;
+    const uint32_t blocks = (uint32_t)cut.blocks();
+    if (cut.splits > 1) ckm_gated_kernel<P, kShares><<<blocks, P::kThreads, 0, s>>>(a);
+    else ckm_gated_kernel<P, kMode><<<blocks, P::kThreads, 0, s>>>(a);
+  };
+  if (cut.rows == 256) go(Tag<Product<T, 256, 256, 2, 4, 2, true, false, 2>>());
+  else go(Tag<Product<T, 128, 128, 2, 2, 2, true, false, 2>>());
+  if (cut.splits > 1) {
+    const uint32_t fours = (uint32_t)(((kMode == kForward ? a.p.n : a.ld_out) + 3) / 4);
+    const int64_t total = a.p.m * (int64_t)fours;
+    ckm_gated_join_kernel<T, kMode><<<(uint32_t)std::min<int64_t>((total + 255) / 256, 1 << 16), 256, 0, s>>>(
+        a, cut.splits, total, fours);
+  }
+}
+
+// Where a call's parts lie in its work buffer.
+struct GatedPlan {
+  bool pack_x, pack_w;
+  int64_t ld_x, ld_w;        // of the operands as multiplied
+  int64_t inner;             // columns of dg, padded to whole groups
+  Cut both, dx, dw;
+  size_t x, w, d, slab, total;
+};
+
+GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
+  const size_t elt = dtype_bytes(type);
+  const int64_t group = 16 / elt, step = kStepBytes / elt;
+  GatedPlan p = {};
+  p.pack_x = !loadable(c.d_x, c.rows, c.hidden, c.ld_x, elt, true);
+  p.pack_w = c.ld_gate != c.ld_up || !loadable(c.d_gate, c.hidden, c.inner, c.ld_gate, elt, back) ||
+             !loadable(c.d_up, c.hidden, c.inner, c.ld_up, elt, back);
+  p.inner = whole(c.inner, group);
+  p.ld_x = p.pack_x || c.rows == 1 ? whole(c.hidden, group) : c.ld_x;   // a single row may have any stride
+  p.ld_w = p.pack_w || c.hidden == 1 ? p.inner : c.ld_gate;
+  const int64_t steps_h = (c.hidden + step - 1) / step, steps_f = (c.inner + step - 1) / step;
+  p.both = cut_product(c.rows, 2 * c.inner, 1, steps_h, 0);
+  p.both.cols /= 2;
+  p.both.tiles_n = (int)((c.inner + p.both.cols - 1) / p.both.cols);
+  size_t at = 0;
+  const auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at = whole(at + bytes, 256);
+    return here;
+  };
+  if (p.pack_x) p.x = take(c.rows * p.ld_x * elt);
+  if (p.pack_w) p.w = take(2 * c.hidden * p.ld_w * elt);
+  size_t slab = p.both.splits > 1 ? (size_t)p.both.splits * 2 * c.rows * whole(c.inner, 4) * 4 : 0;
+  if (back) {
+    p.dx = cut_product(c.rows, c.hidden, 1, 2 * steps_f, 0);
+    p.dw = cut_product(c.hidden, c.inner, 2, (c.rows + step - 1) / step, 0);
+    p.d = take(c.rows * 2 * p.inner * elt);
+    if (p.dx.splits > 1) slab = std::max(slab, (size_t)p.dx.splits * c.rows * whole(c.hidden, 4) * 4);
+    if (p.dw.splits > 1) slab = std::max(slab, (size_t)p.dw.splits * 2 * c.hidden * whole(c.inner, 4) * 4);
+  }
+  p.slab = take(slab);
+  p.total = at;
+  return p;
+}
+
+template <typename T>
+void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const void* dh, int64_t ld_dh, void* out,
+                  int64_t ld_out, void* dgate, int64_t ld_dgate, void* dup, int64_t ld_dup, char* work, hipStream_t s) {
+  const bool back = dh != nullptr;
+  const void *x = c.d_x, *wg = c.d_gate, *wu = c.d_up;
+  if (plan.pack_x) {
+    launch_pack(type, x, c.rows, c.hidden, c.ld_x, work + plan.x, plan.ld_x, s);
+    x = work + plan.x;
+  }
+  if (plan.pack_w) {
+    T* to = (T*)(work + plan.w);
+    launch_pack(type, wg, c.hidden, c.inner, c.ld_gate, to, plan.ld_w, s);
+    launch_pack(type, wu, c.hidden, c.inner, c.ld_up, to + c.hidden * plan.ld_w, plan.ld_w, s);
+    wg = to;
+    wu = to + c.hidden * plan.ld_w;
+  }
+  float* slab = (float*)(work + plan.slab);
+  GatedArgs a = {};
+  a.p = {{{x, x}, plan.ld_x}, {{wg, wu}, plan.ld_w}, (int32_t)c.rows, (int32_t)c.inner, (int32_t)c.hidden, 1};
+  a.act = c.act;
+  a.dh = dh;
+  a.ld_dh = ld_dh;
+  a.slab = slab;
+  a.ld_slab = whole(c.inner, 4);
+  if (!back) {
+    a.out = out;
+    a.ld_out = ld_out;
+    launch_both<T, kForward>(a, plan.both, s);
+    return;
+  }
+  T* d = (T*)(work + plan.d);
+  a.out = d;
+  a.ld_out = plan.inner;
+  launch_both<T, kBackward>(a, plan.both, s);
+  if (out) {   // dx = dg Wg' + du Wu'
+    ResultArgs r = {};
+    r.p = {{{d, d + plan.inner}, 2 * plan.inner}, {{wg, wu}, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden,
+           (int32_t)c.inner, 2};
+    r.c[0] = out;
+    r.ld_c[0] = ld_out;
+    r.factor = 1.0f;
+    r.halves = 1;
+    if (plan.dx.splits > 1) r.slab = slab;
+    r.ld_slab = whole(c.hidden, 4);
+    launch_product<T, true, true>(r, plan.dx, s);
+    if (plan.dx.splits > 1) launch_join(type, r, plan.dx.splits, s);
+  }
+  if (dgate) {   // dWg = x' dg, dWu = x' du
+    ResultArgs r = {};
+    r.p = {{{x, x}, plan.ld_x}, {{d, d + plan.inner}, 2 * plan.inner}, (int32_t)c.hidden, (int32_t)c.inner,
+           (int32_t)c.rows, 1};
+    r.c[0] = dgate;
+    r.c[1] = dup;
+    r.ld_c[0] = ld_dgate;
+    r.ld_c[1] = ld_dup;
+    r.factor = 1.0f;
+    r.halves = 2;
+    if (plan.dw.splits > 1) r.slab = slab;
+    r.ld_slab = whole(c.inner, 4);
+    launch_product<T, false, false>(r, plan.dw, s);
+    if (plan.dw.splits > 1) launch_join(type, r, plan.dw.splits, s);
+  }
+}
+
+ckm_status check_gated(ckm_dtype type, const ckm_gated* c) {
+  if (!dtype_ok(type)) return set_error(CKM_E_INVALID_ARG, "unknown type %d", (int)type);
+  if (!c) return set_error(CKM_E_INVALID_ARG, "gated is NULL");
+  if (c->rows < 0 || c->hidden < 1 || c->inner < 1)
+    return set_error(CKM_E_INVALID_ARG, "gated of %lld rows, %lld x %lld", (long long)c->rows, (long long)c->hidden,
+                     (long long)c->inner);
+  if (c->rows > CKM_MAX_MATRIX_ROWS || c->hidden > CKM_MAX_MATRIX_COLS || c->inner > CKM_MAX_MATRIX_COLS)
+    return set_error(CKM_E_UNSUPPORTED, "gated of %lld rows, %lld x %lld", (long long)c->rows, (long long)c->hidden,
+                     (long long)c->inner);
+  if (c->act != CKM_ACT_SILU && c->act != CKM_ACT_GELU && c->act != CKM_ACT_RELU)
+    return set_error(CKM_E_INVALID_ARG, "unknown activation %d", (int)c->act);
+  const size_t elt = dtype_bytes(type);
+  ckm_status st;
+  if (c->rows && (st = check_matrix(c->d_x, "x", c->rows, c->hidden, c->ld_x, elt, false)) != CKM_OK) return st;
+  if ((st = check_matrix(c->d_gate, "w_gate", c->hidden, c->inner, c->ld_gate, elt, false)) != CKM_OK) return st;
+  return check_matrix(c->d_up, "w_up", c->hidden, c->inner, c->ld_up, elt, false);
+}
+
+ckm_status gated(ckm_dtype type, const ckm_gated* c, bool back, const void* dh, int64_t ld_dh, void* out,
+                 int64_t ld_out, void* dgate, int64_t ld_dgate, void* dup, int64_t ld_dup, void* work,
+                 size_t work_bytes, void* stream) {
+  ckm_status st = check_gated(type, c);
+  if (st != CKM_OK) return st;
+  const size_t elt = dtype_bytes(type);
+  const hipStream_t s = (hipStream_t)stream;
+  if (back) {
+    if ((dgate == nullptr) != (dup == nullptr))
+      return set_error(CKM_E_INVALID_ARG, "one of dw_gate and dw_up is NULL and the other is not");
+    if (dgate && (st = check_matrix(dgate, "dw_gate", c->hidden, c->inner, ld_dgate, elt, true)) != CKM_OK) return st;
+    if (dup && (st = check_matrix(dup, "dw_up", c->hidden, c->inner, ld_dup, elt, true)) != CKM_OK) return st;
+  }
+  if (c->rows == 0) {
+    if (dgate) {
+      launch_zero(type, dgate, c->hidden, c->inner, ld_dgate, s);
+      launch_zero(type, dup, c->hidden, c->inner, ld_dup, s);
+      return launched("gated gradient launch");
+    }
+    return CKM_OK;
+  }
+  if (back && (st = check_matrix(dh, "dh", c->rows, c->inner, ld_dh, elt, false)) != CKM_OK) return st;
+  if ((out || !back) &&
+      (st = check_matrix(out, back ? "dx" : "h", c->rows, back ? c->hidden : c->inner, ld_out, elt, true)) != CKM_OK)
+    return st;
+  if (back && !out && !dgate) return CKM_OK;
+  const GatedPlan plan = plan_of(type, *c, back);
+  if ((st = check_blocks(plan.both)) != CKM_OK) return st;
+  if (back && ((st = check_blocks(plan.dx)) != CKM_OK || (st = check_blocks(plan.dw)) != CKM_OK)) return st;
+  if (plan.total && (!work || work_bytes < plan.total))
+    return set_error(CKM_E_INVALID_ARG, "work buffer of %zu bytes, %zu needed", work ? work_bytes : (size_t)0,
+                     plan.total);
+  if ((uintptr_t)work % 16) return set_error(CKM_E_INVALID_ARG, "work is not aligned to 16 bytes");
+  const auto go = [&](auto t) {
+    launch_gated<decltype(t)>(type, *c, plan, dh, ld_dh, out, ld_out, dgate, ld_dgate, dup, ld_dup, (char*)work, s);
+  };
+  switch (type) {
+    case CKM_F32: go(0.0f); break;
+    case CKM_F16: go((_Float16)0); break;
+    default: go((__bf16)0.0f); break;
+  }
+  return launched(back ? "gated gradient launch" : "gated launch");
+}
+
+}  // namespace
+}  // namespace ckm
+
+extern "C" ckm_status ckm_gated_workspace_size(ckm_dtype type, const ckm_gated* gated, int32_t backward, size_t* bytes) {
+  using namespace ckm;
+  if (!bytes) return set_error(CKM_E_INVALID_ARG, "bytes is NULL");
+  const ckm_status st = check_gated(type, gated);
+  if (st != CKM_OK) return st;
+  *bytes = gated->rows ? plan_of(type, *gated, backward != 0).total : 0;
+  return CKM_OK;
+}
+
+extern "C" ckm_status ckm_gated_async(ckm_dtype type, const ckm_gated* gated, void* d_h, int64_t ld_h, void* d_work,
+                                      size_t work_bytes, void* stream) {
+  return ckm::gated(type, gated, false, nullptr, 0, d_h, ld_h, nullptr, 0, nullptr, 0, d_work, work_bytes, stream);
+}
+
+extern "C" ckm_status ckm_gated_backward_async(ckm_dtype type, const ckm_gated* gated, const void* d_dh, int64_t ld_dh,
+                                               void* d_dx, int64_t ld_dx, void* d_dgate, int64_t ld_dgate, void* d_dup,
+                                               int64_t ld_dup, void* d_work, size_t work_bytes, void* stream) {
+  return ckm::gated(type, gated, true, d_dh, ld_dh, d_dx, ld_dx, d_dgate, ld_dgate, d_dup, ld_dup, d_work, work_bytes,
+                    stream);
+}

@@ -1,0 +1,405 @@
+// Tiled matrix products for the operators that multiply: C[m][n] = sum over k of
+// A[m][k] B[k][n], of which a block computes a tile kM x kN into registers, in
+// binary32, and an operator's kernel makes of it what it needs.
+//
+// Along k a block goes by steps of 128 bytes (64 elements of 16 bits, 32 of
+// binary32). A step's operand tiles are loaded straight into LDS, kStages steps
+// ahead; a wave reads its fragments of 16 x 64 bytes from there half a step ahead
+// of the matrix instructions that take them. Each step has one barrier: the next
+// step's tiles have landed, and every wave has read this step's, whose place the
+// loads after it take.
+//
+// An operand lies along k (rows of m or n, k contiguous) or across it (rows of k, m
+// or n contiguous). A fragment across k is read with the transposing LDS load.
+// Places past m, n or k read as zeros: the loads' range check sees to rows, a
+// comparison to columns.
+#pragma once
+
+#include "ckm_ops.h"
+
+namespace ckm {
+
+typedef float F4 __attribute__((ext_vector_type(4)));
+typedef int I4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) char LdsChar;
+
+constexpr int kStepBytes = 128;                    // of k, in one step
+constexpr uint32_t kNowhere = 0x80000000u;         // an offset past every range
+constexpr int64_t kMaxRowBytes = (int64_t)1 << 22; // a tile's rows then stay within 2^31 bytes
+
+// An operand in memory: up to two matrices of one row stride (parts of k one after
+// the other, or of n side by side).
+struct Operand {
+  const void* p[2];
+  int64_t ld;   // elements
+};
+
+struct ProductArgs {
+  Operand a, b;
+  int32_t m, n, k;      // of one part
+  int32_t parts;        // 1, or 2: k of the first, then k of the second
+};
+
+// Whether a matrix of rows of `cols` elements can be loaded straight to LDS: whole
+// groups of 16 bytes, and for one along k no group that ends past the row.
+inline bool loadable(const void* p, int64_t rows, int64_t cols, int64_t ld, size_t elt, bool along_k) {
+  return (uintptr_t)p % 16 == 0 && (rows == 1 || (ld * elt % 16 == 0 && ld >= cols && ld * (int64_t)elt <= kMaxRowBytes)) &&
+         (!along_k || cols * elt % 16 == 0);
+}
+
+#define CKM_WAIT_LOADS(n) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(n) : "memory")
+
+// A tile of kRows rows (or columns) by one step in LDS: kRows x 128 bytes, loaded
+// by kWaves waves, 1024 bytes a load. Groups of 16 bytes are permuted within a row of
+// the tile so that the lanes of a fragment's read meet in no bank.
+template <typename T, int kRows, bool kAlongK, int kWaves>
+struct TileLoad {
+  static constexpr int kElt = sizeof(T), kStep = kStepBytes / kElt, kGroup = 16 / kElt;
+  static constexpr int kBytes = kRows * kStepBytes;
+  static constexpr int kRowBytes = kAlongK ? kStepBytes : kRows * kElt;
+  static constexpr int kLoads = kBytes / 1024;
+  static constexpr int kPer = (kLoads + kWaves - 1) / kWaves;   // of a wave; a few are made twice where waves are many
+  static_assert(kRowBytes <= 1024 && kBytes % 1024 == 0, "rows of a tile in one load");
+  static_assert(kAlongK || kRowBytes >= 128, "");
+
+  uint32_t off[kPer];
+  uint32_t kpos;   // along k: the first element's k within the step
+
+  // The permutation of row r across k, in groups.
+  __device__ __forceinline__ static int turned(int r) {
+    if constexpr (sizeof(T) == 4) return 4 * ((r >> 2) & 3) & (kRowBytes / 16 - 1);
+    else if constexpr (kRowBytes >= 256) return 2 * ((r & 3) | ((r >> 3) & 1) << 2);
+    else return 2 * (((r >> 1) & 1) | ((r >> 3) & 1) << 1);
+  }
+
+  __device__ __forceinline__ void init(int wave, int lane, int64_t ld, int valid) {
+#pragma unroll
+    for (int t = 0; t < kPer; ++t) {
+      const int at = (wave * kPer + t) % kLoads * 1024 + lane * 16;
+      const int row = at / kRowBytes, slot = at % kRowBytes / 16;
+      const int group = kAlongK ? slot ^ (row & 7) : slot ^ turned(row);
+      off[t] = (uint32_t)(row * (uint32_t)(ld * kElt) + group * 16);
+      if constexpr (kAlongK) kpos = group * kGroup;   // the same for every t
+      else if (group * kGroup >= valid) off[t] = kNowhere;
+    }
+  }
+
+  // Starts the loads of one step: `base` the tile's first element, `valid` rows
+  // (along k) or columns of the tile that are there, `left` the k that are left.
+  __device__ __forceinline__ void issue(const char* base, int64_t ld, int valid, int left, uint32_t lds, int wave) const {
+    const int64_t row = ld * kElt;
+    const int have = min(left, kStep);
+    // whole groups along k (what follows the row's end in its last one is zero or not there); across k whole words
+    const int64_t range = have <= 0 ? 0 : kAlongK ? (min(valid, kRows) - 1) * row + ((have * kElt + 15) & ~15)
+                                                  : (have - 1) * row + ((min(valid, kRows) * kElt + 3) & ~3);
+    const I4 rsrc = {__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)base),
+                     __builtin_amdgcn_readfirstlane((int)(uint32_t)((uintptr_t)base >> 32)),
+                     __builtin_amdgcn_readfirstlane((int)range), 0x00020000};
+#pragma unroll
+    for (int t = 0; t < kPer; ++t) {
+      const uint32_t o = kAlongK && (int)kpos >= left ? kNowhere : off[t];
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (wave * kPer + t) % kLoads * 1024);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                   ::"s"(to), "v"(o), "s"(rsrc) : "memory");
+    }
+  }
+};
+
+// A lane's view of a tile: fragment f (16 rows or columns), half a step each.
+template <typename T, int kRows, bool kAlongK>
+struct TileRead {
+  static constexpr int kElt = sizeof(T);
+  static constexpr int kRowBytes = kAlongK ? kStepBytes : kRows * kElt;
+  uint32_t at;   // of fragment 0 of the wave, first half
+
+  __device__ __forceinline__ void init(int lane, int first) {   // first: of the wave's fragments
+    const int i = lane & 15, g = lane >> 4;
+    if constexpr (kAlongK) {
+      at = (first * 16 + i) * kStepBytes + ((g ^ (i & 7)) * 16);
+    } else if constexpr (sizeof(T) == 4) {
+      at = 4 * g * kRowBytes + i * 4 + ((first * 64) ^ (TileLoad<T, kRows, false, 1>::turned(4 * g) * 16));
+    } else {
+      const int k = 8 * g + i / 4;
+      at = k * kRowBytes + ((first * 32) ^ (TileLoad<T, kRows, false, 1>::turned(k) * 16)) + (i % 4) * 8;
+    }
+  }
+
+  // The fragment's 16 bytes a lane: k = 64 bytes x half + 16 bytes x (lane / 16) on, along k.
+  __device__ __forceinline__ I4 get(LdsChar* tile, int f, int half) const {
+    typedef __attribute__((address_space(3))) I4 LdsI4;
+    typedef __attribute__((address_space(3))) int LdsInt;
+    typedef short S4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) S4 LdsS4;
+    if constexpr (kAlongK) {
+      return *(LdsI4*)(tile + (at ^ (half * 64)) + f * 16 * kStepBytes);
+    } else if constexpr (sizeof(T) == 4) {
+      LdsChar* p = tile + (at ^ (f * 64)) + half * 16 * kRowBytes;
+      return I4{*(LdsInt*)p, *(LdsInt*)(p + kRowBytes), *(LdsInt*)(p + 2 * kRowBytes), *(LdsInt*)(p + 3 * kRowBytes)};
+    } else {
+      LdsChar* p = tile + (at ^ (f * 32)) + half * 32 * kRowBytes;
+      struct Both {
+        S4 lo, hi;
+      } v = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)p),
+             __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4*)(p + 4 * kRowBytes))};
+      return __builtin_bit_cast(I4, v);
+    }
+  }
+};
+
+// acc += over half a step: rows of the result are p's, columns q's.
+template <typename T>
+__device__ __forceinline__ F4 mma(F4 acc, I4 p, I4 q) {
+  if constexpr (std::is_same<T, float>::value) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(p[j]), __int_as_float(q[j]), acc, 0, 0, 0);
+    return acc;
+  } else if constexpr (std::is_same<T, _Float16>::value) {
+    typedef _Float16 H8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(H8, p), __builtin_bit_cast(H8, q), acc, 0, 0, 0);
+  } else {
+    typedef __bf16 B8 __attribute__((ext_vector_type(8)));
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(B8, p), __builtin_bit_cast(B8, q), acc, 0, 0, 0);
+  }
+}
+
+// A block's product: kM x kN of C by kWavesM x kWavesN waves. kSubs = 2: the tile's
+// columns are kN / 2 of each of two matrices, and each wave has as many of both.
+template <typename T_, int kM_, int kN_, int kWavesM_, int kWavesN_, int kStages_, bool kAK_, bool kBK_, int kSubs_>
+struct Product {
+  using T = T_;
+  static constexpr int kM = kM_, kN = kN_, kWavesM = kWavesM_, kWavesN = kWavesN_, kStages = kStages_, kSubs = kSubs_;
+  static constexpr bool kAK = kAK_, kBK = kBK_;
+  static constexpr int kWaves = kWavesM * kWavesN, kThreads = 64 * kWaves, kStep = kStepBytes / sizeof(T);
+  static constexpr int kFM = kM / kWavesM / 16, kFN = kN / kWavesN / 16, kFS = kFN / kSubs;
+  static constexpr int kSubN = kN / kSubs;
+  using LoadA = TileLoad<T, kM, kAK, kWaves>;
+  using LoadB = TileLoad<T, kSubN, kBK, kWaves>;
+  static constexpr int kStage = LoadA::kBytes + kSubs * LoadB::kBytes;
+  static constexpr int kLds = kStages * kStage;
+  static constexpr int kPer = LoadA::kPer + kSubs * LoadB::kPer;   // loads of a wave in a step
+  static_assert(kM % (16 * kWavesM) == 0 && kN % (16 * kWavesN * kSubs) == 0 && kStages >= 2, "");
+
+  // waves of a SIMD, as many blocks as fit a CU's 160 KB
+  static constexpr int kBlocks = 163840 / kLds < 1 ? 1 : 163840 / kLds > 4 ? 4 : 163840 / kLds;
+  static constexpr int kWaveSlots = kBlocks * kWaves / 4 > 4 ? 4 : kBlocks * kWaves / 4;
+
+  int wave, lane, wm, wn;
+
+  __device__ __forceinline__ Product() {
+    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lane = threadIdx.x & 63;
+    wm = wave / kWavesN;
+    wn = wave % kWavesN;
+  }
+  // The row and first column (of four) of acc[j][i] in the tile; columns of sub j / kFS.
+  __device__ __forceinline__ int row(int i) const { return (wm * kFM + i) * 16 + (lane & 15); }
+  __device__ __forceinline__ int col(int j) const { return (wn * kFS + j % kFS) * 16 + (lane >> 4) * 4; }
+
+  // The tile from (m0, n0) on over steps [step0, step1) of k; every wave has passed
+  // its last read of `lds` when this returns, and no load is under way.
+  __device__ __forceinline__ void run(F4 (&acc)[kFN][kFM], const ProductArgs& a, int m0, int n0, int step0, int step1,
+                                      LdsChar* lds) const {
+    LoadA la;
+    LoadB lb;
+    const int validm = a.m - m0, validn = a.n - n0;
+    la.init(wave, lane, a.a.ld, validm);
+    lb.init(wave, lane, a.b.ld, validn);
+    const int per = (a.k + kStep - 1) / kStep;   // steps of a part
+    const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+    const auto issue = [&](int stage, int step) {
+      const int part = kSubs == 1 && step >= per ? 1 : 0;
+      const int64_t k = (int64_t)(step - (part ? per : 0)) * kStep;
+      const int left = step < step1 ? (int)(a.k - k) : 0;
+      const uint32_t to = lds0 + stage * kStage;
+      la.issue((const char*)((const T*)a.a.p[part] + (kAK ? (int64_t)m0 * a.a.ld + k : k * a.a.ld + m0)), a.a.ld,
+               validm, left, to, wave);
+#pragma unroll
+      for (int s = 0; s < kSubs; ++s)
+        lb.issue((const char*)((const T*)a.b.p[kSubs == 1 ? part : s] +
+                               (kBK ? (int64_t)n0 * a.b.ld + k : k * a.b.ld + n0)),
+                 a.b.ld, validn, left, to + LoadA::kBytes + s * LoadB::kBytes, wave);
+    };
+    TileRead<T, kM, kAK> ra;
+    TileRead<T, kSubN, kBK> rb;
+    ra.init(lane, wm * kFM);
+    rb.init(lane, wn * kFS);
+    I4 fa[2][kFM], fb[2][kFN];
+    const auto read_a = [&](int set, int i, int stage) { fa[set][i] = ra.get(lds + stage * kStage, i, set); };
+    const auto read_b = [&](int set, int j, int stage) {
+      fb[set][j] = rb.get(lds + stage * kStage + LoadA::kBytes + j / kFS * LoadB::kBytes, j % kFS, set);
+    };
+    // the matrix instructions of one half step, with the reads of the next
+    const auto half = [&](auto set_, int stage) {
+      constexpr int set = decltype(set_)::value, next = 1 - set;
+#pragma unroll
+      for (int i = 0; i < kFM; ++i) {
+        read_a(next, i, stage);
+#pragma unroll
+        for (int j = i * kFN / kFM; j < (i + 1) * kFN / kFM; ++j) read_b(next, j, stage);
+#pragma unroll
+        for (int j = 0; j < kFN; ++j) acc[j][i] = mma<T>(acc[j][i], fb[set][j], fa[set][i]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < kFN; ++j)
+#pragma unroll
+      for (int i = 0; i < kFM; ++i) acc[j][i] = F4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int s = 0; s < kStages; ++s) issue(s, step0 + s);
+    CKM_WAIT_LOADS((kStages - 1) * kPer);
+    asm volatile("s_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kFM; ++i) read_a(0, i, 0);
+#pragma unroll
+    for (int j = 0; j < kFN; ++j) read_b(0, j, 0);
+    int stage = 0;
+    for (int s = step0; s < step1; ++s) {
+      const int next = stage + 1 == kStages ? 0 : stage + 1;
+      half(std::integral_constant<int, 0>{}, stage);
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kPer) : "memory");
+      issue(stage, s + kStages);
+      half(std::integral_constant<int, 1>{}, next);
+      stage = next;
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+};
+
+template <class S>
+struct Tag {
+  using Shape = S;
+};
+
+// The place in a grid of tiles_m x tiles_n that block `b` of them takes. Blocks go to
+// the eight dies in turn, so each die gets a range of its own, and goes through it in
+// columns of up to eight tiles of m, which share the operands' tiles in its cache.
+__device__ __forceinline__ void tile_of(int b, int tiles_m, int tiles_n, int& tm, int& tn) {
+  const int total = tiles_m * tiles_n, per = total / 8, rest = total % 8;
+  const int die = b % 8, at = die * per + min(die, rest) + b / 8;
+  const int band = at / (8 * tiles_n), first = band * 8, high = min(8, tiles_m - first);
+  const int in = at - first * tiles_n;
+  tm = first + in % high;
+  tn = in / high;
+}
+
+// Up to four consecutive elements of a row at column `col`, rounded to T.
+template <typename T>
+__device__ __forceinline__ void store4(T* row, int col, int cols, F4 v) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 r;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) r[k] = rounded<T>(v[k]);
+  if (col + 4 <= cols) {
+    __builtin_memcpy(row + col, &r, sizeof(r));
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (col + k < cols) row[col + k] = r[k];
+  }
+}
+// Up to four consecutive elements, zeros past the row's end.
+template <typename T>
+__device__ __forceinline__ F4 read4(const T* row, int col, int cols) {
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  F4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (col + 4 <= cols) {
+    T4 r;
+    __builtin_memcpy(&r, row + col, sizeof(r));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = (float)r[k];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+      if (col + k < cols) v[k] = (float)row[col + k];
+  }
+  return v;
+}
+
+// How a product of m x n (n: of one of `halves` results side by side) is cut: the
+// rows of a tile, and shares of k, whose sums are joined in a fixed order.
+struct Cut {
+  int rows, cols;            // of a tile
+  int tiles_m, tiles_n;      // of one half
+  int halves, splits, steps; // steps of k in a share
+  int64_t blocks() const { return (int64_t)tiles_m * tiles_n * halves * splits; }
+};
+Cut cut_product(int64_t m, int64_t n, int halves, int64_t steps, int tile_cols);
+
+__host__ __device__ inline int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of * of; }
+// CKM_E_UNSUPPORTED for a grid past what a launch counts.
+ckm_status check_blocks(const Cut& c);
+
+// Copies rows of cols elements into rows of `ld` (whole groups), zeros between; with
+// targets, a row whose target is outside [0, vocab) as zeros.
+void launch_pack(int type, const void* src, int64_t rows, int64_t cols, int64_t ld_src, void* dst, int64_t ld,
+                 hipStream_t s, const int64_t* targets = nullptr, int64_t vocab = 0);
+// Zeros in rows of cols elements.
+void launch_zero(int type, void* dst, int64_t rows, int64_t cols, int64_t ld, hipStream_t s);
+
+// ---- a product alone, into a result or into shares --------------------------
+struct ResultArgs {
+  ProductArgs p;          // n: of one half
+  void* c[2];             // the result's halves; or
+  float* slab;            // shares [split][half][m][ld_slab] in binary32, when not NULL
+  int64_t ld_c[2], ld_slab;
+  bool add;               // to what the slab holds
+  const float* alpha;     // NULL, or a factor on the device,
+  float factor;           // times this
+  int32_t tiles_m, tiles_n, halves, steps;   // Cut
+};
+
+// Two results' products share a launch: half h takes b.p[h] (parts is 1 then).
+template <class P>
+__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel(ResultArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+  const P p;
+  const int tiles = a.tiles_m * a.tiles_n * a.halves, split = blockIdx.x / tiles;
+  int tm, tn;
+  tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n * a.halves, tm, tn);
+  const int half = tn / a.tiles_n;
+  tn -= half * a.tiles_n;
+  if (a.halves == 2) a.p.b.p[0] = a.p.b.p[half];
+  const int all = (a.p.k + P::kStep - 1) / P::kStep * a.p.parts, from = split * a.steps;
+  F4 acc[P::kFN][P::kFM];
+  p.run(acc, a.p, tm * P::kM, tn * P::kN, from, min(all, from + a.steps), (LdsChar*)lds);
+  float* slab = a.slab ? a.slab + ((int64_t)split * a.halves + half) * a.p.m * a.ld_slab : nullptr;
+  const float factor = a.alpha ? a.factor * *a.alpha : a.factor;
+#pragma unroll
+  for (int i = 0; i < P::kFM; ++i) {
+    const int m = tm * P::kM + p.row(i);
+    if (m >= a.p.m) continue;
+#pragma unroll
+    for (int j = 0; j < P::kFN; ++j) {
+      const int n = tn * P::kN + p.col(j);
+      if (slab) {   // rows of whole fours
+        if (n < a.p.n) {
+          F4* at = (F4*)(slab + (int64_t)m * a.ld_slab + n);
+          *at = a.add ? *at + acc[j][i] : acc[j][i];
+        }
+      } else {
+        store4((typename P::T*)a.c[half] + (int64_t)m * a.ld_c[half], n, a.p.n, acc[j][i] * factor);
+      }
+    }
+  }
+}
+
+// Adds the shares of a result in their order.
+void launch_join(int type, const ResultArgs& a, int splits, hipStream_t s);
+
+template <typename T, bool kAK, bool kBK>
+void launch_product(ResultArgs a, const Cut& cut, hipStream_t s) {
+  a.tiles_m = cut.tiles_m;
+  a.tiles_n = cut.tiles_n;
+  a.halves = cut.halves;
+  a.steps = cut.steps;
+  const auto go = [&](auto p) {
+    using P = typename decltype(p)::Shape;
+    ckm_product_kernel<P><<<(uint32_t)cut.blocks(), P::kThreads, 0, s>>>(a);
+  };
+  if (cut.rows == 256) go(Tag<Product<T, 256, 256, 2, 4, 2, kAK, kBK, 1>>());
+  else go(Tag<Product<T, 128, 128, 2, 2, 2, kAK, kBK, 1>>());
+}
+
+}  // namespace ckm

@@ -7,6 +7,12 @@ computes again first, with their gradients as calls (nodes) of their own:
   layer_norm, layer_norm_backward     with the dropout and residual sum before it
   softmax, softmax_backward           scale, masks, softmax and dropout of scores
 
+and the matrix operators of a training step whose large values never exist:
+
+  gated, gated_backward               both projections, activation and product of a feed-forward block
+  cross_entropy, cross_entropy_backward   the loss against a vocabulary's table, without the logits
+  gradient_norm, clip_gradients       the norm over many tensors, and the tensors scaled by it
+
 A call made again with the same inputs gives the same bits, in whatever stage
 of a plan it runs. Every computation is a HIP kernel of libckm (include/ckm.h
 states each operator's definition); there is no other implementation to fall
@@ -26,6 +32,7 @@ allocates require no gradient, and gradients are the *_backward calls.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 import math
@@ -38,6 +45,7 @@ F32, F16, BF16 = range(3)
 SCORES_CAUSAL = 1
 MASK_NONE, MASK_BOOL, MASK_ADD = range(3)
 MAX_ROWS, MAX_COLS, MAX_NORM_COLS = 0x7fffffff, 1 << 30, 32768
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2}
 _TYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 
@@ -49,6 +57,17 @@ class _Scores(C.Structure):
     _fields_ = [("batch", C.c_int64), ("heads", C.c_int64), ("queries", C.c_int64), ("keys", C.c_int64),
                 ("scale", C.c_float), ("flags", C.c_uint32), ("d_lengths", C.c_void_p), ("d_mask", C.c_void_p),
                 ("mask_kind", C.c_int32), ("mask_stride", C.c_int64 * 3)]
+
+
+class _Gated(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("hidden", C.c_int64), ("inner", C.c_int64), ("act", C.c_int32),
+                ("d_x", C.c_void_p), ("ld_x", C.c_int64), ("d_gate", C.c_void_p), ("ld_gate", C.c_int64),
+                ("d_up", C.c_void_p), ("ld_up", C.c_int64)]
+
+
+class _Vocab(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("hidden", C.c_int64), ("vocab", C.c_int64), ("d_x", C.c_void_p),
+                ("ld_x", C.c_int64), ("d_weight", C.c_void_p), ("ld_weight", C.c_int64), ("d_targets", C.c_void_p)]
 
 
 _Stride = C.c_int64 * 3
@@ -471,3 +490,229 @@ def softmax_backward(dy, scores, stats, scale: float = 1.0, causal: bool = False
     ckm._check(ckm.lib().ckm_softmax_backward_async(_TYPES[dtype], C.byref(c), gp, gs, xp, xs, stats.data_ptr(),
                                                     _drop_ptr(drop, device), op, os_, wp, wb, _raw_stream(device)))
     return dx
+
+
+def _gated(x, w_gate, w_up, act):
+    """(the C struct, device, x's shape, type) of a gated feed-forward's operands."""
+    device, shape, dtype, hidden, rows, xp, ldx = _first(x, "x")
+    if act not in ACTIVATIONS:
+        raise ValueError("act must be one of %s, got %r" % (", ".join(sorted(ACTIVATIONS)), act))
+    if not isinstance(w_gate, torch.Tensor) or w_gate.dim() != 2 or w_gate.shape[0] != hidden:
+        raise ValueError("w_gate must have shape (%d, inner width), got %s"
+                         % (hidden, tuple(w_gate.shape) if isinstance(w_gate, torch.Tensor) else type(w_gate).__name__))
+    wshape = w_gate.shape
+    gp, ldg = _rows(w_gate, "w_gate", wshape, dtype, device)
+    if w_up is None:
+        raise ValueError("w_up is needed")
+    up, ldu = _rows(w_up, "w_up", wshape, dtype, device)
+    return _Gated(rows, hidden, wshape[1], ACTIVATIONS[act], xp, ldx, gp, ldg, up, ldu), device, shape, dtype
+
+
+def _need(size, dtype, c, backward) -> int:
+    out = C.c_size_t()
+    ckm._check(size(_TYPES[dtype], C.byref(c), backward, C.byref(out)))
+    return out.value
+
+
+def gated_workspace(x, w_gate, w_up, backward: bool = False) -> int:
+    """Bytes of work buffer that gated (gated_backward) needs for these operands (ckm_gated_workspace_size)."""
+    c, _, _, dtype = _gated(x, w_gate, w_up, "silu")
+    return _need(ckm.lib().ckm_gated_workspace_size, dtype, c, backward)
+
+
+def gated(x, w_gate, w_up, act: str = "silu", out=None, work=None, stream=None):
+    """h = act(x w_gate) * (x w_up) of a gated feed-forward block (ckm_gated_async).
+
+    x: [..., hidden]; w_gate, w_up: [hidden, inner], of x's type. act: silu, gelu
+    (by erf) or relu. out: for h, [..., inner]; must overlap no operand. work: a
+    uint8 device buffer of gated_workspace(...) bytes to use. The gradient is
+    gated_backward (the call is outside autograd)."""
+    if stream is not None:
+        with _on(stream, None, x, w_gate, w_up, out, work):
+            return gated(x, w_gate, w_up, act, out, work)
+    c, device, shape, dtype = _gated(x, w_gate, w_up, act)
+    shape = shape[:-1] + (c.inner,)
+    if out is None:
+        h = x.new_empty(shape)
+        hp, ldh = h.data_ptr(), c.inner
+    else:
+        h = out
+        hp, ldh = _rows(h, "out", shape, dtype, device)
+    wp, wb, work = _work(work, _need(ckm.lib().ckm_gated_workspace_size, dtype, c, 0), x)
+    ckm._check(ckm.lib().ckm_gated_async(_TYPES[dtype], C.byref(c), hp, ldh, wp, wb, _raw_stream(device)))
+    return h
+
+
+def gated_backward(dh, x, w_gate, w_up, act: str = "silu", work=None, stream=None):
+    """(dx, dw_gate, dw_up) of gated (ckm_gated_backward_async): x w_gate and x w_up are computed again.
+    work: a uint8 device buffer of gated_workspace(..., backward=True) bytes to use."""
+    if stream is not None:
+        with _on(stream, None, dh, x, w_gate, w_up, work):
+            return gated_backward(dh, x, w_gate, w_up, act, work)
+    c, device, shape, dtype = _gated(x, w_gate, w_up, act)
+    if dh is None:
+        raise ValueError("dh is needed")
+    dhp, lddh = _rows(dh, "dh", shape[:-1] + (c.inner,), dtype, device)
+    dx = _like(x)
+    dg, du = x.new_empty((2, c.hidden, c.inner)).unbind(0)
+    wp, wb, work = _work(work, _need(ckm.lib().ckm_gated_workspace_size, dtype, c, 1), x)
+    ckm._check(ckm.lib().ckm_gated_backward_async(_TYPES[dtype], C.byref(c), dhp, lddh, dx.data_ptr(), c.hidden,
+                                                  dg.data_ptr(), c.inner, du.data_ptr(), c.inner, wp, wb,
+                                                  _raw_stream(device)))
+    return dx, dg, du
+
+
+def _vocab(x, weight, targets):
+    """(the C struct, device, x's shape, type) of a cross entropy's operands."""
+    device, shape, dtype, hidden, rows, xp, ldx = _first(x, "x")
+    if not isinstance(weight, torch.Tensor) or weight.dim() != 2 or weight.shape[1] != hidden:
+        raise ValueError("weight must have shape (vocabulary, %d), got %s"
+                         % (hidden, tuple(weight.shape) if isinstance(weight, torch.Tensor) else type(weight).__name__))
+    wp, ldw = _rows(weight, "weight", weight.shape, dtype, device)
+    tp = _each(targets, "targets", shape[:-1], torch.int64, device)
+    return _Vocab(rows, hidden, weight.shape[0], xp, ldx, wp, ldw, tp), device, shape, dtype
+
+
+def _each(t, name: str, shape, dtype, device):
+    """The pointer of a contiguous tensor with an element for each row."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == device and t.shape == shape
+            and t.is_contiguous()):
+        _tensor(t, name, dtype, device)
+        raise ValueError("%s must be contiguous of shape %s, got shape %s, strides %s"
+                         % (name, tuple(shape), tuple(t.shape), t.stride()))
+    return t.data_ptr()
+
+
+def cross_entropy_workspace(x, weight, targets, backward: bool = False) -> int:
+    """Bytes of work buffer that cross_entropy (cross_entropy_backward) needs for these operands
+    (ckm_cross_entropy_workspace_size)."""
+    c, _, _, dtype = _vocab(x, weight, targets)
+    return _need(ckm.lib().ckm_cross_entropy_workspace_size, dtype, c, backward)
+
+
+def cross_entropy(x, weight, targets, work=None, stream=None):
+    """(loss, lse) of each row of x against a vocabulary's table, without the logits (ckm_cross_entropy_async).
+
+    x: [..., hidden]; weight: [vocabulary, hidden], of x's type; targets: int64
+    [...]. loss = lse - x weight[target], float32; 0 where the target lies
+    outside the vocabulary (-100 marks padding). lse: log of the sum of exp(x
+    weight'), float32. work: a uint8 device buffer of
+    cross_entropy_workspace(...) bytes to use. The gradient is
+    cross_entropy_backward (the call is outside autograd)."""
+    if stream is not None:
+        with _on(stream, None, x, weight, targets, work):
+            return cross_entropy(x, weight, targets, work)
+    c, device, shape, dtype = _vocab(x, weight, targets)
+    loss = x.new_empty(shape[:-1], dtype=torch.float32)
+    lse = x.new_empty(shape[:-1], dtype=torch.float32)
+    wp, wb, work = _work(work, _need(ckm.lib().ckm_cross_entropy_workspace_size, dtype, c, 0), x)
+    ckm._check(ckm.lib().ckm_cross_entropy_async(_TYPES[dtype], C.byref(c), loss.data_ptr(), lse.data_ptr(), wp, wb,
+                                                 _raw_stream(device)))
+    return loss, lse
+
+
+def cross_entropy_backward(dloss, x, weight, targets, lse, work=None, stream=None):
+    """(dx, dweight) of cross_entropy (ckm_cross_entropy_backward_async).
+
+    dloss: float32 [...], the gradient of each row's loss (of a mean: 1 / the
+    rows that count, times a loss scale). lse: what cross_entropy returned. work:
+    a uint8 device buffer of cross_entropy_workspace(..., backward=True) bytes."""
+    if stream is not None:
+        with _on(stream, None, dloss, x, weight, targets, lse, work):
+            return cross_entropy_backward(dloss, x, weight, targets, lse, work)
+    c, device, shape, dtype = _vocab(x, weight, targets)
+    gp = _each(dloss, "dloss", shape[:-1], torch.float32, device)
+    lp = _each(lse, "lse", shape[:-1], torch.float32, device)
+    dx = _like(x)
+    dw = _like(weight)
+    wp, wb, work = _work(work, _need(ckm.lib().ckm_cross_entropy_workspace_size, dtype, c, 1), x)
+    ckm._check(ckm.lib().ckm_cross_entropy_backward_async(_TYPES[dtype], C.byref(c), gp, lp, dx.data_ptr(), c.hidden,
+                                                          dw.data_ptr(), c.hidden, wp, wb, _raw_stream(device)))
+    return dx, dw
+
+
+def _dense(t) -> bool:
+    """Whether a tensor's elements fill one range of memory, in any order of its dimensions."""
+    if t.is_contiguous():
+        return True
+    span = 1
+    for s, n in sorted((s, n) for n, s in zip(t.shape, t.stride()) if n != 1):
+        if s != span:
+            return t.numel() == 0
+        span *= n
+    return True
+
+
+def _list(tensors, out):
+    """(device, ckm_tensor array, count) of a list of tensors and, where given, of their outputs."""
+    tensors = list(tensors)
+    device = _current_device()
+    rows = array.array("q")
+    for k, t in enumerate(tensors):
+        if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES or t.get_device() != device:
+            _tensor(t, "tensor %d" % k)
+        if not t.is_contiguous() and not _dense(t):
+            raise ValueError("tensor %d: its elements must fill one range of memory, got shape %s, strides %s"
+                             % (k, tuple(t.shape), t.stride()))
+        p = t.data_ptr()
+        rows.extend((p, p, t.numel(), _TYPES[t.dtype]))
+    if out is not None:
+        if len(out) != len(tensors):
+            raise ValueError("out must hold %d tensors, got %d" % (len(tensors), len(out)))
+        for k, (t, y) in enumerate(zip(tensors, out)):
+            if (not isinstance(y, torch.Tensor) or y.dtype is not t.dtype or y.get_device() != device
+                    or y.shape != t.shape or y.stride() != t.stride()):
+                _tensor(y, "out %d" % k, t.dtype, device)
+                if y.shape != t.shape or (t.numel() and any(
+                        n != 1 and p != q for n, p, q in zip(t.shape, y.stride(), t.stride()))):
+                    raise ValueError("out %d must have shape %s and strides %s, got %s and %s"
+                                     % (k, tuple(t.shape), t.stride(), tuple(y.shape), y.stride()))
+            rows[4 * k + 1] = y.data_ptr()
+    return device, rows, len(tensors)
+
+
+@functools.lru_cache(maxsize=1024)
+def norm_workspace(count: int) -> int:
+    """Bytes of work buffer that gradient_norm and clip_gradients need for `count` tensors (ckm_norm_workspace_size)."""
+    out = C.c_size_t()
+    ckm._check(ckm.lib().ckm_norm_workspace_size(count, C.byref(out)))
+    return out.value
+
+
+def gradient_norm(tensors, work=None, stream=None):
+    """The 2-norm over all elements of all tensors, a float32 tensor of no dimension (ckm_norm_async).
+
+    tensors: float32, float16 and bfloat16 mixed; each must fill one range of
+    memory. Sums are binary64. work: a uint8 device buffer of
+    norm_workspace(len(tensors)) bytes to use."""
+    tensors = list(tensors)
+    if stream is not None:
+        with _on(stream, None, *tensors, work):
+            return gradient_norm(tensors, work)
+    device, rows, n = _list(tensors, None)
+    norm = torch.empty((), dtype=torch.float32, device="cuda")
+    wp, wb, work = _work(work, norm_workspace(n), norm)
+    ckm._check(ckm.lib().ckm_norm_async(n, rows.buffer_info()[0] if n else None, norm.data_ptr(), wp, wb,
+                                        _raw_stream(device)))
+    return norm
+
+
+def clip_gradients(tensors, max_norm: float, eps: float = 1e-6, out=None, work=None, stream=None):
+    """(norm, tensors) with every element times min(1, max_norm / (norm + eps)) (ckm_clip_async).
+
+    In place, or into `out`: as many tensors of the same types, shapes and
+    strides, which must overlap neither each other nor another tensor; so no tensor may
+    be listed twice. norm: what gradient_norm gives, of the tensors before. work:
+    as for gradient_norm."""
+    tensors = list(tensors)
+    if out is not None:
+        out = list(out)
+    if stream is not None:
+        with _on(stream, None, *tensors, *(out or ()), work):
+            return clip_gradients(tensors, max_norm, eps, out, work)
+    device, rows, n = _list(tensors, out)
+    norm = torch.empty((), dtype=torch.float32, device="cuda")
+    wp, wb, work = _work(work, norm_workspace(n), norm)
+    ckm._check(ckm.lib().ckm_clip_async(n, rows.buffer_info()[0] if n else None, max_norm, eps, norm.data_ptr(), wp, wb,
+                                        _raw_stream(device)))
+    return norm, tensors if out is None else out
