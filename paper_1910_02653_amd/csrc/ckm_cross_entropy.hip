@@ -231,7 +231,7 @@ LossPlan plan_of(int type, const ckm_vocab& c, bool back) {
     p.dx = cut_product(c.rows, c.hidden, 1, (p.piece + step - 1) / step, 0);
     p.dw = cut_product(p.piece, c.hidden, 1, (c.rows + step - 1) / step, 0);
     p.most = take(sizeof(float));
-    p.d = take((size_t)c.rows * whole(p.piece, 64) * elt);
+    p.d = take((size_t)c.rows * row_of(p.piece, elt) * elt);
     if (p.dx.splits > 1 || p.piece < c.vocab) p.slab = take((size_t)p.dx.splits * c.rows * whole(c.hidden, 4) * 4);
     if (p.dw.splits > 1) p.dw_slab = take((size_t)p.dw.splits * p.piece * whole(c.hidden, 4) * 4);
   }
@@ -253,7 +253,7 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     w = (const T*)(work + plan.w);
   }
   LossArgs a = {};
-  a.p = {{{x, x}, plan.ld_x}, {{w, w}, plan.ld_w}, (int32_t)c.rows, (int32_t)c.vocab, (int32_t)c.hidden, 1};
+  a.p = {{x, x, plan.ld_x}, {w, w, plan.ld_w}, (int32_t)c.rows, (int32_t)c.vocab, (int32_t)c.hidden, 1};
   a.targets = c.d_targets;
   a.vocab = c.vocab;
   a.lse = lse;
@@ -274,7 +274,7 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     a.most = most;
   }
   a.d = work + plan.d;
-  a.ld_d = whole(plan.piece, 64);
+  a.ld_d = row_of(plan.piece, sizeof(T));
   ResultArgs rx = {}, rw = {};
   rx.alpha = rw.alpha = a.most;
   rx.factor = rw.factor = kHalf ? 1.0f / kHalfGain : 1.0f;
@@ -291,16 +291,16 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     const bool tail = width < plan.piece;
     const T* wv = w + v * plan.ld_w;
     a.first = v;
-    a.p.b.p[0] = a.p.b.p[1] = wv;
+    a.p.b.p = a.p.b.q = wv;
     a.p.n = width;
     launch_logits<T, true>(a, tail ? plan.last : plan.logits, s);
     if (dx) {   // d W; a short last piece leaves shares at the end of k with nothing to add
-      rx.p = {{{a.d, a.d}, a.ld_d}, {{wv, wv}, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, width, 1};
+      rx.p = {{a.d, a.d, a.ld_d}, {wv, wv, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, width, 1};
       launch_product<T, true, false>(rx, plan.dx, s);
       rx.add = true;
     }
     if (dw) {   // d' x
-      rw.p = {{{a.d, a.d}, a.ld_d}, {{x, x}, plan.ld_x}, width, (int32_t)c.hidden, (int32_t)c.rows, 1};
+      rw.p = {{a.d, a.d, a.ld_d}, {x, x, plan.ld_x}, width, (int32_t)c.hidden, (int32_t)c.rows, 1};
       rw.c[0] = (T*)dw + v * ld_dw;
       Cut cut = plan.dw;
       cut.tiles_m = (width + cut.rows - 1) / cut.rows;

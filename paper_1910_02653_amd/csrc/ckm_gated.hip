@@ -29,7 +29,8 @@ struct GatedArgs {
   const void* dh;
   int64_t ld_dh;
   void* out;         // h, or dg | du
-  int64_t ld_out;    // of dg | du: of one of them
+  int64_t ld_out;
+  int32_t up;        // where du begins in a row of dg | du
   float* slab;       // [split][g, u][m][ld_slab]
   int64_t ld_slab;
 };
@@ -98,12 +99,12 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(G
       const int n = tn * P::kSubN + p.col(j);
       F4 g = acc[j][i], u = acc[j + P::kFS][i];
       if constexpr (kMode == kForward) {
-        store4((T*)a.out + (int64_t)m * a.ld_out, n, a.p.n, gated4<T>(a.act, g, u));
+        store4((T*)a.out + m * a.ld_out, n, a.p.n, gated4<T>(a.act, g, u));
       } else if constexpr (kMode == kBackward) {
-        gated4_back<T>(a.act, read4((const T*)a.dh + (int64_t)m * a.ld_dh, n, a.p.n), g, u);
-        T* row = (T*)a.out + (int64_t)m * 2 * a.ld_out;
-        store4(row, n, (int)a.ld_out, g);
-        store4(row + a.ld_out, n, (int)a.ld_out, u);
+        gated4_back<T>(a.act, read4((const T*)a.dh + m * a.ld_dh, n, a.p.n), g, u);
+        T* row = (T*)a.out + m * a.ld_out;
+        store4(row, n, a.up, g);
+        store4(row + a.up, n, a.up, u);
       } else if (n < a.p.n) {
         float* at = a.slab + ((int64_t)split * 2 * a.p.m + m) * a.ld_slab + n;
         *(F4*)at = g;
@@ -135,9 +136,9 @@ __global__ void __launch_bounds__(256) ckm_gated_join_kernel(GatedArgs a, int sp
       store4((T*)a.out + m * a.ld_out, n, a.p.n, gated4<T>(a.act, g, u));
     } else {
       gated4_back<T>(a.act, read4((const T*)a.dh + m * a.ld_dh, n, a.p.n), g, u);
-      T* row = (T*)a.out + m * 2 * a.ld_out;
-      store4(row, n, (int)a.ld_out, g);
-      store4(row + a.ld_out, n, (int)a.ld_out, u);
+      T* row = (T*)a.out + m * a.ld_out;
+      store4(row, n, a.up, g);
+      store4(row + a.up, n, a.up, u);
     }
   }
 }
@@ -156,7 +157,7 @@ void launch_both(GatedArgs a, const Cut& cut, hipStream_t s) {
   if (cut.rows == 256) go(Tag<Product<T, 256, 256, 2, 4, 2, true, false, 2>>());
   else go(Tag<Product<T, 128, 128, 2, 2, 2, true, false, 2>>());
   if (cut.splits > 1) {
-    const uint32_t fours = (uint32_t)(((kMode == kForward ? a.p.n : a.ld_out) + 3) / 4);
+    const uint32_t fours = (uint32_t)(((kMode == kForward ? a.p.n : a.up) + 3) / 4);
     const int64_t total = a.p.m * (int64_t)fours;
     ckm_gated_join_kernel<T, kMode><<<(uint32_t)std::min<int64_t>((total + 255) / 256, 1 << 16), 256, 0, s>>>(
         a, cut.splits, total, fours);
@@ -167,7 +168,7 @@ void launch_both(GatedArgs a, const Cut& cut, hipStream_t s) {
 struct GatedPlan {
   bool pack_x, pack_w;
   int64_t ld_x, ld_w;        // of the operands as multiplied
-  int64_t inner;             // columns of dg, padded to whole groups
+  int64_t inner, ld_d;       // columns of dg, padded to whole groups; a row of dg | du
   Cut both, dx, dw;
   size_t x, w, d, slab, total;
 };
@@ -180,6 +181,7 @@ GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
   p.pack_w = c.ld_gate != c.ld_up || !loadable(c.d_gate, c.hidden, c.inner, c.ld_gate, elt, back) ||
              !loadable(c.d_up, c.hidden, c.inner, c.ld_up, elt, back);
   p.inner = whole(c.inner, group);
+  p.ld_d = row_of(2 * p.inner, elt);
   p.ld_x = p.pack_x || c.rows == 1 ? whole(c.hidden, group) : c.ld_x;   // a single row may have any stride
   p.ld_w = p.pack_w || c.hidden == 1 ? p.inner : c.ld_gate;
   const int64_t steps_h = (c.hidden + step - 1) / step, steps_f = (c.inner + step - 1) / step;
@@ -198,7 +200,7 @@ GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
   if (back) {
     p.dx = cut_product(c.rows, c.hidden, 1, 2 * steps_f, 0);
     p.dw = cut_product(c.hidden, c.inner, 2, (c.rows + step - 1) / step, 0);
-    p.d = take(c.rows * 2 * p.inner * elt);
+    p.d = take(c.rows * p.ld_d * elt);
     if (p.dx.splits > 1) slab = std::max(slab, (size_t)p.dx.splits * c.rows * whole(c.hidden, 4) * 4);
     if (p.dw.splits > 1) slab = std::max(slab, (size_t)p.dw.splits * 2 * c.hidden * whole(c.inner, 4) * 4);
   }
@@ -225,7 +227,7 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
   }
   float* slab = (float*)(work + plan.slab);
   GatedArgs a = {};
-  a.p = {{{x, x}, plan.ld_x}, {{wg, wu}, plan.ld_w}, (int32_t)c.rows, (int32_t)c.inner, (int32_t)c.hidden, 1};
+  a.p = {{x, x, plan.ld_x}, {wg, wu, plan.ld_w}, (int32_t)c.rows, (int32_t)c.inner, (int32_t)c.hidden, 1};
   a.act = c.act;
   a.dh = dh;
   a.ld_dh = ld_dh;
@@ -239,11 +241,12 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
   }
   T* d = (T*)(work + plan.d);
   a.out = d;
-  a.ld_out = plan.inner;
+  a.ld_out = plan.ld_d;
+  a.up = (int32_t)plan.inner;
   launch_both<T, kBackward>(a, plan.both, s);
   if (out) {   // dx = dg Wg' + du Wu'
     ResultArgs r = {};
-    r.p = {{{d, d + plan.inner}, 2 * plan.inner}, {{wg, wu}, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden,
+    r.p = {{d, d + plan.inner, plan.ld_d}, {wg, wu, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden,
            (int32_t)c.inner, 2};
     r.c[0] = out;
     r.ld_c[0] = ld_out;
@@ -256,7 +259,7 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
   }
   if (dgate) {   // dWg = x' dg, dWu = x' du
     ResultArgs r = {};
-    r.p = {{{x, x}, plan.ld_x}, {{d, d + plan.inner}, 2 * plan.inner}, (int32_t)c.hidden, (int32_t)c.inner,
+    r.p = {{x, x, plan.ld_x}, {d, d + plan.inner, plan.ld_d}, (int32_t)c.hidden, (int32_t)c.inner,
            (int32_t)c.rows, 1};
     r.c[0] = dgate;
     r.c[1] = dup;

@@ -30,8 +30,8 @@ constexpr int64_t kMaxRowBytes = (int64_t)1 << 22; // a tile's rows then stay wi
 // An operand in memory: up to two matrices of one row stride (parts of k one after
 // the other, or of n side by side).
 struct Operand {
-  const void* p[2];
-  int64_t ld;   // elements
+  const void *p, *q;   // the first, the second
+  int64_t ld;          // elements
 };
 
 struct ProductArgs {
@@ -212,11 +212,11 @@ struct Product {
       const int64_t k = (int64_t)(step - (part ? per : 0)) * kStep;
       const int left = step < step1 ? (int)(a.k - k) : 0;
       const uint32_t to = lds0 + stage * kStage;
-      la.issue((const char*)((const T*)a.a.p[part] + (kAK ? (int64_t)m0 * a.a.ld + k : k * a.a.ld + m0)), a.a.ld,
+      la.issue((const char*)((const T*)(part ? a.a.q : a.a.p) + (kAK ? (int64_t)m0 * a.a.ld + k : k * a.a.ld + m0)), a.a.ld,
                validm, left, to, wave);
 #pragma unroll
       for (int s = 0; s < kSubs; ++s)
-        lb.issue((const char*)((const T*)a.b.p[kSubs == 1 ? part : s] +
+        lb.issue((const char*)((const T*)((kSubs == 1 ? part : s) ? a.b.q : a.b.p) +
                                (kBK ? (int64_t)n0 * a.b.ld + k : k * a.b.ld + n0)),
                  a.b.ld, validn, left, to + LoadA::kBytes + s * LoadB::kBytes, wave);
     };
@@ -328,6 +328,9 @@ struct Cut {
 Cut cut_product(int64_t m, int64_t n, int halves, int64_t steps, int tile_cols);
 
 __host__ __device__ inline int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of * of; }
+// Elements from row to row of a matrix in the work buffer: 128 bytes past a multiple of
+// 256, so that a tile's rows are spread over the memory's channels.
+inline int64_t row_of(int64_t cols, size_t elt) { return (whole(cols * elt, 256) + 128) / elt; }
 // CKM_E_UNSUPPORTED for a grid past what a launch counts.
 ckm_status check_blocks(const Cut& c);
 
@@ -350,8 +353,8 @@ struct ResultArgs {
   int32_t tiles_m, tiles_n, halves, steps;   // Cut
 };
 
-// Two results' products share a launch: half h takes b.p[h] (parts is 1 then).
-template <class P>
+// Two results' products share a launch: half h takes b's p or q (parts is 1 then).
+template <class P, bool kSlab>
 __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel(ResultArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
   const P p;
@@ -360,12 +363,15 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel
   tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n * a.halves, tm, tn);
   const int half = tn / a.tiles_n;
   tn -= half * a.tiles_n;
-  if (a.halves == 2) a.p.b.p[0] = a.p.b.p[half];
+  ProductArgs product = a.p;
+  if (half) product.b.p = product.b.q;
   const int all = (a.p.k + P::kStep - 1) / P::kStep * a.p.parts, from = split * a.steps;
   F4 acc[P::kFN][P::kFM];
-  p.run(acc, a.p, tm * P::kM, tn * P::kN, from, min(all, from + a.steps), (LdsChar*)lds);
-  float* slab = a.slab ? a.slab + ((int64_t)split * a.halves + half) * a.p.m * a.ld_slab : nullptr;
-  const float factor = a.alpha ? a.factor * *a.alpha : a.factor;
+  p.run(acc, product, tm * P::kM, tn * P::kN, from, min(all, from + a.steps), (LdsChar*)lds);
+  const float factor = kSlab ? 1.0f : a.alpha ? a.factor * *a.alpha : a.factor;
+  typename P::T* c = (typename P::T*)(half ? a.c[1] : a.c[0]);
+  const int64_t ld_c = half ? a.ld_c[1] : a.ld_c[0];
+  const int64_t row0 = kSlab ? ((int64_t)split * a.halves + half) * a.p.m : 0;
 #pragma unroll
   for (int i = 0; i < P::kFM; ++i) {
     const int m = tm * P::kM + p.row(i);
@@ -373,13 +379,13 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel
 #pragma unroll
     for (int j = 0; j < P::kFN; ++j) {
       const int n = tn * P::kN + p.col(j);
-      if (slab) {   // rows of whole fours
+      if constexpr (kSlab) {   // rows of whole fours
         if (n < a.p.n) {
-          F4* at = (F4*)(slab + (int64_t)m * a.ld_slab + n);
+          F4* at = (F4*)(a.slab + (row0 + m) * a.ld_slab + n);
           *at = a.add ? *at + acc[j][i] : acc[j][i];
         }
       } else {
-        store4((typename P::T*)a.c[half] + (int64_t)m * a.ld_c[half], n, a.p.n, acc[j][i] * factor);
+        store4(c + m * ld_c, n, a.p.n, acc[j][i] * factor);
       }
     }
   }
@@ -396,7 +402,8 @@ void launch_product(ResultArgs a, const Cut& cut, hipStream_t s) {
   a.steps = cut.steps;
   const auto go = [&](auto p) {
     using P = typename decltype(p)::Shape;
-    ckm_product_kernel<P><<<(uint32_t)cut.blocks(), P::kThreads, 0, s>>>(a);
+    if (a.slab) ckm_product_kernel<P, true><<<(uint32_t)cut.blocks(), P::kThreads, 0, s>>>(a);
+    else ckm_product_kernel<P, false><<<(uint32_t)cut.blocks(), P::kThreads, 0, s>>>(a);
   };
   if (cut.rows == 256) go(Tag<Product<T, 256, 256, 2, 4, 2, kAK, kBK, 1>>());
   else go(Tag<Product<T, 128, 128, 2, 2, 2, kAK, kBK, 1>>());

@@ -55,7 +55,7 @@ __global__ void __launch_bounds__(kBlock) ckm_join_kernel(ResultArgs a, int spli
     const float* p = a.slab + half * one + row * a.ld_slab + col;
     F4 sum = *(const F4*)p;
     for (int k = 1; k < splits; ++k) sum += *(const F4*)(p + k * a.halves * one);
-    store4((T*)a.c[half] + row * a.ld_c[half], col, a.p.n, sum * factor);
+    store4((T*)(half ? a.c[1] : a.c[0]) + row * (half ? a.ld_c[1] : a.ld_c[0]), col, a.p.n, sum * factor);
   }
 }
 
