@@ -38,9 +38,11 @@ struct Table {
   Entry e[kTensors];
 };
 
-template <typename F>
+// kBack: the last chunks first, which the sums read last and which are in the caches.
+template <bool kBack, typename F>
 __device__ __forceinline__ void each_chunk(const Table& t, F&& f) {
-  for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+  for (int k = blockIdx.x; k < t.chunks; k += gridDim.x) {
+    const int c = kBack ? t.chunks - 1 - k : k;
     int lo = 0, hi = t.tensors;   // the last entry that starts at or before c
     while (hi - lo > 1) {
       const int mid = (lo + hi) / 2;
@@ -90,7 +92,7 @@ __device__ __forceinline__ double squares(const T* p, int64_t from, int64_t coun
 __global__ void __launch_bounds__(kBlock) ckm_norm_parts_kernel(Table t, double* parts) {
   __shared__ double lds[kBlock / 64];
   double sum = 0.0;
-  each_chunk(t, [&](const Entry& e, int64_t from) {
+  each_chunk<false>(t, [&](const Entry& e, int64_t from) {
     if (e.type == CKM_F32) sum += squares((const float*)e.in, from, e.count);
     else if (e.type == CKM_F16) sum += squares((const _Float16*)e.in, from, e.count);
     else sum += squares((const __bf16*)e.in, from, e.count);
@@ -137,7 +139,7 @@ __global__ void __launch_bounds__(kBlock) ckm_clip_kernel(Table t, const double*
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
   const double f = max_norm / (v + eps);
   const float factor = f > 1.0 ? 1.0f : (float)f;   // NaN stays
-  each_chunk(t, [&](const Entry& e, int64_t from) {
+  each_chunk<true>(t, [&](const Entry& e, int64_t from) {
     if (factor == 1.0f && e.out == e.in) return;
     if (e.type == CKM_F32) scaled<float>(e, from, factor);
     else if (e.type == CKM_F16) scaled<_Float16>(e, from, factor);
@@ -149,13 +151,15 @@ int launches(int64_t tensors) { return (int)((tensors + kTensors - 1) / kTensors
 // Blocks of a launch: a list of many launches leaves fewer sums a launch.
 int most_blocks(int64_t tensors) { return std::max(128, kBlocks / std::max(1, launches(tensors))); }
 
-// Calls f(table, blocks) for each launch; returns the number of blocks.
-template <typename F>
+// Calls f(table, blocks, blocks of the launches before) for each launch, from the last
+// one to the first if kBack; returns the number of blocks.
+template <bool kBack, typename F>
 int each_launch(int64_t count, const ckm_tensor* t, F&& f) {
   const int most = most_blocks(count);
   int blocks = 0;
   Table table;
-  for (int64_t k = 0; k < count; k += kTensors) {
+  for (int64_t at = 0; at < count; at += kTensors) {
+    const int64_t k = kBack ? (count - 1) / kTensors * kTensors - at : at;
     table.tensors = (int32_t)std::min<int64_t>(kTensors, count - k);
     int64_t chunks = 0;
     int used = 0;
@@ -236,7 +240,7 @@ ckm_status check_parts(int64_t count, void* work, size_t work_bytes) {
 }
 
 int launch_parts(int64_t count, const ckm_tensor* t, double* parts, hipStream_t s) {
-  return each_launch(count, t, [&](const Table& table, int blocks, int before) {
+  return each_launch<false>(count, t, [&](const Table& table, int blocks, int before) {
     ckm_norm_parts_kernel<<<blocks, kBlock, 0, s>>>(table, parts + before);
   });
 }
@@ -282,7 +286,7 @@ extern "C" ckm_status ckm_clip_async(int64_t count, const ckm_tensor* tensors, d
     if (n == 0) {
       ckm_norm_join_kernel<<<1, kBlock, 0, s>>>(parts, 0, d_norm);
     } else {
-      each_launch(count, tensors, [&](const Table& table, int blocks, int before) {
+      each_launch<true>(count, tensors, [&](const Table& table, int blocks, int before) {
         ckm_clip_kernel<<<blocks, kBlock, 0, s>>>(table, parts, n, max_norm, eps, before == 0 ? d_norm : nullptr);
       });
     }

@@ -25,13 +25,14 @@ namespace {
 
 constexpr float kLog2e = 1.44269504f;
 constexpr float kLog2eRest = 1.92596299e-8f;   // log2(e) = the sum of both
+constexpr float kLn2 = 0.693147182f, kLn2Rest = -1.90465429e-9f;   // ln 2 = the sum of both
 constexpr float kHalfGain = 32768.0f;          // binary16's factor
 
 struct LossArgs {
   ProductArgs p;            // n: of the vocabulary, or of a piece of it
   int32_t tiles_m, tiles_n;
   const int64_t* targets;
-  float2* parts;            // [rows][tiles_n]: largest logit, sum of exponentials
+  float2* parts;            // [rows][tiles_n]: base and sum of exponentials (join_parts)
   float* hit;               // [rows]: the target's logit
   float* loss;
   float* lse;               // written, or the gradient's input
@@ -42,16 +43,33 @@ struct LossArgs {
   int64_t vocab;
 };
 
-// e^v for v <= 0 or so, to a few units in the last place: 2^(v log2 e) with what the product loses.
-__device__ __forceinline__ float exp_of(float v) {
-  const float t = v * kLog2e;
-  const float rest = fmaf(v, kLog2eRest, fmaf(v, kLog2e, -t));
-  const float e = __builtin_amdgcn_exp2f(t);
-  return t > -126.0f && t < 126.0f ? fmaf(e, rest * 0.69314718f, e) : e;
+// (base, sum): sum 2^base of exponentials, whose largest is about 2^base; sum 0: none.
+__device__ __forceinline__ float2 join_parts(float2 p, float2 q) {
+  if (q.y == 0.0f) return p;
+  if (p.y == 0.0f) return q;
+  const float base = fmaxf(p.x, q.x);   // a NaN is in the sums too
+  return make_float2(base, p.y * __builtin_amdgcn_exp2f(p.x - base) + q.y * __builtin_amdgcn_exp2f(q.x - base));
+}
+
+// 2^(v log2 e - base) for v log2 e - base <= 0 or so. With binary32 tensors the products'
+// roundings are made good; with 16-bit ones they are below what the operands' own
+// rounding leaves of v, and `base`, rounded once a row, is what the logarithm adds again.
+template <typename T>
+__device__ __forceinline__ float power_of(float v, float base) {
+  if constexpr (std::is_same<T, float>::value) {
+    const float u = v * kLog2e, rest = fmaf(v, kLog2eRest, fmaf(v, kLog2e, -u));
+    const float w = u - base, back = w - u;
+    const float lost = ((u - (w - back)) - (base + back)) + rest;   // of the difference, and of the product
+    const float e = __builtin_amdgcn_exp2f(w);
+    return w > -126.0f && w < 126.0f ? fmaf(e, lost * kLn2, e) : e;
+  } else {
+    return __builtin_amdgcn_exp2f(fmaf(v, kLog2e, -base));
+  }
 }
 
 template <class P>
 __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_kernel(LossArgs a) {
+  using T = typename P::T;
   __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
   const P p;
   int tm, tn;
@@ -59,48 +77,53 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_kernel(Lo
   F4 acc[P::kFN][P::kFM];
   p.run(acc, a.p, tm * P::kM, tn * P::kN, 0, (a.p.k + P::kStep - 1) / P::kStep, (LdsChar*)lds);
   float2* joined = (float2*)lds;   // [waves of n][rows of the tile]
-#pragma unroll
-  for (int i = 0; i < P::kFM; ++i) {
-    const int m = tm * P::kM + p.row(i);
-    const int64_t target = m < a.p.m ? a.targets[m] : -1;
-    float most = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < P::kFN; ++j)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const int n = tn * P::kN + p.col(j) + k;
-        if (n < a.p.n) {
-          most = fmaxf(most, acc[j][i][k]);
-          if (n == target) a.hit[m] = acc[j][i][k];
-        }
-      }
-    // the four lanes that hold a row
-    most = fmaxf(most, __shfl_xor(most, 16));
-    most = fmaxf(most, __shfl_xor(most, 32));
-    const float base = most == -INFINITY ? 0.0f : most;
-    float sum = 0.0f;
+  if (a.p.n - tn * P::kN < P::kN) {   // columns past the vocabulary count for nothing
 #pragma unroll
     for (int j = 0; j < P::kFN; ++j)
 #pragma unroll
       for (int k = 0; k < 4; ++k)
-        if (tn * P::kN + p.col(j) + k < a.p.n) sum += exp_of(acc[j][i][k] - base);
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (p.lane < 16) joined[p.wn * P::kM + p.row(i)] = make_float2(most, sum);
+        if (tn * P::kN + p.col(j) + k >= a.p.n)
+#pragma unroll
+          for (int i = 0; i < P::kFM; ++i) acc[j][i][k] = -INFINITY;
+  }
+#pragma unroll
+  for (int i = 0; i < P::kFM; ++i) {
+    const int m = tm * P::kM + p.row(i);
+    const int64_t target = m < a.p.m ? a.targets[m] - (int64_t)tn * P::kN : -1;   // within the tile
+    if (target >= 0 && target < P::kN && target < a.p.n - tn * P::kN) {
+#pragma unroll
+      for (int j = 0; j < P::kFN; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (p.col(j) + k == (int)target) a.hit[m] = acc[j][i][k];
+    }
+    float most = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < P::kFN; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) most = fmaxf(most, acc[j][i][k]);
+    // the four lanes that hold a row
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    const float base = most == -INFINITY ? 0.0f : most * kLog2e;
+    float sum[4] = {};
+#pragma unroll
+    for (int j = 0; j < P::kFN; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum[k] += power_of<T>(acc[j][i][k], base);
+    float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    all += __shfl_xor(all, 16);
+    all += __shfl_xor(all, 32);
+    if (p.lane < 16) joined[p.wn * P::kM + p.row(i)] = make_float2(base, all);
   }
   __syncthreads();
   for (int r = threadIdx.x; r < P::kM; r += P::kThreads) {
     const int m = tm * P::kM + r;
     if (m >= a.p.m) continue;
-    float most = joined[r].x;
+    float2 v = joined[r];
 #pragma unroll
-    for (int w = 1; w < P::kWavesN; ++w) most = fmaxf(most, joined[w * P::kM + r].x);
-    const float base = most == -INFINITY ? 0.0f : most;
-    float sum = 0.0f;
-#pragma unroll
-    for (int w = 0; w < P::kWavesN; ++w)
-      sum += joined[w * P::kM + r].y * (joined[w * P::kM + r].x == -INFINITY ? 1.0f : exp_of(joined[w * P::kM + r].x - base));
-    a.parts[(int64_t)m * a.tiles_n + tn] = make_float2(most, sum);
+    for (int w = 1; w < P::kWavesN; ++w) v = join_parts(v, joined[w * P::kM + r]);
+    a.parts[(int64_t)m * a.tiles_n + tn] = v;
   }
 }
 
@@ -110,18 +133,18 @@ __global__ void __launch_bounds__(256) ckm_loss_join_kernel(LossArgs a) {
   const int lane = threadIdx.x & 63;
   if (row >= a.p.m) return;
   const float2* parts = a.parts + row * a.tiles_n;
-  float most = -INFINITY;
-  for (int k = lane; k < a.tiles_n; k += 64) most = fmaxf(most, parts[k].x);
-  most = reduce64<OpMax>(most);
-  const float base = most == -INFINITY ? 0.0f : most;
-  float sum = 0.0f;
+  float base = -INFINITY, sum = 0.0f;
+  for (int k = lane; k < a.tiles_n; k += 64) base = fmaxf(base, parts[k].y == 0.0f ? -INFINITY : parts[k].x);
+  base = reduce64<OpMax>(base);
+  if (base == -INFINITY) base = 0.0f;
   for (int k = lane; k < a.tiles_n; k += 64) {
     const float2 v = parts[k];
-    sum += v.y * (v.x == -INFINITY ? 1.0f : exp_of(v.x - base));
+    if (v.y != 0.0f) sum += v.y * __builtin_amdgcn_exp2f(v.x - base);
   }
   sum = reduce64<OpSum>(sum);
   if (lane == 0) {
-    const float lse = base + logf(sum);
+    // (base + log2 sum) ln 2, the product with what base's loses
+    const float t = base * kLn2, lse = t + (fmaf(base, kLn2, -t) + fmaf(base, kLn2Rest, logf(sum)));
     const int64_t target = a.targets[row];
     if (a.lse) a.lse[row] = lse;
     if (a.loss) a.loss[row] = target >= 0 && target < a.vocab ? lse - a.hit[row] : 0.0f;
@@ -153,39 +176,55 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_back_kern
 #pragma unroll
   for (int i = 0; i < P::kFM; ++i) {
     const int m = tm * P::kM + p.row(i);
-    if (m >= a.p.m) continue;
-    int64_t target = a.targets[m];
+    const bool live = m < a.p.m;
+    int64_t target = live ? a.targets[m] : -1;
     const bool some = target >= 0 && target < a.vocab;
-    target -= a.first;
-    const float lse = a.lse[m];
-    float by = a.dloss[m];
+    target -= a.first + (int64_t)tn * P::kN;   // within the tile
+    const float base = live ? a.lse[m] * kLog2e : 0.0f;
+    float by = some ? a.dloss[m] : 0.0f;
     if constexpr (std::is_same<T, _Float16>::value) by = by / *a.most * kHalfGain;
 #pragma unroll
-    for (int j = 0; j < P::kFN; ++j) {
-      const int n = tn * P::kN + p.col(j);
-      F4 v;
+    for (int j = 0; j < P::kFN; ++j)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const float e = exp_of(acc[j][i][k] - lse);
-        v[k] = some && n + k < a.p.n ? (n + k == target ? e - 1.0f : e) * by : 0.0f;
+        float e;
+        if constexpr (std::is_same<T, float>::value) e = expf(acc[j][i][k] - (live ? a.lse[m] : 0.0f));
+        else e = power_of<T>(acc[j][i][k], base);
+        acc[j][i][k] = some ? e * by : 0.0f;
       }
-      store4((T*)a.d + (int64_t)m * a.ld_d, n, width, v);
+    if (some && target >= 0 && target < P::kN) {
+#pragma unroll
+      for (int j = 0; j < P::kFN; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (p.col(j) + k == (int)target) acc[j][i][k] -= by;
     }
   }
+  if (a.p.n - tn * P::kN < P::kN) {
+#pragma unroll
+    for (int j = 0; j < P::kFN; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (tn * P::kN + p.col(j) + k >= a.p.n)
+#pragma unroll
+          for (int i = 0; i < P::kFM; ++i) acc[j][i][k] = 0.0f;
+  }
+  p.each8(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[1][8]) {
+    const int m = tm * P::kM + row, n = tn * P::kN + col;
+    if (m < a.p.m && n < width) store_part<false>((T*)a.d + m * a.ld_d, rounded8<T>(v[0]), n, width);
+  });
 }
 
 template <typename T, bool kBack>
 void launch_logits(LossArgs a, const Cut& cut, hipStream_t s) {
   a.tiles_m = cut.tiles_m;
   a.tiles_n = cut.tiles_n;
-  const auto go = [&](auto p) {
+  with_shape<T, true, true, 1>(cut, [&](auto p) {
     using P = typename decltype(p)::Shape;
     const uint32_t blocks = (uint32_t)(cut.tiles_m * cut.tiles_n);
     if constexpr (kBack) ckm_loss_back_kernel<P><<<blocks, P::kThreads, 0, s>>>(a);
     else ckm_loss_kernel<P><<<blocks, P::kThreads, 0, s>>>(a);
-  };
-  if (cut.rows == 256) go(Tag<Product<T, 256, 256, 2, 4, 2, true, true, 1>>());
-  else go(Tag<Product<T, 128, 128, 2, 2, 2, true, true, 1>>());
+  });
 }
 
 // Bytes of a piece's d: what stays in the caches between its writer and its readers;
@@ -219,21 +258,27 @@ LossPlan plan_of(int type, const ckm_vocab& c, bool back) {
   };
   if (p.pack_x) p.x = take(c.rows * p.ld_x * elt);
   if (p.pack_w) p.w = take(c.vocab * p.ld_w * elt);
+  const int64_t steps = (c.hidden + step - 1) / step, x_bytes = c.rows * c.hidden * elt;
+  const auto logits = [&](int64_t n) {
+    return cut_product(type, c.rows, n, 1, 1, steps, x_bytes + n * c.hidden * (int64_t)elt, false, true);
+  };
   if (!back) {
-    p.logits = cut_product(c.rows, c.vocab, 1, 1, 0);
+    p.logits = logits(c.vocab);
     p.parts = take((size_t)c.rows * p.logits.tiles_n * sizeof(float2));
     p.hit = take(c.rows * sizeof(float));
   } else {
     p.piece = std::min(c.vocab, std::max(kLeastPiece, kPieceBytes / (int64_t)(c.rows * elt) / 256 * 256));
-    p.logits = cut_product(c.rows, p.piece, 1, 1, 0);
+    p.logits = logits(p.piece);
     const int64_t tail = c.vocab - (c.vocab - 1) / p.piece * p.piece;
-    p.last = cut_product(c.rows, tail, 1, 1, 0);
-    p.dx = cut_product(c.rows, c.hidden, 1, (p.piece + step - 1) / step, 0);
-    p.dw = cut_product(p.piece, c.hidden, 1, (c.rows + step - 1) / step, 0);
+    p.last = logits(tail);
+    const int64_t w_bytes = p.piece * c.hidden * elt, d_bytes = p.piece * c.rows * elt;
+    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, (p.piece + step - 1) / step, d_bytes + w_bytes, true, true);
+    p.dw = cut_product(type, p.piece, c.hidden, 1, 1, (c.rows + step - 1) / step, d_bytes + x_bytes + w_bytes, true,
+                       false);
     p.most = take(sizeof(float));
     p.d = take((size_t)c.rows * row_of(p.piece, elt) * elt);
-    if (p.dx.splits > 1 || p.piece < c.vocab) p.slab = take((size_t)p.dx.splits * c.rows * whole(c.hidden, 4) * 4);
-    if (p.dw.splits > 1) p.dw_slab = take((size_t)p.dw.splits * p.piece * whole(c.hidden, 4) * 4);
+    if (p.dx.splits > 1 || p.piece < c.vocab) p.slab = take((size_t)p.dx.splits * c.rows * whole(c.hidden, 8) * 4);
+    if (p.dw.splits > 1) p.dw_slab = take((size_t)p.dw.splits * p.piece * whole(c.hidden, 8) * 4);
   }
   p.total = at;
   return p;
@@ -244,12 +289,19 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
                  float* lse, void* dx, int64_t ld_dx, void* dw, int64_t ld_dw, char* work, hipStream_t s) {
   const T *x = (const T*)c.d_x, *w = (const T*)c.d_weight;
   if (plan.pack_x) {
-    launch_pack(type, x, c.rows, c.hidden, c.ld_x, work + plan.x, plan.ld_x, s, back ? c.d_targets : nullptr,
-                c.vocab);
+    PackArgs one = {};
+    if (back) {
+      one.targets = c.d_targets;
+      one.vocab = c.vocab;
+    }
+    one.add(x, c.rows, c.hidden, c.ld_x, work + plan.x, plan.ld_x);
+    launch_pack(type, one, s);
     x = (const T*)(work + plan.x);
   }
   if (plan.pack_w) {
-    launch_pack(type, w, c.vocab, c.hidden, c.ld_weight, work + plan.w, plan.ld_w, s);
+    PackArgs one = {};
+    one.add(w, c.vocab, c.hidden, c.ld_weight, work + plan.w, plan.ld_w);
+    launch_pack(type, one, s);
     w = (const T*)(work + plan.w);
   }
   LossArgs a = {};
@@ -280,7 +332,7 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
   rx.factor = rw.factor = kHalf ? 1.0f / kHalfGain : 1.0f;
   const bool slab = plan.dx.splits > 1 || plan.piece < c.vocab;
   if (slab) rx.slab = (float*)(work + plan.slab);
-  rx.ld_slab = rw.ld_slab = whole(c.hidden, 4);
+  rx.ld_slab = rw.ld_slab = whole(c.hidden, 8);
   rx.c[0] = dx;
   rx.ld_c[0] = ld_dx;
   rx.halves = rw.halves = 1;

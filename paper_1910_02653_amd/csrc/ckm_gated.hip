@@ -35,47 +35,80 @@ struct GatedArgs {
   int64_t ld_slab;
 };
 
-// act(z) and its derivative.
+// act(z) and its derivative. For 16-bit results, whose rounding is far above: the
+// logistic function by the hardware's 2^x and 1 / x (some 2^-21), and the normal
+// distribution's as e^(-z^2 / 2) t q(t) of its lower side, t = 1 / (1 + 0.44 |z| / sqrt
+// 2), q a polynomial fitted to erfc(x) e^(x^2) / 2 (relative error below 2e-7, x up to 14).
 template <typename T>
 __device__ __forceinline__ void activation(int act, float z, float& a, float& da) {
+  constexpr bool kFull = std::is_same<T, float>::value;
   if (act == CKM_ACT_SILU) {
-    float s;
-    if constexpr (std::is_same<T, float>::value) {
-      s = 1.0f / (1.0f + expf(-z));
-    } else {   // to some 2^-21: the product's rounding to 16 bits is far above
-      s = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
-    }
+    const float s = kFull ? 1.0f / (1.0f + expf(-z))
+                          : __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
     a = z * s;
     da = s * (1.0f + z * (1.0f - s));
   } else if (act == CKM_ACT_GELU) {
-    const float c = 0.5f * (1.0f + erff(z * 0.70710678f));
+    float c, e;
+    if constexpr (kFull) {
+      c = 0.5f * erfcf(z * -0.70710678f);
+      e = expf(-0.5f * z * z);
+    } else {
+      const float t = __builtin_amdgcn_rcpf(fmaf(0.31112698f, fabsf(z), 1.0f));
+      e = __builtin_amdgcn_exp2f(-0.72134752f * z * z);
+      float q = 0.035749969f;
+      q = fmaf(q, t, -0.13957664f);
+      q = fmaf(q, t, 0.14943397f);
+      q = fmaf(q, t, -0.011147469f);
+      q = fmaf(q, t, 0.10849696f);
+      q = fmaf(q, t, 0.10846730f);
+      q = fmaf(q, t, 0.12446772f);
+      q = fmaf(q, t, 0.12410826f);
+      c = q * t * e;
+      c = z < 0.0f ? c : 1.0f - c;
+    }
     a = z * c;
-    da = c + z * (0.39894228f * expf(-0.5f * z * z));
+    da = c + z * (0.39894228f * e);
   } else {
     a = z > 0.0f ? z : z != z ? z : 0.0f;
     da = z > 0.0f ? 1.0f : z != z ? z : 0.0f;
   }
 }
 
-template <typename T>
-__device__ __forceinline__ F4 gated4(int act, F4 g, F4 u) {
-  F4 h;
+template <typename T, int kCount>
+__device__ __forceinline__ void gated_of(int act, float (&g)[kCount], const float (&u)[kCount]) {   // h in g's place
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < kCount; ++k) {
     float a, da;
     activation<T>(act, g[k], a, da);
-    h[k] = a * u[k];
+    g[k] = a * u[k];
   }
-  return h;
 }
-template <typename T>
-__device__ __forceinline__ void gated4_back(int act, F4 dh, F4& g, F4& u) {   // dg, du in their places
+template <typename T, int kCount>
+__device__ __forceinline__ void gated_back_of(int act, const Raw8<T>& dh, float (&g)[kCount], float (&u)[kCount]) {   // dg, du
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
+  for (int k = 0; k < kCount; ++k) {
     float a, da;
     activation<T>(act, g[k], a, da);
-    g[k] = dh[k] * u[k] * da;
-    u[k] = dh[k] * a;
+    const float d = (float)dh.get(k);
+    g[k] = d * u[k] * da;
+    u[k] = d * a;
+  }
+}
+
+// What becomes of eight columns of g and u.
+template <typename T, int kMode>
+__device__ __forceinline__ void finish(const GatedArgs& a, int64_t m, int n, float (&g)[8], float (&u)[8]) {
+  if constexpr (kMode == kForward) {
+    if (n >= a.p.n) return;
+    gated_of<T>(a.act, g, u);
+    store_part<false>((T*)a.out + m * a.ld_out, rounded8<T>(g), n, a.p.n);
+  } else {   // zeros to the end of dg's last group
+    if (n >= a.up) return;
+    const int left = a.p.n - n;
+    gated_back_of<T>(a.act, load_left((const T*)a.dh + m * a.ld_dh + n, left), g, u);
+    T* row = (T*)a.out + m * a.ld_out;
+    store_part<false>(row, rounded8<T>(g), n, a.up);
+    store_part<false>(row + a.up, rounded8<T>(u), n, a.up);
   }
 }
 
@@ -90,56 +123,43 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(G
   const int all = (a.p.k + P::kStep - 1) / P::kStep, from = split * a.steps;
   F4 acc[P::kFN][P::kFM];
   p.run(acc, a.p, tm * P::kM, tn * P::kSubN, from, min(all, from + a.steps), (LdsChar*)lds);
+  p.each8(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[2][8]) {
+    const int m = tm * P::kM + row, n = tn * P::kSubN + col;
+    if (m >= a.p.m) return;
+    if constexpr (kMode != kShares) {
+      finish<T, kMode>(a, m, n, v[0], v[1]);
+    } else if (n < a.p.n) {
 #pragma unroll
-  for (int i = 0; i < P::kFM; ++i) {
-    const int m = tm * P::kM + p.row(i);
-    if (m >= a.p.m) continue;
-#pragma unroll
-    for (int j = 0; j < P::kFS; ++j) {
-      const int n = tn * P::kSubN + p.col(j);
-      F4 g = acc[j][i], u = acc[j + P::kFS][i];
-      if constexpr (kMode == kForward) {
-        store4((T*)a.out + m * a.ld_out, n, a.p.n, gated4<T>(a.act, g, u));
-      } else if constexpr (kMode == kBackward) {
-        gated4_back<T>(a.act, read4((const T*)a.dh + m * a.ld_dh, n, a.p.n), g, u);
-        T* row = (T*)a.out + m * a.ld_out;
-        store4(row, n, a.up, g);
-        store4(row + a.up, n, a.up, u);
-      } else if (n < a.p.n) {
-        float* at = a.slab + ((int64_t)split * 2 * a.p.m + m) * a.ld_slab + n;
-        *(F4*)at = g;
-        *(F4*)(at + a.p.m * a.ld_slab) = u;
+      for (int s = 0; s < 2; ++s) {
+        F4* at = (F4*)(a.slab + (((int64_t)split * 2 + s) * a.p.m + m) * a.ld_slab + n);
+        at[0] = F4{v[s][0], v[s][1], v[s][2], v[s][3]};
+        at[1] = F4{v[s][4], v[s][5], v[s][6], v[s][7]};
       }
     }
-  }
+  });
 }
 
 // The shares of g and u added in their order, and what kMode makes of them; a thread
-// four columns.
+// eight columns.
 template <typename T, int kMode>
-__global__ void __launch_bounds__(256) ckm_gated_join_kernel(GatedArgs a, int splits, int64_t total, uint32_t fours) {
+__global__ void __launch_bounds__(256) ckm_gated_join_kernel(GatedArgs a, int splits, int64_t total, uint32_t eights) {
   const int64_t one = (int64_t)a.p.m * a.ld_slab;
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
-    const int64_t m = at / fours;
-    const int n = (int)(at - m * fours) * 4;
-    F4 g = {0.0f, 0.0f, 0.0f, 0.0f}, u = g;
-    if (n < a.p.n) {
-      const float* p = a.slab + m * a.ld_slab + n;
-      g = *(const F4*)p;
-      u = *(const F4*)(p + one);
+    const int64_t m = at / eights;
+    const int n = (int)(at - m * eights) * 8;
+    float v[2][8];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const float* p = a.slab + s * one + m * a.ld_slab + n;
+      F4 x = ((const F4*)p)[0], y = ((const F4*)p)[1];
       for (int k = 1; k < splits; ++k) {
-        g += *(const F4*)(p + 2 * k * one);
-        u += *(const F4*)(p + (2 * k + 1) * one);
+        x += ((const F4*)(p + 2 * k * one))[0];
+        y += ((const F4*)(p + 2 * k * one))[1];
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[s][k] = x[k], v[s][k + 4] = y[k];
     }
-    if constexpr (kMode == kForward) {
-      store4((T*)a.out + m * a.ld_out, n, a.p.n, gated4<T>(a.act, g, u));
-    } else {
-      gated4_back<T>(a.act, read4((const T*)a.dh + m * a.ld_dh, n, a.p.n), g, u);
-      T* row = (T*)a.out + m * a.ld_out;
-      store4(row, n, a.up, g);
-      store4(row + a.up, n, a.up, u);
-    }
+    finish<T, kMode>(a, m, n, v[0], v[1]);
   }
 }
 
@@ -148,19 +168,17 @@ void launch_both(GatedArgs a, const Cut& cut, hipStream_t s) {
   a.tiles_m = cut.tiles_m;
   a.tiles_n = cut.tiles_n;
   a.steps = cut.steps;
-  const auto go = [&](auto p) {
+  with_shape<T, true, false, 2>(cut, [&](auto p) {
     using P = typename decltype(p)::Shape;
     const uint32_t blocks = (uint32_t)cut.blocks();
     if (cut.splits > 1) ckm_gated_kernel<P, kShares><<<blocks, P::kThreads, 0, s>>>(a);
     else ckm_gated_kernel<P, kMode><<<blocks, P::kThreads, 0, s>>>(a);
-  };
-  if (cut.rows == 256) go(Tag<Product<T, 256, 256, 2, 4, 2, true, false, 2>>());
-  else go(Tag<Product<T, 128, 128, 2, 2, 2, true, false, 2>>());
+  });
   if (cut.splits > 1) {
-    const uint32_t fours = (uint32_t)(((kMode == kForward ? a.p.n : a.up) + 3) / 4);
-    const int64_t total = a.p.m * (int64_t)fours;
+    const uint32_t eights = (uint32_t)((a.p.n + 7) / 8);
+    const int64_t total = a.p.m * (int64_t)eights;
     ckm_gated_join_kernel<T, kMode><<<(uint32_t)std::min<int64_t>((total + 255) / 256, 1 << 16), 256, 0, s>>>(
-        a, cut.splits, total, fours);
+        a, cut.splits, total, eights);
   }
 }
 
@@ -185,9 +203,8 @@ GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
   p.ld_x = p.pack_x || c.rows == 1 ? whole(c.hidden, group) : c.ld_x;   // a single row may have any stride
   p.ld_w = p.pack_w || c.hidden == 1 ? p.inner : c.ld_gate;
   const int64_t steps_h = (c.hidden + step - 1) / step, steps_f = (c.inner + step - 1) / step;
-  p.both = cut_product(c.rows, 2 * c.inner, 1, steps_h, 0);
-  p.both.cols /= 2;
-  p.both.tiles_n = (int)((c.inner + p.both.cols - 1) / p.both.cols);
+  const int64_t x_bytes = c.rows * c.hidden * elt, w_bytes = 2 * c.hidden * c.inner * elt, h_bytes = c.rows * c.inner * elt;
+  p.both = cut_product(type, c.rows, c.inner, 1, 2, steps_h, x_bytes + w_bytes, true, true);
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -196,13 +213,14 @@ GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
   };
   if (p.pack_x) p.x = take(c.rows * p.ld_x * elt);
   if (p.pack_w) p.w = take(2 * c.hidden * p.ld_w * elt);
-  size_t slab = p.both.splits > 1 ? (size_t)p.both.splits * 2 * c.rows * whole(c.inner, 4) * 4 : 0;
+  size_t slab = p.both.splits > 1 ? (size_t)p.both.splits * 2 * c.rows * whole(c.inner, 8) * 4 : 0;
   if (back) {
-    p.dx = cut_product(c.rows, c.hidden, 1, 2 * steps_f, 0);
-    p.dw = cut_product(c.hidden, c.inner, 2, (c.rows + step - 1) / step, 0);
+    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, 2 * steps_f, 2 * h_bytes + w_bytes, true, true);
+    p.dw = cut_product(type, c.hidden, c.inner, 2, 1, (c.rows + step - 1) / step, x_bytes + 2 * h_bytes + w_bytes, true,
+                       false);
     p.d = take(c.rows * p.ld_d * elt);
-    if (p.dx.splits > 1) slab = std::max(slab, (size_t)p.dx.splits * c.rows * whole(c.hidden, 4) * 4);
-    if (p.dw.splits > 1) slab = std::max(slab, (size_t)p.dw.splits * 2 * c.hidden * whole(c.inner, 4) * 4);
+    if (p.dx.splits > 1) slab = std::max(slab, (size_t)p.dx.splits * c.rows * whole(c.hidden, 8) * 4);
+    if (p.dw.splits > 1) slab = std::max(slab, (size_t)p.dw.splits * 2 * c.hidden * whole(c.inner, 8) * 4);
   }
   p.slab = take(slab);
   p.total = at;
@@ -214,17 +232,19 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
                   int64_t ld_out, void* dgate, int64_t ld_dgate, void* dup, int64_t ld_dup, char* work, hipStream_t s) {
   const bool back = dh != nullptr;
   const void *x = c.d_x, *wg = c.d_gate, *wu = c.d_up;
+  PackArgs packs = {};
   if (plan.pack_x) {
-    launch_pack(type, x, c.rows, c.hidden, c.ld_x, work + plan.x, plan.ld_x, s);
+    packs.add(x, c.rows, c.hidden, c.ld_x, work + plan.x, plan.ld_x);
     x = work + plan.x;
   }
   if (plan.pack_w) {
     T* to = (T*)(work + plan.w);
-    launch_pack(type, wg, c.hidden, c.inner, c.ld_gate, to, plan.ld_w, s);
-    launch_pack(type, wu, c.hidden, c.inner, c.ld_up, to + c.hidden * plan.ld_w, plan.ld_w, s);
+    packs.add(wg, c.hidden, c.inner, c.ld_gate, to, plan.ld_w);
+    packs.add(wu, c.hidden, c.inner, c.ld_up, to + c.hidden * plan.ld_w, plan.ld_w);
     wg = to;
     wu = to + c.hidden * plan.ld_w;
   }
+  launch_pack(type, packs, s);
   float* slab = (float*)(work + plan.slab);
   GatedArgs a = {};
   a.p = {{x, x, plan.ld_x}, {wg, wu, plan.ld_w}, (int32_t)c.rows, (int32_t)c.inner, (int32_t)c.hidden, 1};
@@ -232,7 +252,7 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
   a.dh = dh;
   a.ld_dh = ld_dh;
   a.slab = slab;
-  a.ld_slab = whole(c.inner, 4);
+  a.ld_slab = whole(c.inner, 8);
   if (!back) {
     a.out = out;
     a.ld_out = ld_out;
@@ -253,7 +273,7 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
     r.factor = 1.0f;
     r.halves = 1;
     if (plan.dx.splits > 1) r.slab = slab;
-    r.ld_slab = whole(c.hidden, 4);
+    r.ld_slab = whole(c.hidden, 8);
     launch_product<T, true, true>(r, plan.dx, s);
     if (plan.dx.splits > 1) launch_join(type, r, plan.dx.splits, s);
   }
@@ -268,7 +288,7 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
     r.factor = 1.0f;
     r.halves = 2;
     if (plan.dw.splits > 1) r.slab = slab;
-    r.ld_slab = whole(c.inner, 4);
+    r.ld_slab = whole(c.inner, 8);
     launch_product<T, false, false>(r, plan.dw, s);
     if (plan.dw.splits > 1) launch_join(type, r, plan.dw.splits, s);
   }

@@ -84,24 +84,30 @@ struct TileLoad {
     }
   }
 
-  // Starts the loads of one step: `base` the tile's first element, `valid` rows
-  // (along k) or columns of the tile that are there, `left` the k that are left.
-  __device__ __forceinline__ void issue(const char* base, int64_t ld, int valid, int left, uint32_t lds, int wave) const {
+  // The loads of one step: `base` the tile's first element, `valid` rows (along k) or
+  // columns of the tile that are there, `left` the k that are left.
+  struct Step {
+    I4 rsrc;        // of a buffer that ends where the tile does: what is loaded past it is zero
+    int left;
+    uint32_t lds;   // where to
+  };
+  __device__ __forceinline__ Step step(const char* base, int64_t ld, int valid, int left, uint32_t lds) const {
     const int64_t row = ld * kElt;
     const int have = min(left, kStep);
     // whole groups along k (what follows the row's end in its last one is zero or not there); across k whole words
     const int64_t range = have <= 0 ? 0 : kAlongK ? (min(valid, kRows) - 1) * row + ((have * kElt + 15) & ~15)
                                                   : (have - 1) * row + ((min(valid, kRows) * kElt + 3) & ~3);
-    const I4 rsrc = {__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)base),
-                     __builtin_amdgcn_readfirstlane((int)(uint32_t)((uintptr_t)base >> 32)),
-                     __builtin_amdgcn_readfirstlane((int)range), 0x00020000};
-#pragma unroll
-    for (int t = 0; t < kPer; ++t) {
-      const uint32_t o = kAlongK && (int)kpos >= left ? kNowhere : off[t];
-      const uint32_t to = __builtin_amdgcn_readfirstlane(lds + (wave * kPer + t) % kLoads * 1024);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                   ::"s"(to), "v"(o), "s"(rsrc) : "memory");
-    }
+    return {{__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)base),
+             __builtin_amdgcn_readfirstlane((int)(uint32_t)((uintptr_t)base >> 32)),
+             __builtin_amdgcn_readfirstlane((int)range), 0x00020000},
+            left, lds};
+  }
+  // Load t of a wave's kPer. The compiler does not know of it: the product waits by count.
+  __device__ __forceinline__ void load(const Step& s, int t, int wave) const {
+    const uint32_t o = kAlongK && (int)kpos >= s.left ? kNowhere : off[t];
+    const uint32_t to = __builtin_amdgcn_readfirstlane(s.lds + (wave * kPer + t) % kLoads * 1024);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 ::"s"(to), "v"(o), "s"(s.rsrc) : "memory");
   }
 };
 
@@ -196,6 +202,44 @@ struct Product {
   __device__ __forceinline__ int row(int i) const { return (wm * kFM + i) * 16 + (lane & 15); }
   __device__ __forceinline__ int col(int j) const { return (wn * kFS + j % kFS) * 16 + (lane >> 4) * 4; }
 
+  // Calls f(row, column, v[kSubs][8]) for every eight consecutive columns of the tile's
+  // rows (of each matrix's, for kSubs = 2), which a wave's lanes have side by side: the
+  // sums go through LDS, each wave's by itself. Stores of the four columns that a lane
+  // has in registers touch 16 rows in 32 bytes each, and cost a tile 10 us.
+  template <typename F>
+  __device__ __forceinline__ void each8(const F4 (&acc)[kFN][kFM], LdsChar* lds, F&& f) const {
+    typedef __attribute__((address_space(3))) F4 LdsF4;
+    constexpr int kRow = kFN * 64, kRoom = kLds / kWaves;   // bytes of a row, of a wave
+    constexpr int kFit = kRoom / (16 * kRow), kLanes = kFS * 2;   // fragments that fit
+    constexpr int kPass = kFit >= kFM ? kFM : kFit >= 4 ? 4 : kFit >= 2 ? 2 : 1;
+    static_assert(kFit >= 1 && kFM % kPass == 0, "");
+    LdsChar* room = lds + wave * kRoom;
+    // groups of 16 bytes permuted against meetings in a bank
+    constexpr int kTurn = kRow < 128 ? kRow / 16 - 1 : 7;
+    const auto at = [&](int r, int group) { return (LdsF4*)(room + r * kRow + ((group ^ (r & kTurn)) * 16)); };
+#pragma unroll
+    for (int i0 = 0; i0 < kFM; i0 += kPass) {
+#pragma unroll
+      for (int i = 0; i < kPass; ++i)
+#pragma unroll
+        for (int j = 0; j < kFN; ++j) *at(i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[j][i0 + i];
+      constexpr int kEights = kPass * 16 * kLanes;
+#pragma unroll
+      for (int t = 0; t < (kEights + 63) / 64; ++t) {
+        if (kEights % 64 != 0 && t * 64 + lane >= kEights) break;
+        const int r = (t * 64 + lane) / kLanes, q = lane % kLanes;
+        float v[kSubs][8];
+#pragma unroll
+        for (int s = 0; s < kSubs; ++s) {
+          const F4 x = *at(r, s * kFS * 4 + 2 * q), y = *at(r, s * kFS * 4 + 2 * q + 1);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[s][k] = x[k], v[s][k + 4] = y[k];
+        }
+        f((wm * kFM + i0) * 16 + r, wn * kFS * 16 + 8 * q, v);
+      }
+    }
+  }
+
   // The tile from (m0, n0) on over steps [step0, step1) of k; every wave has passed
   // its last read of `lds` when this returns, and no load is under way.
   __device__ __forceinline__ void run(F4 (&acc)[kFN][kFM], const ProductArgs& a, int m0, int n0, int step0, int step1,
@@ -207,18 +251,29 @@ struct Product {
     lb.init(wave, lane, a.b.ld, validn);
     const int per = (a.k + kStep - 1) / kStep;   // steps of a part
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-    const auto issue = [&](int stage, int step) {
+    struct Steps {
+      typename LoadA::Step a;
+      typename LoadB::Step b[kSubs];
+    };
+    const auto step_of = [&](int stage, int step) {
+      Steps r;
       const int part = kSubs == 1 && step >= per ? 1 : 0;
       const int64_t k = (int64_t)(step - (part ? per : 0)) * kStep;
       const int left = step < step1 ? (int)(a.k - k) : 0;
       const uint32_t to = lds0 + stage * kStage;
-      la.issue((const char*)((const T*)(part ? a.a.q : a.a.p) + (kAK ? (int64_t)m0 * a.a.ld + k : k * a.a.ld + m0)), a.a.ld,
-               validm, left, to, wave);
+      r.a = la.step((const char*)((const T*)(part ? a.a.q : a.a.p) + (kAK ? (int64_t)m0 * a.a.ld + k : k * a.a.ld + m0)),
+                    a.a.ld, validm, left, to);
 #pragma unroll
       for (int s = 0; s < kSubs; ++s)
-        lb.issue((const char*)((const T*)((kSubs == 1 ? part : s) ? a.b.q : a.b.p) +
-                               (kBK ? (int64_t)n0 * a.b.ld + k : k * a.b.ld + n0)),
-                 a.b.ld, validn, left, to + LoadA::kBytes + s * LoadB::kBytes, wave);
+        r.b[s] = lb.step((const char*)((const T*)((kSubs == 1 ? part : s) ? a.b.q : a.b.p) +
+                                       (kBK ? (int64_t)n0 * a.b.ld + k : k * a.b.ld + n0)),
+                         a.b.ld, validn, left, to + LoadA::kBytes + s * LoadB::kBytes);
+      return r;
+    };
+    // load number t of a wave's kPer in a step
+    const auto load = [&](const Steps& r, int t) {
+      if (t < LoadA::kPer) la.load(r.a, t, wave);
+      else lb.load(r.b[(t - LoadA::kPer) / LoadB::kPer], (t - LoadA::kPer) % LoadB::kPer, wave);
     };
     TileRead<T, kM, kAK> ra;
     TileRead<T, kSubN, kBK> rb;
@@ -229,8 +284,10 @@ struct Product {
     const auto read_b = [&](int set, int j, int stage) {
       fb[set][j] = rb.get(lds + stage * kStage + LoadA::kBytes + j / kFS * LoadB::kBytes, j % kFS, set);
     };
-    // the matrix instructions of one half step, with the reads of the next
-    const auto half = [&](auto set_, int stage) {
+    // The matrix instructions of one half step, among them the reads of the next and, in
+    // the second half, the loads, one at a time: a wave that issues a load does nothing
+    // else for some 30 cycles.
+    const auto half = [&](auto set_, int stage, const Steps* r) {
       constexpr int set = decltype(set_)::value, next = 1 - set;
 #pragma unroll
       for (int i = 0; i < kFM; ++i) {
@@ -239,6 +296,10 @@ struct Product {
         for (int j = i * kFN / kFM; j < (i + 1) * kFN / kFM; ++j) read_b(next, j, stage);
 #pragma unroll
         for (int j = 0; j < kFN; ++j) acc[j][i] = mma<T>(acc[j][i], fb[set][j], fa[set][i]);
+        if constexpr (set == 1) {
+#pragma unroll
+          for (int t = i * kPer / kFM; t < (i + 1) * kPer / kFM; ++t) load(*r, t);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     };
@@ -247,7 +308,11 @@ struct Product {
 #pragma unroll
       for (int i = 0; i < kFM; ++i) acc[j][i] = F4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int s = 0; s < kStages; ++s) issue(s, step0 + s);
+    for (int s = 0; s < kStages; ++s) {
+      const Steps r = step_of(s, step0 + s);
+#pragma unroll
+      for (int t = 0; t < kPer; ++t) load(r, t);
+    }
     CKM_WAIT_LOADS((kStages - 1) * kPer);
     asm volatile("s_barrier" ::: "memory");
 #pragma unroll
@@ -257,10 +322,10 @@ struct Product {
     int stage = 0;
     for (int s = step0; s < step1; ++s) {
       const int next = stage + 1 == kStages ? 0 : stage + 1;
-      half(std::integral_constant<int, 0>{}, stage);
+      half(std::integral_constant<int, 0>{}, stage, nullptr);
+      const Steps r = step_of(stage, s + kStages);
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kPer) : "memory");
-      issue(stage, s + kStages);
-      half(std::integral_constant<int, 1>{}, next);
+      half(std::integral_constant<int, 1>{}, next, &r);
       stage = next;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -299,33 +364,20 @@ __device__ __forceinline__ void store4(T* row, int col, int cols, F4 v) {
       if (col + k < cols) row[col + k] = r[k];
   }
 }
-// Up to four consecutive elements, zeros past the row's end.
-template <typename T>
-__device__ __forceinline__ F4 read4(const T* row, int col, int cols) {
-  typedef T T4 __attribute__((ext_vector_type(4)));
-  F4 v = {0.0f, 0.0f, 0.0f, 0.0f};
-  if (col + 4 <= cols) {
-    T4 r;
-    __builtin_memcpy(&r, row + col, sizeof(r));
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = (float)r[k];
-  } else {
-#pragma unroll
-    for (int k = 0; k < 3; ++k)
-      if (col + k < cols) v[k] = (float)row[col + k];
-  }
-  return v;
-}
-
-// How a product of m x n (n: of one of `halves` results side by side) is cut: the
-// rows of a tile, and shares of k, whose sums are joined in a fixed order.
+// How a product of m x n is cut: the shape of a tile, and shares of k, whose sums are
+// joined in a fixed order.
 struct Cut {
-  int rows, cols;            // of a tile
+  int rows;                  // of a tile: names its shape (with_shape)
+  int cols;                  // of n (of each matrix's, for kSubs = 2)
   int tiles_m, tiles_n;      // of one half
-  int halves, splits, steps; // steps of k in a share
+  int halves, splits, steps; // results side by side; steps of k in a share
   int64_t blocks() const { return (int64_t)tiles_m * tiles_n * halves * splits; }
 };
-Cut cut_product(int64_t m, int64_t n, int halves, int64_t steps, int tile_cols);
+// subs: 2 when a tile's columns are of two matrices (n then counts one's). bytes: of
+// the operands. split: whether shares of k are possible. a_along_k: tiles of 16 rows are
+// for an A along k alone.
+Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
+                bool a_along_k);
 
 __host__ __device__ inline int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of * of; }
 // Elements from row to row of a matrix in the work buffer: 128 bytes past a multiple of
@@ -334,10 +386,35 @@ inline int64_t row_of(int64_t cols, size_t elt) { return (whole(cols * elt, 256)
 // CKM_E_UNSUPPORTED for a grid past what a launch counts.
 ckm_status check_blocks(const Cut& c);
 
-// Copies rows of cols elements into rows of `ld` (whole groups), zeros between; with
-// targets, a row whose target is outside [0, vocab) as zeros.
-void launch_pack(int type, const void* src, int64_t rows, int64_t cols, int64_t ld_src, void* dst, int64_t ld,
-                 hipStream_t s, const int64_t* targets = nullptr, int64_t vocab = 0);
+// Calls f with the shape of a cut's tiles: 256 x 256 columns where there are enough of
+// them, smaller ones to fill the CUs, 16 rows for single tokens, whose weights are read
+// once. A tile of two matrices has waves of 128 columns, 64 of each, so that a wave's
+// rows of the result are whole lines of memory.
+template <typename T, bool kAK, bool kBK, int kSubs, typename F>
+void with_shape(const Cut& cut, F&& f) {
+  if (cut.rows == 256) f(Tag<Product<T, 256, 256, kSubs == 2 ? 4 : 2, kSubs == 2 ? 2 : 4, 2, kAK, kBK, kSubs>>());
+  else if (cut.rows == 128) f(Tag<Product<T, 128, 128, 2, 2, 2, kAK, kBK, kSubs>>());
+  else if (cut.rows == 64) f(Tag<Product<T, 64, 128, 2, 2, 3, kAK, kBK, kSubs>>());
+  else if constexpr (kAK) f(Tag<Product<T, 16, 128, 1, 4, 4, kAK, kBK, kSubs>>());
+}
+
+// Up to three copies in a launch: rows of cols elements into rows of `ld` (whole groups),
+// zeros between; with targets, a row whose target is outside [0, vocab) as zeros.
+struct PackArgs {
+  struct One {
+    const void* src;
+    void* dst;
+    int64_t total, ld_src, ld;   // total: groups of eight columns
+    uint32_t groups;             // of a row
+    int32_t cols;
+    uint32_t blocks;
+  } one[3];
+  int count;
+  const int64_t* targets;
+  int64_t vocab;
+  void add(const void* src, int64_t rows, int64_t cols, int64_t ld_src, void* dst, int64_t ld);
+};
+void launch_pack(int type, const PackArgs& a, hipStream_t s);
 // Zeros in rows of cols elements.
 void launch_zero(int type, void* dst, int64_t rows, int64_t cols, int64_t ld, hipStream_t s);
 
@@ -372,23 +449,21 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel
   typename P::T* c = (typename P::T*)(half ? a.c[1] : a.c[0]);
   const int64_t ld_c = half ? a.ld_c[1] : a.ld_c[0];
   const int64_t row0 = kSlab ? ((int64_t)split * a.halves + half) * a.p.m : 0;
+  p.each8(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[1][8]) {
+    const int m = tm * P::kM + row, n = tn * P::kN + col;
+    if (m >= a.p.m || n >= a.p.n) return;
+    if constexpr (kSlab) {   // rows of whole eights
+      F4* at = (F4*)(a.slab + (row0 + m) * a.ld_slab + n);
+      F4 x = {v[0][0], v[0][1], v[0][2], v[0][3]}, y = {v[0][4], v[0][5], v[0][6], v[0][7]};
+      if (a.add) x += at[0], y += at[1];
+      at[0] = x;
+      at[1] = y;
+    } else {
 #pragma unroll
-  for (int i = 0; i < P::kFM; ++i) {
-    const int m = tm * P::kM + p.row(i);
-    if (m >= a.p.m) continue;
-#pragma unroll
-    for (int j = 0; j < P::kFN; ++j) {
-      const int n = tn * P::kN + p.col(j);
-      if constexpr (kSlab) {   // rows of whole fours
-        if (n < a.p.n) {
-          F4* at = (F4*)(a.slab + (row0 + m) * a.ld_slab + n);
-          *at = a.add ? *at + acc[j][i] : acc[j][i];
-        }
-      } else {
-        store4(c + m * ld_c, n, a.p.n, acc[j][i] * factor);
-      }
+      for (int k = 0; k < 8; ++k) v[0][k] *= factor;
+      store_part<false>(c + m * ld_c, rounded8<typename P::T>(v[0]), n, a.p.n);
     }
-  }
+  });
 }
 
 // Adds the shares of a result in their order.
@@ -400,13 +475,11 @@ void launch_product(ResultArgs a, const Cut& cut, hipStream_t s) {
   a.tiles_n = cut.tiles_n;
   a.halves = cut.halves;
   a.steps = cut.steps;
-  const auto go = [&](auto p) {
+  with_shape<T, kAK, kBK, 1>(cut, [&](auto p) {
     using P = typename decltype(p)::Shape;
     if (a.slab) ckm_product_kernel<P, true><<<(uint32_t)cut.blocks(), P::kThreads, 0, s>>>(a);
     else ckm_product_kernel<P, false><<<(uint32_t)cut.blocks(), P::kThreads, 0, s>>>(a);
-  };
-  if (cut.rows == 256) go(Tag<Product<T, 256, 256, 2, 4, 2, kAK, kBK, 1>>());
-  else go(Tag<Product<T, 128, 128, 2, 2, 2, kAK, kBK, 1>>());
+  });
 }
 
 }  // namespace ckm

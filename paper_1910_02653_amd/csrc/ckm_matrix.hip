@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdint>
 
 #include "ckm_matrix.h"
@@ -12,29 +13,27 @@ namespace {
 
 constexpr int kBlock = 256;
 
-// A thread a group of eight columns of the copy.
+// A thread a group of eight columns of a copy; each copy has blocks of its own.
 template <typename T>
-__global__ void __launch_bounds__(kBlock) ckm_pack_kernel(int64_t total, uint32_t groups, int32_t cols, const T* src,
-                                                          int64_t ld_src, T* dst, int64_t ld,
-                                                          const int64_t* targets, int64_t vocab) {
-  for (int64_t at = (int64_t)blockIdx.x * kBlock + threadIdx.x; at < total; at += (int64_t)gridDim.x * kBlock) {
-    const int64_t row = at / groups;
-    const int col = (int)(at - row * groups) * kVec;
-    Raw8<T> r = zero_group<T>();
-    const bool live = !targets || (targets[row] >= 0 && targets[row] < vocab);
-    if (live && col < cols) r = load_left(src + row * ld_src + col, cols - col);
-    store_part<false>(dst + row * ld, r, col, (int)ld);
+__global__ void __launch_bounds__(kBlock) ckm_pack_kernel(PackArgs a) {
+  uint32_t block = blockIdx.x;
+  PackArgs::One p = a.one[0];
+  if (block >= p.blocks) {
+    block -= p.blocks;
+    p = a.one[1];
+    if (block >= p.blocks) {
+      block -= p.blocks;
+      p = a.one[2];
+    }
   }
-}
-
-template <typename T>
-void pack(const void* src, int64_t rows, int64_t cols, int64_t ld_src, void* dst, int64_t ld, hipStream_t s,
-          const int64_t* targets, int64_t vocab) {
-  const uint32_t groups = (uint32_t)((ld + kVec - 1) / kVec);
-  const int64_t total = rows * groups;
-  if (total == 0) return;
-  ckm_pack_kernel<T><<<(uint32_t)std::min<int64_t>((total + kBlock - 1) / kBlock, 1 << 16), kBlock, 0, s>>>(
-      total, groups, (int32_t)cols, (const T*)src, ld_src, (T*)dst, ld, targets, vocab);
+  for (int64_t at = (int64_t)block * kBlock + threadIdx.x; at < p.total; at += (int64_t)p.blocks * kBlock) {
+    const int64_t row = at / p.groups;
+    const int col = (int)(at - row * p.groups) * kVec;
+    Raw8<T> r = zero_group<T>();
+    const bool live = !a.targets || (a.targets[row] >= 0 && a.targets[row] < a.vocab);
+    if (live && col < p.cols) r = load_left((const T*)p.src + row * p.ld_src + col, p.cols - col);
+    store_part<false>((T*)p.dst + row * p.ld, r, col, (int)p.ld);
+  }
 }
 
 template <typename T>
@@ -69,18 +68,57 @@ void join(const ResultArgs& a, int splits, hipStream_t s) {
 
 }  // namespace
 
-Cut cut_product(int64_t m, int64_t n, int halves, int64_t steps, int) {
-  const auto tiles = [&](int64_t t) { return ((m + t - 1) / t) * ((n + t - 1) / t) * halves; };
-  Cut c = {};
-  c.rows = c.cols = tiles(256) >= 192 ? 256 : 128;
-  c.halves = halves;
-  c.tiles_m = (int)((m + c.rows - 1) / c.rows);
-  c.tiles_n = (int)((n + c.cols - 1) / c.cols);
-  const int64_t blocks = tiles(c.rows);
-  int64_t splits = std::max<int64_t>(1, std::min<int64_t>(512 / blocks, steps / 8));
-  c.steps = (int)((steps + splits - 1) / splits);
-  c.splits = (int)((steps + c.steps - 1) / c.steps);
-  return c;
+// The cheapest cut by a model of the time: a CU takes one tile after the other, each as
+// many steps of k at the shape's measured time (longer where a CU has one tile and so
+// half its waves) and a fixed part (start, first loads, stores); no less than the
+// operands take from memory; shares are written and read once more. The steps' times
+// are those of these products (us; rows of a tile, tiles of a CU):
+//   bf16 2048x2048x4096   128 rows, one: 45, two shares 33; 64, two: 42; 16, eight: 113
+//   f32 2048x2048x1024    128 rows, one: 75; 64, two: 71; 16, eight: 97
+//   bf16 2048x8192x4096   256 rows, one: 101 (1357 TFLOP/s); 128, four: 128; 64, eight: 161
+//   bf16 1x16384x2048     16 rows 12, 64 rows 15 (67 MB)
+Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
+                bool a_along_k) {
+  struct Time {
+    double one, more;   // a step where a CU has one tile, or several
+  };
+  struct Shape {
+    int rows, cols;
+    Time half, full;    // 16-bit types, binary32
+    double fixed;
+  };
+  constexpr Shape kShapes[] = {{256, 256, {1.5, 1.5}, {8.1, 8.1}, 7.0},
+                               {128, 128, {0.68, 0.51}, {2.2, 2.1}, 3.0},
+                               {64, 128, {0.38, 0.33}, {1.2, 1.1}, 2.5},
+                               {16, 128, {0.30, 0.225}, {0.56, 0.39}, 2.5}};
+  constexpr double kBytesAUs = 5.0e6, kJoin = 4.0;
+  Cut best = {};
+  double least = 0.0;
+  for (const Shape& shape : kShapes) {
+    if (shape.rows < 64 && !a_along_k) continue;
+    Cut c = {};
+    c.rows = shape.rows;
+    c.cols = shape.cols / subs;
+    c.tiles_m = (int)((m + c.rows - 1) / c.rows);
+    c.tiles_n = (int)((n + c.cols - 1) / c.cols);
+    c.halves = halves;
+    const double tiles = (double)c.tiles_m * c.tiles_n * halves;
+    const Time& time = type == CKM_F32 ? shape.full : shape.half;
+    for (int splits = 1; splits <= 64; ++splits) {
+      if (splits > 1 && (!split || steps / splits < 4 || tiles * splits > 2048.0)) break;
+      c.steps = (int)((steps + splits - 1) / splits);
+      c.splits = (int)((steps + c.steps - 1) / c.steps);
+      const double rounds = std::ceil(tiles * c.splits / 256.0);
+      double t = std::max(rounds * (c.steps * (rounds > 1.0 ? time.more : time.one) + shape.fixed),
+                          bytes / kBytesAUs + shape.fixed);
+      if (c.splits > 1) t += kJoin + 8.0 * c.splits * m * n * halves * subs / kBytesAUs;
+      if (!best.rows || t <= least) {
+        best = c;
+        least = t;
+      }
+    }
+  }
+  return best;
 }
 
 ckm_status check_blocks(const Cut& c) {
@@ -88,12 +126,20 @@ ckm_status check_blocks(const Cut& c) {
                                  : set_error(CKM_E_UNSUPPORTED, "a product of %lld tiles", (long long)c.blocks());
 }
 
-void launch_pack(int type, const void* src, int64_t rows, int64_t cols, int64_t ld_src, void* dst, int64_t ld,
-                 hipStream_t s, const int64_t* targets, int64_t vocab) {
+void PackArgs::add(const void* src, int64_t rows, int64_t cols, int64_t ld_src, void* dst, int64_t ld) {
+  const uint32_t groups = (uint32_t)((ld + kVec - 1) / kVec);
+  const int64_t total = rows * groups;
+  one[count++] = {src, dst, total, ld_src, ld, groups, (int32_t)cols,
+                  (uint32_t)std::min<int64_t>((total + kBlock - 1) / kBlock, 1 << 16)};
+}
+
+void launch_pack(int type, const PackArgs& a, hipStream_t s) {
+  const uint32_t blocks = a.one[0].blocks + a.one[1].blocks + a.one[2].blocks;
+  if (blocks == 0) return;
   switch (type) {
-    case CKM_F32: pack<float>(src, rows, cols, ld_src, dst, ld, s, targets, vocab); break;
-    case CKM_F16: pack<_Float16>(src, rows, cols, ld_src, dst, ld, s, targets, vocab); break;
-    default: pack<__bf16>(src, rows, cols, ld_src, dst, ld, s, targets, vocab); break;
+    case CKM_F32: ckm_pack_kernel<float><<<blocks, kBlock, 0, s>>>(a); break;
+    case CKM_F16: ckm_pack_kernel<_Float16><<<blocks, kBlock, 0, s>>>(a); break;
+    default: ckm_pack_kernel<__bf16><<<blocks, kBlock, 0, s>>>(a); break;
   }
 }
 
