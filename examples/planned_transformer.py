@@ -7,11 +7,15 @@ threshold family rounds one score per value into candidate schedules, the
 cheapest within the budget is chosen, Algorithm 1 turns it into statements,
 and the statements are executed on the GPU: dropout, layer norm, attention
 softmax and their gradients by the package's operators, matrix products by the
-library. A node that a stage computes again has the bits it had before (its
+library. With --gated the feed-forward is the gated one, one node forward and
+one for its gradient, which keeps no projection; with --vocab the loss is the
+cross entropy against a vocabulary, whose logits never exist; with --clip the
+gradients' norm is bounded at the end of the step. A node that a stage computes again has the bits it had before (its
 dropout masks are functions of seed, site, row and column), so a budget changes
 memory and time and no number.
 
     python examples/planned_transformer.py --blocks 4 --tokens 1024 --budgets 100 60 40
+    python examples/planned_transformer.py --gated --vocab 32768 --clip 1.0
 """
 from __future__ import annotations
 
@@ -36,12 +40,15 @@ class Node(NamedTuple):
 
 
 class Stack:
-    """Parameters and nodes of a block stack, one training step long."""
+    """Parameters and nodes of a block stack, one training step long. gated: a gated feed-forward; vocab: the size of
+    a vocabulary whose next tokens are the target (0: a squared error)."""
+
+    LOSS_SCALE = 1024.0   # against underflow
 
     def __init__(self, blocks=2, tokens=512, hidden=512, heads=8, p=0.1, seed=1, step=0, dtype=torch.float16,
-                 matmul=torch.matmul):
+                 matmul=torch.matmul, gated=False, vocab=0):
         self.blocks, self.tokens, self.hidden, self.heads, self.p = blocks, tokens, hidden, heads, p
-        self.seed, self.step, self.mm = seed, step, matmul
+        self.seed, self.step, self.mm, self.gated, self.vocab = seed, step, matmul, gated, vocab
         gen = torch.Generator(device="cuda").manual_seed(seed)
 
         def normal(*shape, gain=1.0):
@@ -50,12 +57,17 @@ class Stack:
         h = hidden
         self.params, self.grads = {}, {}
         for b in range(blocks):
-            for name, shape in (("qkv", (h, 3 * h)), ("proj", (h, h)), ("up", (h, 4 * h)), ("down", (4 * h, h))):
+            for name, shape in (("qkv", (h, 3 * h)), ("proj", (h, h)), ("up", (h, 4 * h)), ("down", (4 * h, h)),
+                                *((("gate", (h, 4 * h)),) if gated else ())):
                 self.params[b, name] = normal(*shape, gain=shape[0] ** -0.5)
             for name in ("ln1", "ln2"):   # norms keep 32-bit weights
                 self.params[b, name] = torch.ones(h, device="cuda")
                 self.params[b, name + "_bias"] = torch.zeros(h, device="cuda")
         self.input, self.target = normal(tokens, h), normal(tokens, h)
+        if vocab:
+            self.params[blocks, "head"] = normal(vocab, h, gain=h ** -0.5)
+            self.target = torch.randint(0, vocab, (tokens,), generator=gen, device="cuda")
+            self.d_loss = torch.full((tokens,), self.LOSS_SCALE / tokens, device="cuda")   # of the mean
         self.nodes = []
         self._build()
 
@@ -80,9 +92,22 @@ class Stack:
         def loss(out):
             diff = out[0].float() - self.target.float()
             self.loss = 0.5 * diff.square().mean()
-            return ((diff / diff.numel()).mul(1024.0).to(out[0].dtype),)   # times 1024 against underflow
+            return ((diff / diff.numel()).mul(self.LOSS_SCALE).to(out[0].dtype),)
 
-        grad = self._add("loss", [x], loss)
+        def token_loss(out):
+            rows, lse = ops.cross_entropy(out[0], self.params[self.blocks, "head"], self.target)
+            self.loss = rows.mean()
+            return rows, lse
+
+        def d_token_loss(out, loss):
+            dx, self.grads[self.blocks, "head"] = ops.cross_entropy_backward(
+                self.d_loss, out[0], self.params[self.blocks, "head"], self.target, loss[1])
+            return (dx,)
+
+        if self.vocab:
+            grad = self._add("d_loss", [x, self._add("loss", [x], token_loss)], d_token_loss)
+        else:
+            grad = self._add("loss", [x], loss)
         for b in reversed(range(self.blocks)):
             grad = self._backward(b, place[b], grad, scale)
 
@@ -119,8 +144,11 @@ class Stack:
         n["context"] = self._add("context", [n["qkv"], n["probs"]], lambda t, p: (self._merged(mm(p[0], t[2])),))
         n["proj"] = self._add("proj", [n["context"]], lambda c: (mm(c[0], P[b, "proj"]),))
         n["ln2"] = self._add("ln2", xs + [n["proj"]], ln2)   # (y, h, statistics)
-        n["up"] = self._add("up", [n["ln2"]], lambda a: (mm(a[0], P[b, "up"]),))
-        n["act"] = self._add("act", [n["up"]], lambda u: (torch.nn.functional.gelu(u[0]),))
+        if self.gated:
+            n["act"] = self._add("gated", [n["ln2"]], lambda a: (ops.gated(a[0], P[b, "gate"], P[b, "up"]),))
+        else:
+            n["up"] = self._add("up", [n["ln2"]], lambda a: (mm(a[0], P[b, "up"]),))
+            n["act"] = self._add("act", [n["up"]], lambda u: (torch.nn.functional.gelu(u[0]),))
         n["down"] = self._add("down", [n["act"]], lambda g: (mm(g[0], P[b, "down"]),))
         n["out"] = self._add("out", [n["ln2"], n["down"]],
                              lambda a, d: (ops.dropout(d[0], drop(b, 2), residual=a[1]),))
@@ -140,6 +168,10 @@ class Stack:
             with torch.enable_grad():
                 v = u[0].detach().requires_grad_()
                 return torch.autograd.grad(torch.nn.functional.gelu(v), v, d[0])
+
+        def d_gated(a, d):
+            dx, G[b, "gate"], G[b, "up"] = ops.gated_backward(d[0], a[0], P[b, "gate"], P[b, "up"])
+            return (dx,)
 
         def d_ln2(a, past, d):
             dx, dh, G[b, "ln2"], G[b, "ln2_bias"] = ops.layer_norm_backward(
@@ -161,8 +193,11 @@ class Stack:
 
         down = self._add("d_out", [grad], lambda g: (ops.dropout_backward(g[0], drop(b, 2)),))
         act = self._add("d_down", [n["act"], down], linear("down"))
-        up = self._add("d_act", [n["up"], act], d_act)
-        ln2 = self._add("d_up", [n["ln2"], up], linear("up"))
+        if self.gated:
+            ln2 = self._add("d_gated", [n["ln2"], act], d_gated)
+        else:
+            up = self._add("d_act", [n["up"], act], d_act)
+            ln2 = self._add("d_up", [n["ln2"], up], linear("up"))
         both = self._add("d_ln2", [n["ln2"], grad, ln2], d_ln2)
         ctx = self._add("d_proj", [n["context"], both], linear("proj"))
         probs = self._add("d_context", [n["qkv"], n["probs"], ctx], d_probs)
@@ -183,6 +218,11 @@ class Stack:
             else:
                 regs.pop(reg)
         return self.grads
+
+    def clip(self, max_norm):
+        """Bounds the norm of all gradients, which carry the loss scale, in place; returns it, without the scale."""
+        norm, _ = ops.clip_gradients([self.grads[k] for k in sorted(self.grads)], max_norm * self.LOSS_SCALE)
+        return norm / self.LOSS_SCALE
 
     def measure(self):
         """(bytes, cost in ns) of every node: one run that keeps everything, then each node timed."""
@@ -238,10 +278,13 @@ def main():
     ap.add_argument("--tokens", type=int, default=1024)
     ap.add_argument("--hidden", type=int, default=1024)
     ap.add_argument("--heads", type=int, default=16)
+    ap.add_argument("--gated", action="store_true", help="a gated feed-forward")
+    ap.add_argument("--vocab", type=int, default=0, help="cross entropy against a vocabulary of this size")
+    ap.add_argument("--clip", type=float, default=0.0, help="the gradients' largest norm")
     ap.add_argument("--budgets", type=float, nargs="+", default=[100.0, 60.0, 40.0],
                     help="percent of the memory that keeping everything takes")
     a = ap.parse_args()
-    stack = Stack(a.blocks, a.tokens, a.hidden, a.heads)
+    stack = Stack(a.blocks, a.tokens, a.hidden, a.heads, gated=a.gated, vocab=a.vocab)
     size, cost = stack.measure()
     g, s = graph_of(stack, size, cost)
     base = 2 * stack.input.numel() * 2 + 2 * sum(t.numel() * t.element_size() for t in stack.params.values())
@@ -255,6 +298,7 @@ def main():
         held = torch.cuda.memory_allocated()
         begin = time.perf_counter()
         grads = stack.execute(plan)
+        norm = stack.clip(a.clip) if a.clip else None
         torch.cuda.synchronize()
         took = time.perf_counter() - begin
         peak = torch.cuda.max_memory_allocated() - held
@@ -264,7 +308,8 @@ def main():
         print("budget %3.0f%%: %d nodes computed (%d in the graph), planned %.1f ms, took %.1f ms; planned peak of the "
               "values %.1f MiB, measured %.1f MiB; loss %.6f, gradients %s the first budget's"
               % (pct, computed, len(stack.nodes), planned / 1e6, took * 1e3, (mem.max() - base) / 2 ** 20, peak / 2 ** 20,
-                 float(stack.loss), "equal" if all(torch.equal(p, q) for p, q in zip(now, first)) else "differ from"))
+                 float(stack.loss), "equal" if all(torch.equal(p, q) for p, q in zip(now, first)) else "differ from")
+              + ("" if norm is None else "; their norm %.4f" % float(norm)))
     g.close()
 
 

@@ -35,6 +35,7 @@ from __future__ import annotations
 import array
 import ctypes as C
 import functools
+import itertools
 import math
 
 import torch
@@ -643,32 +644,38 @@ def _dense(t) -> bool:
     return True
 
 
-def _list(tensors, out):
-    """(device, ckm_tensor array, count) of a list of tensors and, where given, of their outputs."""
-    tensors = list(tensors)
-    device = _current_device()
-    rows = array.array("q")
+def _check_list(tensors, out, device):
+    """Refuses what _list cannot take as it is; tensors of other orders of dimensions pass."""
     for k, t in enumerate(tensors):
-        if not isinstance(t, torch.Tensor) or t.dtype not in _TYPES or t.get_device() != device:
-            _tensor(t, "tensor %d" % k)
-        if not t.is_contiguous() and not _dense(t):
+        _tensor(t, "tensor %d" % k)
+        if not _dense(t):
             raise ValueError("tensor %d: its elements must fill one range of memory, got shape %s, strides %s"
                              % (k, tuple(t.shape), t.stride()))
-        p = t.data_ptr()
-        rows.extend((p, p, t.numel(), _TYPES[t.dtype]))
     if out is not None:
         if len(out) != len(tensors):
             raise ValueError("out must hold %d tensors, got %d" % (len(tensors), len(out)))
         for k, (t, y) in enumerate(zip(tensors, out)):
-            if (not isinstance(y, torch.Tensor) or y.dtype is not t.dtype or y.get_device() != device
-                    or y.shape != t.shape or y.stride() != t.stride()):
-                _tensor(y, "out %d" % k, t.dtype, device)
-                if y.shape != t.shape or (t.numel() and any(
-                        n != 1 and p != q for n, p, q in zip(t.shape, y.stride(), t.stride()))):
-                    raise ValueError("out %d must have shape %s and strides %s, got %s and %s"
-                                     % (k, tuple(t.shape), t.stride(), tuple(y.shape), y.stride()))
-            rows[4 * k + 1] = y.data_ptr()
-    return device, rows, len(tensors)
+            _tensor(y, "out %d" % k, t.dtype, device)
+            if y.shape != t.shape or (t.numel() and any(
+                    n != 1 and p != q for n, p, q in zip(t.shape, y.stride(), t.stride()))):
+                raise ValueError("out %d must have shape %s and strides %s, got %s and %s"
+                                 % (k, tuple(t.shape), t.stride(), tuple(y.shape), y.stride()))
+
+
+def _list(tensors, out):
+    """(device, ckm_tensor array, count) of a list of tensors and, where given, of their outputs."""
+    device, T = _current_device(), torch.Tensor
+    both = tensors if out is None else tensors + out
+    # the common case by whole lists, a third of the time of going through them one by one
+    if not (all(isinstance(t, T) for t in both) and all(map(T.is_contiguous, both))
+            and set(map(T.get_device, both)) <= {device}
+            and (out is None or ([t.dtype for t in tensors] == [y.dtype for y in out]
+                                 and [t.shape for t in tensors] == [y.shape for y in out]))
+            and all(t.dtype in _TYPES for t in tensors)):
+        _check_list(tensors, out, device)
+    at = list(map(T.data_ptr, tensors))
+    values = zip(at, at if out is None else map(T.data_ptr, out), map(T.numel, tensors), [_TYPES[t.dtype] for t in tensors])
+    return device, array.array("q", list(itertools.chain.from_iterable(values))), len(tensors)
 
 
 @functools.lru_cache(maxsize=1024)
