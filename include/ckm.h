@@ -473,7 +473,7 @@ ckm_status ckm_softmax_backward_async(ckm_dtype type, const ckm_scores* scores, 
  * never exist in memory, and the step's end. Pointers, streams, work buffers,
  * alignment and strides as above, except that no output may overlap an input
  * (ckm_clip_async: but its own). Operands of rows that do not start on 16 bytes,
- * or do not end on them, are first copied into the work buffer; the sizes of work
+ * or do not end on them, may be copied into the work buffer first; the sizes of work
  * buffers go by the struct's pointers and strides too. Products are summed in
  * binary32, in an order that the sizes fix. */
 #define CKM_MAX_MATRIX_ROWS (1 << 30) /* rows of x */

@@ -32,7 +32,7 @@ struct LossArgs {
   ProductArgs p;            // n: of the vocabulary, or of a piece of it
   int32_t tiles_m, tiles_n;
   const int64_t* targets;
-  float2* parts;            // [rows][tiles_n]: base and sum of exponentials (join_parts)
+  float2* parts;            // [rows][tiles_all]: base and sum of exponentials (join_parts)
   float* hit;               // [rows]: the target's logit
   float* loss;
   float* lse;               // written, or the gradient's input
@@ -40,6 +40,7 @@ struct LossArgs {
   const float* most;        // binary16: the largest |dloss|
   void* d;                  // [rows][ld_d]
   int64_t ld_d, first;      // first: the piece's first column
+  int32_t tile0, tiles_all; // its first tile, of all
   int64_t vocab;
 };
 
@@ -89,7 +90,7 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_kernel(Lo
 #pragma unroll
   for (int i = 0; i < P::kFM; ++i) {
     const int m = tm * P::kM + p.row(i);
-    const int64_t target = m < a.p.m ? a.targets[m] - (int64_t)tn * P::kN : -1;   // within the tile
+    const int64_t target = m < a.p.m ? a.targets[m] - a.first - (int64_t)tn * P::kN : -1;   // within the tile
     if (target >= 0 && target < P::kN && target < a.p.n - tn * P::kN) {
 #pragma unroll
       for (int j = 0; j < P::kFN; ++j)
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_kernel(Lo
     float2 v = joined[r];
 #pragma unroll
     for (int w = 1; w < P::kWavesN; ++w) v = join_parts(v, joined[w * P::kM + r]);
-    a.parts[(int64_t)m * a.tiles_n + tn] = v;
+    a.parts[(int64_t)m * a.tiles_all + a.tile0 + tn] = v;
   }
 }
 
@@ -132,12 +133,12 @@ __global__ void __launch_bounds__(256) ckm_loss_join_kernel(LossArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= a.p.m) return;
-  const float2* parts = a.parts + row * a.tiles_n;
+  const float2* parts = a.parts + row * a.tiles_all;
   float base = -INFINITY, sum = 0.0f;
-  for (int k = lane; k < a.tiles_n; k += 64) base = fmaxf(base, parts[k].y == 0.0f ? -INFINITY : parts[k].x);
+  for (int k = lane; k < a.tiles_all; k += 64) base = fmaxf(base, parts[k].y == 0.0f ? -INFINITY : parts[k].x);
   base = reduce64<OpMax>(base);
   if (base == -INFINITY) base = 0.0f;
-  for (int k = lane; k < a.tiles_n; k += 64) {
+  for (int k = lane; k < a.tiles_all; k += 64) {
     const float2 v = parts[k];
     if (v.y != 0.0f) sum += v.y * __builtin_amdgcn_exp2f(v.x - base);
   }
@@ -209,7 +210,7 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_back_kern
 #pragma unroll
           for (int i = 0; i < P::kFM; ++i) acc[j][i][k] = 0.0f;
   }
-  p.each8(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[1][8]) {
+  p.template each8<1>(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[1][8]) {
     const int m = tm * P::kM + row, n = tn * P::kN + col;
     if (m < a.p.m && n < width) store_part<false>((T*)a.d + m * a.ld_d, rounded8<T>(v[0]), n, width);
   });
@@ -218,38 +219,41 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_back_kern
 template <typename T, bool kBack>
 void launch_logits(LossArgs a, const Cut& cut, hipStream_t s) {
   a.tiles_m = cut.tiles_m;
-  a.tiles_n = cut.tiles_n;
+  a.tiles_n = (a.p.n + cut.cols - 1) / cut.cols;   // fewer in the last piece
   with_shape<T, true, true, 1>(cut, [&](auto p) {
     using P = typename decltype(p)::Shape;
-    const uint32_t blocks = (uint32_t)(cut.tiles_m * cut.tiles_n);
+    const uint32_t blocks = (uint32_t)(a.tiles_m * a.tiles_n);
     if constexpr (kBack) ckm_loss_back_kernel<P><<<blocks, P::kThreads, 0, s>>>(a);
     else ckm_loss_kernel<P><<<blocks, P::kThreads, 0, s>>>(a);
   });
 }
 
-// Bytes of a piece's d: what stays in the caches between its writer and its readers;
-// never less than 8192 columns, so that dx, summed over pieces in memory, is read and
-// written seldom.
-constexpr int64_t kPieceBytes = (int64_t)128 << 20, kLeastPiece = 8192;
+// A piece of the vocabulary: d of at most 128 MB, and where the table has to be copied 96
+// MB of it, which stay in the caches between their writer and their readers; never fewer
+// than 8192 columns: dx, summed over pieces in memory, is read and written for each.
+constexpr int64_t kPieceBytes = (int64_t)128 << 20, kTableBytes = (int64_t)96 << 20, kLeastPiece = 8192;
 
 struct LossPlan {
   bool pack_x, pack_w;
   int64_t ld_x, ld_w;
   int64_t piece;             // columns
-  Cut logits, dx, dw, last;  // last: logits of the last piece
+  Cut logits, dx, dw;
   size_t x, w, parts, hit, most, d, slab, dw_slab, total;
+  double time;               // the model's, us
 };
 
-LossPlan plan_of(int type, const ckm_vocab& c, bool back) {
+// packed: operands that cannot be loaded as they are are copied, or else staged.
+LossPlan plan_as(int type, const ckm_vocab& c, bool back, bool ragged_x, bool ragged_w, bool packed) {
   const size_t elt = dtype_bytes(type);
   const int64_t group = 16 / elt, step = kStepBytes / elt;
   LossPlan p = {};
   // the gradient takes a copy whose rows without a target are zeros: in d' x they are
   // multiplied by d's zeros, and may hold anything
-  p.pack_x = back || !loadable(c.d_x, c.rows, c.hidden, c.ld_x, elt, true);
-  p.pack_w = !loadable(c.d_weight, c.vocab, c.hidden, c.ld_weight, elt, true);
+  p.pack_x = back || (ragged_x && packed);
+  p.pack_w = ragged_w && packed;
   p.ld_x = p.pack_x || c.rows == 1 ? whole(c.hidden, group) : c.ld_x;
   p.ld_w = p.pack_w || c.vocab == 1 ? whole(c.hidden, group) : c.ld_weight;
+  const bool staged_x = ragged_x && !p.pack_x, staged_w = ragged_w && !packed;
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -257,31 +261,46 @@ LossPlan plan_of(int type, const ckm_vocab& c, bool back) {
     return here;
   };
   if (p.pack_x) p.x = take(c.rows * p.ld_x * elt);
-  if (p.pack_w) p.w = take(c.vocab * p.ld_w * elt);
-  const int64_t steps = (c.hidden + step - 1) / step, x_bytes = c.rows * c.hidden * elt;
-  const auto logits = [&](int64_t n) {
-    return cut_product(type, c.rows, n, 1, 1, steps, x_bytes + n * c.hidden * (int64_t)elt, false, true);
-  };
-  if (!back) {
-    p.logits = logits(c.vocab);
-    p.parts = take((size_t)c.rows * p.logits.tiles_n * sizeof(float2));
+  int64_t most = c.vocab;
+  if (back) most = std::min(most, kPieceBytes / (int64_t)(c.rows * elt));
+  if (p.pack_w) most = std::min(most, kTableBytes / (int64_t)(c.hidden * elt));
+  // as many columns in each
+  const int64_t pieces = (c.vocab + std::max(most, kLeastPiece) - 1) / std::max(most, kLeastPiece);
+  p.piece = std::min(c.vocab, whole((c.vocab + pieces - 1) / pieces, 256));
+  if (p.pack_w) p.w = take(p.piece * p.ld_w * elt);
+  const int64_t steps = (c.hidden + step - 1) / step, x_bytes = c.rows * c.hidden * elt, w_bytes = p.piece * c.hidden * elt;
+  p.logits = cut_product(type, c.rows, p.piece, 1, 1, steps, x_bytes + w_bytes, false, true,
+                         staged_x || staged_w ? kStagedAlong : kStraight);
+  p.time = p.logits.time + (p.pack_w ? copy_time(w_bytes) : 0.0);
+  if (!back) {   // pieces are of whole tiles
+    p.parts = take((size_t)c.rows * ((c.vocab + p.logits.cols - 1) / p.logits.cols) * sizeof(float2));
     p.hit = take(c.rows * sizeof(float));
   } else {
-    p.piece = std::min(c.vocab, std::max(kLeastPiece, kPieceBytes / (int64_t)(c.rows * elt) / 256 * 256));
-    p.logits = logits(p.piece);
-    const int64_t tail = c.vocab - (c.vocab - 1) / p.piece * p.piece;
-    p.last = logits(tail);
-    const int64_t w_bytes = p.piece * c.hidden * elt, d_bytes = p.piece * c.rows * elt;
-    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, (p.piece + step - 1) / step, d_bytes + w_bytes, true, true);
+    const int64_t d_bytes = p.piece * c.rows * elt;
+    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, (p.piece + step - 1) / step, d_bytes + w_bytes, true, true,
+                       staged_w ? kStagedAcross : kStraight);
     p.dw = cut_product(type, p.piece, c.hidden, 1, 1, (c.rows + step - 1) / step, d_bytes + x_bytes + w_bytes, true,
-                       false);
+                       false, kStraight);
+    p.time += p.dx.time + p.dw.time;
     p.most = take(sizeof(float));
     p.d = take((size_t)c.rows * row_of(p.piece, elt) * elt);
     if (p.dx.splits > 1 || p.piece < c.vocab) p.slab = take((size_t)p.dx.splits * c.rows * whole(c.hidden, 8) * 4);
     if (p.dw.splits > 1) p.dw_slab = take((size_t)p.dw.splits * p.piece * whole(c.hidden, 8) * 4);
   }
+  p.time *= (double)c.vocab / p.piece;
+  if (!back && p.pack_x) p.time += copy_time(x_bytes);
   p.total = at;
   return p;
+}
+
+LossPlan plan_of(int type, const ckm_vocab& c, bool back) {
+  const size_t elt = dtype_bytes(type);
+  const bool x = !loadable(c.d_x, c.rows, c.hidden, c.ld_x, elt, true);
+  const bool w = !loadable(c.d_weight, c.vocab, c.hidden, c.ld_weight, elt, true);
+  const LossPlan p = plan_as(type, c, back, x, w, true);
+  if ((!x && !w) || !stageable(c.rows, c.ld_x, elt) || !stageable(c.vocab, c.ld_weight, elt)) return p;
+  const LossPlan q = plan_as(type, c, back, x, w, false);
+  return q.time < p.time ? q : p;
 }
 
 template <typename T>
@@ -298,12 +317,14 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     launch_pack(type, one, s);
     x = (const T*)(work + plan.x);
   }
-  if (plan.pack_w) {
+  // the rows of the table from v on, as they are multiplied
+  const auto rows_from = [&](int64_t v, int32_t width) {
+    if (!plan.pack_w) return w + v * plan.ld_w;
     PackArgs one = {};
-    one.add(w, c.vocab, c.hidden, c.ld_weight, work + plan.w, plan.ld_w);
+    one.add(w + v * c.ld_weight, width, c.hidden, c.ld_weight, work + plan.w, plan.ld_w);
     launch_pack(type, one, s);
-    w = (const T*)(work + plan.w);
-  }
+    return (const T*)(work + plan.w);
+  };
   LossArgs a = {};
   a.p = {{x, x, plan.ld_x}, {w, w, plan.ld_w}, (int32_t)c.rows, (int32_t)c.vocab, (int32_t)c.hidden, 1};
   a.targets = c.d_targets;
@@ -313,8 +334,14 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     a.parts = (float2*)(work + plan.parts);
     a.hit = (float*)(work + plan.hit);
     a.loss = loss;
-    launch_logits<T, false>(a, plan.logits, s);
-    a.tiles_n = plan.logits.tiles_n;
+    a.tiles_all = (int32_t)((c.vocab + plan.logits.cols - 1) / plan.logits.cols);
+    for (int64_t v = 0; v < c.vocab; v += plan.piece) {
+      a.first = v;
+      a.tile0 = (int32_t)(v / plan.logits.cols);
+      a.p.n = (int32_t)std::min(plan.piece, c.vocab - v);
+      a.p.b.p = rows_from(v, a.p.n);
+      launch_logits<T, false>(a, plan.logits, s);
+    }
     ckm_loss_join_kernel<<<(uint32_t)((c.rows + 3) / 4), 256, 0, s>>>(a);
     return;
   }
@@ -340,12 +367,11 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
   rw.ld_c[0] = ld_dw;
   for (int64_t v = 0; v < c.vocab; v += plan.piece) {
     const int32_t width = (int32_t)std::min(plan.piece, c.vocab - v);
-    const bool tail = width < plan.piece;
-    const T* wv = w + v * plan.ld_w;
+    const T* wv = rows_from(v, width);
     a.first = v;
     a.p.b.p = a.p.b.q = wv;
     a.p.n = width;
-    launch_logits<T, true>(a, tail ? plan.last : plan.logits, s);
+    launch_logits<T, true>(a, plan.logits, s);
     if (dx) {   // d W; a short last piece leaves shares at the end of k with nothing to add
       rx.p = {{a.d, a.d, a.ld_d}, {wv, wv, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, width, 1};
       launch_product<T, true, false>(rx, plan.dx, s);

@@ -123,20 +123,37 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(G
   const int all = (a.p.k + P::kStep - 1) / P::kStep, from = split * a.steps;
   F4 acc[P::kFN][P::kFM];
   p.run(acc, a.p, tm * P::kM, tn * P::kSubN, from, min(all, from + a.steps), (LdsChar*)lds);
-  p.each8(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[2][8]) {
-    const int m = tm * P::kM + row, n = tn * P::kSubN + col;
-    if (m >= a.p.m) return;
-    if constexpr (kMode != kShares) {
-      finish<T, kMode>(a, m, n, v[0], v[1]);
-    } else if (n < a.p.n) {
+  if constexpr (kMode == kForward) {   // half as much goes through LDS
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        F4* at = (F4*)(a.slab + (((int64_t)split * 2 + s) * a.p.m + m) * a.ld_slab + n);
-        at[0] = F4{v[s][0], v[s][1], v[s][2], v[s][3]};
-        at[1] = F4{v[s][4], v[s][5], v[s][6], v[s][7]};
+    for (int j = 0; j < P::kFS; ++j)
+#pragma unroll
+      for (int i = 0; i < P::kFM; ++i) {
+        float g[4], u[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) g[k] = acc[j][i][k], u[k] = acc[j + P::kFS][i][k];
+        gated_of<T>(a.act, g, u);
+        acc[j][i] = F4{g[0], g[1], g[2], g[3]};
       }
-    }
-  });
+    p.template each8<1>(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[1][8]) {
+      const int m = tm * P::kM + row, n = tn * P::kSubN + col;
+      if (m < a.p.m && n < a.p.n) store_part<false>((T*)a.out + m * a.ld_out, rounded8<T>(v[0]), n, a.p.n);
+    });
+  } else {
+    p.template each8<2>(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[2][8]) {
+      const int m = tm * P::kM + row, n = tn * P::kSubN + col;
+      if (m >= a.p.m) return;
+      if constexpr (kMode == kBackward) {
+        finish<T, kMode>(a, m, n, v[0], v[1]);
+      } else if (n < a.p.n) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          F4* at = (F4*)(a.slab + (((int64_t)split * 2 + s) * a.p.m + m) * a.ld_slab + n);
+          at[0] = F4{v[s][0], v[s][1], v[s][2], v[s][3]};
+          at[1] = F4{v[s][4], v[s][5], v[s][6], v[s][7]};
+        }
+      }
+    });
+  }
 }
 
 // The shares of g and u added in their order, and what kMode makes of them; a thread
@@ -152,6 +169,7 @@ __global__ void __launch_bounds__(256) ckm_gated_join_kernel(GatedArgs a, int sp
     for (int s = 0; s < 2; ++s) {
       const float* p = a.slab + s * one + m * a.ld_slab + n;
       F4 x = ((const F4*)p)[0], y = ((const F4*)p)[1];
+#pragma unroll 8
       for (int k = 1; k < splits; ++k) {
         x += ((const F4*)(p + 2 * k * one))[0];
         y += ((const F4*)(p + 2 * k * one))[1];
@@ -189,22 +207,26 @@ struct GatedPlan {
   int64_t inner, ld_d;       // columns of dg, padded to whole groups; a row of dg | du
   Cut both, dx, dw;
   size_t x, w, d, slab, total;
+  double time;               // the model's, us
 };
 
-GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
+// packed: operands that cannot be loaded as they are are copied, or else staged.
+GatedPlan plan_as(int type, const ckm_gated& c, bool back, bool ragged_x, bool ragged_w, bool packed) {
   const size_t elt = dtype_bytes(type);
   const int64_t group = 16 / elt, step = kStepBytes / elt;
   GatedPlan p = {};
-  p.pack_x = !loadable(c.d_x, c.rows, c.hidden, c.ld_x, elt, true);
-  p.pack_w = c.ld_gate != c.ld_up || !loadable(c.d_gate, c.hidden, c.inner, c.ld_gate, elt, back) ||
-             !loadable(c.d_up, c.hidden, c.inner, c.ld_up, elt, back);
+  p.pack_x = ragged_x && packed;
+  p.pack_w = ragged_w && packed;
   p.inner = whole(c.inner, group);
   p.ld_d = row_of(2 * p.inner, elt);
   p.ld_x = p.pack_x || c.rows == 1 ? whole(c.hidden, group) : c.ld_x;   // a single row may have any stride
   p.ld_w = p.pack_w || c.hidden == 1 ? p.inner : c.ld_gate;
   const int64_t steps_h = (c.hidden + step - 1) / step, steps_f = (c.inner + step - 1) / step;
   const int64_t x_bytes = c.rows * c.hidden * elt, w_bytes = 2 * c.hidden * c.inner * elt, h_bytes = c.rows * c.inner * elt;
-  p.both = cut_product(type, c.rows, c.inner, 1, 2, steps_h, x_bytes + w_bytes, true, true);
+  const bool staged_x = ragged_x && !packed, staged_w = ragged_w && !packed;
+  p.both = cut_product(type, c.rows, c.inner, 1, 2, steps_h, x_bytes + w_bytes, true, true,
+                       staged_w ? kStagedAcross : staged_x ? kStagedAlong : kStraight);
+  p.time = p.both.time + (p.pack_x || p.pack_w ? copy_time((p.pack_x ? x_bytes : 0) + (p.pack_w ? w_bytes : 0)) : 0.0);
   size_t at = 0;
   const auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -215,9 +237,11 @@ GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
   if (p.pack_w) p.w = take(2 * c.hidden * p.ld_w * elt);
   size_t slab = p.both.splits > 1 ? (size_t)p.both.splits * 2 * c.rows * whole(c.inner, 8) * 4 : 0;
   if (back) {
-    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, 2 * steps_f, 2 * h_bytes + w_bytes, true, true);
+    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, 2 * steps_f, 2 * h_bytes + w_bytes, true, true,
+                       staged_w ? kStagedAlong : kStraight);
     p.dw = cut_product(type, c.hidden, c.inner, 2, 1, (c.rows + step - 1) / step, x_bytes + 2 * h_bytes + w_bytes, true,
-                       false);
+                       false, staged_x ? kStagedAcross : kStraight);
+    p.time += p.dx.time + p.dw.time;
     p.d = take(c.rows * p.ld_d * elt);
     if (p.dx.splits > 1) slab = std::max(slab, (size_t)p.dx.splits * c.rows * whole(c.hidden, 8) * 4);
     if (p.dw.splits > 1) slab = std::max(slab, (size_t)p.dw.splits * 2 * c.hidden * whole(c.inner, 8) * 4);
@@ -225,6 +249,19 @@ GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
   p.slab = take(slab);
   p.total = at;
   return p;
+}
+
+GatedPlan plan_of(int type, const ckm_gated& c, bool back) {
+  const size_t elt = dtype_bytes(type);
+  const bool x = !loadable(c.d_x, c.rows, c.hidden, c.ld_x, elt, true);
+  const bool w = c.ld_gate != c.ld_up || !loadable(c.d_gate, c.hidden, c.inner, c.ld_gate, elt, back) ||
+                 !loadable(c.d_up, c.hidden, c.inner, c.ld_up, elt, back);
+  const GatedPlan p = plan_as(type, c, back, x, w, true);
+  if ((!x && !w) || (c.ld_gate != c.ld_up && c.hidden > 1) || !stageable(c.rows, c.ld_x, elt) ||
+      !stageable(c.hidden, c.ld_gate, elt))
+    return p;
+  const GatedPlan q = plan_as(type, c, back, x, w, false);
+  return q.time < p.time ? q : p;
 }
 
 template <typename T>

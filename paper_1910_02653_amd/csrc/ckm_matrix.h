@@ -111,6 +111,41 @@ struct TileLoad {
   }
 };
 
+// The same tile by way of registers, for rows that start anywhere (groups of 16 bytes
+// at any address, and what is past the range element by element).
+template <typename T, int kRows, bool kAlongK, int kWaves>
+struct TileStage {
+  using Load = TileLoad<T, kRows, kAlongK, kWaves>;
+  static constexpr int kPer = Load::kPer, kGroup = Load::kGroup;
+  I4 held[kPer];
+
+  __device__ __forceinline__ static int place(int t, int wave, int lane) {   // in the tile
+    return (wave * kPer + t) % Load::kLoads * 1024 + lane * 16;
+  }
+  __device__ __forceinline__ void fetch(const char* base, int64_t ld, int valid, int left, int wave, int lane) {
+#pragma unroll
+    for (int t = 0; t < kPer; ++t) {
+      const int at = place(t, wave, lane), row = at / Load::kRowBytes, slot = at % Load::kRowBytes / 16;
+      const int first = (kAlongK ? slot ^ (row & 7) : slot ^ Load::turned(row)) * kGroup;
+      const int n = kAlongK ? (row < valid ? left - first : 0) : (row < left ? valid - first : 0);
+      held[t] = I4{0, 0, 0, 0};
+      const T* p = (const T*)base + row * ld + first;
+      if (n >= kGroup) {
+        __builtin_memcpy(&held[t], p, 16);
+      } else if (n > 0) {
+        const Raw8<T> r = load_left(p, n);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) held[t][k] = r.w[k];
+      }
+    }
+  }
+  __device__ __forceinline__ void put(LdsChar* tile, int wave, int lane) const {
+    typedef __attribute__((address_space(3))) I4 LdsI4;
+#pragma unroll
+    for (int t = 0; t < kPer; ++t) *(LdsI4*)(tile + place(t, wave, lane)) = held[t];
+  }
+};
+
 // A lane's view of a tile: fragment f (16 rows or columns), half a step each.
 template <typename T, int kRows, bool kAlongK>
 struct TileRead {
@@ -171,11 +206,13 @@ __device__ __forceinline__ F4 mma(F4 acc, I4 p, I4 q) {
 
 // A block's product: kM x kN of C by kWavesM x kWavesN waves. kSubs = 2: the tile's
 // columns are kN / 2 of each of two matrices, and each wave has as many of both.
-template <typename T_, int kM_, int kN_, int kWavesM_, int kWavesN_, int kStages_, bool kAK_, bool kBK_, int kSubs_>
+// kStaged: operands by way of registers (TileStage).
+template <typename T_, int kM_, int kN_, int kWavesM_, int kWavesN_, int kStages_, bool kAK_, bool kBK_, int kSubs_,
+          bool kStaged_ = false>
 struct Product {
   using T = T_;
   static constexpr int kM = kM_, kN = kN_, kWavesM = kWavesM_, kWavesN = kWavesN_, kStages = kStages_, kSubs = kSubs_;
-  static constexpr bool kAK = kAK_, kBK = kBK_;
+  static constexpr bool kAK = kAK_, kBK = kBK_, kStaged = kStaged_;
   static constexpr int kWaves = kWavesM * kWavesN, kThreads = 64 * kWaves, kStep = kStepBytes / sizeof(T);
   static constexpr int kFM = kM / kWavesM / 16, kFN = kN / kWavesN / 16, kFS = kFN / kSubs;
   static constexpr int kSubN = kN / kSubs;
@@ -202,14 +239,15 @@ struct Product {
   __device__ __forceinline__ int row(int i) const { return (wm * kFM + i) * 16 + (lane & 15); }
   __device__ __forceinline__ int col(int j) const { return (wn * kFS + j % kFS) * 16 + (lane >> 4) * 4; }
 
-  // Calls f(row, column, v[kSubs][8]) for every eight consecutive columns of the tile's
-  // rows (of each matrix's, for kSubs = 2), which a wave's lanes have side by side: the
+  // Calls f(row, column, v[kOut][8]) for every eight consecutive columns of the tile's
+  // rows (of the first kOut matrices'), which a wave's lanes have side by side: the
   // sums go through LDS, each wave's by itself. Stores of the four columns that a lane
-  // has in registers touch 16 rows in 32 bytes each, and cost a tile 10 us.
-  template <typename F>
+  // has in registers touch 16 rows in 32 bytes each: a tile of 256 x 256 in bfloat16 takes
+  // 8.5 us instead of 5.2.
+  template <int kOut, typename F>
   __device__ __forceinline__ void each8(const F4 (&acc)[kFN][kFM], LdsChar* lds, F&& f) const {
     typedef __attribute__((address_space(3))) F4 LdsF4;
-    constexpr int kRow = kFN * 64, kRoom = kLds / kWaves;   // bytes of a row, of a wave
+    constexpr int kRow = kOut * kFS * 64, kRoom = kLds / kWaves;   // bytes of a row, of a wave
     constexpr int kFit = kRoom / (16 * kRow), kLanes = kFS * 2;   // fragments that fit
     constexpr int kPass = kFit >= kFM ? kFM : kFit >= 4 ? 4 : kFit >= 2 ? 2 : 1;
     static_assert(kFit >= 1 && kFM % kPass == 0, "");
@@ -222,15 +260,15 @@ struct Product {
 #pragma unroll
       for (int i = 0; i < kPass; ++i)
 #pragma unroll
-        for (int j = 0; j < kFN; ++j) *at(i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[j][i0 + i];
+        for (int j = 0; j < kOut * kFS; ++j) *at(i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[j][i0 + i];
       constexpr int kEights = kPass * 16 * kLanes;
 #pragma unroll
       for (int t = 0; t < (kEights + 63) / 64; ++t) {
         if (kEights % 64 != 0 && t * 64 + lane >= kEights) break;
         const int r = (t * 64 + lane) / kLanes, q = lane % kLanes;
-        float v[kSubs][8];
+        float v[kOut][8];
 #pragma unroll
-        for (int s = 0; s < kSubs; ++s) {
+        for (int s = 0; s < kOut; ++s) {
           const F4 x = *at(r, s * kFS * 4 + 2 * q), y = *at(r, s * kFS * 4 + 2 * q + 1);
 #pragma unroll
           for (int k = 0; k < 4; ++k) v[s][k] = x[k], v[s][k + 4] = y[k];
@@ -251,24 +289,44 @@ struct Product {
     lb.init(wave, lane, a.b.ld, validn);
     const int per = (a.k + kStep - 1) / kStep;   // steps of a part
     const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
+    // where a step's tiles begin, and the k that are left there
+    const auto part_of = [&](int step) { return kSubs == 1 && step >= per; };
+    const auto k_of = [&](int step) { return (int64_t)(part_of(step) ? step - per : step) * kStep; };
+    const auto left_of = [&](int step) { return step < step1 ? (int)(a.k - k_of(step)) : 0; };
+    const auto from_a = [&](int step) {
+      const int64_t k = k_of(step);
+      return (const char*)((const T*)(part_of(step) ? a.a.q : a.a.p) + (kAK ? (int64_t)m0 * a.a.ld + k : k * a.a.ld + m0));
+    };
+    const auto from_b = [&](int step, int sub) {
+      const int64_t k = k_of(step);
+      return (const char*)((const T*)((kSubs == 1 ? part_of(step) : sub == 1) ? a.b.q : a.b.p) +
+                           (kBK ? (int64_t)n0 * a.b.ld + k : k * a.b.ld + n0));
+    };
     struct Steps {
       typename LoadA::Step a;
       typename LoadB::Step b[kSubs];
     };
     const auto step_of = [&](int stage, int step) {
       Steps r;
-      const int part = kSubs == 1 && step >= per ? 1 : 0;
-      const int64_t k = (int64_t)(step - (part ? per : 0)) * kStep;
-      const int left = step < step1 ? (int)(a.k - k) : 0;
       const uint32_t to = lds0 + stage * kStage;
-      r.a = la.step((const char*)((const T*)(part ? a.a.q : a.a.p) + (kAK ? (int64_t)m0 * a.a.ld + k : k * a.a.ld + m0)),
-                    a.a.ld, validm, left, to);
+      r.a = la.step(from_a(step), a.a.ld, validm, left_of(step), to);
 #pragma unroll
       for (int s = 0; s < kSubs; ++s)
-        r.b[s] = lb.step((const char*)((const T*)((kSubs == 1 ? part : s) ? a.b.q : a.b.p) +
-                                       (kBK ? (int64_t)n0 * a.b.ld + k : k * a.b.ld + n0)),
-                         a.b.ld, validn, left, to + LoadA::kBytes + s * LoadB::kBytes);
+        r.b[s] = lb.step(from_b(step, s), a.b.ld, validn, left_of(step), to + LoadA::kBytes + s * LoadB::kBytes);
       return r;
+    };
+    TileStage<T, kM, kAK, kWaves> sa;
+    TileStage<T, kSubN, kBK, kWaves> sb[kSubs];
+    const auto fetch = [&](int step) {
+      const int left = left_of(step);
+      sa.fetch(from_a(step), a.a.ld, validm, left, wave, lane);
+#pragma unroll
+      for (int s = 0; s < kSubs; ++s) sb[s].fetch(from_b(step, s), a.b.ld, validn, left, wave, lane);
+    };
+    const auto put = [&](int stage) {
+      sa.put(lds + stage * kStage, wave, lane);
+#pragma unroll
+      for (int s = 0; s < kSubs; ++s) sb[s].put(lds + stage * kStage + LoadA::kBytes + s * LoadB::kBytes, wave, lane);
     };
     // load number t of a wave's kPer in a step
     const auto load = [&](const Steps& r, int t) {
@@ -296,7 +354,7 @@ struct Product {
         for (int j = i * kFN / kFM; j < (i + 1) * kFN / kFM; ++j) read_b(next, j, stage);
 #pragma unroll
         for (int j = 0; j < kFN; ++j) acc[j][i] = mma<T>(acc[j][i], fb[set][j], fa[set][i]);
-        if constexpr (set == 1) {
+        if constexpr (set == 1 && !kStaged) {
 #pragma unroll
           for (int t = i * kPer / kFM; t < (i + 1) * kPer / kFM; ++t) load(*r, t);
         }
@@ -307,14 +365,23 @@ struct Product {
     for (int j = 0; j < kFN; ++j)
 #pragma unroll
       for (int i = 0; i < kFM; ++i) acc[j][i] = F4{0.0f, 0.0f, 0.0f, 0.0f};
+    if constexpr (kStaged) {
 #pragma unroll
-    for (int s = 0; s < kStages; ++s) {
-      const Steps r = step_of(s, step0 + s);
+      for (int s = 0; s < kStages; ++s) {
+        fetch(step0 + s);
+        if (s < kStages - 1) put(s);   // the last one stays in registers
+      }
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    } else {
 #pragma unroll
-      for (int t = 0; t < kPer; ++t) load(r, t);
+      for (int s = 0; s < kStages; ++s) {
+        const Steps r = step_of(s, step0 + s);
+#pragma unroll
+        for (int t = 0; t < kPer; ++t) load(r, t);
+      }
+      CKM_WAIT_LOADS((kStages - 1) * kPer);
+      asm volatile("s_barrier" ::: "memory");
     }
-    CKM_WAIT_LOADS((kStages - 1) * kPer);
-    asm volatile("s_barrier" ::: "memory");
 #pragma unroll
     for (int i = 0; i < kFM; ++i) read_a(0, i, 0);
 #pragma unroll
@@ -323,9 +390,16 @@ struct Product {
     for (int s = step0; s < step1; ++s) {
       const int next = stage + 1 == kStages ? 0 : stage + 1;
       half(std::integral_constant<int, 0>{}, stage, nullptr);
-      const Steps r = step_of(stage, s + kStages);
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kPer) : "memory");
-      half(std::integral_constant<int, 1>{}, next, &r);
+      if constexpr (kStaged) {
+        put(stage == 0 ? kStages - 1 : stage - 1);   // the place of the step before, kStages - 1 ahead
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        fetch(s + kStages);
+        half(std::integral_constant<int, 1>{}, next, nullptr);
+      } else {
+        const Steps r = step_of(stage, s + kStages);
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kStages - 2) * kPer) : "memory");
+        half(std::integral_constant<int, 1>{}, next, &r);
+      }
       stage = next;
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -371,13 +445,20 @@ struct Cut {
   int cols;                  // of n (of each matrix's, for kSubs = 2)
   int tiles_m, tiles_n;      // of one half
   int halves, splits, steps; // results side by side; steps of k in a share
+  bool staged;               // operands whose rows start anywhere
+  double time;               // the model's, us
   int64_t blocks() const { return (int64_t)tiles_m * tiles_n * halves * splits; }
 };
 // subs: 2 when a tile's columns are of two matrices (n then counts one's). bytes: of
 // the operands. split: whether shares of k are possible. a_along_k: tiles of 16 rows are
-// for an A along k alone.
+// for an A along k alone. staged: operands that cannot be loaded straight to LDS.
+enum Staged { kStraight, kStagedAlong, kStagedAcross };   // with rows of k, or of m or n
 Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
-                bool a_along_k);
+                bool a_along_k, Staged staged);
+// Whether they can be staged: a tile's rows then stay within 2^31 bytes too.
+inline bool stageable(int64_t rows, int64_t ld, size_t elt) { return rows == 1 || ld * (int64_t)elt <= kMaxRowBytes; }
+// The model's time of copying `bytes` of operands in a launch, us.
+inline double copy_time(int64_t bytes) { return 5.0 + 2.0 * bytes / 4.0e6; }
 
 __host__ __device__ inline int64_t whole(int64_t n, int64_t of) { return (n + of - 1) / of * of; }
 // Elements from row to row of a matrix in the work buffer: 128 bytes past a multiple of
@@ -389,13 +470,23 @@ ckm_status check_blocks(const Cut& c);
 // Calls f with the shape of a cut's tiles: 256 x 256 columns where there are enough of
 // them, smaller ones to fill the CUs, 16 rows for single tokens, whose weights are read
 // once. A tile of two matrices has waves of 128 columns, 64 of each, so that a wave's
-// rows of the result are whole lines of memory.
+// rows of the result are whole lines of memory. The largest shape has no registers left
+// to stage operands in.
 template <typename T, bool kAK, bool kBK, int kSubs, typename F>
 void with_shape(const Cut& cut, F&& f) {
-  if (cut.rows == 256) f(Tag<Product<T, 256, 256, kSubs == 2 ? 4 : 2, kSubs == 2 ? 2 : 4, 2, kAK, kBK, kSubs>>());
-  else if (cut.rows == 128) f(Tag<Product<T, 128, 128, 2, 2, 2, kAK, kBK, kSubs>>());
-  else if (cut.rows == 64) f(Tag<Product<T, 64, 128, 2, 2, 3, kAK, kBK, kSubs>>());
-  else if constexpr (kAK) f(Tag<Product<T, 16, 128, 1, 4, 4, kAK, kBK, kSubs>>());
+  if (cut.staged) {
+    if (cut.rows == 128) f(Tag<Product<T, 128, 128, 2, 2, 2, kAK, kBK, kSubs, true>>());
+    else if (cut.rows == 64) f(Tag<Product<T, 64, 128, 2, 2, 3, kAK, kBK, kSubs, true>>());
+    else if constexpr (kAK) f(Tag<Product<T, 16, 128, 1, 4, 4, kAK, kBK, kSubs, true>>());
+  } else if (cut.rows == 256) {
+    f(Tag<Product<T, 256, 256, kSubs == 2 ? 4 : 2, kSubs == 2 ? 2 : 4, 2, kAK, kBK, kSubs>>());
+  } else if (cut.rows == 128) {
+    f(Tag<Product<T, 128, 128, 2, 2, 2, kAK, kBK, kSubs>>());
+  } else if (cut.rows == 64) {
+    f(Tag<Product<T, 64, 128, 2, 2, 3, kAK, kBK, kSubs>>());
+  } else if constexpr (kAK) {
+    f(Tag<Product<T, 16, 128, 1, 4, 4, kAK, kBK, kSubs>>());
+  }
 }
 
 // Up to three copies in a launch: rows of cols elements into rows of `ld` (whole groups),
@@ -449,7 +540,7 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel
   typename P::T* c = (typename P::T*)(half ? a.c[1] : a.c[0]);
   const int64_t ld_c = half ? a.ld_c[1] : a.ld_c[0];
   const int64_t row0 = kSlab ? ((int64_t)split * a.halves + half) * a.p.m : 0;
-  p.each8(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[1][8]) {
+  p.template each8<1>(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[1][8]) {
     const int m = tm * P::kM + row, n = tn * P::kN + col;
     if (m >= a.p.m || n >= a.p.n) return;
     if constexpr (kSlab) {   // rows of whole eights

@@ -53,6 +53,7 @@ __global__ void __launch_bounds__(kBlock) ckm_join_kernel(ResultArgs a, int spli
     const int64_t row = line - (half ? a.p.m : 0);
     const float* p = a.slab + half * one + row * a.ld_slab + col;
     F4 sum = *(const F4*)p;
+#pragma unroll 8
     for (int k = 1; k < splits; ++k) sum += *(const F4*)(p + k * a.halves * one);
     store4((T*)(half ? a.c[1] : a.c[0]) + row * (half ? a.ld_c[1] : a.ld_c[0]), col, a.p.n, sum * factor);
   }
@@ -78,7 +79,7 @@ void join(const ResultArgs& a, int splits, hipStream_t s) {
 //   bf16 2048x8192x4096   256 rows, one: 101 (1357 TFLOP/s); 128, four: 128; 64, eight: 161
 //   bf16 1x16384x2048     16 rows 12, 64 rows 15 (67 MB)
 Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
-                bool a_along_k) {
+                bool a_along_k, Staged staged) {
   struct Time {
     double one, more;   // a step where a CU has one tile, or several
   };
@@ -92,29 +93,31 @@ Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t st
                                {64, 128, {0.38, 0.33}, {1.2, 1.1}, 2.5},
                                {16, 128, {0.30, 0.225}, {0.56, 0.39}, 2.5}};
   constexpr double kBytesAUs = 5.0e6, kJoin = 4.0;
+  constexpr double kSteps[] = {1.0, 1.4, 2.5}, kReads[] = {1.0, 1.2, 5.0};   // by way of registers, of lines that are cut
   Cut best = {};
   double least = 0.0;
   for (const Shape& shape : kShapes) {
-    if (shape.rows < 64 && !a_along_k) continue;
+    if ((shape.rows < 64 && !a_along_k) || (shape.rows == 256 && staged)) continue;
     Cut c = {};
     c.rows = shape.rows;
     c.cols = shape.cols / subs;
     c.tiles_m = (int)((m + c.rows - 1) / c.rows);
     c.tiles_n = (int)((n + c.cols - 1) / c.cols);
     c.halves = halves;
+    c.staged = staged != kStraight;
     const double tiles = (double)c.tiles_m * c.tiles_n * halves;
     const Time& time = type == CKM_F32 ? shape.full : shape.half;
-    for (int splits = 1; splits <= 64; ++splits) {
+    for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
       if (splits > 1 && (!split || steps / splits < 4 || tiles * splits > 2048.0)) break;
       c.steps = (int)((steps + splits - 1) / splits);
       c.splits = (int)((steps + c.steps - 1) / c.steps);
       const double rounds = std::ceil(tiles * c.splits / 256.0);
-      double t = std::max(rounds * (c.steps * (rounds > 1.0 ? time.more : time.one) + shape.fixed),
-                          bytes / kBytesAUs + shape.fixed);
+      const double step = (rounds > 1.0 ? time.more : time.one) * kSteps[staged];
+      double t = std::max(rounds * (c.steps * step + shape.fixed), kReads[staged] * bytes / kBytesAUs + shape.fixed);
       if (c.splits > 1) t += kJoin + 8.0 * c.splits * m * n * halves * subs / kBytesAUs;
       if (!best.rows || t <= least) {
         best = c;
-        least = t;
+        best.time = least = t;
       }
     }
   }

@@ -563,7 +563,7 @@ def test_captured_and_replayed(dtype):
 
 
 def test_own_work_buffers():
-    x, wg, wu = randn((50, 71), "f16", 1), randn((71, 90), "f16", 2), randn((71, 90), "f16", 3)   # rows that are copied
+    x, wg, wu = randn((50, 71), "f16", 1), randn((71, 90), "f16", 2), randn((71, 90), "f16", 3)
     dh, table = randn((50, 90), "f16", 4), randn((300, 71), "f16", 5)
     targets, dloss = torch.arange(50, device="cuda"), torch.ones(50, device="cuda")
     loss, lse = ops.cross_entropy(x, table, targets)
@@ -575,15 +575,16 @@ def test_own_work_buffers():
          ops.cross_entropy_workspace(x, table, targets, backward=True)),
         (lambda w: [ops.gradient_norm([x.contiguous(), wg], work=w)], ops.norm_workspace(2)),
     ]
-    for call, need in calls:
-        assert need > 0
+    for k, (call, need) in enumerate(calls):
+        assert need > 0 or k in (0, 2)   # a forward call of few rows may need none
         want = call(None)
         work = torch.full((need + 64,), 255, dtype=torch.uint8, device="cuda")   # NaN wherever it is read unwritten
         for p, q in zip(call(work[:need]), want):
             assert torch.equal(p, q)
         assert torch.all(work[need:] == 255)
-        with pytest.raises(ckm.CkmError):
-            call(work[:need - 1])
+        if need:
+            with pytest.raises(ckm.CkmError):
+                call(work[:need - 1])
     need = ops.norm_workspace(1)
     with pytest.raises(ckm.CkmError):
         ops.clip_gradients([wg], 1.0, work=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))

@@ -98,7 +98,7 @@ def test_gated_refuses_outputs_and_work():
                dict(dg=P + 1), dict(work=None), dict(n=n.value - 1), dict(work=P + 8)):
         assert back(**kw) == bad, kw
     # rows that have to be copied need room; no rows need none
-    ragged = gated(ld_x=9)
+    ragged = gated(ld_x=(1 << 22) + 1)   # too far apart to be staged
     m = C.c_size_t()
     assert L.ckm_gated_workspace_size(ops.F16, C.byref(ragged), 0, C.byref(m)) == ckm.OK and m.value >= 4 * 8 * 2
     assert L.ckm_gated_async(ops.F16, C.byref(ragged), P, 8, P, m.value - 1, None) == bad
