@@ -476,9 +476,9 @@ ckm_status ckm_softmax_backward_async(ckm_dtype type, const ckm_scores* scores, 
  * or do not end on them, may be copied into the work buffer first; the sizes of work
  * buffers go by the struct's pointers and strides too. Products are summed in
  * binary32, in an order that the sizes fix. */
-#define CKM_MAX_MATRIX_ROWS (1 << 30) /* rows of x */
+#define CKM_MAX_MATRIX_ROWS (1 << 24) /* rows of x */
 #define CKM_MAX_MATRIX_COLS (1 << 20) /* hidden and inner width */
-#define CKM_MAX_VOCAB (1 << 30)       /* rows of a vocabulary's table */
+#define CKM_MAX_VOCAB (1 << 24)       /* rows of a vocabulary's table */
 #define CKM_MAX_TENSORS (1 << 20)     /* of a norm */
 
 /* act(z): z / (1 + e^-z); z (1 + erf(z / sqrt 2)) / 2; max(z, 0), whose

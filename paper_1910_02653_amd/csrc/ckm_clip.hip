@@ -185,6 +185,7 @@ ckm_status check_tensors(int64_t count, const ckm_tensor* t) {
   if (count && !t) return set_error(CKM_E_INVALID_ARG, "tensors is NULL");
   int64_t chunks = 0;   // of a launch
   for (int64_t k = 0; k < count; ++k) {
+    if (k % kTensors == 0) chunks = 0;
     if (t[k].type < 0 || t[k].type > CKM_BF16 || !dtype_ok((int)t[k].type))
       return set_error(CKM_E_INVALID_ARG, "tensor %lld: unknown type %lld", (long long)k, (long long)t[k].type);
     if (t[k].count < 0) return set_error(CKM_E_INVALID_ARG, "tensor %lld: %lld elements", (long long)k, (long long)t[k].count);
@@ -193,7 +194,6 @@ ckm_status check_tensors(int64_t count, const ckm_tensor* t) {
     if (!t[k].d_in) return set_error(CKM_E_INVALID_ARG, "tensor %lld is NULL", (long long)k);
     if ((uintptr_t)t[k].d_in % dtype_bytes((int)t[k].type))
       return set_error(CKM_E_INVALID_ARG, "tensor %lld is not aligned to its elements", (long long)k);
-    if (k % kTensors == 0) chunks = 0;
     chunks += (t[k].count + kChunk - 1) / kChunk;
     if (chunks > INT32_MAX - kBlocks) return set_error(CKM_E_UNSUPPORTED, "tensor %lld: %lld elements", (long long)k, (long long)t[k].count);
   }

@@ -264,6 +264,7 @@ LossPlan plan_as(int type, const ckm_vocab& c, bool back, bool ragged_x, bool ra
   int64_t most = c.vocab;
   if (back) most = std::min(most, kPieceBytes / (int64_t)(c.rows * elt));
   if (p.pack_w) most = std::min(most, kTableBytes / (int64_t)(c.hidden * elt));
+  most = std::min(most, ((int64_t)1 << 30) / ((c.rows + 255) / 256));   // 2^22 tiles in a launch
   // as many columns in each
   const int64_t pieces = (c.vocab + std::max(most, kLeastPiece) - 1) / std::max(most, kLeastPiece);
   p.piece = std::min(c.vocab, whole((c.vocab + pieces - 1) / pieces, 256));

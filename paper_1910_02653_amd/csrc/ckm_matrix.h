@@ -107,7 +107,7 @@ struct TileLoad {
     const uint32_t o = kAlongK && (int)kpos >= s.left ? kNowhere : off[t];
     const uint32_t to = __builtin_amdgcn_readfirstlane(s.lds + (wave * kPer + t) % kLoads * 1024);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 ::"s"(to), "v"(o), "s"(s.rsrc) : "memory");
+                 ::"s"(to), "v"(o), "s"(s.rsrc) : "memory", "m0");
   }
 };
 
@@ -438,6 +438,7 @@ __device__ __forceinline__ void store4(T* row, int col, int cols, F4 v) {
       if (col + k < cols) row[col + k] = r[k];
   }
 }
+
 // How a product of m x n is cut: the shape of a tile, and shares of k, whose sums are
 // joined in a fixed order.
 struct Cut {

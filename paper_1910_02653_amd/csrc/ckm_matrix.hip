@@ -125,8 +125,8 @@ Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t st
 }
 
 ckm_status check_blocks(const Cut& c) {
-  return c.blocks() <= INT32_MAX ? CKM_OK
-                                 : set_error(CKM_E_UNSUPPORTED, "a product of %lld tiles", (long long)c.blocks());
+  constexpr int64_t kMost = ((int64_t)1 << 32) / 512 - 1;   // a launch's threads are counted in 32 bits
+  return c.blocks() <= kMost ? CKM_OK : set_error(CKM_E_UNSUPPORTED, "a product of %lld tiles", (long long)c.blocks());
 }
 
 void PackArgs::add(const void* src, int64_t rows, int64_t cols, int64_t ld_src, void* dst, int64_t ld) {

@@ -285,9 +285,10 @@ def test_cross_entropy_weighted_rows_and_peaked_logits(dtype):
 
 
 def test_cross_entropy_pieces():
-    """More rows and a larger vocabulary than one piece of d holds; the reference in 64 bits on the device, norms as in
-    check_gated_on_device."""
-    for dtype, rows, hidden, vocab in (("bf16", 9000, 40, 20011), ("f32", 5000, 24, 9500), ("f16", 8200, 136, 24600)):
+    """More rows and a larger vocabulary than one piece of d holds, and a table that is copied piece by piece (odd rows);
+    the reference in 64 bits on the device, norms as in check_gated_on_device."""
+    for dtype, rows, hidden, vocab in (("bf16", 9000, 40, 20011), ("f32", 5000, 24, 9500), ("f16", 8200, 136, 24600),
+                                       ("f16", 3000, 1001, 60001), ("bf16", 300, 1001, 60001), ("f32", 40, 2003, 30000)):
         log("cross entropy pieces %s" % dtype)
         x, w = randn((rows, hidden), dtype, 1), randn((vocab, hidden), dtype, 2, gain=2 * hidden ** -0.5)
         targets = torch.randint(-1, vocab, (rows,), generator=torch.Generator().manual_seed(3)).cuda()
@@ -295,6 +296,8 @@ def test_cross_entropy_pieces():
         t = x.double() @ w.double().t()
         some = targets >= 0
         want = torch.logsumexp(t, 1)
+        # logits of order 10 from sums of up to 2003 terms, |x| |w| of order 100 in all: (N + 8) u of a random walk's
+        # square root, and the logarithm's own
         assert float((lse - want).abs().max()) < 64 * U * 16
         at = t.gather(1, targets.clamp(min=0)[:, None])[:, 0]
         assert float((loss - torch.where(some, want - at, 0.0)).abs().max()) < 2 * 64 * U * 16
@@ -363,7 +366,7 @@ def test_rows_further_apart_than_32_bits_count():
     for p, q in zip(ops.gated_backward(dh, wide, wg, wu), ops.gated_backward(dh, x, wg, wu)):
         assert torch.equal(p, q)
     assert torch.equal(ops.gated(wg.t().contiguous()[:, :3].contiguous(), wide, wide), ops.gated(wg.t().contiguous()[:, :3].contiguous(), x, x))
-    targets, lse = torch.tensor([1, 2, 0], device="cuda"), None
+    targets = torch.tensor([1, 2, 0], device="cuda")
     w = randn((50, 72), "f16", 8)
     loss, lse = ops.cross_entropy(x, w, targets)
     assert torch.equal(ops.cross_entropy(wide, w, targets)[0], loss)

@@ -65,7 +65,7 @@ def gated(**kw):
 
 BAD_GATED = [
     (dict(rows=-1), ckm.E_INVALID_ARG), (dict(hidden=0), ckm.E_INVALID_ARG), (dict(inner=0), ckm.E_INVALID_ARG),
-    (dict(rows=(1 << 30) + 1), ckm.E_UNSUPPORTED), (dict(hidden=(1 << 20) + 1), ckm.E_UNSUPPORTED),
+    (dict(rows=(1 << 24) + 1), ckm.E_UNSUPPORTED), (dict(hidden=(1 << 20) + 1), ckm.E_UNSUPPORTED),
     (dict(inner=(1 << 20) + 1), ckm.E_UNSUPPORTED), (dict(act=3), ckm.E_INVALID_ARG), (dict(act=-1), ckm.E_INVALID_ARG),
     (dict(d_x=None), ckm.E_INVALID_ARG), (dict(d_gate=None), ckm.E_INVALID_ARG), (dict(d_up=None), ckm.E_INVALID_ARG),
     (dict(d_x=P + 1), ckm.E_INVALID_ARG), (dict(ld_x=-1), ckm.E_INVALID_ARG), (dict(ld_up=-8), ckm.E_INVALID_ARG),
@@ -106,7 +106,7 @@ def test_gated_refuses_outputs_and_work():
     assert L.ckm_gated_workspace_size(ops.F16, C.byref(none), 1, C.byref(m)) == ckm.OK and m.value == 0
     assert L.ckm_gated_async(ops.F16, C.byref(none), None, 8, None, 0, None) == ckm.OK
     # more tiles than a launch counts
-    vast = gated(rows=1 << 30, inner=1 << 20, hidden=1, ld_x=1, ld_gate=1 << 20, ld_up=1 << 20)
+    vast = gated(rows=1 << 24, inner=1 << 20, hidden=1, ld_x=1, ld_gate=1 << 20, ld_up=1 << 20)
     assert L.ckm_gated_async(ops.F16, C.byref(vast), P, 1 << 20, P, 1 << 62, None) == ckm.E_UNSUPPORTED
 
 
@@ -118,8 +118,8 @@ def vocab(**kw):
 
 BAD_VOCAB = [
     (dict(rows=-1), ckm.E_INVALID_ARG), (dict(hidden=0), ckm.E_INVALID_ARG), (dict(vocab=0), ckm.E_INVALID_ARG),
-    (dict(rows=(1 << 30) + 1), ckm.E_UNSUPPORTED), (dict(hidden=(1 << 20) + 1), ckm.E_UNSUPPORTED),
-    (dict(vocab=(1 << 30) + 1), ckm.E_UNSUPPORTED), (dict(d_x=None), ckm.E_INVALID_ARG),
+    (dict(rows=(1 << 24) + 1), ckm.E_UNSUPPORTED), (dict(hidden=(1 << 20) + 1), ckm.E_UNSUPPORTED),
+    (dict(vocab=(1 << 24) + 1), ckm.E_UNSUPPORTED), (dict(d_x=None), ckm.E_INVALID_ARG),
     (dict(d_weight=None), ckm.E_INVALID_ARG), (dict(d_targets=None), ckm.E_INVALID_ARG),
     (dict(d_weight=P + 1), ckm.E_INVALID_ARG), (dict(d_targets=P + 4), ckm.E_INVALID_ARG),
     (dict(ld_x=-1), ckm.E_INVALID_ARG), (dict(ld_weight=-8), ckm.E_INVALID_ARG),
