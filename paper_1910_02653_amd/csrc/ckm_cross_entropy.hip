@@ -238,6 +238,7 @@ struct LossPlan {
   int64_t ld_x, ld_w;
   int64_t piece;             // columns
   Cut logits, dx, dw;
+  bool together;             // dx and dW in a launch
   size_t x, w, parts, hit, most, d, slab, dw_slab, total;
   double time;               // the model's, us
 };
@@ -282,6 +283,8 @@ LossPlan plan_as(int type, const ckm_vocab& c, bool back, bool ragged_x, bool ra
                        staged_w ? kStagedAcross : kStraight);
     p.dw = cut_product(type, p.piece, c.hidden, 1, 1, (c.rows + step - 1) / step, d_bytes + x_bytes + w_bytes, true,
                        false, kStraight);
+    p.together = cut_together(type, p.dx, c.rows, c.hidden, (p.piece + step - 1) / step, p.dw, p.piece, c.hidden,
+                              (c.rows + step - 1) / step, d_bytes + x_bytes + 2 * w_bytes);
     p.time += p.dx.time + p.dw.time;
     p.most = take(sizeof(float));
     p.d = take((size_t)c.rows * row_of(p.piece, elt) * elt);
@@ -373,16 +376,18 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     a.p.b.p = a.p.b.q = wv;
     a.p.n = width;
     launch_logits<T, true>(a, plan.logits, s);
-    if (dx) {   // d W; a short last piece leaves shares at the end of k with nothing to add
-      rx.p = {{a.d, a.d, a.ld_d}, {wv, wv, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, width, 1};
-      launch_product<T, true, false>(rx, plan.dx, s);
-      rx.add = true;
-    }
-    if (dw) {   // d' x
-      rw.p = {{a.d, a.d, a.ld_d}, {x, x, plan.ld_x}, width, (int32_t)c.hidden, (int32_t)c.rows, 1};
-      rw.c[0] = (T*)dw + v * ld_dw;
-      Cut cut = plan.dw;
-      cut.tiles_m = (width + cut.rows - 1) / cut.rows;
+    // d W; a short last piece leaves shares at the end of k with nothing to add
+    rx.p = {{a.d, a.d, a.ld_d}, {wv, wv, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, width, 1};
+    // d' x
+    rw.p = {{a.d, a.d, a.ld_d}, {x, x, plan.ld_x}, width, (int32_t)c.hidden, (int32_t)c.rows, 1};
+    rw.c[0] = (T*)dw + v * ld_dw;
+    Cut cut = plan.dw;
+    cut.tiles_m = (width + cut.rows - 1) / cut.rows;
+    const bool both = plan.together && dx && dw;
+    if (both) launch_two<T, false>(rx, plan.dx, rw, cut, s);
+    else if (dx) launch_product<T, true, false>(rx, plan.dx, s);
+    rx.add = true;
+    if (dw && !both) {
       launch_product<T, false, false>(rw, cut, s);
       if (cut.splits > 1) launch_join(type, rw, cut.splits, s);
     }

@@ -206,6 +206,7 @@ struct GatedPlan {
   int64_t ld_x, ld_w;        // of the operands as multiplied
   int64_t inner, ld_d;       // columns of dg, padded to whole groups; a row of dg | du
   Cut both, dx, dw;
+  bool together;             // dx and the weights' gradients in a launch
   size_t x, w, d, slab, total;
   double time;               // the model's, us
 };
@@ -241,6 +242,8 @@ GatedPlan plan_as(int type, const ckm_gated& c, bool back, bool ragged_x, bool r
                        staged_w ? kStagedAlong : kStraight);
     p.dw = cut_product(type, c.hidden, c.inner, 2, 1, (c.rows + step - 1) / step, x_bytes + 2 * h_bytes + w_bytes, true,
                        false, staged_x ? kStagedAcross : kStraight);
+    p.together = cut_together(type, p.dx, c.rows, c.hidden, 2 * steps_f, p.dw, c.hidden, c.inner,
+                              (c.rows + step - 1) / step, x_bytes + 2 * h_bytes + 2 * w_bytes);
     p.time += p.dx.time + p.dw.time;
     p.d = take(c.rows * p.ld_d * elt);
     if (p.dx.splits > 1) slab = std::max(slab, (size_t)p.dx.splits * c.rows * whole(c.hidden, 8) * 4);
@@ -301,33 +304,33 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
   a.ld_out = plan.ld_d;
   a.up = (int32_t)plan.inner;
   launch_both<T, kBackward>(a, plan.both, s);
-  if (out) {   // dx = dg Wg' + du Wu'
-    ResultArgs r = {};
-    r.p = {{d, d + plan.inner, plan.ld_d}, {wg, wu, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden,
-           (int32_t)c.inner, 2};
-    r.c[0] = out;
-    r.ld_c[0] = ld_out;
-    r.factor = 1.0f;
-    r.halves = 1;
-    if (plan.dx.splits > 1) r.slab = slab;
-    r.ld_slab = whole(c.hidden, 8);
-    launch_product<T, true, true>(r, plan.dx, s);
-    if (plan.dx.splits > 1) launch_join(type, r, plan.dx.splits, s);
+  // dx = dg Wg' + du Wu'
+  ResultArgs rx = {}, rw = {};
+  rx.p = {{d, d + plan.inner, plan.ld_d}, {wg, wu, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, (int32_t)c.inner, 2};
+  rx.c[0] = out;
+  rx.ld_c[0] = ld_out;
+  rx.factor = rw.factor = 1.0f;
+  rx.halves = 1;
+  if (plan.dx.splits > 1) rx.slab = slab;
+  rx.ld_slab = whole(c.hidden, 8);
+  // dWg = x' dg, dWu = x' du
+  rw.p = {{x, x, plan.ld_x}, {d, d + plan.inner, plan.ld_d}, (int32_t)c.hidden, (int32_t)c.inner, (int32_t)c.rows, 1};
+  rw.c[0] = dgate;
+  rw.c[1] = dup;
+  rw.ld_c[0] = ld_dgate;
+  rw.ld_c[1] = ld_dup;
+  rw.halves = 2;
+  if (plan.dw.splits > 1) rw.slab = slab;
+  rw.ld_slab = whole(c.inner, 8);
+  if (plan.together && out && dgate) {
+    launch_two<T, true>(rx, plan.dx, rw, plan.dw, s);
+  } else if (out) {
+    launch_product<T, true, true>(rx, plan.dx, s);
   }
-  if (dgate) {   // dWg = x' dg, dWu = x' du
-    ResultArgs r = {};
-    r.p = {{x, x, plan.ld_x}, {d, d + plan.inner, plan.ld_d}, (int32_t)c.hidden, (int32_t)c.inner,
-           (int32_t)c.rows, 1};
-    r.c[0] = dgate;
-    r.c[1] = dup;
-    r.ld_c[0] = ld_dgate;
-    r.ld_c[1] = ld_dup;
-    r.factor = 1.0f;
-    r.halves = 2;
-    if (plan.dw.splits > 1) r.slab = slab;
-    r.ld_slab = whole(c.inner, 8);
-    launch_product<T, false, false>(r, plan.dw, s);
-    if (plan.dw.splits > 1) launch_join(type, r, plan.dw.splits, s);
+  if (out && plan.dx.splits > 1) launch_join(type, rx, plan.dx.splits, s);
+  if (dgate && !(plan.together && out)) {
+    launch_product<T, false, false>(rw, plan.dw, s);
+    if (plan.dw.splits > 1) launch_join(type, rw, plan.dw.splits, s);
   }
 }
 

@@ -456,6 +456,11 @@ struct Cut {
 enum Staged { kStraight, kStagedAlong, kStagedAcross };   // with rows of k, or of m or n
 Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
                 bool a_along_k, Staged staged);
+// Cuts of two products that share a launch, in place of the two given, if the model has
+// them done sooner; whether that is so. The first's tiles have 64 or 128 rows, the
+// second's 128, and no shares.
+bool cut_together(int type, Cut& a, int64_t m_a, int64_t n_a, int64_t steps_a, Cut& b, int64_t m_b, int64_t n_b,
+                  int64_t steps_b, int64_t bytes);
 // Whether they can be staged: a tile's rows then stay within 2^31 bytes too.
 inline bool stageable(int64_t rows, int64_t ld, size_t elt) { return rows == 1 || ld * (int64_t)elt <= kMaxRowBytes; }
 // The model's time of copying `bytes` of operands in a launch, us.
@@ -522,14 +527,14 @@ struct ResultArgs {
   int32_t tiles_m, tiles_n, halves, steps;   // Cut
 };
 
-// Two results' products share a launch: half h takes b's p or q (parts is 1 then).
+// A block's tile of a result. Two results side by side: half h takes b's p or q (parts
+// is 1 then).
 template <class P, bool kSlab>
-__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel(ResultArgs a) {
-  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+__device__ __forceinline__ void product_tile(const ResultArgs& a, int block, char* lds) {
   const P p;
-  const int tiles = a.tiles_m * a.tiles_n * a.halves, split = blockIdx.x / tiles;
+  const int tiles = a.tiles_m * a.tiles_n * a.halves, split = block / tiles;
   int tm, tn;
-  tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n * a.halves, tm, tn);
+  tile_of(block % tiles, a.tiles_m, a.tiles_n * a.halves, tm, tn);
   const int half = tn / a.tiles_n;
   tn -= half * a.tiles_n;
   ProductArgs product = a.p;
@@ -558,20 +563,56 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel
   });
 }
 
+template <class P, bool kSlab>
+__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_product_kernel(ResultArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+  product_tile<P, kSlab>(a, blockIdx.x, lds);
+}
+// Two results that need not wait for one another, each with blocks of its own: where
+// neither fills the CUs.
+template <class P, bool kSlab, class Q>
+__global__ void __launch_bounds__(P::kThreads, 2) ckm_two_products_kernel(ResultArgs a, int blocks_a, ResultArgs b) {
+  static_assert(P::kThreads == Q::kThreads, "");
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds > Q::kLds ? P::kLds : Q::kLds];
+  if ((int)blockIdx.x < blocks_a) product_tile<P, kSlab>(a, blockIdx.x, lds);
+  else product_tile<Q, false>(b, blockIdx.x - blocks_a, lds);
+}
+
 // Adds the shares of a result in their order.
 void launch_join(int type, const ResultArgs& a, int splits, hipStream_t s);
 
-template <typename T, bool kAK, bool kBK>
-void launch_product(ResultArgs a, const Cut& cut, hipStream_t s) {
+inline void set_cut(ResultArgs& a, const Cut& cut) {
   a.tiles_m = cut.tiles_m;
   a.tiles_n = cut.tiles_n;
   a.halves = cut.halves;
   a.steps = cut.steps;
+}
+
+template <typename T, bool kAK, bool kBK>
+void launch_product(ResultArgs a, const Cut& cut, hipStream_t s) {
+  set_cut(a, cut);
   with_shape<T, kAK, kBK, 1>(cut, [&](auto p) {
     using P = typename decltype(p)::Shape;
     if (a.slab) ckm_product_kernel<P, true><<<(uint32_t)cut.blocks(), P::kThreads, 0, s>>>(a);
     else ckm_product_kernel<P, false><<<(uint32_t)cut.blocks(), P::kThreads, 0, s>>>(a);
   });
+}
+
+// a: A along k, B along k or across it (kBK); b: both across. The cuts are together's.
+template <typename T, bool kBK>
+void launch_two(ResultArgs a, const Cut& cut_a, ResultArgs b, const Cut& cut_b, hipStream_t s) {
+  set_cut(a, cut_a);
+  set_cut(b, cut_b);
+  using Q = Product<T, 128, 128, 2, 2, 2, false, false, 1>;
+  const auto go = [&](auto p) {
+    using P = typename decltype(p)::Shape;
+    const uint32_t blocks = (uint32_t)(cut_a.blocks() + cut_b.blocks());
+    const int blocks_a = (int)cut_a.blocks();
+    if (a.slab) ckm_two_products_kernel<P, true, Q><<<blocks, P::kThreads, 0, s>>>(a, blocks_a, b);
+    else ckm_two_products_kernel<P, false, Q><<<blocks, P::kThreads, 0, s>>>(a, blocks_a, b);
+  };
+  if (cut_a.rows == 128) go(Tag<Product<T, 128, 128, 2, 2, 2, true, kBK, 1>>());
+  else go(Tag<Product<T, 64, 128, 2, 2, 3, true, kBK, 1>>());
 }
 
 }  // namespace ckm

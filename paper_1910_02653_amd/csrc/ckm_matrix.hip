@@ -69,6 +69,40 @@ void join(const ResultArgs& a, int splits, hipStream_t s) {
 
 }  // namespace
 
+struct Time {
+  double one, more;   // a step where a CU has one tile, or several
+};
+struct Shape {
+  int rows, cols;
+  Time half, full;    // 16-bit types, binary32
+  double fixed;
+  const Time& step(int type) const { return type == CKM_F32 ? full : half; }
+};
+// Largest first.
+constexpr Shape kShapes[] = {{256, 256, {1.5, 1.5}, {8.1, 8.1}, 7.0},
+                             {128, 128, {0.68, 0.51}, {2.2, 2.1}, 3.0},
+                             {64, 128, {0.38, 0.33}, {1.2, 1.1}, 2.5},
+                             {16, 128, {0.30, 0.225}, {0.56, 0.39}, 2.5}};
+constexpr double kCUs = 256.0, kBytesAUs = 5.0e6, kJoin = 4.0, kLaunch = 4.0;
+
+// The first values of a cut: its tiles and shares.
+Cut cut_as(const Shape& shape, int64_t m, int64_t n, int halves, int subs, int64_t steps, int splits, bool staged) {
+  Cut c = {};
+  c.rows = shape.rows;
+  c.cols = shape.cols / subs;
+  c.tiles_m = (int)((m + c.rows - 1) / c.rows);
+  c.tiles_n = (int)((n + c.cols - 1) / c.cols);
+  c.halves = halves;
+  c.steps = (int)((steps + splits - 1) / splits);
+  c.splits = (int)((steps + c.steps - 1) / c.steps);
+  c.staged = staged;
+  return c;
+}
+// The shares' way through memory.
+double join_time(const Cut& c, int64_t m, int64_t n, int subs) {
+  return c.splits > 1 ? kJoin + 8.0 * c.splits * m * n * c.halves * subs / kBytesAUs : 0.0;
+}
+
 // The cheapest cut by a model of the time: a CU takes one tile after the other, each as
 // many steps of k at the shape's measured time (longer where a CU has one tile and so
 // half its waves) and a fixed part (start, first loads, stores); no less than the
@@ -80,41 +114,19 @@ void join(const ResultArgs& a, int splits, hipStream_t s) {
 //   bf16 1x16384x2048     16 rows 12, 64 rows 15 (67 MB)
 Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
                 bool a_along_k, Staged staged) {
-  struct Time {
-    double one, more;   // a step where a CU has one tile, or several
-  };
-  struct Shape {
-    int rows, cols;
-    Time half, full;    // 16-bit types, binary32
-    double fixed;
-  };
-  constexpr Shape kShapes[] = {{256, 256, {1.5, 1.5}, {8.1, 8.1}, 7.0},
-                               {128, 128, {0.68, 0.51}, {2.2, 2.1}, 3.0},
-                               {64, 128, {0.38, 0.33}, {1.2, 1.1}, 2.5},
-                               {16, 128, {0.30, 0.225}, {0.56, 0.39}, 2.5}};
-  constexpr double kBytesAUs = 5.0e6, kJoin = 4.0;
   constexpr double kSteps[] = {1.0, 1.4, 2.5}, kReads[] = {1.0, 1.2, 5.0};   // by way of registers, of lines that are cut
   Cut best = {};
   double least = 0.0;
   for (const Shape& shape : kShapes) {
     if ((shape.rows < 64 && !a_along_k) || (shape.rows == 256 && staged)) continue;
-    Cut c = {};
-    c.rows = shape.rows;
-    c.cols = shape.cols / subs;
-    c.tiles_m = (int)((m + c.rows - 1) / c.rows);
-    c.tiles_n = (int)((n + c.cols - 1) / c.cols);
-    c.halves = halves;
-    c.staged = staged != kStraight;
-    const double tiles = (double)c.tiles_m * c.tiles_n * halves;
-    const Time& time = type == CKM_F32 ? shape.full : shape.half;
     for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
-      if (splits > 1 && (!split || steps / splits < 4 || tiles * splits > 2048.0)) break;
-      c.steps = (int)((steps + splits - 1) / splits);
-      c.splits = (int)((steps + c.steps - 1) / c.steps);
-      const double rounds = std::ceil(tiles * c.splits / 256.0);
+      const Cut c = cut_as(shape, m, n, halves, subs, steps, splits, staged != kStraight);
+      if (splits > 1 && (!split || steps / splits < 4 || c.blocks() > 2048)) break;
+      const double rounds = std::ceil(c.blocks() / kCUs);
+      const Time& time = shape.step(type);
       const double step = (rounds > 1.0 ? time.more : time.one) * kSteps[staged];
-      double t = std::max(rounds * (c.steps * step + shape.fixed), kReads[staged] * bytes / kBytesAUs + shape.fixed);
-      if (c.splits > 1) t += kJoin + 8.0 * c.splits * m * n * halves * subs / kBytesAUs;
+      const double t = std::max(rounds * (c.steps * step + shape.fixed), kReads[staged] * bytes / kBytesAUs + shape.fixed) +
+                       join_time(c, m, n, subs);
       if (!best.rows || t <= least) {
         best = c;
         best.time = least = t;
@@ -122,6 +134,43 @@ Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t st
     }
   }
   return best;
+}
+
+bool cut_together(int type, Cut& a, int64_t m_a, int64_t n_a, int64_t steps_a, Cut& b, int64_t m_b, int64_t n_b,
+                  int64_t steps_b, int64_t bytes) {
+  // long products have the larger tiles' rate to lose, and little to gain (f16
+  // 2048x2048x8192, gated gradient: 404 us apart, 448 together)
+  constexpr double kLong = 60.0, kGain = 0.92;
+  if (a.staged || b.staged || a.time + b.time > kLong) return false;
+  const Shape& shape_b = kShapes[1];
+  Cut d = cut_as(shape_b, m_b, n_b, b.halves, 1, steps_b, 1, false);
+  const Time& time_b = shape_b.step(type);
+  double least = kGain * (a.time + b.time + kLaunch);
+  bool found = false;
+  Cut best = {};
+  for (int k = 1; k <= 2; ++k) {
+    const Shape& shape = kShapes[k];
+    const Time& time = shape.step(type);
+    for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      const Cut c = cut_as(shape, m_a, n_a, 1, 1, steps_a, splits, false);
+      if (splits > 1 && (steps_a / splits < 4 || c.blocks() > 2048)) break;
+      // all the work shared out evenly, no less than the longest tile
+      const double work = (c.blocks() * (c.steps * time.more + shape.fixed) + d.blocks() * (d.steps * time_b.more + shape_b.fixed)) / kCUs;
+      const double longest = std::max(c.steps * time.one + shape.fixed, d.steps * time_b.one + shape_b.fixed);
+      const double t = std::max({work, longest, bytes / kBytesAUs + shape.fixed}) + join_time(c, m_a, n_a, 1);
+      if (t < least) {
+        least = t;
+        best = c;
+        found = true;
+      }
+    }
+  }
+  if (!found) return false;
+  a = best;
+  a.time = least;
+  b = d;
+  b.time = 0.0;
+  return true;
 }
 
 ckm_status check_blocks(const Cut& c) {
