@@ -532,9 +532,9 @@ ckm_status ckm_cross_entropy_async(ckm_dtype type, const ckm_vocab* vocab, float
                                    size_t work_bytes, void* stream);
 
 /* Its gradient from dloss [rows] and the forward call's lse: d = (exp(l - lse) -
- * 1[v = target]) dloss, rounded to `type`, dx = d W, dW = d' x. In binary16, d is
- * held relative to the largest |dloss|: rows whose dloss is less than 2^-12 of it
- * lose digits. dx or dW may be NULL. rows = 0 gives a zero dW. */
+ * 1[v = target]) dloss, rounded to `type`, dx = d W, dW = d' x. In 16 bits, d is
+ * held relative to the largest |dloss|; in binary16 rows whose dloss is less than
+ * 2^-12 of it lose digits. dx or dW may be NULL. rows = 0 gives a zero dW. */
 ckm_status ckm_cross_entropy_backward_async(ckm_dtype type, const ckm_vocab* vocab, const float* d_dloss,
                                             const float* d_lse, void* d_dx, int64_t ld_dx, void* d_dweight,
                                             int64_t ld_dweight, void* d_work, size_t work_bytes, void* stream);

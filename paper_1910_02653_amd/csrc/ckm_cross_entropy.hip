@@ -10,9 +10,11 @@
 // computed again, d is written for that piece alone, in the tensors' type, and the two
 // products after it read it from the caches; dx is summed over pieces in binary32.
 //
-// binary16 has too few exponents for d: exp(l - lse) is about 1 / vocab and dloss 1 /
-// rows. It holds d 2^15 / s, s the largest |dloss|, of at most 32768, and the
-// products' results are multiplied by s / 2^15.
+// In 16 bits d is held relative to s, the largest |dloss|, and the products' results are
+// multiplied by s: of a mean, where every row has the same dloss, a target's d is then
+// near -1, whose rounding is small; that of dloss itself would be off by as much in
+// every row, up to 2^-9 in bfloat16 and the same way. binary16, whose exponents are
+// too few (exp(l - lse) is about 1 / vocab), holds d 2^15 / s, of at most 32768.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -26,7 +28,10 @@ namespace {
 constexpr float kLog2e = 1.44269504f;
 constexpr float kLog2eRest = 1.92596299e-8f;   // log2(e) = the sum of both
 constexpr float kLn2 = 0.693147182f, kLn2Rest = -1.90465429e-9f;   // ln 2 = the sum of both
-constexpr float kHalfGain = 32768.0f;          // binary16's factor
+template <typename T>
+constexpr float kGain = std::is_same<T, _Float16>::value ? 32768.0f : 1.0f;
+template <typename T>
+constexpr bool kRelative = sizeof(T) == 2;       // d relative to the largest |dloss|
 
 struct LossArgs {
   ProductArgs p;            // n: of the vocabulary, or of a piece of it
@@ -37,7 +42,7 @@ struct LossArgs {
   float* loss;
   float* lse;               // written, or the gradient's input
   const float* dloss;
-  const float* most;        // binary16: the largest |dloss|
+  const float* most;        // 16 bits: the largest |dloss|
   void* d;                  // [rows][ld_d]
   int64_t ld_d, first;      // first: the piece's first column
   int32_t tile0, tiles_all; // its first tile, of all
@@ -152,18 +157,6 @@ __global__ void __launch_bounds__(256) ckm_loss_join_kernel(LossArgs a) {
   }
 }
 
-// The largest finite |dloss| of rows that have a target; 1 if that is 0.
-__global__ void __launch_bounds__(1024) ckm_loss_most_kernel(LossArgs a, float* out) {
-  __shared__ float lds[2 * 16];
-  float most = 0.0f;
-  for (int64_t r = threadIdx.x; r < a.p.m; r += 1024) {
-    const float v = fabsf(a.dloss[r]);
-    if (a.targets[r] >= 0 && a.targets[r] < a.vocab && v < INFINITY) most = fmaxf(most, v);
-  }
-  most = reduce_row<OpMax, 1024, 1024>(most, lds, 0);
-  if (threadIdx.x == 0) *out = most > 0.0f ? most : 1.0f;
-}
-
 template <class P>
 __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_back_kernel(LossArgs a) {
   using T = typename P::T;
@@ -183,7 +176,7 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_back_kern
     target -= a.first + (int64_t)tn * P::kN;   // within the tile
     const float base = live ? a.lse[m] * kLog2e : 0.0f;
     float by = some ? a.dloss[m] : 0.0f;
-    if constexpr (std::is_same<T, _Float16>::value) by = by / *a.most * kHalfGain;
+    if constexpr (kRelative<T>) by = by / *a.most * kGain<T>;
 #pragma unroll
     for (int j = 0; j < P::kFN; ++j)
 #pragma unroll
@@ -316,6 +309,9 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     if (back) {
       one.targets = c.d_targets;
       one.vocab = c.vocab;
+      one.dloss = dloss;
+      one.rows = c.rows;
+      if (kRelative<T>) one.most = (float*)(work + plan.most);
     }
     one.add(x, c.rows, c.hidden, c.ld_x, work + plan.x, plan.ld_x);
     launch_pack(type, one, s);
@@ -350,17 +346,12 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     return;
   }
   a.dloss = dloss;
-  constexpr bool kHalf = std::is_same<T, _Float16>::value;
-  float* most = (float*)(work + plan.most);
-  if (kHalf) {
-    ckm_loss_most_kernel<<<1, 1024, 0, s>>>(a, most);
-    a.most = most;
-  }
+  if (kRelative<T>) a.most = (const float*)(work + plan.most);
   a.d = work + plan.d;
   a.ld_d = row_of(plan.piece, sizeof(T));
   ResultArgs rx = {}, rw = {};
   rx.alpha = rw.alpha = a.most;
-  rx.factor = rw.factor = kHalf ? 1.0f / kHalfGain : 1.0f;
+  rx.factor = rw.factor = 1.0f / kGain<T>;
   const bool slab = plan.dx.splits > 1 || plan.piece < c.vocab;
   if (slab) rx.slab = (float*)(work + plan.slab);
   rx.ld_slab = rw.ld_slab = whole(c.hidden, 8);

@@ -509,6 +509,11 @@ struct PackArgs {
   int count;
   const int64_t* targets;
   int64_t vocab;
+  // with `most`, one more block: the largest finite |dloss| of rows that have a target,
+  // 1 if that is 0
+  const float* dloss;
+  float* most;
+  int64_t rows;
   void add(const void* src, int64_t rows, int64_t cols, int64_t ld_src, void* dst, int64_t ld);
 };
 void launch_pack(int type, const PackArgs& a, hipStream_t s);

@@ -17,6 +17,18 @@ constexpr int kBlock = 256;
 template <typename T>
 __global__ void __launch_bounds__(kBlock) ckm_pack_kernel(PackArgs a) {
   uint32_t block = blockIdx.x;
+  if (a.most && block == gridDim.x - 1) {
+    __shared__ float lds[2 * kBlock / 64];
+    float most = 0.0f;
+#pragma unroll 4
+    for (int64_t r = threadIdx.x; r < a.rows; r += kBlock) {
+      const float v = fabsf(a.dloss[r]);
+      if (a.targets[r] >= 0 && a.targets[r] < a.vocab && v < INFINITY) most = fmaxf(most, v);
+    }
+    most = reduce_row<OpMax, kBlock, kBlock>(most, lds, 0);
+    if (threadIdx.x == 0) *a.most = most > 0.0f ? most : 1.0f;
+    return;
+  }
   PackArgs::One p = a.one[0];
   if (block >= p.blocks) {
     block -= p.blocks;
@@ -186,7 +198,7 @@ void PackArgs::add(const void* src, int64_t rows, int64_t cols, int64_t ld_src, 
 }
 
 void launch_pack(int type, const PackArgs& a, hipStream_t s) {
-  const uint32_t blocks = a.one[0].blocks + a.one[1].blocks + a.one[2].blocks;
+  const uint32_t blocks = a.one[0].blocks + a.one[1].blocks + a.one[2].blocks + (a.most ? 1 : 0);
   if (blocks == 0) return;
   switch (type) {
     case CKM_F32: ckm_pack_kernel<float><<<blocks, kBlock, 0, s>>>(a); break;
