@@ -50,7 +50,7 @@ __device__ __forceinline__ void activation(int act, float z, float& a, float& da
   } else if (act == CKM_ACT_GELU) {
     float c, e;
     if constexpr (kFull) {
-      c = 0.5f * erfcf(z * -0.70710678f);
+      c = 0.5f * (1.0f + erff(z * 0.70710678f));
       e = expf(-0.5f * z * z);
     } else {
       const float t = __builtin_amdgcn_rcpf(fmaf(0.31112698f, fabsf(z), 1.0f));

@@ -92,10 +92,11 @@ struct Shape {
 };
 // Largest first.
 constexpr Shape kShapes[] = {{256, 256, {1.5, 1.5}, {8.1, 8.1}, 7.0},
-                             {128, 128, {0.68, 0.51}, {2.2, 2.1}, 3.0},
-                             {64, 128, {0.38, 0.33}, {1.2, 1.1}, 2.5},
-                             {16, 128, {0.30, 0.225}, {0.56, 0.39}, 2.5}};
+                             {128, 128, {0.68, 0.51}, {2.05, 1.95}, 4.0},
+                             {64, 128, {0.38, 0.33}, {1.15, 1.03}, 2.5},
+                             {16, 128, {0.30, 0.225}, {0.50, 0.38}, 2.5}};
 constexpr double kCUs = 256.0, kBytesAUs = 5.0e6, kJoin = 4.0, kLaunch = 4.0;
+constexpr double kSharesAUs = 9.0e6;   // bytes of shares, which the caches hold
 
 // The first values of a cut: its tiles and shares.
 Cut cut_as(const Shape& shape, int64_t m, int64_t n, int halves, int subs, int64_t steps, int splits, bool staged) {
@@ -112,7 +113,7 @@ Cut cut_as(const Shape& shape, int64_t m, int64_t n, int halves, int subs, int64
 }
 // The shares' way through memory.
 double join_time(const Cut& c, int64_t m, int64_t n, int subs) {
-  return c.splits > 1 ? kJoin + 8.0 * c.splits * m * n * c.halves * subs / kBytesAUs : 0.0;
+  return c.splits > 1 ? kJoin + 8.0 * c.splits * m * n * c.halves * subs / kSharesAUs : 0.0;
 }
 
 // The cheapest cut by a model of the time: a CU takes one tile after the other, each as
@@ -137,7 +138,9 @@ Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t st
       const double rounds = std::ceil(c.blocks() / kCUs);
       const Time& time = shape.step(type);
       const double step = (rounds > 1.0 ? time.more : time.one) * kSteps[staged];
-      const double t = std::max(rounds * (c.steps * step + shape.fixed), kReads[staged] * bytes / kBytesAUs + shape.fixed) +
+      // where a CU holds two tiles, one's fixed part is half hidden behind the other's steps
+      const double fixed = shape.fixed * (shape.rows == 256 ? rounds : 1.0 + 0.5 * (rounds - 1.0));
+      const double t = std::max(rounds * c.steps * step + fixed, kReads[staged] * bytes / kBytesAUs + shape.fixed) +
                        join_time(c, m, n, subs);
       if (!best.rows || t <= least) {
         best = c;
