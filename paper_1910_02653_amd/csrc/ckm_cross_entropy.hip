@@ -15,6 +15,12 @@
 // near -1, whose rounding is small; that of dloss itself would be off by as much in
 // every row, up to 2^-9 in bfloat16 and the same way. binary16, whose exponents are
 // too few (exp(l - lse) is about 1 / vocab), holds d 2^15 / s, of at most 32768.
+//
+// Bound by the products: f16 2048x2048x32768 238 us (1160 TFLOP/s), its gradient 753
+// (logits 290, dx 260 and 20 for its shares, dW 289 in a trace); bf16 4096x4096x131072
+// 10.2 ms (1290 TFLOP/s) in eight pieces. A tile's exponentials are one multiply-add and
+// one 2^x each. Few rows are bound by reading the table: bf16 16x4096x50021 82 to 87 us,
+// 410 MB at 4.8 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
