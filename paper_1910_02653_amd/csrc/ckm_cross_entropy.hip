@@ -431,6 +431,12 @@ ckm_status loss(ckm_dtype type, const ckm_vocab* c, bool back, const float* dlos
       return set_error(CKM_E_INVALID_ARG, "loss or lse is not aligned to 4 bytes");
     if (!loss_out && !lse) return CKM_OK;
   }
+  const Place x = {"x", c->d_x, c->rows, c->hidden, c->ld_x, elt}, w = {"weight", c->d_weight, c->vocab, c->hidden, c->ld_weight, elt},
+              targets = {"targets", c->d_targets, 1, c->rows, 0, 8}, sums = {"lse", lse, 1, c->rows, 0, 4};
+  st = back ? check_apart({{"dx", dx, c->rows, c->hidden, ld_dx, elt}, {"dweight", dw, c->vocab, c->hidden, ld_dw, elt}},
+                          {x, w, targets, sums, {"dloss", dloss, 1, c->rows, 0, 4}})
+            : check_apart({{"loss", loss_out, 1, c->rows, 0, 4}, sums}, {x, w, targets});
+  if (st != CKM_OK) return st;
   const LossPlan plan = plan_of(type, *c, back);
   if ((st = check_blocks(plan.logits)) != CKM_OK) return st;
   if (back && ((st = check_blocks(plan.dx)) != CKM_OK || (st = check_blocks(plan.dw)) != CKM_OK)) return st;

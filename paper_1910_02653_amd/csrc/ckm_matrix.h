@@ -28,6 +28,8 @@
 // 3 %); loads at once at the step's begin (232 instead of 209).
 #pragma once
 
+#include <initializer_list>
+
 #include "ckm_ops.h"
 
 namespace ckm {
@@ -483,6 +485,15 @@ __host__ __device__ inline int64_t whole(int64_t n, int64_t of) { return (n + of
 // Elements from row to row of a matrix in the work buffer: 128 bytes past a multiple of
 // 256, so that a tile's rows are spread over the memory's channels.
 inline int64_t row_of(int64_t cols, size_t elt) { return (whole(cols * elt, 256) + 128) / elt; }
+// A matrix that a call writes or reads, and whether two share an element: by their
+// ranges, and where their rows lie at one stride by the columns.
+struct Place {
+  const char* name;
+  const void* p;
+  int64_t rows, cols, ld;
+  size_t elt;
+};
+ckm_status check_apart(std::initializer_list<Place> outputs, std::initializer_list<Place> inputs);
 // CKM_E_UNSUPPORTED for a grid past what a launch counts.
 ckm_status check_blocks(const Cut& c);
 

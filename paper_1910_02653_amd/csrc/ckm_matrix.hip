@@ -199,6 +199,27 @@ bool cut_together(int type, Cut& a, int64_t m_a, int64_t n_a, int64_t steps_a, C
   return true;
 }
 
+static bool share(const Place& a, const Place& b) {
+  if (!a.p || !b.p || !a.rows || !b.rows || !a.cols || !b.cols) return false;
+  const __int128 pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+  const __int128 ca = (__int128)a.cols * a.elt, cb = (__int128)b.cols * b.elt, ra = (__int128)a.ld * a.elt, rb = (__int128)b.ld * b.elt;
+  if (pa + (a.rows - 1) * ra + ca <= pb || pb + (b.rows - 1) * rb + cb <= pa) return false;
+  if (a.rows == 1 || b.rows == 1 || ra != rb || ra < ca || ra < cb) return true;
+  // rows of one stride: from a's columns to b's, around the stride
+  const __int128 by = ((pb - pa) % ra + ra) % ra;
+  return by < ca || by + cb > ra;
+}
+
+ckm_status check_apart(std::initializer_list<Place> outputs, std::initializer_list<Place> inputs) {
+  for (const Place* o = outputs.begin(); o != outputs.end(); ++o) {
+    for (const Place& i : inputs)
+      if (share(*o, i)) return set_error(CKM_E_INVALID_ARG, "%s overlaps %s", o->name, i.name);
+    for (const Place* q = o + 1; q != outputs.end(); ++q)
+      if (share(*o, *q)) return set_error(CKM_E_INVALID_ARG, "%s overlaps %s", o->name, q->name);
+  }
+  return CKM_OK;
+}
+
 ckm_status check_blocks(const Cut& c) {
   constexpr int64_t kMost = ((int64_t)1 << 32) / 512 - 1;   // a launch's threads are counted in 32 bits
   return c.blocks() <= kMost ? CKM_OK : set_error(CKM_E_UNSUPPORTED, "a product of %lld tiles", (long long)c.blocks());

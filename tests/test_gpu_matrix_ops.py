@@ -595,7 +595,7 @@ def test_own_work_buffers():
 
 def test_refusals():
     x, w = randn((6, 40), "f16", 1), randn((40, 24), "f16", 2)
-    dh, table = randn((6, 24), "f16", 3), randn((50, 40), "f16", 4)
+    dh, table, square = randn((6, 24), "f16", 3), randn((50, 40), "f16", 4), randn((40, 40), "f16", 5)
     targets = torch.zeros(6, dtype=torch.int64, device="cuda")
     dloss = torch.ones(6, device="cuda")
     lse = torch.zeros(6, device="cuda")
@@ -611,6 +611,8 @@ def test_refusals():
         lambda: ops.gated(x, w, w, act="tanh"),
         lambda: ops.gated(x, w, w, out=dh[:5]),
         lambda: ops.gated(x, w, w, out=dh.float()),
+        lambda: ops.gated(x, square, square, out=x),               # over its own operands
+        lambda: ops.gated(x, square, square, out=square[5:11]),
         lambda: ops.gated(x[:, :0], w[:0], w[:0]),
         lambda: ops.gated(x, w[:, :0], w[:, :0]),
         lambda: ops.gated_backward(dh[:, :23], x, w, w),
@@ -645,6 +647,11 @@ def test_refusals():
         with pytest.raises((ValueError, ckm.CkmError)):
             f()
             print("not refused: %d" % k)
+    # in the rows of its own operand's matrix, but past its columns
+    both = torch.zeros((6, 80), dtype=torch.float16, device="cuda")
+    both[:, :40] = x
+    assert torch.equal(ops.gated(both[:, :40], square, square, out=both[:, 40:]), ops.gated(x, square, square))
+    assert torch.equal(both[:, :40], x)
     # listed in another's place: the outputs swap
     a, b = torch.ones(4, device="cuda"), torch.full((4,), 2.0, device="cuda")
     with pytest.raises(ckm.CkmError):

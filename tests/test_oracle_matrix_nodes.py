@@ -53,12 +53,13 @@ def test_known_values():
     assert np.isclose(loss[0], np.log(8)) and np.isclose(lse[0], np.log(8))
 
 
-# pointers that are aligned and never followed: every call below is refused before a launch
-P = 1 << 20
+# pointers that are aligned and never followed: every call below is refused before a launch (operands from P on, far
+# from one another, outputs from Q on)
+P, Q = 1 << 20, 1 << 40
 
 
 def gated(**kw):
-    v = dict(rows=4, hidden=8, inner=8, act=0, d_x=P, ld_x=8, d_gate=P, ld_gate=8, d_up=P, ld_up=8)
+    v = dict(rows=4, hidden=8, inner=8, act=0, d_x=P, ld_x=8, d_gate=2 * P, ld_gate=8, d_up=3 * P, ld_up=8)
     v.update(kw)
     return ops._Gated(*(v[n] for n, _ in ops._Gated._fields_))
 
@@ -93,7 +94,7 @@ def test_gated_refuses_outputs_and_work():
     assert L.ckm_gated_workspace_size(ops.F16, C.byref(c), 0, None) == bad
     assert L.ckm_gated_workspace_size(ops.F16, C.byref(c), 1, C.byref(n)) == ckm.OK and n.value >= 4 * 2 * 8 * 2
     back = lambda **kw: L.ckm_gated_backward_async(ops.F16, C.byref(c), *(   # noqa: E731
-        {**dict(dh=P, ldh=8, dx=P, ldx=8, dg=P, ldg=8, du=P, ldu=8, work=P, n=n.value), **kw}).values(), None)
+        {**dict(dh=4 * P, ldh=8, dx=Q, ldx=8, dg=2 * Q, ldg=8, du=3 * Q, ldu=8, work=P, n=n.value), **kw}).values(), None)
     for kw in (dict(dh=None), dict(ldx=7), dict(ldg=7), dict(ldu=7), dict(dg=None), dict(du=None), dict(dx=P + 1),
                dict(dg=P + 1), dict(work=None), dict(n=n.value - 1), dict(work=P + 8)):
         assert back(**kw) == bad, kw
@@ -101,17 +102,25 @@ def test_gated_refuses_outputs_and_work():
     ragged = gated(ld_x=(1 << 22) + 1)   # too far apart to be staged
     m = C.c_size_t()
     assert L.ckm_gated_workspace_size(ops.F16, C.byref(ragged), 0, C.byref(m)) == ckm.OK and m.value >= 4 * 8 * 2
-    assert L.ckm_gated_async(ops.F16, C.byref(ragged), P, 8, P, m.value - 1, None) == bad
+    assert L.ckm_gated_async(ops.F16, C.byref(ragged), Q, 8, P, m.value - 1, None) == bad
     none = gated(rows=0, d_x=None)
     assert L.ckm_gated_workspace_size(ops.F16, C.byref(none), 1, C.byref(m)) == ckm.OK and m.value == 0
     assert L.ckm_gated_async(ops.F16, C.byref(none), None, 8, None, 0, None) == ckm.OK
     # more tiles than a launch counts
     vast = gated(rows=1 << 24, inner=1 << 20, hidden=1, ld_x=1, ld_gate=1 << 20, ld_up=1 << 20)
-    assert L.ckm_gated_async(ops.F16, C.byref(vast), P, 1 << 20, P, 1 << 62, None) == ckm.E_UNSUPPORTED
+    assert L.ckm_gated_async(ops.F16, C.byref(vast), 1 << 60, 1 << 20, P, 1 << 62, None) == ckm.E_UNSUPPORTED
+    # outputs over operands or one another, by an element; side by side in one matrix's rows they are apart
+    for kw in (dict(dx=P), dict(dx=P + 62), dict(dx=P - 62), dict(dx=2 * P), dict(dg=3 * P), dict(du=2 * Q), dict(dg=Q, ldg=8),
+               dict(dx=4 * P + 2), dict(du=2 * Q + 126)):
+        assert back(**kw) == bad and b"overlaps" in L.ckm_last_error(), kw
+    for kw in (dict(du=2 * Q + 16, ldg=16, ldu=16), dict(dx=P + 64)):
+        assert back(**kw, n=0) == bad and b"work buffer" in L.ckm_last_error(), kw   # past the check
+    for p in (P, 2 * P, 3 * P, 3 * P + 126):
+        assert L.ckm_gated_async(ops.F16, C.byref(c), p, 8, P, 1 << 40, None) == bad and b"overlaps" in L.ckm_last_error()
 
 
 def vocab(**kw):
-    v = dict(rows=4, hidden=8, vocab=100, d_x=P, ld_x=8, d_weight=P, ld_weight=8, d_targets=P)
+    v = dict(rows=4, hidden=8, vocab=100, d_x=P, ld_x=8, d_weight=2 * P, ld_weight=8, d_targets=3 * P)
     v.update(kw)
     return ops._Vocab(*(v[n] for n, _ in ops._Vocab._fields_))
 
@@ -137,22 +146,28 @@ def test_cross_entropy_refusals(kw, status):
 def test_cross_entropy_refuses_outputs_and_work():
     L, c, n, bad = ckm.lib(), vocab(), C.c_size_t(), ckm.E_INVALID_ARG
     assert L.ckm_cross_entropy_workspace_size(ops.BF16, C.byref(c), 0, C.byref(n)) == ckm.OK and n.value > 0
-    assert L.ckm_cross_entropy_async(7, C.byref(c), P, P, P, n.value, None) == bad
-    assert L.ckm_cross_entropy_async(ops.BF16, None, P, P, P, n.value, None) == bad
-    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), P + 2, P, P, n.value, None) == bad
-    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), P, P + 2, P, n.value, None) == bad
-    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), P, P, None, n.value, None) == bad
-    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), P, P, P, n.value - 1, None) == bad
-    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), P, P, P + 8, n.value, None) == bad
+    assert L.ckm_cross_entropy_async(7, C.byref(c), Q, 2 * Q, P, n.value, None) == bad
+    assert L.ckm_cross_entropy_async(ops.BF16, None, Q, 2 * Q, P, n.value, None) == bad
+    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), Q + 2, 2 * Q, P, n.value, None) == bad
+    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), Q, 2 * Q + 2, P, n.value, None) == bad
+    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), Q, 2 * Q, None, n.value, None) == bad
+    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), Q, 2 * Q, P, n.value - 1, None) == bad
+    assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), Q, 2 * Q, P + 8, n.value, None) == bad
     assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), None, None, None, 0, None) == ckm.OK   # nothing asked
     assert L.ckm_cross_entropy_workspace_size(ops.BF16, C.byref(c), 0, None) == bad
     assert L.ckm_cross_entropy_workspace_size(ops.BF16, C.byref(c), 1, C.byref(n)) == ckm.OK and n.value >= 4 * 100 * 2
     back = lambda **kw: L.ckm_cross_entropy_backward_async(ops.BF16, C.byref(c), *(   # noqa: E731
-        {**dict(dl=P, lse=P, dx=P, ldx=8, dw=P, ldw=8, work=P, n=n.value), **kw}).values(), None)
+        {**dict(dl=4 * P, lse=5 * P, dx=Q, ldx=8, dw=2 * Q, ldw=8, work=P, n=n.value), **kw}).values(), None)
     for kw in (dict(dl=None), dict(dl=P + 2), dict(lse=None), dict(lse=P + 2), dict(ldx=7), dict(ldw=7), dict(dx=P + 1),
                dict(dw=P + 1), dict(work=None), dict(n=n.value - 1), dict(work=P + 8)):
         assert back(**kw) == bad, kw
     assert back(dx=None, dw=None) == ckm.OK
+    for kw in (dict(dx=P), dict(dw=2 * P), dict(dx=3 * P), dict(dw=4 * P), dict(dx=5 * P), dict(dx=2 * Q), dict(dw=P + 62)):
+        assert back(**kw) == bad and b"overlaps" in L.ckm_last_error(), kw
+    assert L.ckm_cross_entropy_workspace_size(ops.BF16, C.byref(c), 0, C.byref(n)) == ckm.OK
+    for loss, lse in ((P, Q), (Q, 2 * P), (Q, Q), (Q, Q + 12), (3 * P, Q)):
+        assert L.ckm_cross_entropy_async(ops.BF16, C.byref(c), loss, lse, P, n.value, None) == bad
+        assert b"overlaps" in L.ckm_last_error()
     # the work buffer holds a piece of the vocabulary at most, not its logits
     big = vocab(rows=1 << 16, hidden=64, vocab=1 << 18, ld_x=64, ld_weight=64)
     assert L.ckm_cross_entropy_workspace_size(ops.BF16, C.byref(big), 1, C.byref(n)) == ckm.OK
