@@ -18,8 +18,8 @@
 //
 // Bound by the products: f16 2048x2048x32768 238 us (1160 TFLOP/s), its gradient 753
 // (logits 290, dx 260 and 20 for its shares, dW 289 in a trace); bf16 4096x4096x131072
-// 10.2 ms (1290 TFLOP/s) in eight pieces. A tile's exponentials are one multiply-add and
-// one 2^x each. Few rows are bound by reading the table: bf16 16x4096x50021 82 to 87 us,
+// 10.2 ms (1290 TFLOP/s) in eight pieces. A tile's exponentials are a difference, a
+// product and one 2^x each. Few rows are bound by reading the table: bf16 16x4096x50021 82 to 87 us,
 // 410 MB at 4.8 TB/s.
 #include <hip/hip_runtime.h>
 
@@ -32,8 +32,6 @@ namespace ckm {
 namespace {
 
 constexpr float kLog2e = 1.44269504f;
-constexpr float kLog2eRest = 1.92596299e-8f;   // log2(e) = the sum of both
-constexpr float kLn2 = 0.693147182f, kLn2Rest = -1.90465429e-9f;   // ln 2 = the sum of both
 template <typename T>
 constexpr float kGain = std::is_same<T, _Float16>::value ? 32768.0f : 1.0f;
 template <typename T>
@@ -55,28 +53,22 @@ struct LossArgs {
   int64_t vocab;
 };
 
-// (base, sum): sum 2^base of exponentials, whose largest is about 2^base; sum 0: none.
+// e^(v - base) for v <= base or so. The difference first: its rounding is relative to
+// itself, so that logits of any size keep their distances (v log2 e less a rounded base
+// log2 e, one operation instead of two, is off by 2^7 and more past logits of 2^31, and was
+// no faster: f16 2048x2048x32768 255 to 259 us both).
+template <typename T>
+__device__ __forceinline__ float power_of(float v, float base) {
+  if constexpr (std::is_same<T, float>::value) return expf(v - base);
+  else return __builtin_amdgcn_exp2f((v - base) * kLog2e);
+}
+
+// (base, sum): sum e^base of exponentials, whose largest is e^base; sum 0: none.
 __device__ __forceinline__ float2 join_parts(float2 p, float2 q) {
   if (q.y == 0.0f) return p;
   if (p.y == 0.0f) return q;
   const float base = fmaxf(p.x, q.x);   // a NaN is in the sums too
-  return make_float2(base, p.y * __builtin_amdgcn_exp2f(p.x - base) + q.y * __builtin_amdgcn_exp2f(q.x - base));
-}
-
-// 2^(v log2 e - base) for v log2 e - base <= 0 or so. With binary32 tensors the products'
-// roundings are made good; with 16-bit ones they are below what the operands' own
-// rounding leaves of v, and `base`, rounded once a row, is what the logarithm adds again.
-template <typename T>
-__device__ __forceinline__ float power_of(float v, float base) {
-  if constexpr (std::is_same<T, float>::value) {
-    const float u = v * kLog2e, rest = fmaf(v, kLog2eRest, fmaf(v, kLog2e, -u));
-    const float w = u - base, back = w - u;
-    const float lost = ((u - (w - back)) - (base + back)) + rest;   // of the difference, and of the product
-    const float e = __builtin_amdgcn_exp2f(w);
-    return w > -126.0f && w < 126.0f ? fmaf(e, lost * kLn2, e) : e;
-  } else {
-    return __builtin_amdgcn_exp2f(fmaf(v, kLog2e, -base));
-  }
+  return make_float2(base, p.y * power_of<_Float16>(p.x, base) + q.y * power_of<_Float16>(q.x, base));
 }
 
 template <class P>
@@ -117,7 +109,7 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_kernel(Lo
     // the four lanes that hold a row
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
-    const float base = most == -INFINITY ? 0.0f : most * kLog2e;
+    const float base = most == -INFINITY ? 0.0f : most;
     float sum[4] = {};
 #pragma unroll
     for (int j = 0; j < P::kFN; ++j)
@@ -151,12 +143,11 @@ __global__ void __launch_bounds__(256) ckm_loss_join_kernel(LossArgs a) {
   if (base == -INFINITY) base = 0.0f;
   for (int k = lane; k < a.tiles_all; k += 64) {
     const float2 v = parts[k];
-    if (v.y != 0.0f) sum += v.y * __builtin_amdgcn_exp2f(v.x - base);
+    if (v.y != 0.0f) sum += v.y * power_of<_Float16>(v.x, base);
   }
   sum = reduce64<OpSum>(sum);
   if (lane == 0) {
-    // (base + log2 sum) ln 2, the product with what base's loses
-    const float t = base * kLn2, lse = t + (fmaf(base, kLn2, -t) + fmaf(base, kLn2Rest, logf(sum)));
+    const float lse = base + logf(sum);
     const int64_t target = a.targets[row];
     if (a.lse) a.lse[row] = lse;
     if (a.loss) a.loss[row] = target >= 0 && target < a.vocab ? lse - a.hit[row] : 0.0f;
@@ -180,18 +171,13 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_back_kern
     int64_t target = live ? a.targets[m] : -1;
     const bool some = target >= 0 && target < a.vocab;
     target -= a.first + (int64_t)tn * P::kN;   // within the tile
-    const float base = live ? a.lse[m] * kLog2e : 0.0f;
+    const float base = live ? a.lse[m] : 0.0f;
     float by = some ? a.dloss[m] : 0.0f;
     if constexpr (kRelative<T>) by = by / *a.most * kGain<T>;
 #pragma unroll
     for (int j = 0; j < P::kFN; ++j)
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float e;
-        if constexpr (std::is_same<T, float>::value) e = expf(acc[j][i][k] - (live ? a.lse[m] : 0.0f));
-        else e = power_of<T>(acc[j][i][k], base);
-        acc[j][i][k] = some ? e * by : 0.0f;
-      }
+      for (int k = 0; k < 4; ++k) acc[j][i][k] = some ? power_of<T>(acc[j][i][k], base) * by : 0.0f;
     if (some && target >= 0 && target < P::kN) {
 #pragma unroll
       for (int j = 0; j < P::kFN; ++j)

@@ -313,6 +313,33 @@ def test_cross_entropy_pieces():
         del t
 
 
+@pytest.mark.parametrize("dtype,log_step", [("bf16", 12), ("bf16", 33), ("bf16", 100), ("f16", 10), ("f16", 28), ("f32", 12),
+                                            ("f32", 33), ("f32", 100)])
+def test_cross_entropy_of_vast_logits(dtype, log_step):
+    """Exact logits, whole steps of 2^log_step apart: lse is the largest, a row's d 1 there and -1 at its target."""
+    side, unit = 2.0 ** ((log_step + 2) // 2), 2.0 ** (log_step - 3 - (log_step + 2) // 2)   # 8 products of both are a step
+    for rows, vocab in ((5, 300), (300, 1030)):
+        log("cross entropy of vast logits %s 2^%d %dx%d" % (dtype, log_step, rows, vocab))
+        gen = torch.Generator().manual_seed(rows)
+        steps = torch.randint(-15, 16, (vocab,), generator=gen)
+        steps[7], steps[11] = 31, -31
+        targets = torch.randint(0, vocab, (rows,), generator=gen)
+        targets[:3] = torch.tensor([7, 11, -1])
+        x = torch.full((rows, 8), side, dtype=TYPES[dtype], device="cuda")
+        w = (steps[:, None] * unit).expand(vocab, 8).to(TYPES[dtype]).contiguous().cuda()
+        loss, lse = ops.cross_entropy(x, w, targets.cuda())
+        some = targets >= 0
+        assert torch.all(lse.cpu().double() == 31 * 2.0 ** log_step)
+        assert torch.equal(loss.cpu().double(), torch.where(some, (31 - steps[targets.clamp(min=0)]) * 2.0 ** log_step, 0.0))
+        by = 2.0 ** -10
+        dx, dw = ops.cross_entropy_backward(torch.full((rows,), by, device="cuda"), x, w, targets.cuda(), lse)
+        d = torch.zeros((rows, vocab), dtype=torch.float64)
+        d[some, 7] = by
+        d[some.nonzero()[:, 0], targets[some]] -= by
+        for y, z in ((dx, d @ w.cpu().double()), (dw, d.t() @ x.cpu().double())):   # exact sums, rounded once
+            assert torch.all((y.cpu().double() - z).abs() <= HALF_ULP[dtype] * z.abs())
+
+
 def test_cross_entropy_extremes():
     x, w = randn((5, 40), "f16", 1), randn((70, 40), "f16", 2)
     targets = torch.tensor([3, -100, 69, 70, 0], device="cuda")
