@@ -10,12 +10,12 @@ softmax and their gradients by the package's operators, matrix products by the
 library. With --gated the feed-forward is the gated one, one node forward and
 one for its gradient, which keeps no projection; with --vocab the loss is the
 cross entropy against a vocabulary, whose logits never exist; with --clip the
-gradients' norm is bounded at the end of the step. A node that a stage computes again has the bits it had before (its
-dropout masks are functions of seed, site, row and column), so a budget changes
-memory and time and no number.
+gradients' norm is bounded at the end of the step. A node that a stage computes
+again has the bits it had before (its dropout masks are functions of seed, site,
+row and column), so a budget changes memory and time and no number.
 
     python examples/planned_transformer.py --blocks 4 --tokens 1024 --budgets 100 60 40
-    python examples/planned_transformer.py --gated --vocab 32768 --clip 1.0
+    python examples/planned_transformer.py --gated --vocab 32768 --clip 1.0 --budgets 100 60 50
 """
 from __future__ import annotations
 

@@ -1,5 +1,7 @@
 """The planned transformer with its gated feed-forward, its loss against a vocabulary and its gradients clipped: the
 same bits at every budget, and gradients against automatic differentiation in 64 bits."""
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -83,3 +85,14 @@ def test_gradients_against_automatic_differentiation_in_64_bits():
     assert abs(norm - float(whole)) < 2.4e-4 * float(whole)
     for k, v in stack.grads.items():   # the factor is off by as much, and rounded
         assert float((v - before[k] * 0.5).norm()) <= 2.5e-4 * float(before[k].norm())
+
+
+def test_the_commands_that_the_example_names(monkeypatch, capsys):
+    commands = [line.split()[1:] for line in example.__doc__.split("\n") if line.startswith("    python ")]
+    assert any("--gated" in c for c in commands)
+    for c in commands:
+        print("%s" % c, flush=True)
+        monkeypatch.setattr(sys, "argv", c)
+        example.main()
+    out = capsys.readouterr().out
+    assert out.count("equal the first budget's") == 3 * len(commands), out
