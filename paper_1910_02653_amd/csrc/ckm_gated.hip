@@ -42,10 +42,14 @@ struct GatedArgs {
   int64_t ld_slab;
 };
 
-// act(z) and its derivative. For 16-bit results, whose rounding is far above: the
-// logistic function by the hardware's 2^x and 1 / x (some 2^-21), and the normal
-// distribution's as e^(-z^2 / 2) t q(t) of its lower side, t = 1 / (1 + 0.44 |z| / sqrt
-// 2), q a polynomial fitted to erfc(x) e^(x^2) / 2 (relative error below 2e-7, x up to 14).
+// act(z) and its derivative. The normal distribution's lower side is e^(-z^2 / 2) t q(t),
+// t = 1 / (1 + 0.44 |z| / sqrt 2), q a polynomial fitted to erfc(x) e^(x^2) / 2: no
+// difference of numbers near 1 (half of 1 + erf(z / sqrt 2) in binary32 is off by 3e-4 at
+// -4, by 4 % at -5, and 0 from -6 on). For 16-bit results, whose rounding is far above: the
+// logistic function by the hardware's 2^x and 1 / x (some 2^-21), and q of degree 7
+// (2.3e-7, in binary32's arithmetic 4.3e-7; at z = -12.6 the exponential's rounded argument
+// adds 7e-6). For binary32: degree 9 (1e-8), and the exponential corrected by the rounding
+// of z^2: within 10 units of 2^-24 of the value down to z = -12.9, where it is subnormal.
 template <typename T>
 __device__ __forceinline__ void activation(int act, float z, float& a, float& da) {
   constexpr bool kFull = std::is_same<T, float>::value;
@@ -57,8 +61,23 @@ __device__ __forceinline__ void activation(int act, float z, float& a, float& da
   } else if (act == CKM_ACT_GELU) {
     float c, e;
     if constexpr (kFull) {
-      c = 0.5f * (1.0f + erff(z * 0.70710678f));
-      e = expf(-0.5f * z * z);
+      const float y = fminf(fabsf(z), 16.0f);   // past it e is 0
+      const float d = fmaf(0.31112698f, y, 1.0f), r = __builtin_amdgcn_rcpf(d), t = fmaf(r, fmaf(-d, r, 1.0f), r);
+      const float y2 = y * y;
+      e = expf(-0.5f * y2);
+      e = fmaf(e, -0.5f * fmaf(y, y, -y2), e);
+      float q = -0.0194131676f;
+      q = fmaf(q, t, 0.0947795957f);
+      q = fmaf(q, t, -0.161439314f);
+      q = fmaf(q, t, 0.0886825845f);
+      q = fmaf(q, t, -0.0116111515f);
+      q = fmaf(q, t, 0.0601861700f);
+      q = fmaf(q, t, 0.0888089538f);
+      q = fmaf(q, t, 0.111705750f);
+      q = fmaf(q, t, 0.124182113f);
+      q = fmaf(q, t, 0.124118462f);
+      c = q * t * e;
+      c = z < 0.0f ? c : 1.0f - c;
     } else {
       const float t = __builtin_amdgcn_rcpf(fmaf(0.31112698f, fabsf(z), 1.0f));
       e = __builtin_amdgcn_exp2f(-0.72134752f * z * z);

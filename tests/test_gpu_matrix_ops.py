@@ -120,6 +120,31 @@ def test_gated_activations(dtype, act):
     check_gated(dtype, 40, 72, 136, act, seed=11)
 
 
+def test_gelu_keeps_its_lower_tail():
+    """Exact pre-activations (one hidden element, 1), a bound relative to the value. Binary32: the lower side's factor is
+    off by 1 / (1 + k |z|) (3 u), ten multiply-adds of falling weight (8 u), the exponential (4 u, its corrected argument
+    none) and two products: below 24 u in all, the derivative's two terms as much each, and its constant and products 4 u.
+    16 bits: a relative 4.3e-7 and the argument's three roundings of z^2 / 2, against half a unit v of the result."""
+    z = -torch.arange(0, 12 * 16 + 1, device="cuda").double() / 16
+    for dtype in sorted(TYPES):
+        log("gelu tail %s" % dtype)
+        w = z.to(TYPES[dtype])[None]
+        one, ones = torch.ones((1, 1), dtype=TYPES[dtype], device="cuda"), torch.ones_like(w)
+        assert torch.equal(w[0].double(), z)
+        c, e = 0.5 * torch.erfc(-z / 2 ** 0.5), torch.exp(-0.5 * z * z) / (2 * np.pi) ** 0.5
+        own = 28 * U if dtype == "f32" else 5e-7 + (1.5 * z * z + 16) * U
+        dx, dg, du = ops.gated_backward(ones, one, w, ones, act="gelu")
+        for got, want, size in ((ops.gated(one, w, ones, act="gelu"), z * c, (z * c).abs()), (du, z * c, (z * c).abs()),
+                                (dg, c + z * e, c + (z * e).abs())):
+            bound = own * size
+            bound = bound + (HALF_ULP[dtype] * (want.abs() + bound) + TINY[dtype] if dtype != "f32" else 0.0)
+            worst = ((got[0].double() - want).abs() - bound).max()
+            assert worst <= 0, (dtype, float(worst))
+    up = ops.gated(torch.ones((1, 1), device="cuda"), torch.tensor([[3.0, 20.0, 1e30, float("inf")]], device="cuda"),
+                   torch.ones((1, 4), device="cuda"), act="gelu")[0].double().cpu()
+    assert abs(float(up[0]) - 2.995950305904595) < 4 * U * 3 and torch.equal(up[1:], torch.tensor([20.0, 1e30, float("inf")]).double())
+
+
 def check_gated_on_device(dtype, rows, hidden, inner, act="silu", seed=21):
     """Larger sizes: products of the reference in 64 bits on the device; norms of the differences, since the bounds'
     products cost as much again. Rounding errors are independent: each result is off by at most its own rounding and
