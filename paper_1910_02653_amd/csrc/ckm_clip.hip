@@ -74,18 +74,10 @@ __device__ __forceinline__ double squares(const T* p, int64_t from, int64_t coun
   double sum = 0.0;
 #pragma unroll
   for (int i = 0; i < kGroups; ++i) {
-    if constexpr (std::is_same<T, _Float16>::value) {
-      // exact in binary32, and 32 of them far from its range
-      float s = 0.0f;
 #pragma unroll
-      for (int j = 0; j < kVec; ++j) s = fmaf((float)r[i].get(j), (float)r[i].get(j), s);
-      sum += (double)s;
-    } else {
-#pragma unroll
-      for (int j = 0; j < kVec; ++j) {
-        const double v = (double)(float)r[i].get(j);
-        sum = fma(v, v, sum);
-      }
+    for (int j = 0; j < kVec; ++j) {
+      const double v = (double)(float)r[i].get(j);
+      sum = fma(v, v, sum);
     }
   }
   return sum;

@@ -478,6 +478,18 @@ def test_clip_large_and_uneven():
     check_clip(grads([2_000_000] * 8 + [10] * 200, ["f16"] * 208), 10.0)
 
 
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+def test_norm_of_equal_elements(dtype):
+    """Where every group of squares rounds the same way: sums in binary64, so one rounding, of the result to binary32
+    (u of the norm), and 1e-12 of the sums."""
+    for value in (1.8017578125, 1.3330078125, 0.2998046875, 3.0517578125e-05):
+        for n in (8, 100, 8000, 1 << 20):
+            t = torch.full((n,), value, device="cuda").to(TYPES[dtype])
+            want = float(t[0].double()) * n ** 0.5
+            got = float(ops.gradient_norm([t]))
+            assert abs(got - want) <= (U + 1e-12) * want, (value, n, (got / want - 1) / U)
+
+
 def test_norm_extremes():
     big = torch.full((1000,), 1e30, device="cuda")          # squares past binary32's range
     small = torch.full((1000,), 1e-30, device="cuda")       # and below it
