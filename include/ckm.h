@@ -505,8 +505,9 @@ ckm_status ckm_gated_async(ckm_dtype type, const ckm_gated* gated, void* d_h, in
                            size_t work_bytes, void* stream);
 
 /* Its gradient from dh: with g = x Wg, u = x Wu (computed again), dg = dh u
- * act'(g) and du = dh act(g), both rounded to `type`: dx = dg Wg' + du Wu', dWg =
- * x' dg, dWu = x' du. dx may be NULL, and dWg and dWu together. rows = 0 gives
+ * act'(g) and du = dh act(g), both rounded to `type` (in binary16 times a power of
+ * two where the largest of them is past its range or below 2^-6): dx = dg Wg' + du
+ * Wu', dWg = x' dg, dWu = x' du. dx may be NULL, and dWg and dWu together. rows = 0 gives
  * zero weight gradients. */
 ckm_status ckm_gated_backward_async(ckm_dtype type, const ckm_gated* gated, const void* d_dh, int64_t ld_dh,
                                     void* d_dx, int64_t ld_dx, void* d_dgate, int64_t ld_dgate, void* d_dup,

@@ -12,6 +12,14 @@
 // independent of one another); dx is one product over both, dWg and dWu one launch,
 // and where there are few tiles all three.
 //
+// binary16's range may be too small for dg and du where dx and dW are well inside it: they
+// are products of two factors, and dW sums many rows. Each block leaves the largest finite
+// |dg|, |du| it has seen; a second launch takes the largest of all and, if it is past the
+// range or below 2^-6 (elements less than 2^-8 of it have begun to lose digits), computes
+// dg and du again times the power of two that brings it between 2^14 and 2^15. The results
+// are multiplied by the inverse. In range, which is the rule, its blocks return at once: f16
+// 2048x2048x8192 408 us without it and 412 with it, 512x1024x2048 33 and 36; out of range 553 and 45.
+//
 // Bound by the products: f16 2048x2048x8192 121 us (1140 TFLOP/s; the library's product
 // alone 126 to 137), its gradient 395 (recomputation 135, dx 136 and 13 for its shares, dW
 // 123); bf16 8192x4096x16384 1650 us (1330). A tile's end, activation and stores, is 6
@@ -27,7 +35,9 @@
 namespace ckm {
 namespace {
 
-enum { kForward, kBackward, kShares };   // what a kernel makes of g and u
+enum { kForward, kBackward, kAgain, kShares };   // what a kernel makes of g and u; again: dg and du times a power of two
+template <typename T>
+constexpr bool kHeld = std::is_same<T, _Float16>::value;   // dg and du times a power of two where they need it
 
 struct GatedArgs {
   ProductArgs p;
@@ -40,7 +50,32 @@ struct GatedArgs {
   int32_t up;        // where du begins in a row of dg | du
   float* slab;       // [split][g, u][m][ld_slab]
   int64_t ld_slab;
+  float* most;       // kHeld: the blocks' largest |dg|, |du|,
+  int32_t mosts;     // so many,
+  float* alpha;      // and one over the power of two that dg and du are held times
 };
+
+// The exponent of the power of two for a largest value.
+__device__ __forceinline__ int held_by(float most) {
+  if (most == 0.0f || (most >= 0x1p-6f && most <= 65504.0f)) return 0;
+  return max(-126, min(126, 14 - ((int)(__float_as_uint(most) >> 23) - 127)));
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+// The largest of a block's threads' values, for the block; lds: its threads have passed their last use of it.
+template <int kThreads>
+__device__ __forceinline__ void leave_most(const GatedArgs& a, float most, float* lds) {
+  most = reduce_row<OpMax, kThreads, kThreads>(most, lds, 0);
+  if (threadIdx.x == 0) a.most[blockIdx.x] = most;
+}
+// The power of two for all blocks' values, 1 if dg and du are as they have to be.
+template <int kThreads>
+__device__ __forceinline__ float held_times(const GatedArgs& a, float* lds) {
+  float most = 0.0f;
+  for (int k = threadIdx.x; k < a.mosts; k += kThreads) most = fmaxf(most, a.most[k]);
+  const int e = held_by(reduce_row<OpMax, kThreads, kThreads>(most, lds, 0));
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.alpha = power_of_two(-e);
+  return power_of_two(e);
+}
 
 // act(z) and its derivative. The normal distribution's lower side is e^(-z^2 / 2) t q(t),
 // t = 1 / (1 + 0.44 |z| / sqrt 2), q a polynomial fitted to erfc(x) e^(x^2) / 2: no
@@ -121,9 +156,10 @@ __device__ __forceinline__ void gated_back_of(int act, const Raw8<T>& dh, float 
   }
 }
 
-// What becomes of eight columns of g and u.
+// What becomes of eight columns of g and u. held: the largest finite |dg|, |du| so far, or (again) what they are
+// multiplied by.
 template <typename T, int kMode>
-__device__ __forceinline__ void finish(const GatedArgs& a, int64_t m, int n, float (&g)[8], float (&u)[8]) {
+__device__ __forceinline__ void finish(const GatedArgs& a, int64_t m, int n, float (&g)[8], float (&u)[8], float& held) {
   if constexpr (kMode == kForward) {
     if (n >= a.p.n) return;
     gated_of<T>(a.act, g, u);
@@ -132,6 +168,23 @@ __device__ __forceinline__ void finish(const GatedArgs& a, int64_t m, int n, flo
     if (n >= a.up) return;
     const int left = a.p.n - n;
     gated_back_of<T>(a.act, load_left((const T*)a.dh + m * a.ld_dh + n, left), g, u);
+    if constexpr (kMode == kAgain) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) g[k] *= held, u[k] *= held;
+    } else if constexpr (kHeld<T>) {
+      float most = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) most = fmaxf(fmaxf(most, fabsf(g[k])), fabsf(u[k]));   // a NaN counts for nothing
+      if (most == INFINITY) {
+        most = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          if (fabsf(g[k]) < INFINITY) most = fmaxf(most, fabsf(g[k]));
+          if (fabsf(u[k]) < INFINITY) most = fmaxf(most, fabsf(u[k]));
+        }
+      }
+      held = fmaxf(held, most);
+    }
     T* row = (T*)a.out + m * a.ld_out;
     store_part<false>(row, rounded8<T>(g), n, a.up);
     store_part<false>(row + a.up, rounded8<T>(u), n, a.up);
@@ -139,13 +192,12 @@ __device__ __forceinline__ void finish(const GatedArgs& a, int64_t m, int n, flo
 }
 
 template <class P, int kMode>
-__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(GatedArgs a) {
+__device__ __forceinline__ void gated_tile(const GatedArgs& a, int block, char* lds, float& held) {
   using T = typename P::T;
-  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
   const P p;
-  const int tiles = a.tiles_m * a.tiles_n, split = blockIdx.x / tiles;
+  const int tiles = a.tiles_m * a.tiles_n, split = block / tiles;
   int tm, tn;
-  tile_of(blockIdx.x % tiles, a.tiles_m, a.tiles_n, tm, tn);
+  tile_of(block % tiles, a.tiles_m, a.tiles_n, tm, tn);
   const int all = (a.p.k + P::kStep - 1) / P::kStep, from = split * a.steps;
   F4 acc[P::kFN][P::kFM];
   p.run(acc, a.p, tm * P::kM, tn * P::kSubN, from, min(all, from + a.steps), (LdsChar*)lds);
@@ -168,8 +220,8 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(G
     p.template each8<2>(acc, (LdsChar*)lds, [&](int row, int col, float (&v)[2][8]) {
       const int m = tm * P::kM + row, n = tn * P::kSubN + col;
       if (m >= a.p.m) return;
-      if constexpr (kMode == kBackward) {
-        finish<T, kMode>(a, m, n, v[0], v[1]);
+      if constexpr (kMode == kBackward || kMode == kAgain) {
+        finish<T, kMode>(a, m, n, v[0], v[1], held);
       } else if (n < a.p.n) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -182,11 +234,40 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(G
   }
 }
 
+template <class P, int kMode>
+__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(GatedArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+  float held = 0.0f;
+  gated_tile<P, kMode>(a, blockIdx.x, lds, held);
+  if constexpr (kMode == kBackward && kHeld<typename P::T>) {
+    __syncthreads();
+    leave_most<P::kThreads>(a, held, (float*)lds);
+  }
+}
+// dg and du again, where the first time's do not fit: a block takes several tiles.
+template <class P>
+__global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_again_kernel(GatedArgs a) {
+  __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
+  float held = held_times<P::kThreads>(a, (float*)lds);
+  if (held == 1.0f) return;
+  for (int block = blockIdx.x; block < a.tiles_m * a.tiles_n; block += gridDim.x) {
+    __syncthreads();   // the tile before has been read from lds
+    gated_tile<P, kAgain>(a, block, lds, held);
+  }
+}
+
 // The shares of g and u added in their order, and what kMode makes of them; a thread
 // eight columns.
 template <typename T, int kMode>
 __global__ void __launch_bounds__(256) ckm_gated_join_kernel(GatedArgs a, int splits, int64_t total, uint32_t eights) {
   const int64_t one = (int64_t)a.p.m * a.ld_slab;
+  constexpr bool kLeaves = kMode == kBackward && kHeld<T>;
+  __shared__ float lds[kLeaves || kMode == kAgain ? 8 : 1];
+  float held = 0.0f;
+  if constexpr (kMode == kAgain) {
+    held = held_times<256>(a, lds);
+    if (held == 1.0f) return;
+  }
   for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < total; at += (int64_t)gridDim.x * 256) {
     const int64_t m = at / eights;
     const int n = (int)(at - m * eights) * 8;
@@ -203,9 +284,15 @@ __global__ void __launch_bounds__(256) ckm_gated_join_kernel(GatedArgs a, int sp
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[s][k] = x[k], v[s][k + 4] = y[k];
     }
-    finish<T, kMode>(a, m, n, v[0], v[1]);
+    finish<T, kMode>(a, m, n, v[0], v[1], held);
   }
+  if constexpr (kLeaves) leave_most<256>(a, held, lds);
 }
+
+// Blocks of the join of shares.
+int64_t join_blocks(int64_t m, int64_t n) { return std::min<int64_t>((m * ((n + 7) / 8) + 255) / 256, 1 << 16); }
+// The blocks that leave a largest |dg|, |du|.
+int64_t leaving(const Cut& cut, int64_t m, int64_t n) { return cut.splits > 1 ? join_blocks(m, n) : cut.blocks(); }
 
 template <typename T, int kMode>
 void launch_both(GatedArgs a, const Cut& cut, hipStream_t s) {
@@ -215,14 +302,20 @@ void launch_both(GatedArgs a, const Cut& cut, hipStream_t s) {
   with_shape<T, true, false, 2>(cut, [&](auto p) {
     using P = typename decltype(p)::Shape;
     const uint32_t blocks = (uint32_t)cut.blocks();
-    if (cut.splits > 1) ckm_gated_kernel<P, kShares><<<blocks, P::kThreads, 0, s>>>(a);
-    else ckm_gated_kernel<P, kMode><<<blocks, P::kThreads, 0, s>>>(a);
+    if (cut.splits > 1) {
+      ckm_gated_kernel<P, kShares><<<blocks, P::kThreads, 0, s>>>(a);
+      return;
+    }
+    ckm_gated_kernel<P, kMode><<<blocks, P::kThreads, 0, s>>>(a);
+    if constexpr (kMode == kBackward && kHeld<T>)
+      ckm_gated_again_kernel<P><<<std::min(blocks, 256u * P::kBlocks), P::kThreads, 0, s>>>(a);
   });
   if (cut.splits > 1) {
-    const uint32_t eights = (uint32_t)((a.p.n + 7) / 8);
+    const uint32_t eights = (uint32_t)((a.p.n + 7) / 8), blocks = (uint32_t)join_blocks(a.p.m, a.p.n);
     const int64_t total = a.p.m * (int64_t)eights;
-    ckm_gated_join_kernel<T, kMode><<<(uint32_t)std::min<int64_t>((total + 255) / 256, 1 << 16), 256, 0, s>>>(
-        a, cut.splits, total, eights);
+    ckm_gated_join_kernel<T, kMode><<<blocks, 256, 0, s>>>(a, cut.splits, total, eights);
+    if constexpr (kMode == kBackward && kHeld<T>)
+      ckm_gated_join_kernel<T, kAgain><<<std::min(blocks, 1024u), 256, 0, s>>>(a, cut.splits, total, eights);
   }
 }
 
@@ -233,7 +326,7 @@ struct GatedPlan {
   int64_t inner, ld_d;       // columns of dg, padded to whole groups; a row of dg | du
   Cut both, dx, dw;
   bool together;             // dx and the weights' gradients in a launch
-  size_t x, w, d, slab, total;
+  size_t x, w, d, most, alpha, slab, total;
   double time;               // the model's, us
 };
 
@@ -272,6 +365,10 @@ GatedPlan plan_as(int type, const ckm_gated& c, bool back, bool ragged_x, bool r
                               (c.rows + step - 1) / step, x_bytes + 2 * h_bytes + 2 * w_bytes);
     p.time += p.dx.time + p.dw.time;
     p.d = take(c.rows * p.ld_d * elt);
+    if (type == CKM_F16) {
+      p.most = take(leaving(p.both, c.rows, c.inner) * sizeof(float));
+      p.alpha = take(sizeof(float));
+    }
     if (p.dx.splits > 1) slab = std::max(slab, (size_t)p.dx.splits * c.rows * whole(c.hidden, 8) * 4);
     if (p.dw.splits > 1) slab = std::max(slab, (size_t)p.dw.splits * 2 * c.hidden * whole(c.inner, 8) * 4);
   }
@@ -329,6 +426,11 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
   a.out = d;
   a.ld_out = plan.ld_d;
   a.up = (int32_t)plan.inner;
+  if (kHeld<T>) {
+    a.most = (float*)(work + plan.most);
+    a.mosts = (int32_t)leaving(plan.both, c.rows, c.inner);
+    a.alpha = (float*)(work + plan.alpha);
+  }
   launch_both<T, kBackward>(a, plan.both, s);
   // dx = dg Wg' + du Wu'
   ResultArgs rx = {}, rw = {};
@@ -336,6 +438,7 @@ void launch_gated(int type, const ckm_gated& c, const GatedPlan& plan, const voi
   rx.c[0] = out;
   rx.ld_c[0] = ld_out;
   rx.factor = rw.factor = 1.0f;
+  rx.alpha = rw.alpha = a.alpha;
   rx.halves = 1;
   if (plan.dx.splits > 1) rx.slab = slab;
   rx.ld_slab = whole(c.hidden, 8);

@@ -179,6 +179,55 @@ def test_gated_large(dtype, rows, hidden, inner):
     check_gated_on_device(dtype, rows, hidden, inner)
 
 
+def check_held(rows, hidden, inner, gains, offset=0, pad=0, act="silu"):
+    """binary16's dg and du past its range, with results inside it. They are rounded relative to the power of two that they
+    are held times: with the largest M of them outside [2^-6, 65504], M is brought to at least 2^14, so that the smallest
+    step's half is below 2^-25 2^-14 M; inside, it is 2^-25."""
+    x, wg, wu, dh = (randn(s, "f16", 61 + k, gain=g, offset=offset, pad=pad) for k, (s, g) in enumerate(
+        zip(((rows, hidden), (hidden, inner), (hidden, inner), (rows, inner)), gains)))
+    X, G, W, D = (host(t) for t in (x, wg, wu, dh))
+    g, u, a, da, eu, ea, eda = gated_bounds(X, G, W, act)
+    pg, pu = D * u * da, D * a
+    most = max(np.abs(pg).max(), np.abs(pu).max())
+    tiny, v = TINY["f16"] if 2.0 ** -6 <= most <= 65504 else most * 2.0 ** -39, HALF_ULP["f16"]
+    epg = np.abs(D) * (eda * (np.abs(u) + eu) + np.abs(da) * eu) + 3 * U * np.abs(pg)
+    epu = np.abs(D) * ea + 2 * U * np.abs(pu)
+    epg, epu = epg + v * (np.abs(pg) + epg) + tiny, epu + v * (np.abs(pu) + epu) + tiny
+    dx, dg, du = ops.gated_backward(dh, x, wg, wu, act=act)
+    both, eboth = product(np.concatenate([pg, pu], 1), np.concatenate([G, W], 1).T, da=np.concatenate([epg, epu], 1))
+    wants = [(dx, both, eboth, "dx")]
+    for got, p, e, what in ((dg, pg, epg, "dw_gate"), (du, pu, epu, "dw_up")):
+        wants.append((got,) + product(X.T, p, db=e) + (what,))
+    for got, want, bound, what in wants:
+        assert np.abs(want).max() < 60000, (what, np.abs(want).max())
+        check(got, want, bound, "f16", what)
+    return most, (x, wg, wu, dh), (dx, dg, du)
+
+
+@pytest.mark.parametrize("rows,hidden,inner,offset,pad", [
+    (4, 64, 64, 0, 0), (4, 64, 72, 1, 3), (129, 64, 200, 0, 0), (129, 65, 201, 1, 3), (300, 72, 1032, 0, 0),
+    (16, 1024, 64, 0, 0), (16, 1024, 65, 1, 1), (600, 64, 2048, 0, 0)])
+def test_gated_gradient_past_the_range_of_binary16(rows, hidden, inner, offset, pad):
+    """dg = dh u act'(g) vanishes with dh and u small; it overflows with both large, while x and Wg are small enough for dW
+    and dx."""
+    root, wide = hidden ** -0.5, inner ** -0.5
+    for step in (10, 14, 20):
+        log("gated gradient %dx%dx%d of about 2^-%d" % (rows, hidden, inner, 2 * step))
+        most, _, got = check_held(rows, hidden, inner, (8.0, root / 8, 2.0 ** -step, 2.0 ** -step), offset, pad)
+        assert most < 2.0 ** -6 and (step > 10 or float(got[1].abs().max()) > 0)
+    # u is 2^9 / sqrt(rows), dg 2^16 to 2^18 and its largest several times that; act(g) is far below 1
+    log("gated gradient %dx%dx%d of about 2^18" % (rows, hidden, inner))
+    gains = (2.0 ** -6 * rows ** -0.5, 2.0 ** -6 * wide, 2.0 ** 15 * root, min(2.0 ** 12.5, 2.0 ** 10 * rows ** 0.5))
+    most, args, got = check_held(rows, hidden, inner, gains, offset, pad)
+    x, wg, wu, dh = args
+    assert most > 65504
+    dh = dh.clone()   # what is infinite stays in its row of dx
+    dh[1, 3] = float("inf")
+    again = ops.gated_backward(dh, x, wg, wu)
+    rest = [k for k in range(rows) if k != 1]
+    assert torch.equal(again[0][rest], got[0][rest]) and not torch.isfinite(again[0][1]).all()
+
+
 def test_gated_extremes():
     x, wg, wu = randn((6, 40), "bf16", 1), randn((40, 24), "bf16", 2), randn((40, 24), "bf16", 3)
     h = ops.gated(x, wg, wu)
