@@ -6,7 +6,8 @@
 //
 // Forward: a tile of the logits stays in registers; of each of its rows remain the
 // largest logit and the sum of exponentials, which a second launch joins over the
-// tiles in their order. Gradient: the vocabulary in pieces; a piece's logits are
+// tiles in their order. 64 columns have one base and one sum, two of them are joined, and two
+// of these: the same sums in every shape of tile. Gradient: the vocabulary in pieces; a piece's logits are
 // computed again, d is written for that piece alone, in the tensors' type, and the two
 // products after it read it from the caches; dx is summed over pieces in binary32.
 //
@@ -50,6 +51,7 @@ struct LossArgs {
   void* d;                  // [rows][ld_d]
   int64_t ld_d, first;      // first: the piece's first column
   int32_t tile0, tiles_all; // its first tile, of all
+  bool pairs;               // tiles of 128 columns
   int64_t vocab;
 };
 
@@ -80,7 +82,10 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_kernel(Lo
   tile_of(blockIdx.x, a.tiles_m, a.tiles_n, tm, tn);
   F4 acc[P::kFN][P::kFM];
   p.run(acc, a.p, tm * P::kM, tn * P::kN, 0, (a.p.k + P::kStep - 1) / P::kStep, (LdsChar*)lds);
-  float2* joined = (float2*)lds;   // [waves of n][rows of the tile]
+  // a group: 64 columns, which one wave has, or two
+  constexpr bool kWhole = P::kFN == 4;
+  static_assert(kWhole || (P::kFN == 2 && P::kFM == 1 && P::kWavesN == 4), "");
+  float2* joined = (float2*)lds;   // [groups of the tile][its rows]
   if (a.p.n - tn * P::kN < P::kN) {   // columns past the vocabulary count for nothing
 #pragma unroll
     for (int j = 0; j < P::kFN; ++j)
@@ -109,40 +114,67 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_loss_kernel(Lo
     // the four lanes that hold a row
     most = fmaxf(most, __shfl_xor(most, 16));
     most = fmaxf(most, __shfl_xor(most, 32));
+    if constexpr (!kWhole) {
+      float* mosts = (float*)(lds + 4096);   // [waves][rows]
+      if (p.lane < 16) mosts[p.wn * 16 + p.lane] = most;
+      __syncthreads();
+      most = fmaxf(most, mosts[(p.wn ^ 1) * 16 + (p.lane & 15)]);
+    }
     const float base = most == -INFINITY ? 0.0f : most;
     float sum[4] = {};
+    if constexpr (!kWhole) {   // the second wave of a group adds to the first one's sums
+      F4* sums = (F4*)(lds + 8192);   // [groups][lanes]
+      F4 first = {power_of<T>(acc[0][i][0], base), power_of<T>(acc[0][i][1], base), power_of<T>(acc[0][i][2], base),
+                  power_of<T>(acc[0][i][3], base)};
 #pragma unroll
-    for (int j = 0; j < P::kFN; ++j)
+      for (int k = 0; k < 4; ++k) sum[k] = power_of<T>(acc[1][i][k], base);
+      if (p.wn % 2 == 0) sums[p.wn / 2 * 64 + p.lane] = F4{first[0] + sum[0], first[1] + sum[1], first[2] + sum[2], first[3] + sum[3]};
+      __syncthreads();
+      first += sums[p.wn / 2 * 64 + p.lane];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) sum[k] += power_of<T>(acc[j][i][k], base);
+      for (int k = 0; k < 4; ++k) sum[k] += first[k];
+    } else {
+#pragma unroll
+      for (int j = 0; j < P::kFN; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[k] += power_of<T>(acc[j][i][k], base);
+    }
     float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
     all += __shfl_xor(all, 16);
     all += __shfl_xor(all, 32);
-    if (p.lane < 16) joined[p.wn * P::kM + p.row(i)] = make_float2(base, all);
+    if (p.lane < 16 && (kWhole || p.wn % 2 == 1)) joined[(kWhole ? p.wn : p.wn / 2) * P::kM + p.row(i)] = make_float2(base, all);
   }
   __syncthreads();
   for (int r = threadIdx.x; r < P::kM; r += P::kThreads) {
     const int m = tm * P::kM + r;
     if (m >= a.p.m) continue;
-    float2 v = joined[r];
-#pragma unroll
-    for (int w = 1; w < P::kWavesN; ++w) v = join_parts(v, joined[w * P::kM + r]);
+    float2 v = join_parts(joined[r], joined[P::kM + r]);
+    if constexpr (P::kN == 256) v = join_parts(v, join_parts(joined[2 * P::kM + r], joined[3 * P::kM + r]));
     a.parts[(int64_t)m * a.tiles_all + a.tile0 + tn] = v;
   }
 }
 
-// A wave a row: the tiles' parts in their order (each lane every 64th, then the lanes).
+// Part k of a row's `all`, of 256 columns (two of 128 where tiles have so many).
+__device__ __forceinline__ float2 part_of(const LossArgs& a, const float2* parts, int k) {
+  if (!a.pairs) return parts[k];
+  return 2 * k + 1 < a.tiles_all ? join_parts(parts[2 * k], parts[2 * k + 1]) : parts[2 * k];
+}
+// A wave a row: the parts in their order (each lane every 64th, then the lanes).
 __global__ void __launch_bounds__(256) ckm_loss_join_kernel(LossArgs a) {
   const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= a.p.m) return;
   const float2* parts = a.parts + row * a.tiles_all;
+  const int all = a.pairs ? (a.tiles_all + 1) / 2 : a.tiles_all;
   float base = -INFINITY, sum = 0.0f;
-  for (int k = lane; k < a.tiles_all; k += 64) base = fmaxf(base, parts[k].y == 0.0f ? -INFINITY : parts[k].x);
+  for (int k = lane; k < all; k += 64) {
+    const float2 v = part_of(a, parts, k);
+    base = fmaxf(base, v.y == 0.0f ? -INFINITY : v.x);
+  }
   base = reduce64<OpMax>(base);
   if (base == -INFINITY) base = 0.0f;
-  for (int k = lane; k < a.tiles_all; k += 64) {
-    const float2 v = parts[k];
+  for (int k = lane; k < all; k += 64) {
+    const float2 v = part_of(a, parts, k);
     if (v.y != 0.0f) sum += v.y * power_of<_Float16>(v.x, base);
   }
   sum = reduce64<OpSum>(sum);
@@ -213,9 +245,10 @@ void launch_logits(LossArgs a, const Cut& cut, hipStream_t s) {
   });
 }
 
-// A piece of the vocabulary: d of at most 128 MB, and where the table has to be copied 96
-// MB of it, which stay in the caches between their writer and their readers; never fewer
-// than 8192 columns: dx, summed over pieces in memory, is read and written for each.
+// A piece of the vocabulary: in the gradient d of at most 128 MB, which stays in the caches
+// between its writer and its readers, but never fewer than 8192 columns: dx, summed over
+// pieces in memory, is read and written for each. Pieces of the gradient go by the sizes, as
+// the sums' order does. Forward, where the table has to be copied, 96 MB of it.
 constexpr int64_t kPieceBytes = (int64_t)128 << 20, kTableBytes = (int64_t)96 << 20, kLeastPiece = 8192;
 
 struct LossPlan {
@@ -247,29 +280,36 @@ LossPlan plan_as(int type, const ckm_vocab& c, bool back, bool ragged_x, bool ra
     return here;
   };
   if (p.pack_x) p.x = take(c.rows * p.ld_x * elt);
-  int64_t most = c.vocab;
+  // pieces of at most so many columns, as many in each
+  const auto piece_of = [&](int64_t most) {
+    const int64_t pieces = (c.vocab + std::max(most, kLeastPiece) - 1) / std::max(most, kLeastPiece);
+    return std::min(c.vocab, whole((c.vocab + pieces - 1) / pieces, 256));
+  };
+  int64_t most = ((int64_t)1 << 30) / ((c.rows + 255) / 256);   // 2^22 tiles in a launch
   if (back) most = std::min(most, kPieceBytes / (int64_t)(c.rows * elt));
-  if (p.pack_w) most = std::min(most, kTableBytes / (int64_t)(c.hidden * elt));
-  most = std::min(most, ((int64_t)1 << 30) / ((c.rows + 255) / 256));   // 2^22 tiles in a launch
-  // as many columns in each
-  const int64_t pieces = (c.vocab + std::max(most, kLeastPiece) - 1) / std::max(most, kLeastPiece);
-  p.piece = std::min(c.vocab, whole((c.vocab + pieces - 1) / pieces, 256));
+  const int64_t all = piece_of(most);   // were the table not copied
+  p.piece = p.pack_w && !back ? std::min(all, piece_of(std::min(most, kTableBytes / (int64_t)(c.hidden * elt)))) : all;
   if (p.pack_w) p.w = take(p.piece * p.ld_w * elt);
   const int64_t steps = (c.hidden + step - 1) / step, x_bytes = c.rows * c.hidden * elt, w_bytes = p.piece * c.hidden * elt;
-  p.logits = cut_product(type, c.rows, p.piece, 1, 1, steps, x_bytes + w_bytes, false, true,
-                         staged_x || staged_w ? kStagedAlong : kStraight);
+  p.logits = cut_product(type, c.rows, p.piece, 1, 1, steps, x_bytes + w_bytes, false, true);
+  if (staged_x || staged_w)
+    p.logits = cut_like(type, c.rows, p.piece, 1, 1, steps, x_bytes + w_bytes, true, kStagedAlong, p.logits);
   p.time = p.logits.time + (p.pack_w ? copy_time(w_bytes) : 0.0);
-  if (!back) {   // pieces are of whole tiles
+  if (!back) {   // pieces are of whole tiles, and of whole pairs
     p.parts = take((size_t)c.rows * ((c.vocab + p.logits.cols - 1) / p.logits.cols) * sizeof(float2));
     p.hit = take(c.rows * sizeof(float));
   } else {
     const int64_t d_bytes = p.piece * c.rows * elt;
-    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, (p.piece + step - 1) / step, d_bytes + w_bytes, true, true,
-                       staged_w ? kStagedAcross : kStraight);
-    p.dw = cut_product(type, p.piece, c.hidden, 1, 1, (c.rows + step - 1) / step, d_bytes + x_bytes + w_bytes, true,
-                       false, kStraight);
-    p.together = cut_together(type, p.dx, c.rows, c.hidden, (p.piece + step - 1) / step, p.dw, p.piece, c.hidden,
-                              (c.rows + step - 1) / step, d_bytes + x_bytes + 2 * w_bytes);
+    const int64_t steps_v = (p.piece + step - 1) / step, steps_m = (c.rows + step - 1) / step;
+    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, steps_v, d_bytes + w_bytes, true, true);
+    p.dw = cut_product(type, p.piece, c.hidden, 1, 1, steps_m, d_bytes + x_bytes + w_bytes, true, false);
+    p.together = cut_together(type, p.dx, c.rows, c.hidden, steps_v, p.dw, p.piece, c.hidden, steps_m,
+                              d_bytes + x_bytes + 2 * w_bytes);
+    if (staged_w) {
+      p.together = false;
+      p.dx = cut_like(type, c.rows, c.hidden, 1, 1, steps_v, d_bytes + w_bytes, true, kStagedAcross, p.dx);
+      p.dw = cut_like(type, p.piece, c.hidden, 1, 1, steps_m, d_bytes + x_bytes + w_bytes, false, kStraight, p.dw);
+    }
     p.time += p.dx.time + p.dw.time;
     p.most = take(sizeof(float));
     p.d = take((size_t)c.rows * row_of(p.piece, elt) * elt);
@@ -327,6 +367,7 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
     a.hit = (float*)(work + plan.hit);
     a.loss = loss;
     a.tiles_all = (int32_t)((c.vocab + plan.logits.cols - 1) / plan.logits.cols);
+    a.pairs = plan.logits.cols == 128;
     for (int64_t v = 0; v < c.vocab; v += plan.piece) {
       a.first = v;
       a.tile0 = (int32_t)(v / plan.logits.cols);

@@ -330,7 +330,8 @@ struct GatedPlan {
   double time;               // the model's, us
 };
 
-// packed: operands that cannot be loaded as they are are copied, or else staged.
+// packed: operands that cannot be loaded as they are are copied, or else staged. The cuts of
+// k are those of operands that can be loaded, in either form.
 GatedPlan plan_as(int type, const ckm_gated& c, bool back, bool ragged_x, bool ragged_w, bool packed) {
   const size_t elt = dtype_bytes(type);
   const int64_t group = 16 / elt, step = kStepBytes / elt;
@@ -344,8 +345,10 @@ GatedPlan plan_as(int type, const ckm_gated& c, bool back, bool ragged_x, bool r
   const int64_t steps_h = (c.hidden + step - 1) / step, steps_f = (c.inner + step - 1) / step;
   const int64_t x_bytes = c.rows * c.hidden * elt, w_bytes = 2 * c.hidden * c.inner * elt, h_bytes = c.rows * c.inner * elt;
   const bool staged_x = ragged_x && !packed, staged_w = ragged_w && !packed;
-  p.both = cut_product(type, c.rows, c.inner, 1, 2, steps_h, x_bytes + w_bytes, true, true,
-                       staged_w ? kStagedAcross : staged_x ? kStagedAlong : kStraight);
+  p.both = cut_product(type, c.rows, c.inner, 1, 2, steps_h, x_bytes + w_bytes, true, true);
+  if (staged_x || staged_w)
+    p.both = cut_like(type, c.rows, c.inner, 1, 2, steps_h, x_bytes + w_bytes, true,
+                      staged_w ? kStagedAcross : kStagedAlong, p.both);
   p.time = p.both.time + (p.pack_x || p.pack_w ? copy_time((p.pack_x ? x_bytes : 0) + (p.pack_w ? w_bytes : 0)) : 0.0);
   size_t at = 0;
   const auto take = [&](size_t bytes) {
@@ -357,12 +360,16 @@ GatedPlan plan_as(int type, const ckm_gated& c, bool back, bool ragged_x, bool r
   if (p.pack_w) p.w = take(2 * c.hidden * p.ld_w * elt);
   size_t slab = p.both.splits > 1 ? (size_t)p.both.splits * 2 * c.rows * whole(c.inner, 8) * 4 : 0;
   if (back) {
-    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, 2 * steps_f, 2 * h_bytes + w_bytes, true, true,
-                       staged_w ? kStagedAlong : kStraight);
-    p.dw = cut_product(type, c.hidden, c.inner, 2, 1, (c.rows + step - 1) / step, x_bytes + 2 * h_bytes + w_bytes, true,
-                       false, staged_x ? kStagedAcross : kStraight);
-    p.together = cut_together(type, p.dx, c.rows, c.hidden, 2 * steps_f, p.dw, c.hidden, c.inner,
-                              (c.rows + step - 1) / step, x_bytes + 2 * h_bytes + 2 * w_bytes);
+    const int64_t steps_m = (c.rows + step - 1) / step, dx_bytes = 2 * h_bytes + w_bytes, dw_bytes = dx_bytes + x_bytes;
+    p.dx = cut_product(type, c.rows, c.hidden, 1, 1, 2 * steps_f, dx_bytes, true, true);
+    p.dw = cut_product(type, c.hidden, c.inner, 2, 1, steps_m, dw_bytes, true, false);
+    p.together = cut_together(type, p.dx, c.rows, c.hidden, 2 * steps_f, p.dw, c.hidden, c.inner, steps_m,
+                              dw_bytes + w_bytes);
+    if (staged_x || staged_w) {
+      p.together = false;
+      p.dx = cut_like(type, c.rows, c.hidden, 1, 1, 2 * steps_f, dx_bytes, true, staged_w ? kStagedAlong : kStraight, p.dx);
+      p.dw = cut_like(type, c.hidden, c.inner, 2, 1, steps_m, dw_bytes, false, staged_x ? kStagedAcross : kStraight, p.dw);
+    }
     p.time += p.dx.time + p.dw.time;
     p.d = take(c.rows * p.ld_d * elt);
     if (type == CKM_F16) {

@@ -467,10 +467,16 @@ struct Cut {
 };
 // subs: 2 when a tile's columns are of two matrices (n then counts one's). bytes: of
 // the operands. split: whether shares of k are possible. a_along_k: tiles of 16 rows are
-// for an A along k alone. staged: operands that cannot be loaded straight to LDS.
-enum Staged { kStraight, kStagedAlong, kStagedAcross };   // with rows of k, or of m or n
+// for an A along k alone.
 Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
-                bool a_along_k, Staged staged);
+                bool a_along_k);
+// The best cut of the same product with the shares of `as`, which cut_product gave, for
+// operands that cannot be loaded straight to LDS too: the sums' order, and so every bit of
+// a result, goes by the sizes and not by where operands lie (left to the model, f16
+// 16x2048x2048 has three shares or four).
+enum Staged { kStraight, kStagedAlong, kStagedAcross };   // with rows of k, or of m or n
+Cut cut_like(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool a_along_k,
+             Staged staged, const Cut& as);
 // Cuts of two products that share a launch, in place of the two given, if the model has
 // them done sooner; whether that is so. The first's tiles have 64 or 128 rows, the
 // second's 128, and no shares.

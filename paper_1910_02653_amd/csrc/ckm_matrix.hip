@@ -138,28 +138,40 @@ double join_time(const Cut& c, int64_t m, int64_t n, int subs) {
 //   bf16 2048x8192x4096   256 rows, one: 101 (1357 TFLOP/s); 128, four: 128; 64, eight: 161
 //   bf16 1x16384x2048     16 rows 12, 64 rows 15 (67 MB)
 // Of every cut of the products of 37 calls it takes the best or one within 4 %, twice 8 %.
-Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
-                bool a_along_k, Staged staged) {
+double time_of(int type, const Shape& shape, const Cut& c, int64_t m, int64_t n, int subs, int64_t bytes, Staged staged) {
   constexpr double kSteps[] = {1.0, 1.4, 2.5}, kReads[] = {1.0, 1.2, 5.0};   // by way of registers, of lines that are cut
+  const double rounds = std::ceil(c.blocks() / kCUs);
+  const Time& time = shape.step(type);
+  const double step = (rounds > 1.0 ? time.more : time.one) * kSteps[staged];
+  // where a CU holds two tiles, one's fixed part is half hidden behind the other's steps
+  const double fixed = shape.fixed * (shape.rows == 256 ? rounds : 1.0 + 0.5 * (rounds - 1.0));
+  return std::max(rounds * c.steps * step + fixed, kReads[staged] * bytes / kBytesAUs + shape.fixed) +
+         join_time(c, m, n, subs);
+}
+
+Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
+                bool a_along_k) {
   Cut best = {};
-  double least = 0.0;
+  for (const Shape& shape : kShapes) {
+    if (shape.rows < 64 && !a_along_k) continue;
+    for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
+      Cut c = cut_as(shape, m, n, halves, subs, steps, splits, false);
+      if (splits > 1 && (!split || steps / splits < 4 || c.blocks() > 2048)) break;
+      c.time = time_of(type, shape, c, m, n, subs, bytes, kStraight);
+      if (!best.rows || c.time <= best.time) best = c;
+    }
+  }
+  return best;
+}
+
+Cut cut_like(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool a_along_k,
+             Staged staged, const Cut& as) {
+  Cut best = {};
   for (const Shape& shape : kShapes) {
     if ((shape.rows < 64 && !a_along_k) || (shape.rows == 256 && staged)) continue;
-    for (const int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128, 192, 256}) {
-      const Cut c = cut_as(shape, m, n, halves, subs, steps, splits, staged != kStraight);
-      if (splits > 1 && (!split || steps / splits < 4 || c.blocks() > 2048)) break;
-      const double rounds = std::ceil(c.blocks() / kCUs);
-      const Time& time = shape.step(type);
-      const double step = (rounds > 1.0 ? time.more : time.one) * kSteps[staged];
-      // where a CU holds two tiles, one's fixed part is half hidden behind the other's steps
-      const double fixed = shape.fixed * (shape.rows == 256 ? rounds : 1.0 + 0.5 * (rounds - 1.0));
-      const double t = std::max(rounds * c.steps * step + fixed, kReads[staged] * bytes / kBytesAUs + shape.fixed) +
-                       join_time(c, m, n, subs);
-      if (!best.rows || t <= least) {
-        best = c;
-        best.time = least = t;
-      }
-    }
+    Cut c = cut_as(shape, m, n, halves, subs, steps, as.splits, staged != kStraight);
+    c.time = time_of(type, shape, c, m, n, subs, bytes, staged);
+    if (!best.rows || c.time <= best.time) best = c;
   }
   return best;
 }
@@ -169,7 +181,7 @@ bool cut_together(int type, Cut& a, int64_t m_a, int64_t n_a, int64_t steps_a, C
   // long products have the larger tiles' rate to lose, and little to gain (f16
   // 2048x2048x8192, gated gradient: 404 us apart, 448 together)
   constexpr double kLong = 60.0, kGain = 0.92;
-  if (a.staged || b.staged || a.time + b.time > kLong) return false;
+  if (a.time + b.time > kLong) return false;
   const Shape& shape_b = kShapes[1];
   Cut d = cut_as(shape_b, m_b, n_b, b.halves, 1, steps_b, 1, false);
   const Time& time_b = shape_b.step(type);

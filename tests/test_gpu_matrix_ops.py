@@ -456,6 +456,52 @@ def test_cross_entropy_extremes():
     assert all(float(g.abs().max()) < 64 * U * float(s1.abs().max() + 1) * 40 for g in ops.cross_entropy_backward(dl, x, w[:1], one, s1))
 
 
+def moved(t, offset, pad):
+    """t's values in rows that start `offset` elements into an allocation, `pad` elements apart."""
+    view = randn(tuple(t.shape), {v: k for k, v in TYPES.items()}[t.dtype], 0, offset=offset, pad=pad)
+    view.copy_(t)
+    return view
+
+
+PLACES = [(0, 0), (1, 0), (1, 3), (8, 8), (0, 5)]
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("rows,hidden,inner", [(16, 2048, 2048), (16, 4096, 1024), (3, 1040, 264), (64, 1024, 4096), (130, 2056, 520),
+                                               (700, 264, 1032)])
+def test_gated_bits_go_by_the_sizes(dtype, rows, hidden, inner):
+    """The same values give the same bits wherever x's, the weights' or dh's rows lie."""
+    x, dh = randn((rows, hidden), dtype, 1), randn((rows, inner), dtype, 2)
+    wg, wu = (randn((hidden, inner), dtype, k, gain=hidden ** -0.5) for k in (3, 4))
+    h, grads = ops.gated(x, wg, wu), ops.gated_backward(dh, x, wg, wu)
+    for at in PLACES[1:]:
+        for which in (1, 2, 3):
+            log("gated bits %s %dx%dx%d %s %d" % (dtype, rows, hidden, inner, at, which))
+            a = [moved(t, *at) if which & bit else t for t, bit in ((x, 1), (wg, 2), (wu, 2), (dh, 1))]
+            assert torch.equal(ops.gated(*a[:3]), h)
+            for p, q in zip(ops.gated_backward(a[3], *a[:3]), grads):
+                assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("dtype", sorted(TYPES))
+@pytest.mark.parametrize("rows,hidden,vocab", [(16, 2048, 2048), (16, 1040, 50000), (3, 4104, 9000), (100, 1032, 30000), (520, 264, 20000),
+                                               (2000, 264, 10000), (9000, 64, 17000), (40, 2008, 60000)])
+def test_cross_entropy_bits_go_by_the_sizes(dtype, rows, hidden, vocab):
+    x, w = randn((rows, hidden), dtype, 1), randn((vocab, hidden), dtype, 2, gain=2 * hidden ** -0.5)
+    targets = torch.randint(-1, vocab, (rows,), generator=torch.Generator().manual_seed(3)).cuda()
+    dloss = torch.full((rows,), 0.5, device="cuda")
+    want = ops.cross_entropy(x, w, targets)
+    grads = ops.cross_entropy_backward(dloss, x, w, targets, want[1])
+    for at in PLACES[1:4]:
+        for which in (1, 2, 3):
+            log("cross entropy bits %s %dx%dx%d %s %d" % (dtype, rows, hidden, vocab, at, which))
+            a = [moved(t, *at) if which & bit else t for t, bit in ((x, 1), (w, 2))]
+            for p, q in zip(ops.cross_entropy(*a, targets), want):
+                assert torch.equal(p, q)
+            for p, q in zip(ops.cross_entropy_backward(dloss, *a, targets, want[1]), grads):
+                assert torch.equal(p, q)
+
+
 def test_rows_further_apart_than_32_bits_count():
     ld = (1 << 31) + 24
     flat = torch.empty(2 * ld + 72, dtype=torch.float16, device="cuda")
