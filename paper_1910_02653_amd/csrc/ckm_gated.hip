@@ -74,7 +74,7 @@ __device__ __forceinline__ float held_times(const GatedArgs& a, float* lds) {
   for (int k = threadIdx.x; k < a.mosts; k += kThreads) most = fmaxf(most, a.most[k]);
   const int e = held_by(reduce_row<OpMax, kThreads, kThreads>(most, lds, 0));
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.alpha = power_of_two(-e);
-  return power_of_two(e);
+  return power_of_two(__builtin_amdgcn_readfirstlane(e));
 }
 
 // act(z) and its derivative. The normal distribution's lower side is e^(-z^2 / 2) t q(t),
@@ -192,9 +192,9 @@ __device__ __forceinline__ void finish(const GatedArgs& a, int64_t m, int n, flo
 }
 
 template <class P, int kMode>
-__device__ __forceinline__ void gated_tile(const GatedArgs& a, int block, char* lds, float& held) {
+__device__ __forceinline__ void gated_tile(const GatedArgs& a, int block, int thread, char* lds, float& held) {
   using T = typename P::T;
-  const P p;
+  const P p(thread);
   const int tiles = a.tiles_m * a.tiles_n, split = block / tiles;
   int tm, tn;
   tile_of(block % tiles, a.tiles_m, a.tiles_n, tm, tn);
@@ -238,7 +238,7 @@ template <class P, int kMode>
 __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_kernel(GatedArgs a) {
   __shared__ __attribute__((aligned(1024))) char lds[P::kLds];
   float held = 0.0f;
-  gated_tile<P, kMode>(a, blockIdx.x, lds, held);
+  gated_tile<P, kMode>(a, blockIdx.x, threadIdx.x, lds, held);
   if constexpr (kMode == kBackward && kHeld<typename P::T>) {
     __syncthreads();
     leave_most<P::kThreads>(a, held, (float*)lds);
@@ -252,7 +252,9 @@ __global__ void __launch_bounds__(P::kThreads, P::kWaveSlots) ckm_gated_again_ke
   if (held == 1.0f) return;
   for (int block = blockIdx.x; block < a.tiles_m * a.tiles_n; block += gridDim.x) {
     __syncthreads();   // the tile before has been read from lds
-    gated_tile<P, kAgain>(a, block, lds, held);
+    int thread = threadIdx.x;
+    asm volatile("" : "+v"(thread));   // a lane's places are worked out for each tile: kept over the loop they take registers that are not there
+    gated_tile<P, kAgain>(a, block, thread, lds, held);
   }
 }
 

@@ -244,9 +244,9 @@ struct Product {
 
   int wave, lane, wm, wn;
 
-  __device__ __forceinline__ Product() {
-    wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    lane = threadIdx.x & 63;
+  __device__ __forceinline__ Product(int thread = threadIdx.x) {
+    wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+    lane = thread & 63;
     wm = wave / kWavesN;
     wn = wave % kWavesN;
   }
