@@ -219,6 +219,15 @@ __device__ __forceinline__ F4 mma(F4 acc, I4 p, I4 q) {
   }
 }
 
+// Between a wave's LDS stores and its other lanes' loads of them, and such loads and the
+// next stores there. The hardware keeps a wave's order; the compiler, which sees that one
+// lane's addresses differ, may not. No instruction of its own.
+__device__ __forceinline__ void lanes_meet() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 // A block's product: kM x kN of C by kWavesM x kWavesN waves. kSubs = 2: the tile's
 // columns are kN / 2 of each of two matrices, and each wave has as many of both.
 // kStaged: operands by way of registers (TileStage).
@@ -276,6 +285,7 @@ struct Product {
       for (int i = 0; i < kPass; ++i)
 #pragma unroll
         for (int j = 0; j < kOut * kFS; ++j) *at(i * 16 + (lane & 15), j * 4 + (lane >> 4)) = acc[j][i0 + i];
+      lanes_meet();
       constexpr int kEights = kPass * 16 * kLanes;
 #pragma unroll
       for (int t = 0; t < (kEights + 63) / 64; ++t) {
@@ -290,6 +300,7 @@ struct Product {
         }
         f((wm * kFM + i0) * 16 + r, wn * kFS * 16 + 8 * q, v);
       }
+      if (i0 + kPass < kFM) lanes_meet();
     }
   }
 
