@@ -443,8 +443,10 @@ ckm_status loss(ckm_dtype type, const ckm_vocab* c, bool back, const float* dlos
   const size_t elt = dtype_bytes(type);
   const hipStream_t s = (hipStream_t)stream;
   if (dw && (st = check_matrix(dw, "dweight", c->vocab, c->hidden, ld_dw, elt, true)) != CKM_OK) return st;
+  const Place x = {"x", c->d_x, c->rows, c->hidden, c->ld_x, elt}, w = {"weight", c->d_weight, c->vocab, c->hidden, c->ld_weight, elt};
   if (c->rows == 0) {
     if (!dw) return CKM_OK;
+    if ((st = check_apart({{"dweight", dw, c->vocab, c->hidden, ld_dw, elt}}, {w})) != CKM_OK) return st;
     launch_zero(type, dw, c->vocab, c->hidden, ld_dw, s);
     return launched("cross entropy gradient launch");
   }
@@ -458,8 +460,7 @@ ckm_status loss(ckm_dtype type, const ckm_vocab* c, bool back, const float* dlos
       return set_error(CKM_E_INVALID_ARG, "loss or lse is not aligned to 4 bytes");
     if (!loss_out && !lse) return CKM_OK;
   }
-  const Place x = {"x", c->d_x, c->rows, c->hidden, c->ld_x, elt}, w = {"weight", c->d_weight, c->vocab, c->hidden, c->ld_weight, elt},
-              targets = {"targets", c->d_targets, 1, c->rows, 0, 8}, sums = {"lse", lse, 1, c->rows, 0, 4};
+  const Place targets = {"targets", c->d_targets, 1, c->rows, 0, 8}, sums = {"lse", lse, 1, c->rows, 0, 4};
   st = back ? check_apart({{"dx", dx, c->rows, c->hidden, ld_dx, elt}, {"dweight", dw, c->vocab, c->hidden, ld_dw, elt}},
                           {x, w, targets, sums, {"dloss", dloss, 1, c->rows, 0, 4}})
             : check_apart({{"loss", loss_out, 1, c->rows, 0, 4}, sums}, {x, w, targets});

@@ -503,7 +503,17 @@ ckm_status gated(ckm_dtype type, const ckm_gated* c, bool back, const void* dh, 
     if (dgate && (st = check_matrix(dgate, "dw_gate", c->hidden, c->inner, ld_dgate, elt, true)) != CKM_OK) return st;
     if (dup && (st = check_matrix(dup, "dw_up", c->hidden, c->inner, ld_dup, elt, true)) != CKM_OK) return st;
   }
+  const Place x = {"x", c->d_x, c->rows, c->hidden, c->ld_x, elt}, wg = {"w_gate", c->d_gate, c->hidden, c->inner, c->ld_gate, elt},
+              wu = {"w_up", c->d_up, c->hidden, c->inner, c->ld_up, elt};
+  const auto apart = [&] {
+    return back ? check_apart({{"dx", out, c->rows, c->hidden, ld_out, elt},
+                               {"dw_gate", dgate, c->hidden, c->inner, ld_dgate, elt},
+                               {"dw_up", dup, c->hidden, c->inner, ld_dup, elt}},
+                              {x, wg, wu, {"dh", dh, c->rows, c->inner, ld_dh, elt}})
+                : check_apart({{"h", out, c->rows, c->inner, ld_out, elt}}, {x, wg, wu});
+  };
   if (c->rows == 0) {
+    if ((st = apart()) != CKM_OK) return st;
     if (dgate) {
       launch_zero(type, dgate, c->hidden, c->inner, ld_dgate, s);
       launch_zero(type, dup, c->hidden, c->inner, ld_dup, s);
@@ -516,14 +526,7 @@ ckm_status gated(ckm_dtype type, const ckm_gated* c, bool back, const void* dh, 
       (st = check_matrix(out, back ? "dx" : "h", c->rows, back ? c->hidden : c->inner, ld_out, elt, true)) != CKM_OK)
     return st;
   if (back && !out && !dgate) return CKM_OK;
-  const Place x = {"x", c->d_x, c->rows, c->hidden, c->ld_x, elt}, wg = {"w_gate", c->d_gate, c->hidden, c->inner, c->ld_gate, elt},
-              wu = {"w_up", c->d_up, c->hidden, c->inner, c->ld_up, elt};
-  st = back ? check_apart({{"dx", out, c->rows, c->hidden, ld_out, elt},
-                           {"dw_gate", dgate, c->hidden, c->inner, ld_dgate, elt},
-                           {"dw_up", dup, c->hidden, c->inner, ld_dup, elt}},
-                          {x, wg, wu, {"dh", dh, c->rows, c->inner, ld_dh, elt}})
-            : check_apart({{"h", out, c->rows, c->inner, ld_out, elt}}, {x, wg, wu});
-  if (st != CKM_OK) return st;
+  if ((st = apart()) != CKM_OK) return st;
   const GatedPlan plan = plan_of(type, *c, back);
   if ((st = check_blocks(plan.both)) != CKM_OK) return st;
   if (back && ((st = check_blocks(plan.dx)) != CKM_OK || (st = check_blocks(plan.dw)) != CKM_OK)) return st;

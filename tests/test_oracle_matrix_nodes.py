@@ -174,6 +174,19 @@ def test_cross_entropy_refuses_outputs_and_work():
     assert n.value < (1 << 16) * (1 << 18) * 2 // 16
 
 
+def test_no_rows_refuse_outputs_over_the_weights():
+    """Zero weight gradients are written without rows too, and so not over the weights or one another."""
+    L, bad = ckm.lib(), ckm.E_INVALID_ARG
+    c = gated(rows=0, d_x=None)
+    for dg, du in ((2 * P, Q), (Q, 3 * P), (Q, 2 * P + 126), (Q, Q), (Q, Q + 64)):
+        assert L.ckm_gated_backward_async(ops.F16, C.byref(c), None, 8, None, 8, dg, 8, du, 8, None, 0, None) == bad
+        assert b"overlaps" in L.ckm_last_error(), (dg, du)
+    v = vocab(rows=0, d_x=None, d_targets=None)
+    for dw in (2 * P, 2 * P + 1598, 2 * P - 16):
+        assert L.ckm_cross_entropy_backward_async(ops.F16, C.byref(v), None, None, None, 8, dw, 8, None, 0, None) == bad
+        assert b"overlaps" in L.ckm_last_error(), dw
+
+
 def tensors(*rows):
     return (C.c_int64 * (4 * len(rows)))(*(v for r in rows for v in r))
 
