@@ -225,6 +225,19 @@ ckm_status check_outputs(int64_t count, const ckm_tensor* t) {
   return CKM_OK;
 }
 
+// The norm: there, and not inside a tensor or, given outputs, one of them.
+ckm_status check_norm(int64_t count, const ckm_tensor* t, const float* norm, bool outputs) {
+  if (!norm || (uintptr_t)norm % 4) return set_error(CKM_E_INVALID_ARG, "norm is NULL or not aligned to 4 bytes");
+  const uintptr_t at = (uintptr_t)norm;
+  for (int64_t k = 0; k < count; ++k) {
+    const size_t bytes = t[k].count * dtype_bytes((int)t[k].type);
+    const auto over = [&](const void* p) { return bytes && (uintptr_t)p < at + 4 && at < (uintptr_t)p + bytes; };
+    if (over(t[k].d_in) || (outputs && over(t[k].d_out)))
+      return set_error(CKM_E_INVALID_ARG, "norm overlaps tensor %lld", (long long)k);
+  }
+  return CKM_OK;
+}
+
 ckm_status check_parts(int64_t count, void* work, size_t work_bytes) {
   const size_t need = (size_t)launches(count) * most_blocks(count) * sizeof(double);
   if (need && (!work || work_bytes < need))
@@ -256,7 +269,7 @@ extern "C" ckm_status ckm_norm_async(int64_t count, const ckm_tensor* tensors, f
   using namespace ckm;
   ckm_status st = check_tensors(count, tensors);
   if (st != CKM_OK) return st;
-  if (!d_norm || (uintptr_t)d_norm % 4) return set_error(CKM_E_INVALID_ARG, "norm is NULL or not aligned to 4 bytes");
+  if ((st = check_norm(count, tensors, d_norm, false)) != CKM_OK) return st;
   if ((st = check_parts(count, d_work, work_bytes)) != CKM_OK) return st;
   const int n = launch_parts(count, tensors, (double*)d_work, (hipStream_t)stream);
   ckm_norm_join_kernel<<<1, kBlock, 0, (hipStream_t)stream>>>((const double*)d_work, n, d_norm);
@@ -271,7 +284,7 @@ extern "C" ckm_status ckm_clip_async(int64_t count, const ckm_tensor* tensors, d
     if (st != CKM_OK) return st;
     if (!(max_norm >= 0.0)) return set_error(CKM_E_INVALID_ARG, "max_norm = %g", max_norm);
     if (!(eps >= 0.0 && std::isfinite(eps))) return set_error(CKM_E_INVALID_ARG, "eps = %g", eps);
-    if (!d_norm || (uintptr_t)d_norm % 4) return set_error(CKM_E_INVALID_ARG, "norm is NULL or not aligned to 4 bytes");
+    if ((st = check_norm(count, tensors, d_norm, true)) != CKM_OK) return st;
     if ((st = check_outputs(count, tensors)) != CKM_OK) return st;
     if ((st = check_parts(count, d_work, work_bytes)) != CKM_OK) return st;
     const hipStream_t s = (hipStream_t)stream;

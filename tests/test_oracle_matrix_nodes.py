@@ -219,6 +219,19 @@ def test_clip_refuses_outputs_over_one_another(rows):
     assert ckm.lib().ckm_clip_async(len(rows), tensors(*rows), 1.0, 0.0, P, P, 1 << 40, None) == ckm.E_INVALID_ARG
 
 
+def test_norm_may_not_lie_in_a_tensor():
+    L, bad = ckm.lib(), ckm.E_INVALID_ARG
+    t = tensors((P, 2 * P, 4, 0), (3 * P, 3 * P, 5, 2), (4 * P, 5 * P, 0, 0))
+    for at in (P, P + 12, 3 * P, 3 * P + 8):
+        assert L.ckm_norm_async(3, t, at, None, 0, None) == bad and b"norm overlaps" in L.ckm_last_error()
+    for at in (P, P + 12, 2 * P, 2 * P + 12, 3 * P + 8):
+        assert L.ckm_clip_async(3, t, 1.0, 0.0, at, None, 0, None) == bad and b"norm overlaps" in L.ckm_last_error()
+    for at in (P + 16, P - 4, 3 * P + 12, 4 * P, 5 * P):   # beside them
+        assert L.ckm_norm_async(3, t, at, None, 0, None) == bad and b"work buffer" in L.ckm_last_error()
+        assert L.ckm_clip_async(3, t, 1.0, 0.0, at, None, 0, None) == bad and b"work buffer" in L.ckm_last_error()
+    assert L.ckm_norm_async(3, t, 2 * P, None, 0, None) == bad and b"work buffer" in L.ckm_last_error()   # writes no output
+
+
 def test_norm_refuses_the_rest():
     L, t, n, bad = ckm.lib(), tensors((P, P, 4, 0)), C.c_size_t(), ckm.E_INVALID_ARG
     assert L.ckm_norm_workspace_size(1, C.byref(n)) == ckm.OK and n.value > 0
