@@ -552,7 +552,8 @@ typedef struct ckm_tensor {
  * squares (binary64, rounded once); 0 for none. ckm_clip_async also writes every
  * element times min(1, max_norm / (norm + eps)) to its tensor's d_out; outputs must
  * overlap neither each other nor another tensor. A norm of inf gives 0 for finite
- * elements, a norm of NaN gives NaN. norm: one float. work:
+ * elements, but a max_norm of inf leaves them as they are; a norm of NaN gives NaN,
+ * and so does 0 / 0. norm: one float. work:
  * ckm_norm_workspace_size bytes, aligned to 8. */
 ckm_status ckm_norm_workspace_size(int64_t count, size_t* bytes);
 ckm_status ckm_norm_async(int64_t count, const ckm_tensor* tensors, float* d_norm, void* d_work, size_t work_bytes,

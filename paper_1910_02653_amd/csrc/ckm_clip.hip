@@ -107,8 +107,9 @@ __global__ void __launch_bounds__(kBlock) ckm_norm_join_kernel(const double* par
   if (threadIdx.x == 0) *norm = (float)v;
 }
 
+// factor 2^shift: a factor below binary32's normal range has lost digits there, or all.
 template <typename T>
-__device__ __forceinline__ void scaled(const Entry& e, int64_t from, float factor) {
+__device__ __forceinline__ void scaled(const Entry& e, int64_t from, float factor, int shift) {
   Raw8<T> r[kGroups];
 #pragma unroll
   for (int i = 0; i < kGroups; ++i) {
@@ -121,7 +122,7 @@ __device__ __forceinline__ void scaled(const Entry& e, int64_t from, float facto
     if (at >= e.count) continue;
     float v[kVec];
 #pragma unroll
-    for (int j = 0; j < kVec; ++j) v[j] = (float)r[i].get(j) * factor;
+    for (int j = 0; j < kVec; ++j) v[j] = ldexpf((float)r[i].get(j) * factor, shift);
     store_part<false>((T*)e.out + at, rounded8<T>(v), 0, (int)min(e.count - at, (int64_t)kVec));
   }
 }
@@ -131,13 +132,15 @@ __global__ void __launch_bounds__(kBlock) ckm_clip_kernel(Table t, const double*
   __shared__ double lds[kBlock / 64];
   const double v = norm_of(parts, n, lds);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)v;
-  const double f = max_norm / (v + eps);
-  const float factor = f > 1.0 ? 1.0f : (float)f;   // NaN stays
+  // NaN stays; a max_norm of inf bounds nothing, a norm of inf neither
+  const double f = max_norm == INFINITY && v == INFINITY ? 1.0 : max_norm / (v + eps);
+  int shift = 0;
+  const float factor = f > 1.0 ? 1.0f : f < 0x1p-126 ? (float)frexp(f, &shift) : (float)f;
   each_chunk<true>(t, [&](const Entry& e, int64_t from) {
-    if (factor == 1.0f && e.out == e.in) return;
-    if (e.type == CKM_F32) scaled<float>(e, from, factor);
-    else if (e.type == CKM_F16) scaled<_Float16>(e, from, factor);
-    else scaled<__bf16>(e, from, factor);
+    if (factor == 1.0f && shift == 0 && e.out == e.in) return;
+    if (e.type == CKM_F32) scaled<float>(e, from, factor, shift);
+    else if (e.type == CKM_F16) scaled<_Float16>(e, from, factor, shift);
+    else scaled<__bf16>(e, from, factor, shift);
   });
 }
 

@@ -614,6 +614,30 @@ def test_norm_extremes():
     assert torch.equal(y.t(), ops.clip_gradients([t], 0.1, out=[torch.empty_like(t)])[1][0])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_clip_by_factors_below_the_normal_range(dtype):
+    """Elements near binary32's largest against a small bound: the product is normal where the factor is not. One rounding in
+    binary64 and one to binary32 (2 u), and the type's."""
+    g = torch.tensor([3.0e38, -1.0e37, 2.0e30, 0.0] * 5000, device="cuda").to(TYPES[dtype])
+    for most in (1e-2, 1e-6, 1e-9):
+        norm, (y,) = ops.clip_gradients([g], most, eps=0.0, out=[torch.empty_like(g)])
+        wide = g.double()
+        want = wide * (most / float(wide.square().sum().sqrt()))
+        assert torch.all((y.double() - want).abs() <= (HALF_ULP[dtype] + 2 * U) * want.abs() + TINY[dtype]), most
+        assert abs(float(y.double().norm()) / most - 1) < 2.0 ** -8
+
+
+def test_clip_with_bounds_of_infinity():
+    """A bound of inf leaves every element, whatever the norm; a smaller one with a norm of inf gives 0."""
+    g = torch.tensor([1.0, float("inf"), -2.0], device="cuda")
+    n, (y,) = ops.clip_gradients([g], float("inf"), out=[torch.empty_like(g)])
+    assert float(n) == float("inf") and torch.equal(y, g)
+    n, (y,) = ops.clip_gradients([g.clone()], float("inf"))
+    assert float(n) == float("inf") and torch.equal(y, g)
+    n, (y,) = ops.clip_gradients([g.clone()], 1e30)
+    assert float(n) == float("inf") and torch.isnan(y[1]) and y[0] == 0 and y[2] == 0
+
+
 # ---------------------------------------------------------------------------
 # together: streams, graphs, work buffers
 # ---------------------------------------------------------------------------
