@@ -247,7 +247,8 @@ void launch_logits(LossArgs a, const Cut& cut, hipStream_t s) {
 
 // A piece of the vocabulary: in the gradient d of at most 128 MB, which stays in the caches
 // between its writer and its readers, but never fewer than 8192 columns: dx, summed over
-// pieces in memory, is read and written for each. Pieces of the gradient go by the sizes, as
+// pieces in memory, is read and written for each. Past 8192 rows (4096 of binary32) d grows
+// with them, out of the caches: 1 GB at 65536 rows of 16 bits, as much as dx's sums at width 4096. Pieces of the gradient go by the sizes, as
 // the sums' order does. Forward, where the table has to be copied, 96 MB of it.
 constexpr int64_t kPieceBytes = (int64_t)128 << 20, kTableBytes = (int64_t)96 << 20, kLeastPiece = 8192;
 

@@ -174,6 +174,19 @@ def test_cross_entropy_refuses_outputs_and_work():
     assert n.value < (1 << 16) * (1 << 18) * 2 // 16
 
 
+@pytest.mark.parametrize("dtype", [ops.F32, ops.F16, ops.BF16])
+@pytest.mark.parametrize("rows", [1024, 8192, 16384, 65536, 1 << 20])
+def test_cross_entropy_gradient_work_at_many_rows(dtype, rows):
+    """x's copy, dx's sums, and d: 128 MB (its rows padded), or 8192 columns of it; each part is rounded up to 256 bytes, and
+    a row of d has up to 384 more."""
+    elt, hidden, words, L, n = 4 if dtype == ops.F32 else 2, 4096, 131072, ckm.lib(), C.c_size_t()
+    c = vocab(rows=rows, hidden=hidden, vocab=words, ld_x=hidden, ld_weight=hidden, d_x=1 << 44, d_weight=1 << 45)
+    assert L.ckm_cross_entropy_workspace_size(dtype, C.byref(c), 1, C.byref(n)) == ckm.OK
+    d = max(128 << 20, rows * 8192 * elt)
+    most = rows * hidden * elt + max(rows * hidden * 4, 512 << 20 if rows <= 8192 else 0) + d + rows * 384
+    assert rows * hidden * (elt + 4) + rows * 8192 * elt // 2 <= n.value <= most + (1 << 20), (n.value >> 20, most >> 20)
+
+
 def test_no_rows_refuse_outputs_over_the_weights():
     """Zero weight gradients are written without rows too, and so not over the weights or one another."""
     L, bad = ckm.lib(), ckm.E_INVALID_ARG
