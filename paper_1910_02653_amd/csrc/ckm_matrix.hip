@@ -121,10 +121,14 @@ Cut cut_as(const Shape& shape, int64_t m, int64_t n, int halves, int subs, int64
   c.staged = staged;
   return c;
 }
-// The shares' way through memory: written, which other tiles' steps hide where a CU has
-// several at once, and read (gated f32 777x1023x2731: 108 us in two shares, 117 in one).
-double join_time(const Cut& c, int64_t m, int64_t n, int subs) {
-  const double bytes = c.rows < 256 && c.blocks() > 2 * kCUs ? 4.0 : 8.0;
+// The shares' way through memory: written and read. In binary32's products of two matrices,
+// whose steps are the longest, the other tiles of a CU hide the writing where it has several:
+// where that changes the cut, 65 sizes drawn over the operator's range, calls take 0.998 of
+// the time in the mean, 0.86 to 1.15 (777x1023x2731: 108 us in two shares, 117 in one). It
+// does not hold in 16 bits (71 sizes: 1.04, up to 1.28) or for the loss's gradient in
+// binary32 (39 sizes: 1.004).
+double join_time(int type, const Cut& c, int64_t m, int64_t n, int subs) {
+  const double bytes = type == CKM_F32 && subs == 2 && c.rows < 256 && c.blocks() > 2 * kCUs ? 4.0 : 8.0;
   return c.splits > 1 ? kJoin + bytes * c.splits * m * n * c.halves * subs / kSharesAUs : 0.0;
 }
 
@@ -137,7 +141,6 @@ double join_time(const Cut& c, int64_t m, int64_t n, int subs) {
 //   f32 2048x2048x1024    128 rows, one: 75; 64, two: 71; 16, eight: 97
 //   bf16 2048x8192x4096   256 rows, one: 101 (1357 TFLOP/s); 128, four: 128; 64, eight: 161
 //   bf16 1x16384x2048     16 rows 12, 64 rows 15 (67 MB)
-// Of every cut of the products of 37 calls it takes the best or one within 4 %, twice 8 %.
 double time_of(int type, const Shape& shape, const Cut& c, int64_t m, int64_t n, int subs, int64_t bytes, Staged staged) {
   constexpr double kSteps[] = {1.0, 1.4, 2.5}, kReads[] = {1.0, 1.2, 5.0};   // by way of registers, of lines that are cut
   const double rounds = std::ceil(c.blocks() / kCUs);
@@ -146,7 +149,7 @@ double time_of(int type, const Shape& shape, const Cut& c, int64_t m, int64_t n,
   // where a CU holds two tiles, one's fixed part is half hidden behind the other's steps
   const double fixed = shape.fixed * (shape.rows == 256 ? rounds : 1.0 + 0.5 * (rounds - 1.0));
   return std::max(rounds * c.steps * step + fixed, kReads[staged] * bytes / kBytesAUs + shape.fixed) +
-         join_time(c, m, n, subs);
+         join_time(type, c, m, n, subs);
 }
 
 Cut cut_product(int type, int64_t m, int64_t n, int halves, int subs, int64_t steps, int64_t bytes, bool split,
@@ -197,7 +200,7 @@ bool cut_together(int type, Cut& a, int64_t m_a, int64_t n_a, int64_t steps_a, C
       // all the work shared out evenly, no less than the longest tile
       const double work = (c.blocks() * (c.steps * time.more + shape.fixed) + d.blocks() * (d.steps * time_b.more + shape_b.fixed)) / kCUs;
       const double longest = std::max(c.steps * time.one + shape.fixed, d.steps * time_b.one + shape_b.fixed);
-      const double t = std::max({work, longest, bytes / kBytesAUs + shape.fixed}) + join_time(c, m_a, n_a, 1);
+      const double t = std::max({work, longest, bytes / kBytesAUs + shape.fixed}) + join_time(type, c, m_a, n_a, 1);
       if (t < least) {
         least = t;
         best = c;
