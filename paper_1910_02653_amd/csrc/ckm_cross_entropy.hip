@@ -17,11 +17,11 @@
 // every row, up to 2^-9 in bfloat16 and the same way. binary16, whose exponents are
 // too few (exp(l - lse) is about 1 / vocab), holds d 2^15 / s, of at most 32768.
 //
-// Bound by the products: f16 2048x2048x32768 238 us (1160 TFLOP/s), its gradient 753
-// (logits 290, dx 260 and 20 for its shares, dW 289 in a trace); bf16 4096x4096x131072
-// 10.2 ms (1290 TFLOP/s) in eight pieces. A tile's exponentials are a difference, a
-// product and one 2^x each. Few rows are bound by reading the table: bf16 16x4096x50021 82 to 87 us,
-// 410 MB at 4.8 TB/s.
+// Bound by the products: f16 2048x2048x32768 234 us (1180 TFLOP/s), its gradient 739 (the
+// least of a trace: the copy 6, logits 262, dx 221 and 19 for its shares, dW 239); bf16
+// 4096x4096x131072 10.0 ms (1320 TFLOP/s) in eight pieces; f32 2048x1024x32768 986 us and 2980,
+// 139 of 154 TFLOP/s. A tile's exponentials are a difference, a product and one 2^x each. Few
+// rows are bound by reading the table: bf16 16x4096x50021 85 us, 410 MB at 4.8 TB/s.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -20,11 +20,12 @@
 // are multiplied by the inverse. In range, which is the rule, its blocks return at once: f16
 // 2048x2048x8192 408 us without it and 412 with it, 512x1024x2048 33 and 36; out of range 553 and 45.
 //
-// Bound by the products: f16 2048x2048x8192 121 us (1140 TFLOP/s; the library's product
-// alone 126 to 137), its gradient 395 (recomputation 135, dx 136 and 13 for its shares, dW
-// 123); bf16 8192x4096x16384 1650 us (1330). A tile's end, activation and stores, is 6
-// to 10 us of some 58 and not hidden: one block is on a CU. A single token is bound by
-// reading the weights: f16 1x2048x8192 14.6 us, 67 MB.
+// Bound by the products: f16 2048x2048x8192 119 us (1150 TFLOP/s; the library's product
+// alone 117 to 137), its gradient 398 (the least of a trace: recomputation 136 and 5 for the
+// second launch, dx 135 and 13 for its shares, dW 123); bf16 8192x4096x16384 1610 to 1650 us
+// (1330 to 1370); f32 2048x1024x4096 256 us and 758, 134 to 136 of 154 TFLOP/s. A tile's end,
+// activation and stores, is 6 to 10 us of some 58 and not hidden: one block is on a CU. A
+// single token is bound by reading the weights: f16 1x2048x8192 14.7 us, 67 MB; f32 27.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

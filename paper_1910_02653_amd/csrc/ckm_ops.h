@@ -1,9 +1,10 @@
-// Device helpers and launch declarations shared by the training-node
-// operators: dropout (ckm_dropout.hip), layer norm (ckm_layer_norm.hip) and
-// the attention softmax (ckm_softmax.hip).
+// Device helpers and launch declarations shared by the training-node operators:
+// dropout (ckm_dropout.hip), layer norm (ckm_layer_norm.hip), the attention softmax
+// (ckm_softmax.hip), the matrix operators (ckm_matrix.h) and the norm over many
+// tensors (ckm_clip.hip).
 //
-// All three work on rows. A thread holds groups of eight consecutive columns:
-// 16 bytes of a 16-bit type, and exactly the eight draws of one Philox output.
+// A thread loads and stores groups of eight consecutive columns: 16 bytes of a 16-bit
+// type, and exactly the eight draws of one Philox output.
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -709,8 +709,8 @@ def clip_gradients(tensors, max_norm: float, eps: float = 1e-6, out=None, work=N
 
     In place, or into `out`: as many tensors of the same types, shapes and
     strides, which must overlap neither each other nor another tensor; so no tensor may
-    be listed twice. norm: what gradient_norm gives, of the tensors before. work:
-    as for gradient_norm."""
+    be listed twice. norm: what gradient_norm gives, of the tensors before. A
+    max_norm of inf leaves every element as it is. work: as for gradient_norm."""
     tensors = list(tensors)
     if out is not None:
         out = list(out)
