@@ -540,7 +540,7 @@ ckm_status ckm_cross_entropy_async(ckm_dtype type, const ckm_vocab* vocab, float
  * shares of dx or dW, at most 512 MB of each), and d of a piece of the vocabulary, 128
  * MB or, past 8192 rows (4096 of binary32), 8192 columns: for bfloat16 65536 rows of
  * 4096 against 131072 2.5 GB. A table whose rows do not lie on 16 bytes may be copied as
- * well, by the same pieces: where rows are few, whole. */
+ * well, by the same pieces: where rows are few, whole, but some 4 GB at a time. */
 ckm_status ckm_cross_entropy_backward_async(ckm_dtype type, const ckm_vocab* vocab, const float* d_dloss,
                                             const float* d_lse, void* d_dx, int64_t ld_dx, void* d_dweight,
                                             int64_t ld_dweight, void* d_work, size_t work_bytes, void* stream);

@@ -249,13 +249,18 @@ void launch_logits(LossArgs a, const Cut& cut, hipStream_t s) {
 // between its writer and its readers, but never fewer than 8192 columns: dx, summed over
 // pieces in memory, is read and written for each. Past 8192 rows (4096 of binary32) d grows
 // with them, out of the caches: 1 GB at 65536 rows of 16 bits, as much as dx's sums at width 4096. Pieces of the gradient go by the sizes, as
-// the sums' order does. Forward, where the table has to be copied, 96 MB of it.
+// the sums' order does. Where the table has to be copied: forward 96 MB pieces of it; in the
+// gradient a piece; of a piece of more than 4 GB (vast tables, few rows) as many shares of dx
+// as take that, so that the copy's room has a bound (their launches fill fewer CUs: bf16
+// 16x4097x300000, 2.5 GB, 2.9 ms whole and 4.2 in three parts).
 constexpr int64_t kPieceBytes = (int64_t)128 << 20, kTableBytes = (int64_t)96 << 20, kLeastPiece = 8192;
+constexpr int64_t kCopyBytes = (int64_t)4 << 30;
 
 struct LossPlan {
   bool pack_x, pack_w;
   int64_t ld_x, ld_w;
   int64_t piece;             // columns
+  int64_t copied;            // columns of the table in the work buffer at a time: of a piece, or of some of dx's shares
   Cut logits, dx, dw;
   bool together;             // dx and dW in a launch
   size_t x, w, parts, hit, most, d, slab, dw_slab, total;
@@ -290,7 +295,7 @@ LossPlan plan_as(int type, const ckm_vocab& c, bool back, bool ragged_x, bool ra
   if (back) most = std::min(most, kPieceBytes / (int64_t)(c.rows * elt));
   const int64_t all = piece_of(most);   // were the table not copied
   p.piece = p.pack_w && !back ? std::min(all, piece_of(std::min(most, kTableBytes / (int64_t)(c.hidden * elt)))) : all;
-  if (p.pack_w) p.w = take(p.piece * p.ld_w * elt);
+  p.copied = p.piece;
   const int64_t steps = (c.hidden + step - 1) / step, x_bytes = c.rows * c.hidden * elt, w_bytes = p.piece * c.hidden * elt;
   p.logits = cut_product(type, c.rows, p.piece, 1, 1, steps, x_bytes + w_bytes, false, true);
   if (staged_x || staged_w)
@@ -312,11 +317,14 @@ LossPlan plan_as(int type, const ckm_vocab& c, bool back, bool ragged_x, bool ra
       p.dw = cut_like(type, p.piece, c.hidden, 1, 1, steps_m, d_bytes + x_bytes + w_bytes, false, kStraight, p.dw);
     }
     p.time += p.dx.time + p.dw.time;
+    const int64_t share = p.dx.steps * step, most_shares = kCopyBytes / (int64_t)(share * p.ld_w * elt);
+    if (p.pack_w && p.dx.splits > 1) p.copied = std::min(p.piece, std::max<int64_t>(1, most_shares) * share);
     p.most = take(sizeof(float));
     p.d = take((size_t)c.rows * row_of(p.piece, elt) * elt);
     if (p.dx.splits > 1 || p.piece < c.vocab) p.slab = take((size_t)p.dx.splits * c.rows * whole(c.hidden, 8) * 4);
     if (p.dw.splits > 1) p.dw_slab = take((size_t)p.dw.splits * p.piece * whole(c.hidden, 8) * 4);
   }
+  if (p.pack_w) p.w = take(p.copied * p.ld_w * elt);
   p.time *= (double)c.vocab / p.piece;
   if (!back && p.pack_x) p.time += copy_time(x_bytes);
   p.total = at;
@@ -381,7 +389,6 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
   }
   a.dloss = dloss;
   if (kRelative<T>) a.most = (const float*)(work + plan.most);
-  a.d = work + plan.d;
   a.ld_d = row_of(plan.piece, sizeof(T));
   ResultArgs rx = {}, rw = {};
   rx.alpha = rw.alpha = a.most;
@@ -394,23 +401,35 @@ void launch_loss(int type, const ckm_vocab& c, const LossPlan& plan, bool back, 
   rx.halves = rw.halves = 1;
   if (plan.dw.splits > 1) rw.slab = (float*)(work + plan.dw_slab);
   rw.ld_c[0] = ld_dw;
+  T* const d = (T*)(work + plan.d);
   for (int64_t v = 0; v < c.vocab; v += plan.piece) {
     const int32_t width = (int32_t)std::min(plan.piece, c.vocab - v);
-    const T* wv = rows_from(v, width);
-    a.first = v;
-    a.p.b.p = a.p.b.q = wv;
-    a.p.n = width;
-    launch_logits<T, true>(a, plan.logits, s);
-    // d W; a short last piece leaves shares at the end of k with nothing to add
-    rx.p = {{a.d, a.d, a.ld_d}, {wv, wv, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, width, 1};
+    const bool whole = width <= plan.copied, both = plan.together && dx && dw && whole;
     // d' x
-    rw.p = {{a.d, a.d, a.ld_d}, {x, x, plan.ld_x}, width, (int32_t)c.hidden, (int32_t)c.rows, 1};
+    rw.p = {{d, d, a.ld_d}, {x, x, plan.ld_x}, width, (int32_t)c.hidden, (int32_t)c.rows, 1};
     rw.c[0] = (T*)dw + v * ld_dw;
     Cut cut = plan.dw;
     cut.tiles_m = (width + cut.rows - 1) / cut.rows;
-    const bool both = plan.together && dx && dw;
-    if (both) launch_two<T, false>(rx, plan.dx, rw, cut, s);
-    else if (dx) launch_product<T, true, false>(rx, plan.dx, s);
+    for (int64_t u = 0; u < width; u += plan.copied) {
+      const int32_t now = (int32_t)std::min(plan.copied, width - u);
+      const T* wv = rows_from(v + u, now);
+      a.first = v + u;
+      a.p.b.p = a.p.b.q = wv;
+      a.p.n = now;
+      a.d = d + u;
+      launch_logits<T, true>(a, plan.logits, s);
+      // d W, all shares or those of these columns; a short last piece leaves shares at the end of k with nothing to add
+      rx.p = {{d + u, d + u, a.ld_d}, {wv, wv, plan.ld_w}, (int32_t)c.rows, (int32_t)c.hidden, now, 1};
+      Cut shares = plan.dx;
+      if (!whole) {
+        const int64_t share = plan.dx.steps * (kStepBytes / (int64_t)sizeof(T));
+        shares.splits = (int)((now + share - 1) / share);
+        rx.slab = (float*)(work + plan.slab) + u / share * c.rows * rx.ld_slab;
+      }
+      if (both) launch_two<T, false>(rx, shares, rw, cut, s);
+      else if (dx) launch_product<T, true, false>(rx, shares, s);
+    }
+    if (slab) rx.slab = (float*)(work + plan.slab);
     rx.add = true;
     if (dw && !both) {
       launch_product<T, false, false>(rw, cut, s);

@@ -502,6 +502,28 @@ def test_cross_entropy_bits_go_by_the_sizes(dtype, rows, hidden, vocab):
                 assert torch.equal(p, q)
 
 
+def test_cross_entropy_gradient_of_a_vast_table_off_16_bytes():
+    """Copied by shares of dx, past 4 GB: the bits of the table that need not be copied, within a bound of room."""
+    rows, hidden, vocab = 8, 1000, 1250000
+    x, dloss = randn((rows, hidden), "f32", 1), torch.ones(rows, device="cuda")
+    flat = torch.empty(vocab * hidden + 1, dtype=torch.float32, device="cuda")
+    w = flat[:-1].view(vocab, hidden).normal_(0.0, hidden ** -0.5, generator=torch.Generator(device="cuda").manual_seed(2))
+    targets = torch.tensor([0, 1, vocab - 1, 1100000, 1073000, -1, 600000, vocab // 2], device="cuda")
+    loss, lse = ops.cross_entropy(x, w, targets)
+    dx, dw = ops.cross_entropy_backward(dloss, x, w, targets, lse)
+    need = ops.cross_entropy_workspace(x, w, targets, backward=True)
+    d = torch.exp(x.double() @ w[-2000:].double().t() - lse.double()[:, None])
+    d[2, -1] -= 1.0
+    d[5] = 0.0
+    want = d.t() @ x.double()
+    assert float((dw[-2000:].double() - want).norm() / want.norm()) < 16 * (rows + 8) ** 0.5 * U
+    aside = torch.empty_like(flat)[1:].view(vocab, hidden)
+    aside.copy_(w)
+    assert need < ops.cross_entropy_workspace(x, aside, targets, backward=True) < need + (4 << 30) + (1 << 20)
+    for p, q in zip(ops.cross_entropy_backward(dloss, x, aside, targets, lse), (dx, dw)):
+        assert torch.equal(p, q)
+
+
 def test_rows_further_apart_than_32_bits_count():
     ld = (1 << 31) + 24
     flat = torch.empty(2 * ld + 72, dtype=torch.float16, device="cuda")
